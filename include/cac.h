@@ -276,6 +276,77 @@ int conv_bwd_bias(const cac_desc *d, const void *dY, void *db, void *stream);
 int cac_grad_cosine(const cac_desc *d, const void *dW_a, const void *dW_b, void *out,
                     void *ws, size_t ws_bytes, void *stream);
 
+/* ---- The two ends of a training step around the convolutions ------------------------------------
+ *
+ * The loss a network's gradients start from, and the update that takes its weight gradients. */
+
+/* Softmax cross entropy of a linear classifier: z = H W^T + b, H [T, D] (a row for every image, pixel or token),
+ * W [V, D] (a row for every class), b [V];
+ *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,labels[t].
+ * The logits are never kept: they pass through registers, and in the backward pass their gradients through the
+ * workspace, a piece of the classes at a time.
+ *   - A row whose label is ignore_index, or is no class (below 0, V or more), is left out: its loss and lse are 0, its
+ *     gradient is 0, and its H is not read into any sum, whatever it holds.
+ *   - A class can be masked by b = -infinity.  The loss of a row whose label is masked is +infinity (its gradient is
+ *     that of the formula, probability 0 - 1); a row whose classes are all masked has probabilities of 0.
+ *   - dtype CAC_F32: operands are multiplied as pairs of half-precision numbers, which keep 23 bits; numbers below
+ *     2^-28 of their matrix's largest keep fewer.  An infinity or NaN in H or W comes out as NaN in every row and
+ *     gradient that it meets.  dtype CAC_BF16: the logits' gradients are rounded to bfloat16 (times the row's gradient over the
+ *     largest row's) before they are multiplied with H and W.  Sums are float in both; loss, lse and gloss are float. */
+typedef enum cac_loss_op { CAC_LOSS_FWD = 0, CAC_LOSS_BWD = 1 } cac_loss_op;
+
+typedef struct cac_loss_desc {
+    uint32_t size;               /* sizeof(cac_loss_desc) */
+    int32_t T, D, V;             /* rows, features, classes: at most 2^22, 2^18, 2^24 */
+    int32_t ld_h, ld_w;          /* elements from a row of H (W) to the next, at most 2^20; 0: D */
+    int32_t dtype;               /* cac_dtype of H, W, b, dH, dW, db */
+    int32_t has_bias;
+    int32_t ignore_index;
+} cac_loss_desc;
+
+/* Host only. */
+int cac_loss_workspace_size(const cac_loss_desc *d, int op, size_t *bytes);
+int cac_loss_describe_plan(const cac_loss_desc *d, int op, char *buf, size_t buf_len);
+
+int cac_loss_fwd(const cac_loss_desc *d, const void *H, const void *W, const void *b, const int64_t *labels, float *loss, float *lse,
+                 void *ws, size_t ws_bytes, void *stream);
+
+/* gloss [T]: the gradient of what is minimised by every row's loss (1 / T for a mean).  With G_tv = gloss_t *
+ * (exp(z_tv - lse_t) - [v = labels_t]):  dH = G W [T, D], dW = G^T H [V, D], db = column sums of G [V], all dense.  Any of
+ * the three may be NULL and is not computed then.  `lse` is what the forward pass wrote. */
+int cac_loss_bwd(const cac_loss_desc *d, const void *H, const void *W, const void *b, const int64_t *labels, const float *lse,
+                 const float *gloss, void *dH, void *dW, void *db, void *ws, size_t ws_bytes, void *stream);
+
+/* Orthogonalised updates (Newton-Schulz products) of a batch of dense matrices [batch][rows][cols], such as a
+ * convolution's dW as [C_out][C_in * R * S].  From X = U / (|U|_F + 1e-7), `steps` times:
+ *   A = X X^T,  X <- a X + (b A + c A A) X,   (a, b, c) = (3.4445, -4.7750, 2.0315),
+ * which brings every singular value near 1 and keeps the singular vectors.  Both dtypes are computed as pairs of
+ * half-precision numbers (23 bits) with float sums; CAC_BF16 rounds the result once.  A matrix of zeros stays zero;
+ * an infinity or NaN comes out as NaN in the matrix that it stands in. */
+typedef enum cac_muon_op { CAC_MUON_ORTHOGONALISE = 0, CAC_MUON_STEP = 1 } cac_muon_op;
+
+typedef struct cac_muon_desc {
+    uint32_t size;               /* sizeof(cac_muon_desc) */
+    int32_t batch, rows, cols;   /* rows and cols at most 2^18, batch at most 65535 */
+    int32_t dtype;               /* cac_dtype of O and W */
+    int32_t grad_dtype;          /* cac_dtype of G (a convolution's dW is float for both dtypes) */
+    int32_t steps;               /* 1 to 32; 5 is usual */
+    int32_t nesterov;            /* of cac_muon_step */
+} cac_muon_desc;
+
+/* Host only. */
+int cac_muon_workspace_size(const cac_muon_desc *d, int op, size_t *bytes);
+int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf_len);
+
+/* O = the orthogonalised G.  O may be G where their types are the same. */
+int cac_orthogonalise(const cac_muon_desc *d, const void *G, void *O, void *ws, size_t ws_bytes, void *stream);
+
+/* The optimiser's step, in place:  M <- momentum * M + G,  U = G + momentum * M (U = M without nesterov),
+ * W <- keep * W - lr * orthogonalised U.  M is float; keep is 1 - lr * weight decay, and lr takes any factor for the
+ * matrix's shape with it. */
+int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, float momentum, float keep, float lr, void *ws,
+                  size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,7 +30,11 @@ EXPORTS = (
     "cac_dw_executed_flops",
     "conv_fwd_and_compress", "cac_compress", "conv_bwd_weight_compressed", "conv_bwd_data", "conv_bwd_bias", "cac_grad_cosine",
     "conv_bwd_weight_and_data", "conv_bwd_weight_compressed_noalloc", "cac_bn_relu_fwd_compress", "cac_bn_bwd_compressed", "cac_probe",
+    "cac_loss_workspace_size", "cac_loss_describe_plan", "cac_loss_fwd", "cac_loss_bwd",
+    "cac_muon_workspace_size", "cac_muon_describe_plan", "cac_orthogonalise", "cac_muon_step",
 )
+LOSS_FWD, LOSS_BWD = 0, 1
+MUON_ORTHOGONALISE, MUON_STEP = 0, 1
 PROBE_MFMA, PROBE_COPY, PROBE_READ, PROBE_MFMA_16X16, PROBE_MFMA_1WAVE = 0, 1, 2, 3, 4
 NOALLOC_SCRATCH_BYTES = 40 << 20
 
@@ -40,6 +44,18 @@ class cac_desc(ctypes.Structure):
         (n, ctypes.c_int32) for n in (
             "N", "C_in", "C_out", "H", "W", "R", "S", "stride_h", "stride_w", "pad_h", "pad_w",
             "pool_kh", "pool_kw", "edge_mode", "dtype", "has_bias", "pool_mode", "dw_algo")
+    ]
+
+
+class cac_loss_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("T", "D", "V", "ld_h", "ld_w", "dtype", "has_bias", "ignore_index")
+    ]
+
+
+class cac_muon_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("batch", "rows", "cols", "dtype", "grad_dtype", "steps", "nesterov")
     ]
 
 
@@ -83,6 +99,15 @@ def lib() -> ctypes.CDLL:
         L.cac_bn_relu_fwd_compress.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp]
         L.cac_bn_bwd_compressed.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.cac_grad_cosine.argtypes = [dp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        lp, mp, fl = ctypes.POINTER(cac_loss_desc), ctypes.POINTER(cac_muon_desc), ctypes.c_float
+        L.cac_loss_workspace_size.argtypes = [lp, ctypes.c_int, szp]
+        L.cac_loss_describe_plan.argtypes = [lp, ctypes.c_int, ctypes.c_char_p, sz]
+        L.cac_loss_fwd.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cac_loss_bwd.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.cac_muon_workspace_size.argtypes = [mp, ctypes.c_int, szp]
+        L.cac_muon_describe_plan.argtypes = [mp, ctypes.c_int, ctypes.c_char_p, sz]
+        L.cac_orthogonalise.argtypes = [mp, vp, vp, vp, sz, vp]
+        L.cac_muon_step.argtypes = [mp, vp, vp, vp, fl, fl, fl, vp, sz, vp]
         for n in EXPORTS[2:]:
             getattr(L, n).restype = ctypes.c_int
         _lib = L
@@ -98,6 +123,14 @@ def make_desc(N, C_in, C_out, H, W, R, S, stride_h=1, stride_w=1, pad_h=0, pad_w
               edge_mode=EDGE_CEIL_VALID, dtype=BF16, has_bias=1, pool_mode=POOL_MEAN, dw_algo=DW_INFLATE) -> cac_desc:
     return cac_desc(ctypes.sizeof(cac_desc), N, C_in, C_out, H, W, R, S, stride_h, stride_w, pad_h, pad_w,
                     pool_kh, pool_kw, edge_mode, dtype, has_bias, pool_mode, dw_algo)
+
+
+def make_loss_desc(T, D, V, dtype=BF16, has_bias=0, ignore_index=-100, ld_h=0, ld_w=0) -> cac_loss_desc:
+    return cac_loss_desc(ctypes.sizeof(cac_loss_desc), T, D, V, ld_h, ld_w, dtype, has_bias, ignore_index)
+
+
+def make_muon_desc(rows, cols, batch=1, dtype=F32, grad_dtype=F32, steps=5, nesterov=1) -> cac_muon_desc:
+    return cac_muon_desc(ctypes.sizeof(cac_muon_desc), batch, rows, cols, dtype, grad_dtype, steps, nesterov)
 
 
 def desc_from_spec(spec: synth.LayerSpec, has_bias: int = 1, **over) -> cac_desc:
@@ -220,6 +253,51 @@ def conv_bwd_bias(d, dY, db, stream=None):
 
 def cac_grad_cosine(d, dW_a, dW_b, out, ws=None, stream=None):
     _check((_lib or lib()).cac_grad_cosine(d, _ptr(dW_a), _ptr(dW_b), _ptr(out), *_ws(ws), _stream(stream)))
+
+
+def _size_of(fn, d, op) -> int:
+    n = ctypes.c_size_t()
+    _check(fn(ctypes.byref(d), op, ctypes.byref(n)))
+    return n.value
+
+
+def _plan_of(fn, d, op) -> str:
+    buf = ctypes.create_string_buffer(2048)
+    _check(fn(ctypes.byref(d), op, buf, len(buf)))
+    return buf.value.decode()
+
+
+def cac_loss_workspace_size(d: cac_loss_desc, op: int) -> int:
+    return _size_of(lib().cac_loss_workspace_size, d, op)
+
+
+def cac_loss_describe_plan(d: cac_loss_desc, op: int) -> str:
+    return _plan_of(lib().cac_loss_describe_plan, d, op)
+
+
+def cac_loss_fwd(d, H, W, b, labels, loss, lse, ws=None, stream=None):
+    _check((_lib or lib()).cac_loss_fwd(d, _ptr(H), _ptr(W), _ptr(b), _ptr(labels), _ptr(loss), _ptr(lse), *_ws(ws), _stream(stream)))
+
+
+def cac_loss_bwd(d, H, W, b, labels, lse, gloss, dH, dW, db, ws=None, stream=None):
+    _check((_lib or lib()).cac_loss_bwd(d, _ptr(H), _ptr(W), _ptr(b), _ptr(labels), _ptr(lse), _ptr(gloss), _ptr(dH), _ptr(dW), _ptr(db),
+                                        *_ws(ws), _stream(stream)))
+
+
+def cac_muon_workspace_size(d: cac_muon_desc, op: int) -> int:
+    return _size_of(lib().cac_muon_workspace_size, d, op)
+
+
+def cac_muon_describe_plan(d: cac_muon_desc, op: int) -> str:
+    return _plan_of(lib().cac_muon_describe_plan, d, op)
+
+
+def cac_orthogonalise(d, G, O, ws=None, stream=None):
+    _check((_lib or lib()).cac_orthogonalise(d, _ptr(G), _ptr(O), *_ws(ws), _stream(stream)))
+
+
+def cac_muon_step(d, G, M, W, momentum, keep, lr, ws=None, stream=None):
+    _check((_lib or lib()).cac_muon_step(d, _ptr(G), _ptr(M), _ptr(W), momentum, keep, lr, *_ws(ws), _stream(stream)))
 
 
 # ---- host <-> device marshalling (type conversion only, no arithmetic)

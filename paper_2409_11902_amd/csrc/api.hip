@@ -7,6 +7,7 @@
 
 #include <mutex>
 
+#include "api_check.h"
 #include "common.h"
 #include "conv_mfma.h"
 #include "dw_mfma.h"
@@ -17,7 +18,7 @@ namespace cac {
 
 static thread_local char g_err[256] = "";
 
-static int fail(int code, const char *fmt, ...)
+int fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -90,7 +91,7 @@ static int make_geom(const cac_desc *d, Geom *g, bool for_kernel)
     return CAC_OK;
 }
 
-static int check_ptr(const void *p, const char *name)
+int check_ptr(const void *p, const char *name)
 {
     if (!p) return fail(CAC_ERR_INVALID_ARG, "%s is NULL", name);
     if (((uintptr_t)p) & 15) return fail(CAC_ERR_ALIGNMENT, "%s is not 16-byte aligned", name);
@@ -102,7 +103,7 @@ static bool share_memory(const void *a, size_t a_bytes, const void *b, size_t b_
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
 
-static int launched(hipError_t e, const char *what)
+int launched(hipError_t e, const char *what)
 {
     if (e != hipSuccess) return fail(CAC_ERR_LAUNCH_FAILED, "%s: %s", what, hipGetErrorString(e));
     return CAC_OK;
@@ -171,7 +172,7 @@ static size_t workspace_bytes(const Geom &g, int dtype, int op)
     return 0;
 }
 
-static int check_ws(size_t need, const void *ws, size_t ws_bytes)
+int check_ws(size_t need, const void *ws, size_t ws_bytes)
 {
     if (need == 0) return CAC_OK;
     if (!ws) return fail(CAC_ERR_WORKSPACE_TOO_SMALL, "workspace is NULL, %zu bytes needed", need);

@@ -1,0 +1,52 @@
+// What the entry points (api_train.hip) ask of the loss' and the update's kernels: plans (host only) and launches.
+#pragma once
+#include "common.h"
+
+namespace cac {
+
+// ---- loss.hip: softmax cross entropy of a linear classifier
+struct LossGeom {
+    long T, D, V;
+    long ld_h, ld_w; // elements
+    int dtype;
+    bool bias;
+    long ignore;
+};
+struct LossPlan {
+    bool split;       // float: operands as two halves
+    bool pack_w;      // the weights go through the workspace, piece by piece
+    long dp;          // features, in whole chunks of 8
+    long row_bytes;   // of a packed row
+    long piece;       // classes in one piece
+    int pieces;
+    // forward: tile of the logits; backward: tiles and slices of the three products
+    int tile_z, tile_w, tile_h, slices_h;
+    long parts;       // forward: maximum and sum, this many for every row
+    size_t o_meta, o_h, o_w, o_part, o_g, o_acc, bytes;
+};
+void plan_loss(const LossGeom &g, bool backward, LossPlan *p);
+hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
+                           float *loss, float *lse, void *ws, hipStream_t st);
+hipError_t launch_loss_bwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
+                           const float *lse, const float *gloss, void *dH, void *dW, void *db, void *ws, hipStream_t st);
+
+// ---- muon.hip: Newton-Schulz products and the update made of them
+struct MuonGeom {
+    long rows, cols;
+    int batch, steps, dtype, grad_dtype;
+    bool nesterov;
+};
+struct MuonPlan {
+    bool tall;          // more rows than columns: X^T X in the place of X X^T
+    long r;             // the shorter side
+    long ld_x, ld_a;    // bytes of a row
+    int tile_gram, tile_poly, tile_apply;
+    int sum_blocks;     // partial sums of squares of one matrix
+    size_t o_sum, o_x[2], o_a, o_b, bytes;
+};
+void plan_muon(const MuonGeom &g, MuonPlan *p);
+// M, W: null where only O is asked for; O: null where the weights are updated
+hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, float *M, void *W, void *O, float momentum, float keep,
+                       float lr, void *ws, hipStream_t st);
+
+} // namespace cac
