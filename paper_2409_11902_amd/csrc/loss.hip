@@ -268,7 +268,7 @@ template <typename T> __device__ __forceinline__ void load_bias(const T *b, int 
 }
 
 // ---- endings of the products
-// forward: maximum and sum of exp of a row over a wave's 32 I columns, and the label's logit
+// forward: maximum and sum of exp of a row over a wave's columns, and the label's logit
 template <typename T> struct Stats {
     static constexpr bool kSymmetric = false;
     struct Params {
@@ -278,17 +278,17 @@ template <typename T> struct Stats {
         long T_rows;
         int part0, v0;    // the piece's first part, its first class
     };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
-        const int part = e.part0 + p.tn * 2 + p.wn;
+        const int part = e.part0 + p.part;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
             const int label = m < p.M ? e.meta.label[m] - e.v0 : -1;
-            float top = -INFINITY, sum = 0.f, z[I][16];
+            float top = -INFINITY, sum = 0.f, z[NI][16];
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -305,7 +305,7 @@ template <typename T> struct Stats {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float shift = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f((z[j][k] - shift) * kLog2e);
             sum += __shfl_xor(sum, 32, 64);
@@ -358,19 +358,19 @@ template <typename T> struct Grad {
         long ld;
         int v0;
     };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
         const int Np = (p.N + 7) & ~7;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
             if (m >= p.M) continue;
             const int label = e.meta.label[m] - e.v0;
             const float q_row = e.meta.q[m], lse = e.meta.lse[m];
             char *row = e.out + (long)m * e.ld;
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -416,14 +416,14 @@ template <typename T> __device__ __forceinline__ void store_four(T *o, int n, in
 template <typename T> struct OutW {
     static constexpr bool kSymmetric = false;
     struct Params { T *out; Meta meta; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const float s = sizeof(T) == 4 ? ldexpf(*e.meta.c, -kStoreG - e.meta.exps[0]) : *e.meta.c;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -440,17 +440,17 @@ template <typename T> struct OutW {
 template <typename T> struct OutH {
     static constexpr bool kSymmetric = false;
     struct Params { T *out; float *sums; long slice_stride; int add; Meta meta; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const float s = sizeof(T) == 4 ? ldexpf(*e.meta.c, -kStoreG - e.meta.exps[1]) : *e.meta.c;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
             if (m >= p.M) continue;
             const int row = e.sums ? m : e.meta.row[m];
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -561,7 +561,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     const long tiles_h = (long)cdiv(g.T, 64 * p->tile_h) * cdiv(g.D, 64 * p->tile_h), passes = cdiv(piece, p->split ? 32 : 64);
     while (tiles_h * p->slices_h < 256 && passes / (p->slices_h * 2) >= 8 && p->slices_h < 16) p->slices_h *= 2;
     p->parts = 0;
-    for (int k = 0; k < p->pieces; ++k) p->parts += 2 * cdiv((k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece), 64 * p->tile_z);
+    for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->tile_z);
     size_t o = 0;
     p->o_meta = o;
     o += meta_bytes(g.T);
@@ -660,7 +660,7 @@ hipError_t forward(const LossGeom &g, const LossPlan &p, const T *H, const T *W,
         m.batch = 1;
         e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(m, {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.tile_z, 1, st);
         if (e != hipSuccess) return e;
-        part0 += 2 * cdiv(n, 64 * p.tile_z);
+        part0 += (int)wave_columns(n, p.tile_z);
     }
     hipLaunchKernelGGL(join_kernel, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
     return hipGetLastError();

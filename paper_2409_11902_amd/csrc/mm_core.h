@@ -13,9 +13,10 @@
 //           the other, so that both formats are staged alike, 128 bytes of K to a row and pass.  Numbers are stored times a
 //           power of two that the caller takes out again, which keeps lo out of the subnormal range.
 //
-// A workgroup of four waves (2 x 2) owns a tile of 64 I x 64 I; a wave holds I x I accumulators of 32 x 32.  Tiles go from global memory
-// straight into one of two LDS buffers while the other is multiplied.  Lanes past a matrix's edge are given an offset past the
-// descriptor's range and load zeros.
+// A workgroup of WM x WN waves owns a tile of C; a wave holds MI x NI accumulators of 32 x 32.  Tiles go from global memory straight
+// into one of two LDS buffers while the other is multiplied, and a step's fragments are read while the step before is multiplied: the
+// workgroup meets once a pass, after the last fragments of a buffer are in registers, with a step's products still to issue.  Lanes past
+// a matrix's edge are given an offset past the descriptor's range and load zeros.
 #pragma once
 #include "common.h"
 
@@ -48,82 +49,82 @@ struct Params {
     int kt_slice;              // passes over K of one slice of the sum (blockIdx.y)
 };
 
-template <class P> constexpr int kPass = 64 / P::kParts; // terms of the sum in one pass
+template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of the sum in one pass, R bytes of K to a row
 
-// Which chunk of 16 bytes of a memory row stands where in LDS.  kAlong: 128-byte rows of which 32 are read at one chunk; kDown: 8
-// rows (0-3 and 8-11 of 16) are read together at 16 neighbouring columns.
-template <class P, Lay L, int T> __device__ __forceinline__ int swizzle(int row)
+// Which chunk of 16 bytes of a memory row stands where in LDS.  kAlong: rows of R bytes of which 16 are read together at one chunk; kDown: half a
+// wave reads 4 rows together at 32 neighbouring columns (of every other chunk where a row has two parts).
+template <class P, Lay L, int T, int R> __device__ __forceinline__ int swizzle(int row)
 {
-    if (L == Lay::kAlong) return (row >> 1) & 7;
-    if (P::kParts == 2) return ((row & 3) << 2) ^ ((row >> 3) & 1);
-    if (T == 64) return (((row >> 1) & 1) | ((row >> 2) & 2)) << 1;
-    return ((row & 3) | ((row >> 1) & 4)) << 1;
+    if (L == Lay::kAlong) return R == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+    if (P::kParts == 2) return ((row & 1) << 3) ^ ((row >> 1) & 1);
+    if (T == 64) return (row & 2) << 1;
+    return (row & 3) << 2;
 }
 
-// One operand's way into LDS: T rows of C (T = 64 I) by one pass of K, 128 T bytes.
-template <class P, Lay L, int T> struct Stage {
-    static constexpr int kLoads = T / 32;                                  // per wave and pass, 1 KiB each
-    static constexpr int kRowBytes = L == Lay::kAlong ? 128 : T * 2 * P::kParts;
-    static constexpr int kChunks = kRowBytes / 16;
-    const char *base;
-    long step;     // bytes from a pass to the next
-    uint32_t off[kLoads];
-    int row0, chunk, left_total;
-    long ld;
+// 16 bytes a lane from `offset` in `rs` to LDS, side by side from the uniform address `to` on.  Written out, because the compiler makes
+// every transposing LDS read that follows one of its own wait for all of them; meet() says when they have arrived.  No register is
+// written, so there is nothing that could be overwritten under way.
+__device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory"); // (m0 has no other use in these kernels)
+}
 
-    // first: first row of C; count: rows of C in the matrix; K: terms
-    __device__ __forceinline__ void init(const char *p, long ld_, int first, int count, int K, int kt0, int wave, int lane)
+// One operand's way into LDS: T rows of C by one pass of K, R T bytes, by NW waves.
+template <class P, Lay L, int T, int R, int NW> struct Stage {
+    static constexpr int kLoads = T * R / 1024 / NW;                       // per wave and pass, 1 KiB each
+    static constexpr int kRowBytes = L == Lay::kAlong ? R : T * 2 * P::kParts;
+    static constexpr int kChunks = kRowBytes / 16, kStep = NW * 64 / kChunks; // chunks of a row; rows from a load to the next
+    static_assert(kLoads * 1024 * NW == T * R && kStep * kChunks == NW * 64, "whole loads");
+    const char *base; // of the pass to load next
+    long step;        // bytes from a pass to the next
+    uint32_t off[kLoads];
+    int at;           // the lane's chunk of a row (kAlong), its first row (kDown)
+    int left;         // chunks (kAlong) or rows (kDown) of K from the pass to load next on
+
+    // first: first row of C; count: rows of C in the matrix; K: terms; kt: first pass, kt1: behind the last
+    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane)
     {
-        ld = ld_;
+        const int row0 = (wave * 64 + lane) / kChunks, slot = (wave * 64 + lane) % kChunks;
+        const int columns = P::kParts * ((count + 7) / 8) - first / 8 * P::kParts; // kDown: chunks from the tile's first on
         if (L == Lay::kAlong) {
-            chunk = (lane & 7) ^ (((wave & 1) << 2) + (lane >> 4));
-            row0 = 0;
-            left_total = P::kParts * ((K + 7) / 8); // chunks of a row
-            base = p + (long)first * ld + (long)kt0 * 128;
-            step = 128;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int row = (i * 4 + wave) * 8 + (lane >> 3);
-                off[i] = first + row < count ? (uint32_t)(row * (int)ld + chunk * 16) : kNowhere;
-            }
+            static_assert(L != Lay::kAlong || kStep % 16 == 0, "a lane's chunk is the same in every load");
+            at = slot ^ swizzle<P, L, T, R>(row0);
+            left = min(P::kParts * ((K + 7) / 8), kt1 * kChunks) - kt * kChunks;
+            base = p + (long)first * ld + (long)kt * R;
+            step = R;
         } else {
-            left_total = K; // rows of memory
-            base = p + (long)first * 2 * P::kParts + (long)kt0 * kPass<P> * ld;
-            step = kPass<P> * ld;
-            row0 = (wave * 64 + lane) / kChunks;
-            const int columns = P::kParts * ((count + 7) / 8) - first / 8 * P::kParts; // chunks from the tile's first on
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int row = row0 + i * (256 / kChunks);
-                const int c = ((wave * 64 + lane) % kChunks) ^ swizzle<P, L, T>(row);
-                off[i] = c < columns ? (uint32_t)(row * (int)ld + c * 16) : kNowhere;
-            }
-            chunk = 0;
+            at = row0;
+            left = min(K, kt1 * kPass<P, R>) - kt * kPass<P, R>;
+            base = p + (long)first * 2 * P::kParts + (long)kt * kPass<P, R> * ld;
+            step = kPass<P, R> * ld;
         }
-    }
-    // pass kt into LDS at byte address `lds`
-    __device__ __forceinline__ void load(int kt, int kt0, uint32_t lds, int wave)
-    {
-        const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base + (long)(kt - kt0) * step), 0, 0x7fffffff, 0x00020000);
-        const int left = L == Lay::kAlong ? left_total - kt * 8 : left_total - kt * kPass<P>;
-        const bool whole = left >= (L == Lay::kAlong ? 8 : kPass<P>);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            uint32_t o = off[i];
-            if (!whole) {
-                const int at = L == Lay::kAlong ? chunk : row0 + i * (256 / kChunks);
-                if (at >= left) o = kNowhere;
-            }
-            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * 4 + wave) * 1024);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(uintptr_t)to, 16, o, 0, 0, 0);
+            const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row);
+            const bool there = L == Lay::kAlong ? first + row < count : c < columns;
+            off[i] = there ? (uint32_t)(row * (int)ld + c * 16) : kNowhere;
         }
+    }
+    // the next pass into LDS at byte address `lds`; behind the last that is zeros
+    __device__ __forceinline__ void load(uint32_t lds, int wave)
+    {
+        const uint64_t from = (uint64_t)(uintptr_t)base;
+        const u32x4 rs = {(uint32_t)from, (uint32_t)(from >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t o = at + (L == Lay::kAlong ? 0 : i * kStep) < left ? off[i] : kNowhere;
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 1024);
+            load_to_lds(rs, o, to);
+        }
+        base += step;
+        left -= L == Lay::kAlong ? kChunks : kPass<P, R>;
     }
 };
 
 // Fragments of one operand: 32 rows of C by 16 terms, 8 terms to a lane (terms 8 * (lane / 32) on, row lane % 32).
-template <class P, Lay L, int T> struct Frag {
-    static constexpr int kRowBytes = Stage<P, L, T>::kRowBytes;
-    uint32_t at;  // the lane's place in block 0
+template <class P, Lay L, int T, int R> struct Frag {
+    static constexpr int kRowBytes = L == Lay::kAlong ? R : T * 2 * P::kParts;
+    uint32_t at;  // the lane's place in the wave's first block
     uint32_t x;   // what a chunk's number is combined with
     int block0;   // the wave's first block of 32 rows of C
 
@@ -131,12 +132,12 @@ template <class P, Lay L, int T> struct Frag {
     {
         block0 = block;
         if (L == Lay::kAlong) {
-            at = (block * 32 + (lane & 31)) * 128;
-            x = ((lane >> 1) & 7) ^ ((lane >> 5) * P::kParts);
+            at = (block * 32 + (lane & 31)) * R;
+            x = swizzle<P, L, T, R>(lane & 31) ^ ((lane >> 5) * P::kParts);
         } else {
             const int row = 8 * (lane >> 5) + ((lane & 15) >> 2);
             at = row * kRowBytes + (lane & 1) * 8;
-            x = swizzle<P, L, T>(row);
+            x = swizzle<P, L, T, R>(row);
         }
     }
     // block blk of the wave, 16 terms from 16 s on, part 0 (hi, or the only one) or 1 (lo)
@@ -146,7 +147,7 @@ template <class P, Lay L, int T> struct Frag {
         typedef __attribute__((address_space(3))) s16x8 lds8;
         if (L == Lay::kAlong) {
             const uint32_t c = x ^ (uint32_t)(s * 2 * P::kParts + part);
-            return *(lds8 *)(uintptr_t)(lds + at + blk * 4096 + (c << 4));
+            return *(lds8 *)(uintptr_t)(lds + at + blk * 32 * R + (c << 4));
         }
         const uint32_t col = (block0 + blk) * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
         const uint32_t c = (col * P::kParts + part) ^ x;
@@ -173,15 +174,33 @@ struct Place {
     int m0, n0;         // the wave's first row and column
     int M, N;           // extents, M as it really is
     int batch, slice;
-    int tn, wn;         // the tile's column, the wave's column in it
+    int tm, tn;         // the tile
+    int part;           // the wave's place among the waves that share a row of C
     int lane;
 };
 
-template <class P, Lay LA, Lay LB, int I, class Epi>
-__global__ void __launch_bounds__(256, I == 4 ? 1 : 2) mm_kernel(const Params p, const typename Epi::Params e)
+// How a workgroup's tile is made of waves' parts, and how it is staged: R bytes of K to a row and pass, ST passes in LDS.
+template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU> struct Shape {
+    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, R = R_, ST = ST_, kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int TM = 32 * MI * WM, TN = 32 * NI * WN, kBuffer = (TM + TN) * R, kLds = ST * kBuffer;
+    static constexpr int kPerSimd = PER_CU * kWaves / 4; // waves that registers are shared by
+};
+typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256
+typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128
+typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64
+
+// All but the N youngest loads have arrived, the fragments asked for are in registers, and every wave of the workgroup says so.
+template <int N> __device__ __forceinline__ void meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <class P, Lay LA, Lay LB, class S, class Epi>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Params p, const typename Epi::Params e)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    constexpr int T = 64 * I, kTile = T * 128;
+    constexpr int MI = S::MI, NI = S::NI, TM = S::TM, TN = S::TN;
+    constexpr int kSteps = S::R / 32 / P::kParts; // of 16 terms, in a pass
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = p.m_dev ? min(p.M, *p.m_dev) : p.M, K = p.k_dev ? min(p.K, *p.k_dev) : p.K;
 
@@ -193,80 +212,98 @@ __global__ void __launch_bounds__(256, I == 4 ? 1 : 2) mm_kernel(const Params p,
     const int batch = t / tiles, tt = t - batch * tiles;
     const int g0 = tt / (p.group * p.tiles_n) * p.group, gr = min(p.group, p.tiles_m - g0), gi = tt - g0 * p.tiles_n;
     const int tm = g0 + gi % gr, tn = gi / gr;
-    if (tm * T >= M) return;
+    if (tm * TM >= M) return;
     if (Epi::kSymmetric && tn < tm) return;
 
-    const int passes = (K + kPass<P> - 1) / kPass<P>;
+    const int passes = (K + kPass<P, S::R> - 1) / kPass<P, S::R>;
     const int kt0 = blockIdx.y * p.kt_slice, kt1 = min(passes, kt0 + p.kt_slice);
 
-    f32x16 acc[I][I];
+    f32x16 acc[MI][NI];
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < I; ++j)
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    Stage<P, LA, T> sa;
-    Stage<P, LB, T> sb;
-    sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * T, M, K, kt0, wave, lane);
-    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * T, p.N, K, kt0, wave, lane);
-    Frag<P, LA, T> fa;
-    Frag<P, LB, T> fb;
-    fa.init((wave >> 1) * I, lane);
-    fb.init((wave & 1) * I, lane);
+    Stage<P, LA, TM, S::R, S::kWaves> sa;
+    Stage<P, LB, TN, S::R, S::kWaves> sb;
+    sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane);
+    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane);
+    const int wm = wave / S::WN, wn = wave % S::WN;
+    Frag<P, LA, TM, S::R> fa;
+    Frag<P, LB, TN, S::R> fb;
+    fa.init(wm * MI, lane);
+    fb.init(wn * NI, lane);
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    const uint32_t lds_end = lds + S::kLds;
 
+    auto load = [&](uint32_t to) {
+        sa.load(to, wave);
+        sb.load(to + TM * S::R, wave);
+    };
+    s16x8 a[2][P::kParts][MI], b[2][P::kParts][NI];
+    auto read = [&](int r, uint32_t from, int s) {
+#pragma unroll
+        for (int h = 0; h < P::kParts; ++h) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) a[r][h][i] = fa.get(from, i, s, h, lane);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) b[r][h][j] = fb.get(from + TM * S::R, j, s, h, lane);
+        }
+    };
+    constexpr int kAhead = (S::ST - 2) * (decltype(sa)::kLoads + decltype(sb)::kLoads); // loads younger than the next pass's
     if (kt0 < kt1) {
-        sa.load(kt0, kt0, lds, wave);
-        sb.load(kt0, kt0, lds + kTile, wave);
-    }
-    for (int kt = kt0; kt < kt1; ++kt) {
-        const uint32_t cur = lds + ((kt - kt0) & 1) * 2 * kTile, nxt = lds + ((kt - kt0 + 1) & 1) * 2 * kTile;
-        __syncthreads();
-        if (kt + 1 < kt1) {
-            sa.load(kt + 1, kt0, nxt, wave);
-            sb.load(kt + 1, kt0, nxt + kTile, wave);
-        }
+        uint32_t cur = lds;
 #pragma unroll
-        for (int s = 0; s < 4 / P::kParts; ++s) {
-            s16x8 a[P::kParts][I], b[P::kParts][I];
+        for (int i = 0; i < S::ST - 1; ++i) load(lds + i * S::kBuffer);
+        meet<kAhead>();
+        load(lds_end - S::kBuffer);
+        read(0, lds, 0);
+        // (two passes a turn, for the fragments' registers to take turns; a pass past the end is zeros)
+        for (int kt = kt0; kt < kt1; kt += 2) {
 #pragma unroll
-            for (int h = 0; h < P::kParts; ++h)
-#pragma unroll
-                for (int i = 0; i < I; ++i) {
-                    a[h][i] = fa.get(cur, i, s, h, lane);
-                    b[h][i] = fb.get(cur + kTile, i, s, h, lane);
+            for (int k = 0; k < 2 * kSteps; ++k) {
+                const int s = k % kSteps;
+                if (s + 1 < kSteps) {
+                    read((k + 1) & 1, cur, s + 1);
+                } else {
+                    const uint32_t next = cur + S::kBuffer == lds_end ? lds : cur + S::kBuffer;
+                    meet<kAhead>(); // the next pass has arrived; this one's last fragments are in registers
+                    load(cur);
+                    read((k + 1) & 1, next, 0);
+                    cur = next;
                 }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < I; ++i)
+                for (int h = 0; h < 2 * P::kParts - 1; ++h) // hi hi, then hi lo and lo hi
 #pragma unroll
-                for (int j = 0; j < I; ++j) {
-                    acc[i][j] = product<P>(b[0][j], a[0][i], acc[i][j]);
-                    if (P::kParts == 2) {
-                        acc[i][j] = product<P>(b[P::kParts - 1][j], a[0][i], acc[i][j]);
-                        acc[i][j] = product<P>(b[0][j], a[P::kParts - 1][i], acc[i][j]);
-                    }
-                }
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) acc[i][j] = product<P>(b[k & 1][h & 1][j], a[k & 1][h >> 1][i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+        meet<0>(); // nothing is on its way into LDS when the workgroup ends
     }
     Place at;
-    at.m0 = tm * T + (wave >> 1) * 32 * I;
-    at.n0 = tn * T + (wave & 1) * 32 * I;
+    at.m0 = tm * TM + wm * 32 * MI;
+    at.n0 = tn * TN + wn * 32 * NI;
     at.M = M;
     at.N = p.N;
     at.batch = batch;
     at.slice = blockIdx.y;
+    at.tm = tm;
     at.tn = tn;
-    at.wn = wave & 1;
+    at.part = tn * S::WN + wn;
     at.lane = lane;
-    Epi::template run<I>(e, acc, at);
+    Epi::template run<MI, NI>(e, acc, at);
 }
 
 // ---- host
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
-// The tile's edge for a product of this size, in units of 64.
+// The tile's edge for a product of this size, in units of 64: the largest that gives every compute unit one.
 inline int choose_tile(long M, long N, int batch, int slices)
 {
     for (int i : {4, 2}) {
@@ -275,29 +312,30 @@ inline int choose_tile(long M, long N, int batch, int slices)
     }
     return 1;
 }
+// parts that a row's columns fall into, one to a wave
+inline long wave_columns(long N, int tile) { return tile == 4 ? cdiv(N, Big::TN) * Big::WN : tile == 2 ? cdiv(N, Middle::TN) * Middle::WN : cdiv(N, Small::TN) * Small::WN; }
 
-template <class P, Lay LA, Lay LB, class Epi, int I>
-hipError_t launch_tile(Params p, const typename Epi::Params &e, int slices, hipStream_t st)
+template <class P, Lay LA, Lay LB, class S, class Epi>
+hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hipStream_t st)
 {
-    constexpr int lds = 4 * 64 * I * 128;
-    static const hipError_t attr =
-        hipFuncSetAttribute(reinterpret_cast<const void *>(mm_kernel<P, LA, LB, I, Epi>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(mm_kernel<P, LA, LB, S, Epi>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
     if (attr != hipSuccess) return attr;
-    p.tiles_m = cdiv(p.M, 64 * I);
-    p.tiles_n = cdiv(p.N, 64 * I);
+    p.tiles_m = cdiv(p.M, S::TM);
+    p.tiles_n = cdiv(p.N, S::TN);
     p.group = 8;
-    p.kt_slice = cdiv(cdiv(p.K, kPass<P>), slices);
+    p.kt_slice = cdiv(cdiv(p.K, kPass<P, S::R>), slices);
     const long total = (long)p.tiles_m * p.tiles_n * p.batch;
-    hipLaunchKernelGGL((mm_kernel<P, LA, LB, I, Epi>), dim3((unsigned)(8 * ((total + 7) / 8)), slices), dim3(256), lds, st, p, e);
+    hipLaunchKernelGGL((mm_kernel<P, LA, LB, S, Epi>), dim3((unsigned)(8 * ((total + 7) / 8)), slices), dim3(S::kThreads), S::kLds, st, p, e);
     return hipGetLastError();
 }
 
 template <class P, Lay LA, Lay LB, class Epi>
 hipError_t launch(const Params &p, const typename Epi::Params &e, int tile, int slices, hipStream_t st)
 {
-    if (tile == 4) return launch_tile<P, LA, LB, Epi, 4>(p, e, slices, st);
-    if (tile == 2) return launch_tile<P, LA, LB, Epi, 2>(p, e, slices, st);
-    return launch_tile<P, LA, LB, Epi, 1>(p, e, slices, st);
+    if (tile == 4) return launch_shape<P, LA, LB, Big, Epi>(p, e, slices, st);
+    if (tile == 2) return launch_shape<P, LA, LB, Middle, Epi>(p, e, slices, st);
+    return launch_shape<P, LA, LB, Small, Epi>(p, e, slices, st);
 }
 
 // ---- a float as two halves

@@ -27,13 +27,13 @@ constexpr int kMaxSumBlocks = 256;
 struct Gram {
     static constexpr bool kSymmetric = true;
     struct Params { char *out; long ld, stride; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p);
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p);
 };
 // a I + b A + c A A
 struct Poly {
     static constexpr bool kSymmetric = true;
     struct Params { char *out; long ld, stride; const char *a; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p);
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p);
 };
 
 // v of row m, columns n..n+3 of a symmetric matrix, to its place and, off the diagonal tiles, to the mirrored one
@@ -53,15 +53,15 @@ __device__ __forceinline__ void store_symmetric(char *out, long ld, int m, int n
         }
 }
 
-template <int I> __device__ __forceinline__ void Gram::run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+template <int MI, int NI> __device__ __forceinline__ void Gram::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
 {
     char *out = e.out + p.batch * e.stride;
     const int Np = (p.N + 7) & ~7;
-    const bool mirror = p.m0 / (64 * I) != p.tn;
+    const bool mirror = p.tm != p.tn;
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < I; ++j)
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -72,16 +72,16 @@ template <int I> __device__ __forceinline__ void Gram::run(const Params &e, cons
             }
 }
 
-template <int I> __device__ __forceinline__ void Poly::run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+template <int MI, int NI> __device__ __forceinline__ void Poly::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
 {
     char *out = e.out + p.batch * e.stride;
     const char *a = e.a + p.batch * e.stride;
     const int Np = (p.N + 7) & ~7;
-    const bool mirror = p.m0 / (64 * I) != p.tn;
+    const bool mirror = p.tm != p.tn;
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < I; ++j)
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -98,14 +98,14 @@ template <int I> __device__ __forceinline__ void Poly::run(const Params &e, cons
 struct Next {
     static constexpr bool kSymmetric = false;
     struct Params { char *out; long ld, stride; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         char *out = e.out + p.batch * e.stride;
         const int Np = (p.N + 7) & ~7;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
@@ -121,14 +121,14 @@ struct Next {
 template <typename T, bool UPDATE> struct Last {
     static constexpr bool kSymmetric = false;
     struct Params { T *out; float keep, scale; };
-    template <int I> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[I][I], const Place &p)
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         T *out = e.out + (long)p.batch * p.M * p.N;
         const bool wide = (p.N & 3) == 0; // rows in whole groups of four: one access for a lane's four
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < I; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
