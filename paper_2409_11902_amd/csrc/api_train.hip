@@ -6,6 +6,8 @@
 
 namespace cac {
 
+static int tile_edge(const TileChoice &c) { return 64 * (c.shape + 1); }
+
 static int make_loss_geom(const cac_loss_desc *d, LossGeom *g)
 {
     if (!d) return fail(CAC_ERR_INVALID_ARG, "descriptor is NULL");
@@ -80,13 +82,10 @@ int cac_loss_describe_plan(const cac_loss_desc *d, int op, char *buf, size_t buf
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
     LossPlan p;
     plan_loss(g, op == CAC_LOSS_BWD, &p);
-    if (op == CAC_LOSS_FWD)
-        snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d", p.split ? "two halves" : "bfloat16",
-                 p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, 64 * p.tile_z);
-    else
-        snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d, dW tile %d, dH tile %d in %d slices",
-                 p.split ? "two halves" : "bfloat16", p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, 64 * p.tile_z, 64 * p.tile_w,
-                 64 * p.tile_h, p.slices_h);
+    const int n = snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d", p.split ? "two halves" : "bfloat16",
+                           p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, tile_edge(p.z));
+    if (op == CAC_LOSS_BWD && n > 0 && (size_t)n < buf_len)
+        snprintf(buf + n, buf_len - n, ", dW tile %d, dH tile %d in %d slices", tile_edge(p.w), tile_edge(p.h), p.h.slices);
     return CAC_OK;
 }
 
@@ -147,8 +146,8 @@ int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
     MuonPlan p;
     plan_muon(g, &p);
-    snprintf(buf, buf_len, "%s, square products of %ld, tiles %d (square) and %d", p.tall ? "X^T X" : "X X^T", p.r, 64 * p.tile_gram,
-             64 * p.tile_apply);
+    snprintf(buf, buf_len, "%s, square products of %ld: tile %d in %d slices, then %d; tile %d", p.tall ? "X^T X" : "X X^T", p.r, tile_edge(p.gram),
+             p.gram.slices, tile_edge(p.poly), tile_edge(p.apply));
     return CAC_OK;
 }
 

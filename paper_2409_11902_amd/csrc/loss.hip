@@ -326,10 +326,21 @@ __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float 
     const int j = blockIdx.x * 16 + r;
     float top = -INFINITY, sum = 0.f;
     if (j < count)
-        for (int k = s; k < parts; k += 16) {
-            const float t = part[2L * k * T_rows + j], u = part[(2L * k + 1) * T_rows + j];
-            const float m = fmaxf(top, t), shift = m == -INFINITY ? 0.f : m;
-            sum = sum * __builtin_amdgcn_exp2f((top - shift) * kLog2e) + u * __builtin_amdgcn_exp2f((t - shift) * kLog2e);
+        for (int k0 = s; k0 < parts; k0 += 128) { // eight parts on their way at a time
+            float t[8], u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = k0 + e * 16;
+                t[e] = k < parts ? part[2L * k * T_rows + j] : -INFINITY;
+                u[e] = k < parts ? part[(2L * k + 1) * T_rows + j] : 0.f;
+            }
+            float m = top;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, t[e]);
+            const float shift = m == -INFINITY ? 0.f : m;
+            sum *= __builtin_amdgcn_exp2f((top - shift) * kLog2e);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += u[e] * __builtin_amdgcn_exp2f((t[e] - shift) * kLog2e);
             top = m;
         }
     __shared__ float tops[16][17], sums[16][17];
@@ -554,14 +565,11 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     if (p->pieces > 1) piece = ((g.V + p->pieces - 1) / p->pieces + 255) / 256 * 256;
     p->pieces = (int)((g.V + piece - 1) / piece);
     p->piece = piece;
-    p->tile_z = choose_tile(g.T, piece, 1, 1);
-    p->tile_w = choose_tile(piece, g.D, 1, 1);
-    p->tile_h = choose_tile(g.T, g.D, 1, 1);
-    p->slices_h = 1;
-    const long tiles_h = (long)cdiv(g.T, 64 * p->tile_h) * cdiv(g.D, 64 * p->tile_h), passes = cdiv(piece, p->split ? 32 : 64);
-    while (tiles_h * p->slices_h < 256 && passes / (p->slices_h * 2) >= 8 && p->slices_h < 16) p->slices_h *= 2;
+    p->z = choose(p->split, g.T, piece, 1, g.D, false, 1);
+    p->w = choose(p->split, piece, g.D, 1, g.T, false, 1);
+    p->h = choose(p->split, g.T, g.D, 1, piece, false, 16);
     p->parts = 0;
-    for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->tile_z);
+    for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->z.shape);
     size_t o = 0;
     p->o_meta = o;
     o += meta_bytes(g.T);
@@ -574,7 +582,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->o_g = o;
     if (backward) o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * (p->split ? 4 : 2));
     p->o_acc = o;
-    if (backward && (p->pieces > 1 || p->slices_h > 1)) o += up256((size_t)p->slices_h * g.T * g.D * 4);
+    if (backward && (p->pieces > 1 || p->h.slices > 1)) o += up256((size_t)p->h.slices * g.T * g.D * 4);
     p->bytes = o;
 }
 
@@ -658,9 +666,9 @@ hipError_t forward(const LossGeom &g, const LossPlan &p, const T *H, const T *W,
         m.K = (int)g.D;
         m.m_dev = meta.count;
         m.batch = 1;
-        e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(m, {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.tile_z, 1, st);
+        e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(m, {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.z, st);
         if (e != hipSuccess) return e;
-        part0 += (int)wave_columns(n, p.tile_z);
+        part0 += (int)wave_columns(n, p.z.shape);
     }
     hipLaunchKernelGGL(join_kernel, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
     return hipGetLastError();
@@ -676,7 +684,7 @@ hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W
     if (e != hipSuccess) return e;
     char *G = ws + p.o_g;
     const long ld_g = (p.piece + 7) / 8 * 8 * (p.split ? 4 : 2);
-    const bool sums = p.pieces > 1 || p.slices_h > 1;
+    const bool sums = p.pieces > 1 || p.h.slices > 1;
     for (long v0 = 0; v0 < g.V; v0 += p.piece) {
         const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
         const void *w;
@@ -692,7 +700,7 @@ hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W
         m.K = (int)g.D;
         m.m_dev = meta.count;
         m.batch = 1;
-        e = launch<P, Lay::kAlong, Lay::kAlong, Grad<T>>(m, {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.tile_z, 1, st);
+        e = launch<P, Lay::kAlong, Lay::kAlong, Grad<T>>(m, {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
         if (e != hipSuccess) return e;
         if (dW) {
             Params d{};
@@ -705,7 +713,7 @@ hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W
             d.K = (int)g.T;
             d.k_dev = meta.count;
             d.batch = 1;
-            e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(d, {dW + v0 * g.D, meta}, p.tile_w, 1, st);
+            e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(d, {dW + v0 * g.D, meta}, p.w, st);
             if (e != hipSuccess) return e;
         }
         if (dH) {
@@ -719,8 +727,7 @@ hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W
             d.K = (int)n;
             d.m_dev = meta.count;
             d.batch = 1;
-            e = launch<P, Lay::kAlong, Lay::kDown, OutH<T>>(d, {dH, sums ? (float *)(ws + p.o_acc) : nullptr, g.T * g.D, v0 > 0, meta}, p.tile_h,
-                                                           p.slices_h, st);
+            e = launch<P, Lay::kAlong, Lay::kDown, OutH<T>>(d, {dH, sums ? (float *)(ws + p.o_acc) : nullptr, g.T * g.D, v0 > 0, meta}, p.h, st);
             if (e != hipSuccess) return e;
         }
         if (db) {
@@ -730,7 +737,7 @@ hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W
     }
     if (dH && sums) {
         hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_acc), g.T * g.D,
-                           p.slices_h, (int)g.D, dH);
+                           p.h.slices, (int)g.D, dH);
         e = hipGetLastError();
     }
     return e;

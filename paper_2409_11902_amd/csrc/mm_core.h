@@ -18,7 +18,7 @@
 // workgroup meets once a pass, after the last fragments of a buffer are in registers, with a step's products still to issue.  Lanes past
 // a matrix's edge are given an offset past the descriptor's range and load zeros.
 #pragma once
-#include "common.h"
+#include "train_ends.h"
 
 namespace cac {
 namespace mm {
@@ -45,8 +45,9 @@ struct Params {
     int M, N, K;
     const int *m_dev, *k_dev;  // where set: the rows (the terms) that there really are, at most M (K)
     int tiles_m, tiles_n, batch;
+    int tiles;                 // of one matrix: tiles_m * tiles_n, or those on and above the diagonal
     int group;                 // tile rows that one XCD walks together
-    int kt_slice;              // passes over K of one slice of the sum (blockIdx.y)
+    int kt_slice;              // passes over K of one slice of the sum
 };
 
 template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of the sum in one pass, R bytes of K to a row
@@ -186,6 +187,7 @@ template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU> struc
     static constexpr int kPerSimd = PER_CU * kWaves / 4; // waves that registers are shared by
 };
 typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256
+typedef Shape<2, 6, 3, 1, 128, 3, 1> Wide;   // 192 x 192
 typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128
 typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64
 
@@ -195,28 +197,36 @@ template <int N> __device__ __forceinline__ void meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// One workgroup's tile, as workgroup `block` of the product; slice: which part of the sum.
 template <class P, Lay LA, Lay LB, class S, class Epi>
-__global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Params p, const typename Epi::Params e)
+__device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Params &e, int block, int slice, unsigned char *smem)
 {
-    extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int MI = S::MI, NI = S::NI, TM = S::TM, TN = S::TN;
     constexpr int kSteps = S::R / 32 / P::kParts; // of 16 terms, in a pass
+    constexpr int kTurn = kSteps % 2 ? 2 : 1;     // passes after which the fragments' registers are the same again
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = p.m_dev ? min(p.M, *p.m_dev) : p.M, K = p.k_dev ? min(p.K, *p.k_dev) : p.K;
 
     // Workgroups go round the eight XCDs: each XCD gets a run of neighbouring tiles, and walks it in groups of `group` tile rows.
-    const int tiles = p.tiles_m * p.tiles_n;
-    const int per = (tiles * p.batch + 7) / 8;
-    const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || t >= tiles * p.batch) return;
-    const int batch = t / tiles, tt = t - batch * tiles;
-    const int g0 = tt / (p.group * p.tiles_n) * p.group, gr = min(p.group, p.tiles_m - g0), gi = tt - g0 * p.tiles_n;
-    const int tm = g0 + gi % gr, tn = gi / gr;
+    const int per = (p.tiles * p.batch + 7) / 8;
+    const int t = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || t >= p.tiles * p.batch) return;
+    const int batch = t / p.tiles, tt = t - batch * p.tiles;
+    int tm, tn;
+    if (Epi::kSymmetric) { // the tiles on and above the diagonal, row by row: row i has tiles_m - i
+        tm = (int)(p.tiles_m + 0.5f - sqrtf((p.tiles_m + 0.5f) * (p.tiles_m + 0.5f) - 2.f * tt));
+        while (tm > 0 && tm * p.tiles_m - tm * (tm - 1) / 2 > tt) --tm;
+        while ((tm + 1) * p.tiles_m - (tm + 1) * tm / 2 <= tt) ++tm;
+        tn = tt - (tm * p.tiles_m - tm * (tm - 1) / 2) + tm;
+    } else {
+        const int g0 = tt / (p.group * p.tiles_n) * p.group, gr = min(p.group, p.tiles_m - g0), gi = tt - g0 * p.tiles_n;
+        tm = g0 + gi % gr;
+        tn = gi / gr;
+    }
     if (tm * TM >= M) return;
-    if (Epi::kSymmetric && tn < tm) return;
 
     const int passes = (K + kPass<P, S::R> - 1) / kPass<P, S::R>;
-    const int kt0 = blockIdx.y * p.kt_slice, kt1 = min(passes, kt0 + p.kt_slice);
+    const int kt0 = slice * p.kt_slice, kt1 = min(passes, kt0 + p.kt_slice);
 
     f32x16 acc[MI][NI];
 #pragma unroll
@@ -260,10 +270,9 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Para
         meet<kAhead>();
         load(lds_end - S::kBuffer);
         read(0, lds, 0);
-        // (two passes a turn, for the fragments' registers to take turns; a pass past the end is zeros)
-        for (int kt = kt0; kt < kt1; kt += 2) {
+        for (int kt = kt0; kt < kt1; kt += kTurn) { // (a pass behind the last is zeros)
 #pragma unroll
-            for (int k = 0; k < 2 * kSteps; ++k) {
+            for (int k = 0; k < kTurn * kSteps; ++k) {
                 const int s = k % kSteps;
                 if (s + 1 < kSteps) {
                     read((k + 1) & 1, cur, s + 1);
@@ -292,7 +301,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Para
     at.M = M;
     at.N = p.N;
     at.batch = batch;
-    at.slice = blockIdx.y;
+    at.slice = slice;
     at.tm = tm;
     at.tn = tn;
     at.part = tn * S::WN + wn;
@@ -300,42 +309,96 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Para
     Epi::template run<MI, NI>(e, acc, at);
 }
 
+template <class P, Lay LA, Lay LB, class S, class Epi>
+__global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Params p, const typename Epi::Params e)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    mm_tile<P, LA, LB, S, Epi>(p, e, blockIdx.x, blockIdx.y, smem);
+}
+
 // ---- host
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
-// The tile's edge for a product of this size, in units of 64: the largest that gives every compute unit one.
-inline int choose_tile(long M, long N, int batch, int slices)
+// Which tile a product takes, and in how many slices its sum is formed.
+enum { kSmall, kMiddle, kWide, kBig, kShapes };
+typedef TileChoice Choice;
+constexpr int kEdge[kShapes] = {64, 128, 192, 256};
+inline int wave_columns_of(int shape) { return shape == kSmall ? Small::WN : shape == kMiddle ? Middle::WN : shape == kWide ? Wide::WN : Big::WN; }
+
+// Microseconds of a product, from what a pass measured: on a compute unit with one workgroup, and with as many as it holds.
+inline double product_us(int shape, bool split, long tiles, int passes, int slices)
 {
-    for (int i : {4, 2}) {
-        const long tiles = (long)cdiv(M, 64 * i) * cdiv(N, 64 * i) * batch * slices;
-        if (tiles >= 256) return i;
+    static const int kHolds[kShapes] = {3, 2, 1, 1};
+    static const double kAlone[kShapes][2] = {{0.27, 0.27}, {0.77, 0.80}, {1.4, 1.75}, {1.95, 2.85}}, kFull[kShapes][2] = {{0.62, 0.95}, {1.12, 1.5}, {1.4, 1.75}, {1.95, 2.85}},
+                        kOnce[kShapes] = {2.5, 3.5, 5.0, 6.0};
+    const long wgs = tiles * slices, round = 256L * kHolds[shape];
+    const double n = cdiv(passes, slices), rest = (double)(wgs % round);
+    double us = (wgs / round) * (kFull[shape][split] * n + kOnce[shape]);
+    if (rest > 0) {
+        const double share = rest <= 256 ? 0.0 : (rest - 256) / (round - 256);
+        us += (kAlone[shape][split] + share * (kFull[shape][split] - kAlone[shape][split])) * n + kOnce[shape];
     }
-    return 1;
+    return us;
+}
+inline long tiles_of(int shape, long M, long N, bool symmetric)
+{
+    const long m = cdiv(M, kEdge[shape]), n = cdiv(N, kEdge[shape]);
+    return symmetric ? m * (m + 1) / 2 : m * n;
+}
+// The cheapest of them; more than one slice costs the writing and reading of that many sums of 32 bits, and a launch.
+inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetric, int max_slices)
+{
+    Choice best{kSmall, 1};
+    double least = 1e30;
+    for (int shape = 0; shape < kShapes; ++shape) {
+        if (shape == kWide && !split) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
+        const long tiles = tiles_of(shape, M, N, symmetric) * batch;
+        const int passes = cdiv(K, split ? 32 : 64);
+        for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices < 8 ? 2 : 4) {
+            if (slices > 1 && passes / slices < 4) break;
+            if (slices > 1 && tiles * slices > 2048) break;
+            double us = product_us(shape, split, tiles, passes, slices);
+            if (slices > 1) us += 4.0 + 8e-6 / 2.5 * slices * tiles * kEdge[shape] * kEdge[shape];
+            if (us < least) {
+                least = us;
+                best = Choice{shape, slices};
+            }
+        }
+    }
+    return best;
 }
 // parts that a row's columns fall into, one to a wave
-inline long wave_columns(long N, int tile) { return tile == 4 ? cdiv(N, Big::TN) * Big::WN : tile == 2 ? cdiv(N, Middle::TN) * Middle::WN : cdiv(N, Small::TN) * Small::WN; }
+inline long wave_columns(long N, int shape) { return (long)cdiv(N, kEdge[shape]) * wave_columns_of(shape); }
 
+// Fills in the tiles; returns the workgroups of one slice.
+template <class S> inline unsigned place_tiles(Params *p, bool symmetric, int slices, int pass)
+{
+    p->tiles_m = cdiv(p->M, S::TM);
+    p->tiles_n = cdiv(p->N, S::TN);
+    p->tiles = symmetric ? p->tiles_m * (p->tiles_m + 1) / 2 : p->tiles_m * p->tiles_n;
+    p->group = 8;
+    p->kt_slice = cdiv(cdiv(p->K, pass), slices);
+    return (unsigned)(8 * (((long)p->tiles * p->batch + 7) / 8));
+}
 template <class P, Lay LA, Lay LB, class S, class Epi>
 hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hipStream_t st)
 {
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(mm_kernel<P, LA, LB, S, Epi>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
     if (attr != hipSuccess) return attr;
-    p.tiles_m = cdiv(p.M, S::TM);
-    p.tiles_n = cdiv(p.N, S::TN);
-    p.group = 8;
-    p.kt_slice = cdiv(cdiv(p.K, kPass<P, S::R>), slices);
-    const long total = (long)p.tiles_m * p.tiles_n * p.batch;
-    hipLaunchKernelGGL((mm_kernel<P, LA, LB, S, Epi>), dim3((unsigned)(8 * ((total + 7) / 8)), slices), dim3(S::kThreads), S::kLds, st, p, e);
+    const unsigned blocks = place_tiles<S>(&p, Epi::kSymmetric, slices, kPass<P, S::R>);
+    hipLaunchKernelGGL((mm_kernel<P, LA, LB, S, Epi>), dim3(blocks, slices), dim3(S::kThreads), S::kLds, st, p, e);
     return hipGetLastError();
 }
 
 template <class P, Lay LA, Lay LB, class Epi>
-hipError_t launch(const Params &p, const typename Epi::Params &e, int tile, int slices, hipStream_t st)
+hipError_t launch(const Params &p, const typename Epi::Params &e, Choice c, hipStream_t st)
 {
-    if (tile == 4) return launch_shape<P, LA, LB, Big, Epi>(p, e, slices, st);
-    if (tile == 2) return launch_shape<P, LA, LB, Middle, Epi>(p, e, slices, st);
-    return launch_shape<P, LA, LB, Small, Epi>(p, e, slices, st);
+    if (c.shape == kBig) return launch_shape<P, LA, LB, Big, Epi>(p, e, c.slices, st);
+    if constexpr (P::kParts == 2)
+        if (c.shape == kWide) return launch_shape<P, LA, LB, Wide, Epi>(p, e, c.slices, st);
+    if (c.shape == kMiddle) return launch_shape<P, LA, LB, Middle, Epi>(p, e, c.slices, st);
+    return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
 }
 
 // ---- a float as two halves

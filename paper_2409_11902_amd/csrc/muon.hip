@@ -94,6 +94,45 @@ template <int MI, int NI> __device__ __forceinline__ void Poly::run(const Params
             }
 }
 
+// a slice's part of S, in float, [slice][batch][r][ld]
+struct GramPart {
+    static constexpr bool kSymmetric = true;
+    struct Params { float *out; int ld, batch; };
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+    {
+        float *out = e.out + ((long)p.slice * e.batch + p.batch) * p.N * e.ld;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
+                    if (m < p.M && n < e.ld)
+                        *(f32x4 *)(out + (long)m * e.ld + n) = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                }
+    }
+};
+// ... and S from the slices' parts: 32 x 32 of it to a block, of which a thread has four neighbours of a row
+__global__ void __launch_bounds__(256) join_gram_kernel(const float *__restrict__ part, int r, int ld, int batches, int slices, int tile,
+                                                        char *__restrict__ out, long ld_out)
+{
+    if (blockIdx.x * 32 / tile < blockIdx.y * 32 / tile) return; // (below the diagonal's tiles: written as the mirror image)
+    const bool mirror = blockIdx.x * 32 / tile != blockIdx.y * 32 / tile;
+    // neighbouring threads take neighbouring rows, as the mirrored stores want them
+    const int m = blockIdx.y * 32 + (threadIdx.x & 31), n = blockIdx.x * 32 + (threadIdx.x >> 5) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (m < r && n < ld)
+        for (int s = 0; s < slices; ++s) {
+            const f32x4 x = *(const f32x4 *)(part + (((long)s * batches + blockIdx.z) * r + m) * ld + n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= kTake;
+    store_symmetric(out + blockIdx.z * r * ld_out, ld_out, m, n, r, (r + 7) & ~7, mirror, v);
+}
+
 // the next X
 struct Next {
     static constexpr bool kSymmetric = false;
@@ -271,8 +310,9 @@ void plan_muon(const MuonGeom &g, MuonPlan *p)
     p->r = p->tall ? g.cols : g.rows;
     p->ld_x = (g.cols + 31) / 32 * 128;
     p->ld_a = (p->r + 31) / 32 * 128;
-    p->tile_gram = p->tile_poly = choose_tile(p->r, p->r, g.batch, 1);
-    p->tile_apply = choose_tile(g.rows, g.cols, g.batch, 1);
+    p->gram = choose(true, p->r, p->r, g.batch, p->tall ? g.rows : g.cols, true, 16);
+    p->poly = choose(true, p->r, p->r, g.batch, p->r, true, 1);
+    p->apply = choose(true, g.rows, g.cols, g.batch, p->r, false, 1);
     const long size = g.rows * g.cols;
     p->sum_blocks = (int)(size / 8192 < 1 ? 1 : size / 8192 > kMaxSumBlocks ? kMaxSumBlocks : size / 8192);
     size_t o = 0;
@@ -286,6 +326,8 @@ void plan_muon(const MuonGeom &g, MuonPlan *p)
     o += up((size_t)g.batch * p->r * p->ld_a);
     p->o_b = o;
     o += up((size_t)g.batch * p->r * p->ld_a);
+    p->o_part = o;
+    if (p->gram.slices > 1) o += up((size_t)p->gram.slices * g.batch * p->r * ((p->r + 3) & ~3L) * 4);
     p->bytes = o;
 }
 
@@ -317,8 +359,8 @@ hipError_t launch_apply(const MuonGeom &g, const MuonPlan &p, const char *x, con
     m.ldb = p.tall ? p.ld_a : p.ld_x;
     m.a_batch = p.tall ? sx : sb;
     m.b_batch = p.tall ? sb : sx;
-    if (p.tall) return launch<Split, Lay::kAlong, Lay::kAlong, Epi>(m, e, p.tile_apply, 1, st);
-    return launch<Split, Lay::kAlong, Lay::kDown, Epi>(m, e, p.tile_apply, 1, st);
+    if (p.tall) return launch<Split, Lay::kAlong, Lay::kAlong, Epi>(m, e, p.apply, st);
+    return launch<Split, Lay::kAlong, Lay::kDown, Epi>(m, e, p.apply, st);
 }
 
 } // namespace
@@ -341,15 +383,26 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
         m.M = m.N = (int)p.r;
         m.K = (int)(p.tall ? g.rows : g.cols);
         m.batch = g.batch;
-        const Gram::Params eg{a, p.ld_a, sa};
-        e = p.tall ? launch<Split, Lay::kDown, Lay::kDown, Gram>(m, eg, p.tile_gram, 1, st)
-                   : launch<Split, Lay::kAlong, Lay::kAlong, Gram>(m, eg, p.tile_gram, 1, st);
+        if (p.gram.slices == 1) {
+            const Gram::Params eg{a, p.ld_a, sa};
+            e = p.tall ? launch<Split, Lay::kDown, Lay::kDown, Gram>(m, eg, p.gram, st) : launch<Split, Lay::kAlong, Lay::kAlong, Gram>(m, eg, p.gram, st);
+        } else {
+            float *part = (float *)(ws + p.o_part);
+            const int ld = (int)((p.r + 3) & ~3L);
+            const GramPart::Params eg{part, ld, g.batch};
+            e = p.tall ? launch<Split, Lay::kDown, Lay::kDown, GramPart>(m, eg, p.gram, st)
+                       : launch<Split, Lay::kAlong, Lay::kAlong, GramPart>(m, eg, p.gram, st);
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL(join_gram_kernel, dim3(cdiv(p.r, 32), cdiv(p.r, 32), g.batch), dim3(256), 0, st, (const float *)part, (int)p.r, ld, g.batch,
+                               p.gram.slices, kEdge[p.gram.shape], a, p.ld_a);
+            e = hipGetLastError();
+        }
         if (e != hipSuccess) return e;
         m.a = m.b = a;
         m.lda = m.ldb = p.ld_a;
         m.a_batch = m.b_batch = sa;
         m.K = (int)p.r;
-        e = launch<Split, Lay::kAlong, Lay::kAlong, Poly>(m, Poly::Params{b, p.ld_a, sa, a}, p.tile_poly, 1, st);
+        e = launch<Split, Lay::kAlong, Lay::kAlong, Poly>(m, Poly::Params{b, p.ld_a, sa, a}, p.poly, st);
         if (e != hipSuccess) return e;
         if (s + 1 < g.steps) {
             e = launch_apply<Next>(g, p, x, b, Next::Params{ws + p.o_x[(s + 1) & 1], p.ld_x, sx}, st);

@@ -4,6 +4,8 @@
 
 namespace cac {
 
+struct TileChoice { int shape, slices; }; // of a product (mm_core.h)
+
 // ---- loss.hip: softmax cross entropy of a linear classifier
 struct LossGeom {
     long T, D, V;
@@ -19,8 +21,7 @@ struct LossPlan {
     long row_bytes;   // of a packed row
     long piece;       // classes in one piece
     int pieces;
-    // forward: tile of the logits; backward: tiles and slices of the three products
-    int tile_z, tile_w, tile_h, slices_h;
+    TileChoice z, w, h; // the logits' product, dW's, dH's
     long parts;       // forward: maximum and sum, this many for every row
     size_t o_meta, o_h, o_w, o_part, o_g, o_acc, bytes;
 };
@@ -40,9 +41,9 @@ struct MuonPlan {
     bool tall;          // more rows than columns: X^T X in the place of X X^T
     long r;             // the shorter side
     long ld_x, ld_a;    // bytes of a row
-    int tile_gram, tile_poly, tile_apply;
+    TileChoice gram, poly, apply;
     int sum_blocks;     // partial sums of squares of one matrix
-    size_t o_sum, o_x[2], o_a, o_b, bytes;
+    size_t o_sum, o_x[2], o_a, o_b, o_part, bytes;
 };
 void plan_muon(const MuonGeom &g, MuonPlan *p);
 // M, W: null where only O is asked for; O: null where the weights are updated
