@@ -19,10 +19,22 @@ using namespace mm;
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStoreG = 14;        // G is stored times 2^14 as two halves: |G| <= 1, and 1e-8 is still a normal number
-constexpr int kMaxParts = 512;     // blocks that look for a matrix's largest number
+constexpr int kMaxParts = 1024;    // blocks that look for a matrix's largest number
 
-// What the passes over compact rows know about them.
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+}
+
+// What the passes over compact rows know about them.  With few rows nothing is compacted: row m is row m of H, and what is known
+// about it is looked up where the caller has it.
 struct Meta {
+    bool direct;
+    int T;
+    Counts counts;
+    const float *lse_in, *gloss;
     int *count;       // [0]: rows that count
     int *exps;        // H and W are stored times 2^exps[0] and 2^exps[1] as two halves
     float *c;         // [0]: the largest of the rows' gradients
@@ -31,12 +43,34 @@ struct Meta {
     float *q, *lse;
     float *zlabel;    // forward: the label's logit
     float *top;       // kMaxParts of H, then of W: largest magnitudes
+
+    __device__ __forceinline__ int rows() const { return direct ? T : *count; }
+    __device__ __forceinline__ int row_of(int m) const { return direct ? m : row[m]; }
+    // of row m: its class, no class (kOut) where it does not count
+    __device__ __forceinline__ int label_of(int m) const { return direct ? (counts(m) ? (int)counts.labels[m] : kOut) : label[m]; }
+    __device__ __forceinline__ float lse_of(int m) const
+    {
+        if (!direct) return lse[m];
+        const float l = lse_in[m];
+        return l == -INFINITY ? INFINITY : l;
+    }
+    // the largest finite gradient of a row that counts (called by whole waves)
+    __device__ __forceinline__ float largest(int lane) const
+    {
+        if (!direct) return *c;
+        const float g = lane < T && counts(lane) ? fabsf(gloss[lane]) : 0.f;
+        return wave_max(g <= 3.4028235e38f ? g : 0.f);
+    }
+    __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
+    static constexpr int kOut = -(1 << 30);
 };
+constexpr int kDirectRows = 64; // one pass over them as terms of dW; a wave looks them all up at once
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
 inline Meta meta_at(char *p, long T)
 {
-    Meta m;
+    Meta m{};
+    m.T = (int)T;
     const size_t n = up256(4 * (size_t)T);
     m.count = (int *)p;
     m.exps = (int *)(p + 64);
@@ -51,14 +85,6 @@ inline Meta meta_at(char *p, long T)
     return m;
 }
 
-__device__ __forceinline__ bool counts(int64_t label, int64_t ignore, long V) { return label != ignore && label >= 0 && label < V; }
-
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
-}
 __device__ __forceinline__ int wave_add(int v)
 {
 #pragma unroll
@@ -68,7 +94,7 @@ __device__ __forceinline__ int wave_add(int v)
 
 // Largest finite magnitude of H (rows that count) and of W, a part from every block.
 __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, long ld_h, long T, const float *__restrict__ W, long ld_w, long V,
-                                                  long D, const int64_t *__restrict__ labels, int64_t ignore, int blocks_h, float *__restrict__ top)
+                                                  long D, const Counts counts, int blocks_h, float *__restrict__ top)
 {
     const bool is_h = (int)blockIdx.x < blocks_h;
     const int block = is_h ? blockIdx.x : blockIdx.x - blocks_h, blocks = is_h ? blocks_h : gridDim.x - blocks_h;
@@ -76,20 +102,32 @@ __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, l
     const long rows = is_h ? T : V, ld = is_h ? ld_h : ld_w;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float m = 0.f;
+    auto see = [&](float x) {
+        const float v = fabsf(x);
+        m = v <= 3.4028235e38f ? fmaxf(m, v) : m;
+    };
+    const bool wide = (((uintptr_t)x & 15) | (ld & 3) | (D & 3)) == 0;
     for (long r = (long)block * 4 + wave; r < rows; r += blocks * 4) {
-        if (is_h && !counts(labels[r], ignore, V)) continue;
+        if (is_h && !counts((int)r)) continue;
         const float *p = x + r * ld;
-        long d = lane;
-        for (; d + 192 < D; d += 256) {
+        if (wide) {
+            for (long d = lane * 4; d < D; d += 1024) { // four accesses of 16 bytes on their way at a time
+                f32x4 v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float v = fabsf(p[d + e * 64]);
-                m = v <= 3.4028235e38f ? fmaxf(m, v) : m;
+                for (int e = 0; e < 4; ++e) v[e] = d + e * 256 < D ? *(const f32x4 *)(p + d + e * 256) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) see(v[e][k]);
             }
-        }
-        for (; d < D; d += 64) {
-            const float v = fabsf(p[d]);
-            m = v <= 3.4028235e38f ? fmaxf(m, v) : m;
+        } else {
+            for (long d = lane; d < D; d += 512) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = d + e * 64 < D ? p[d + e * 64] : 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) see(v[e]);
+            }
         }
     }
     __shared__ float red[4];
@@ -103,8 +141,14 @@ __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, l
 // a wave calls, and gets it.)
 __device__ __forceinline__ int stored_exp(const float *__restrict__ top, int parts)
 {
-    float m = 0.f;
-    for (int i = threadIdx.x & 63; i < parts; i += 64) m = fmaxf(m, top[i]);
+    float m = 0.f, v[kMaxParts / 64];
+#pragma unroll
+    for (int k = 0; k < kMaxParts / 64; ++k) { // (all on their way at once)
+        const int i = k * 64 + (threadIdx.x & 63);
+        v[k] = i < parts ? top[i] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kMaxParts / 64; ++k) m = fmaxf(m, v[k]);
     m = wave_max(m);
     if (!(m > 0.f)) return 0;
     int e;
@@ -113,12 +157,12 @@ __device__ __forceinline__ int stored_exp(const float *__restrict__ top, int par
 }
 
 struct PackRows {
-    const void *H;
-    const int64_t *labels;
-    int64_t ignore;
-    long ld_h;
-    int T, D, V;
-    int rows_per_block;
+    const void *H, *W;
+    long ld_h, ld_w;
+    int T, D;
+    int rows_per_block, row_blocks; // the blocks behind the row blocks pack weights
+    int classes;                    // of the weights, from W on
+    char *out_w;
     int parts_h, parts_w;  // of the largest magnitudes (float)
     char *out;
     long row_bytes;
@@ -165,8 +209,9 @@ __device__ __forceinline__ void store8(float, char *row, int n, const float (&v)
 
 // Rows that count, one behind the other, and what is known about them.  A block takes a run of rows; where they go follows from the
 // labels before them.
-template <typename T> __global__ void __launch_bounds__(256) pack_rows_kernel(const PackRows p)
+template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &p)
 {
+    const Counts &counts = p.meta.counts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int first = blockIdx.x * p.rows_per_block, last = min(p.T, first + p.rows_per_block);
     __shared__ int red_n[4];
@@ -174,7 +219,7 @@ template <typename T> __global__ void __launch_bounds__(256) pack_rows_kernel(co
     int before = 0;
     float c = 0.f;
     for (int t = threadIdx.x; t < (p.gloss ? p.T : first); t += 256) {
-        const bool in = counts(p.labels[t], p.ignore, p.V);
+        const bool in = counts(t);
         if (t < first) before += in;
         if (p.gloss && in) {
             const float g = fabsf(p.gloss[t]); // (an infinite or undefined one spoils its own row alone)
@@ -205,14 +250,13 @@ template <typename T> __global__ void __launch_bounds__(256) pack_rows_kernel(co
     int place = before;
     for (int r0 = first; r0 < last; r0 += 64) {
         const int t = r0 + lane;
-        const int64_t label = t < last ? p.labels[t] : 0;
-        const bool in = t < last && counts(label, p.ignore, p.V);
+        const bool in = t < last && counts(t);
         const uint64_t mask = __ballot(in);
         const int j = place + __popcll(mask & (((uint64_t)1 << lane) - 1));
         if (wave == 0 && t < last) {
             if (in) {
                 p.meta.row[j] = t;
-                p.meta.label[j] = (int)label;
+                p.meta.label[j] = (int)counts.labels[t];
                 if (p.gloss) {
                     const float l = p.lse[t];
                     p.meta.q[j] = c > 0.f ? p.gloss[t] / c : p.gloss[t];
@@ -246,18 +290,25 @@ template <typename T> __global__ void __launch_bounds__(256) pack_rows_kernel(co
 }
 
 // A piece of the weights, its rows padded to whole chunks.
-template <typename T> __global__ void __launch_bounds__(256)
-pack_weights_kernel(const T *__restrict__ W, long ld, int rows, int D, const int *__restrict__ exps, char *__restrict__ out, long row_bytes)
+template <typename T> __device__ __forceinline__ void pack_weights(const PackRows &p)
 {
-    const float s = sizeof(T) == 4 ? ldexpf(1.f, exps[1]) : 1.f;
-    const int per_row = (D + 7) / 8;
-    const bool aligned = ((uintptr_t)W & 15) == 0 && (ld * sizeof(T)) % 16 == 0;
-    for (long c = (long)blockIdx.x * 256 + threadIdx.x; c < (long)rows * per_row; c += (long)gridDim.x * 256) {
-        const int row = (int)(c / per_row), n = (int)(c - (long)row * per_row) * 8;
-        float v[8];
-        load8(W + row * ld, n, D, aligned, v);
-        store8(T(), out + row * row_bytes, n, v, s);
+    const float s = sizeof(T) == 4 ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
+    const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
+    const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks); // a wave to a row
+    for (int row = 4 * (blockIdx.x - p.row_blocks) + (threadIdx.x >> 6); row < p.classes; row += rows) {
+        const T *w = (const T *)p.W + row * p.ld_w;
+        char *out = p.out_w + row * p.row_bytes;
+        for (int n = lane * 8; n < p.D; n += 512) {
+            float v[8];
+            load8(w, n, p.D, aligned, v);
+            store8(T(), out, n, v, s);
+        }
     }
+}
+template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const PackRows p)
+{
+    if ((int)blockIdx.x < p.row_blocks) pack_rows<T>(p);
+    else pack_weights<T>(p);
 }
 
 // four neighbours of b from n on, zeros past its end
@@ -285,7 +336,7 @@ template <typename T> struct Stats {
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
-            const int label = m < p.M ? e.meta.label[m] - e.v0 : -1;
+            const int label = m < p.M ? e.meta.label_of(m) - e.v0 : Meta::kOut;
             float top = -INFINITY, sum = 0.f, z[NI][16];
 #pragma unroll
             for (int j = 0; j < NI; ++j)
@@ -321,7 +372,7 @@ template <typename T> struct Stats {
 __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float *__restrict__ part, int parts, long T_rows, float *__restrict__ loss,
                                                    float *__restrict__ lse)
 {
-    const int count = *meta.count;
+    const int count = meta.rows();
     const int r = threadIdx.x & 15, s = threadIdx.x >> 4;
     const int j = blockIdx.x * 16 + r;
     float top = -INFINITY, sum = 0.f;
@@ -352,11 +403,30 @@ __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float 
         const float shift = top == -INFINITY ? 0.f : top;
         float total = 0.f;
         for (int k = 0; k < 16; ++k) total += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - shift) * kLog2e);
-        const float l = top + logf(total), z = meta.zlabel[j];
-        const int t = meta.row[j];
-        lse[t] = l;
-        loss[t] = z == -INFINITY ? INFINITY : l - z; // (a masked label's loss, also where every class is masked)
+        const float l = top + logf(total);
+        const int t = meta.row_of(j);
+        if (meta.label_of(j) == Meta::kOut) {
+            loss[t] = lse[t] = 0.f;
+        } else {
+            const float z = meta.zlabel[j];
+            lse[t] = l;
+            loss[t] = z == -INFINITY ? INFINITY : l - z; // (a masked label's loss, also where every class is masked)
+        }
     }
+}
+
+// four neighbours of a row of G
+__device__ __forceinline__ void store_gradient(float, char *row, int n, const float (&g)[4])
+{
+    const float v[4] = {g[0] * (float)(1 << kStoreG), g[1] * (float)(1 << kStoreG), g[2] * (float)(1 << kStoreG), g[3] * (float)(1 << kStoreG)};
+    store_split(row, n, v);
+}
+__device__ __forceinline__ void store_gradient(bf16_t, char *row, int n, const float (&g)[4])
+{
+    u32x2 u;
+    u[0] = f32x2_to_bf16x2(g[0], g[1]);
+    u[1] = f32x2_to_bf16x2(g[2], g[3]);
+    *(u32x2 *)(row + n * 2) = u;
 }
 
 // backward: G of a piece
@@ -372,13 +442,15 @@ template <typename T> struct Grad {
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
+        const float largest = e.meta.largest(p.lane);
         const int Np = (p.N + 7) & ~7;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
             if (m >= p.M) continue;
-            const int label = e.meta.label[m] - e.v0;
-            const float q_row = e.meta.q[m], lse = e.meta.lse[m];
+            const int label = e.meta.label_of(m) - e.v0;
+            const bool in = label > Meta::kOut / 2;
+            const float q_row = e.meta.q_of(m, largest), lse = e.meta.lse_of(m);
             char *row = e.out + (long)m * e.ld;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
@@ -392,18 +464,9 @@ template <typename T> struct Grad {
                     for (int k = 0; k < 4; ++k) {
                         const float z = (sizeof(T) == 4 ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
                         const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        g[k] = n + k < p.N ? x : 0.f;
+                        g[k] = n + k < p.N && in ? x : 0.f;
                     }
-                    if (sizeof(T) == 4) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) g[k] *= (float)(1 << kStoreG);
-                        store_split(row, n, g);
-                    } else {
-                        u32x2 u;
-                        u[0] = f32x2_to_bf16x2(g[0], g[1]);
-                        u[1] = f32x2_to_bf16x2(g[2], g[3]);
-                        *(u32x2 *)(row + n * 2) = u;
-                    }
+                    store_gradient(T(), row, n, g);
                 }
         }
     }
@@ -429,7 +492,7 @@ template <typename T> struct OutW {
     struct Params { T *out; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = sizeof(T) == 4 ? ldexpf(*e.meta.c, -kStoreG - e.meta.exps[0]) : *e.meta.c;
+        const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[0]) : e.meta.largest(p.lane);
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
@@ -453,13 +516,13 @@ template <typename T> struct OutH {
     struct Params { T *out; float *sums; long slice_stride; int add; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = sizeof(T) == 4 ? ldexpf(*e.meta.c, -kStoreG - e.meta.exps[1]) : *e.meta.c;
+        const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m = p.m0 + i * 32 + (p.lane & 31);
             if (m >= p.M) continue;
-            const int row = e.sums ? m : e.meta.row[m];
+            const int row = e.sums ? m : e.meta.row_of(m);
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
@@ -488,7 +551,7 @@ template <typename T> struct OutH {
 template <typename T> __global__ void __launch_bounds__(256)
 finish_rows_kernel(const Meta meta, const float *__restrict__ sums, long slice_stride, int slices, int D, T *__restrict__ dH)
 {
-    if ((int)blockIdx.x >= *meta.count) return;
+    if ((int)blockIdx.x >= meta.rows()) return;
     const int n = blockIdx.y * 1024 + threadIdx.x * 4;
     if (n >= D) return;
     const long at = (long)blockIdx.x * D + n;
@@ -506,33 +569,39 @@ finish_rows_kernel(const Meta meta, const float *__restrict__ sums, long slice_s
                 if (n + k < D) v[k] += p[k];
         }
     }
-    store_four(dH + (long)meta.row[blockIdx.x] * D + n, n, D, wide, v);
+    store_four(dH + (long)meta.row_of(blockIdx.x) * D + n, n, D, wide, v);
 }
 
 // db of a piece: the columns' sums of G, eight columns to a thread, the block's four waves over the rows
-template <typename T> __global__ void __launch_bounds__(256)
-bias_kernel(const Meta meta, const char *__restrict__ G, long ld, int V, T *__restrict__ db)
+template <typename T> struct Bias {
+    Meta meta;
+    const char *G;
+    long ld;
+    int V;
+    T *db;
+};
+template <typename T> __device__ __forceinline__ void bias_sums(const Bias<T> &p, int block, float (*red)[64])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int count = *meta.count;
+    const int count = p.meta.rows();
+    const float largest = p.meta.largest(lane);
     // 8 chunks of columns by 8 rows to a wave
-    const int chunk = blockIdx.x * 8 + (lane & 7), n = chunk * 8;
+    const int chunk = block * 8 + (lane & 7), n = chunk * 8;
     float s[8] = {};
-    if (n < V)
+    if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
-            const char *p = G + (long)m * ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
+            const char *g = p.G + (long)m * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
             if (sizeof(T) == 4) {
-                const f16x8 hi = *(const f16x8 *)p, lo = *(const f16x8 *)(p + 16);
+                const f16x8 hi = *(const f16x8 *)g, lo = *(const f16x8 *)(g + 16);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] += (float)hi[e] + (float)lo[e];
             } else {
                 struct alignas(16) Eight { bf16_t v[8]; };
-                const Eight v = *(const Eight *)p;
+                const Eight v = *(const Eight *)g;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] += bf16_to_f32(v.v[e]);
             }
         }
-    __shared__ float red[4][64];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         s[e] += __shfl_xor(s[e], 8, 64);
@@ -541,10 +610,145 @@ bias_kernel(const Meta meta, const char *__restrict__ G, long ld, int V, T *__re
         if (lane < 8) red[wave][lane * 8 + e] = s[e];
     }
     __syncthreads();
-    if (threadIdx.x < 64 && (int)(blockIdx.x * 64 + threadIdx.x) < V) {
-        const float c = sizeof(T) == 4 ? ldexpf(*meta.c, -kStoreG) : *meta.c;
-        Elem<T>::store(db + blockIdx.x * 64 + threadIdx.x, c * (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
+    if (threadIdx.x < 64 && block * 64 + (int)threadIdx.x < p.V) {
+        const float c = sizeof(T) == 4 ? ldexpf(largest, -kStoreG) : largest;
+        Elem<T>::store(p.db + block * 64 + threadIdx.x, c * (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
     }
+}
+template <typename T> __global__ void __launch_bounds__(256) bias_kernel(const Bias<T> p)
+{
+    __shared__ float red[4][64];
+    bias_sums(p, blockIdx.x, red);
+}
+
+template <typename T> struct FormatOf { typedef Bf16 type; };
+template <> struct FormatOf<float> { typedef Split type; };
+
+// dW, dH and db of a piece in one launch: small products end sooner than a launch begins
+template <typename T> struct PairParams {
+    Params w, h;
+    typename OutW<T>::Params ew;
+    typename OutH<T>::Params eh;
+    Bias<T> b;
+    unsigned blocks_w, blocks_h; // of dW; of one of dH's slices
+    int slices_h;
+};
+template <typename T> __global__ void __launch_bounds__(Small::kThreads, Small::kPerSimd) pair_kernel(const PairParams<T> p)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    typedef typename FormatOf<T>::type P;
+    unsigned block = blockIdx.x;
+    if (block < p.blocks_w) {
+        mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, 0, smem);
+        return;
+    }
+    block -= p.blocks_w;
+    if (block < p.blocks_h * p.slices_h) {
+        const unsigned slice = block / p.blocks_h;
+        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block - slice * p.blocks_h, slice, smem);
+        return;
+    }
+    bias_sums(p.b, block - p.blocks_h * p.slices_h, (float(*)[64])smem);
+}
+
+// a slice's part of the logits' products, [slice][T][ld]
+struct Logits {
+    static constexpr bool kSymmetric = false;
+    struct Params { float *out; int T, ld; };
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+    {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int m = p.m0 + i * 32 + (p.lane & 31);
+            float *row = e.out + ((long)p.slice * e.T + m) * e.ld;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
+                    if (m < p.M && n < e.ld) *(f32x4 *)(row + n) = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                }
+        }
+    }
+};
+// ... joined: four logits of row m
+template <typename T> __device__ __forceinline__ void join_logits(const float *part, long slice_stride, int slices, const T *b, int n, int V, int ze, float (&z)[4])
+{
+    float bias[4];
+    load_bias(b, n, V, bias);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < slices; ++k) s += *(const f32x4 *)(part + k * slice_stride + n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = n + e < V ? (sizeof(T) == 4 ? ldexpf(s[e], ze) : s[e]) + bias[e] : -INFINITY;
+}
+// loss and lse of a compact row from the slices' logits, a block to a row
+template <typename T> __global__ void __launch_bounds__(256)
+row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const T *__restrict__ b, int V,
+                float *__restrict__ loss, float *__restrict__ lse)
+{
+    const int m = blockIdx.x;
+    if (m >= meta.rows()) return;
+    const int label = meta.label_of(m), t = meta.row_of(m);
+    if (label == Meta::kOut) {
+        if (threadIdx.x == 0) loss[t] = lse[t] = 0.f;
+        return;
+    }
+    const int ze = sizeof(T) == 4 ? -(meta.exps[0] + meta.exps[1]) : 0;
+    const float *row = part + (long)m * ld;
+    float top = -INFINITY, sum = 0.f;
+    __shared__ float at_label, tops[4], sums[4];
+    for (int n = threadIdx.x * 4; n < V; n += 1024) {
+        float z[4];
+        join_logits(row, slice_stride, slices, b, n, V, ze, z);
+        float m4 = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+        if (label >= n && label < n + 4) at_label = label == n ? z[0] : label == n + 1 ? z[1] : label == n + 2 ? z[2] : z[3];
+        m4 = fmaxf(m4, top);
+        const float shift = m4 == -INFINITY ? 0.f : m4;
+        sum *= __builtin_amdgcn_exp2f((top - shift) * kLog2e);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[e] - shift) * kLog2e);
+        top = m4;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float wtop = wave_max(top);
+    sum *= __builtin_amdgcn_exp2f((top - (wtop == -INFINITY ? 0.f : wtop)) * kLog2e);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (lane == 0) {
+        tops[wave] = wtop;
+        sums[wave] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        const float shift = top == -INFINITY ? 0.f : top;
+        sum = 0.f;
+        for (int w = 0; w < 4; ++w) sum += sums[w] * __builtin_amdgcn_exp2f((tops[w] - shift) * kLog2e);
+        const float l = top + logf(sum);
+        lse[t] = l;
+        loss[t] = at_label == -INFINITY ? INFINITY : l - at_label;
+    }
+}
+// G of a compact row, 1024 classes to a block
+template <typename T> __global__ void __launch_bounds__(256)
+row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const T *__restrict__ b, int V,
+                char *__restrict__ G, long ld_g)
+{
+    const int m = blockIdx.x, n = blockIdx.y * 1024 + threadIdx.x * 4;
+    const float largest = meta.largest(threadIdx.x & 63);
+    if (m >= meta.rows() || n >= ((V + 7) & ~7)) return;
+    const int label = meta.label_of(m);
+    const float q = meta.q_of(m, largest), lse = meta.lse_of(m);
+    float g[4] = {0.f, 0.f, 0.f, 0.f};
+    if (label != Meta::kOut && n < V) {
+        const int ze = sizeof(T) == 4 ? -(meta.exps[0] + meta.exps[1]) : 0;
+        float z[4];
+        join_logits(part + (long)m * ld, slice_stride, slices, b, n, V, ze, z);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < V) g[e] = q * (__builtin_amdgcn_exp2f((z[e] - lse) * kLog2e) - (n + e == label ? 1.f : 0.f));
+    }
+    store_gradient(T(), G + (long)m * ld_g, n, g);
 }
 
 } // namespace
@@ -555,7 +759,8 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->dp = (g.D + 7) / 8 * 8;
     p->row_bytes = (p->split ? 4 : 2) * p->dp;
     p->pack_w = p->split || g.D % 8 || g.ld_w % 8;
-    // A piece's G (and its packed weights) stay within half of the 256 MiB that the chip caches; at least 4096 classes, in whole tiles.
+    p->direct = !p->split && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % 8 == 0;
+    // A piece's G (and its packed weights) stay within the 256 MiB that the chip caches; at least 4096 classes, in whole tiles.
     const long per_class = (backward ? g.T * (p->split ? 4 : 2) : 0) + (p->pack_w ? p->row_bytes : 0);
     long piece = per_class ? (256L << 20) / per_class / 256 * 256 : g.V;
     if (piece < 4096) piece = 4096;
@@ -565,20 +770,31 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     if (p->pieces > 1) piece = ((g.V + p->pieces - 1) / p->pieces + 255) / 256 * 256;
     p->pieces = (int)((g.V + piece - 1) / piece);
     p->piece = piece;
-    p->z = choose(p->split, g.T, piece, 1, g.D, false, 1);
+    // A sum over D in slices leaves its parts of the logits in the workspace: for few rows and classes only.
+    const long logits = g.T * ((piece + 3) & ~3L) * 4;
+    p->z = choose(p->split, g.T, piece, 1, g.D, false, p->pieces > 1 || logits * 16 > 32L << 20 ? 1 : 16);
     p->w = choose(p->split, piece, g.D, 1, g.T, false, 1);
     p->h = choose(p->split, g.T, g.D, 1, piece, false, 16);
+    // dW and dH together where both would take the smallest tiles anyway, or are over before a launch is
+    const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
+    p->pair = backward && (work < 4e9 || (p->w.shape == kSmall && p->h.shape == kSmall));
+    if (p->pair) {
+        p->w = Choice{kSmall, 1};
+        p->h = choose(p->split, g.T, g.D, 1, piece, false, 16, true);
+    }
     p->parts = 0;
     for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->z.shape);
     size_t o = 0;
     p->o_meta = o;
     o += meta_bytes(g.T);
     p->o_h = o;
-    o += up256((size_t)g.T * p->row_bytes);
+    if (!p->direct) o += up256((size_t)g.T * p->row_bytes);
     p->o_w = o;
     if (p->pack_w) o += up256((size_t)piece * p->row_bytes);
     p->o_part = o;
-    if (!backward) o += up256((size_t)p->parts * 2 * g.T * 4);
+    if (!backward && p->z.slices == 1) o += up256((size_t)p->parts * 2 * g.T * 4);
+    p->o_z = o;
+    if (p->z.slices > 1) o += up256((size_t)logits * p->z.slices);
     p->o_g = o;
     if (backward) o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * (p->split ? 4 : 2));
     p->o_acc = o;
@@ -588,178 +804,201 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 
 namespace {
 
-// H's rows that count into the workspace, and what is known about them
-template <typename T>
-hipError_t launch_rows(const LossGeom &g, const LossPlan &p, const T *H, const T *W, const int64_t *labels, float *loss, float *lse_out,
-                       const float *lse, const float *gloss, void *dH, char *ws, const Meta &meta, hipStream_t st)
-{
+template <typename T> class Loss {
+    typedef typename FormatOf<T>::type P;
+    const LossGeom &g;
+    const LossPlan &p;
+    const T *H, *W, *b;
+    char *ws;
+    hipStream_t st;
+    Meta meta;
     int parts_h = 0, parts_w = 0;
-    if (p.split) {
-        parts_h = (int)(g.T / 8 < 1 ? 1 : g.T / 8 > kMaxParts ? kMaxParts : g.T / 8);
-        parts_w = (int)(g.V / 8 < 1 ? 1 : g.V / 8 > kMaxParts ? kMaxParts : g.V / 8);
-        hipLaunchKernelGGL(top_kernel, dim3(parts_h + parts_w), dim3(256), 0, st, (const float *)H, g.ld_h, g.T, (const float *)W, g.ld_w, g.V, g.D,
-                           labels, (int64_t)g.ignore, parts_h, meta.top);
+    const void *h = nullptr, *w = nullptr; // the operands of the piece at hand
+    long ld_h = 0, ld_w = 0;
+
+    // How the products read H and the weights of classes v0 .. v0 + n; packs what has to be, H's rows with the first piece.
+    hipError_t operands(long v0, long n, PackRows *rows)
+    {
+        const bool pack_h = v0 == 0 && !p.direct;
+        h = p.direct ? (const void *)H : ws + p.o_h;
+        ld_h = p.direct ? g.ld_h * (long)sizeof(T) : p.row_bytes;
+        w = p.pack_w ? (const void *)(ws + p.o_w) : W + v0 * g.ld_w;
+        ld_w = p.pack_w ? p.row_bytes : g.ld_w * (long)sizeof(T);
+        if (!pack_h && !p.pack_w) return hipSuccess;
+        rows->H = H;
+        rows->W = W + v0 * g.ld_w;
+        rows->ld_h = g.ld_h;
+        rows->ld_w = g.ld_w;
+        rows->T = (int)g.T;
+        rows->D = (int)g.D;
+        rows->rows_per_block = (int)(g.T / 1024 < 4 ? 4 : g.T / 1024); // every block counts the labels before its own
+        rows->row_blocks = pack_h ? cdiv(g.T, rows->rows_per_block) : 0;
+        rows->classes = (int)n;
+        rows->parts_h = parts_h;
+        rows->parts_w = parts_w;
+        rows->out = ws + p.o_h;
+        rows->out_w = ws + p.o_w;
+        rows->row_bytes = p.row_bytes;
+        rows->meta = meta;
+        const long weight_blocks = !p.pack_w ? 0 : n > 4 * 4096 ? 4096 : (n + 3) / 4;
+        hipLaunchKernelGGL(pack_kernel<T>, dim3((unsigned)(rows->row_blocks + weight_blocks)), dim3(256), 0, st, *rows);
+        return hipGetLastError();
     }
-    PackRows r{};
-    r.H = H;
-    r.labels = labels;
-    r.ignore = g.ignore;
-    r.ld_h = g.ld_h;
-    r.T = (int)g.T;
-    r.D = (int)g.D;
-    r.V = (int)g.V;
-    r.rows_per_block = (int)(g.T / 1024 < 8 ? 8 : g.T / 1024); // every block counts the labels before its own
-    r.parts_h = parts_h;
-    r.parts_w = parts_w;
-    r.out = ws + p.o_h;
-    r.row_bytes = p.row_bytes;
-    r.meta = meta;
-    r.loss = loss;
-    r.lse_out = lse_out;
-    r.lse = lse;
-    r.gloss = gloss;
-    r.dH = dH;
-    hipLaunchKernelGGL(pack_rows_kernel<T>, dim3(cdiv(g.T, r.rows_per_block)), dim3(256), 0, st, r);
-    return hipGetLastError();
-}
-
-// classes v0 .. v0 + n of the weights as the products read them
-template <typename T>
-hipError_t piece_of_weights(const LossGeom &g, const LossPlan &p, const T *W, long v0, long n, const Meta &meta, char *ws, hipStream_t st,
-                            const void **at, long *ld)
-{
-    const T *w = W + v0 * g.ld_w;
-    if (!p.pack_w) {
-        *at = w;
-        *ld = g.ld_w * (long)sizeof(T);
-        return hipSuccess;
-    }
-    const long chunks = n * ((g.D + 7) / 8);
-    hipLaunchKernelGGL(pack_weights_kernel<T>, dim3((unsigned)(chunks > 256 * 4096 ? 4096 : (chunks + 255) / 256)), dim3(256), 0, st, w, g.ld_w, (int)n,
-                       (int)g.D, (const int *)meta.exps, ws + p.o_w, p.row_bytes);
-    *at = ws + p.o_w;
-    *ld = p.row_bytes;
-    return hipGetLastError();
-}
-
-template <typename T> struct FormatOf { typedef Bf16 type; };
-template <> struct FormatOf<float> { typedef Split type; };
-
-template <typename T>
-hipError_t forward(const LossGeom &g, const LossPlan &p, const T *H, const T *W, const T *b, const int64_t *labels, float *loss, float *lse,
-                   char *ws, hipStream_t st)
-{
-    typedef typename FormatOf<T>::type P;
-    const Meta meta = meta_at(ws + p.o_meta, g.T);
-    hipError_t e = launch_rows(g, p, H, W, labels, loss, lse, (const float *)nullptr, (const float *)nullptr, nullptr, ws, meta, st);
-    if (e != hipSuccess) return e;
-    float *part = (float *)(ws + p.o_part);
-    int part0 = 0;
-    for (long v0 = 0; v0 < g.V; v0 += p.piece) {
-        const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
+    Params logits_params(long n) const
+    {
         Params m{};
-        if ((e = piece_of_weights(g, p, W, v0, n, meta, ws, st, &m.b, &m.ldb)) != hipSuccess) return e;
-        m.a = ws + p.o_h;
-        m.lda = p.row_bytes;
-        m.M = (int)g.T;
-        m.N = (int)n;
-        m.K = (int)g.D;
-        m.m_dev = meta.count;
-        m.batch = 1;
-        e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(m, {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.z, st);
-        if (e != hipSuccess) return e;
-        part0 += (int)wave_columns(n, p.z.shape);
-    }
-    hipLaunchKernelGGL(join_kernel, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t backward(const LossGeom &g, const LossPlan &p, const T *H, const T *W, const T *b, const int64_t *labels, const float *lse,
-                    const float *gloss, T *dH, T *dW, T *db, char *ws, hipStream_t st)
-{
-    typedef typename FormatOf<T>::type P;
-    const Meta meta = meta_at(ws + p.o_meta, g.T);
-    hipError_t e = launch_rows(g, p, H, W, labels, nullptr, nullptr, lse, gloss, dH, ws, meta, st);
-    if (e != hipSuccess) return e;
-    char *G = ws + p.o_g;
-    const long ld_g = (p.piece + 7) / 8 * 8 * (p.split ? 4 : 2);
-    const bool sums = p.pieces > 1 || p.h.slices > 1;
-    for (long v0 = 0; v0 < g.V; v0 += p.piece) {
-        const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
-        const void *w;
-        long ld_w;
-        if ((e = piece_of_weights(g, p, W, v0, n, meta, ws, st, &w, &ld_w)) != hipSuccess) return e;
-        Params m{};
-        m.a = ws + p.o_h;
-        m.lda = p.row_bytes;
+        m.a = h;
+        m.lda = ld_h;
         m.b = w;
         m.ldb = ld_w;
         m.M = (int)g.T;
         m.N = (int)n;
         m.K = (int)g.D;
-        m.m_dev = meta.count;
         m.batch = 1;
-        e = launch<P, Lay::kAlong, Lay::kAlong, Grad<T>>(m, {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
+        if (p.direct) m.counts_m = meta.counts;
+        else m.m_dev = meta.count;
+        return m;
+    }
+    long ld_logits() const { return (p.piece + 3) & ~3L; }
+    hipError_t logits_in_slices(long n)
+    {
+        return launch<P, Lay::kAlong, Lay::kAlong, Logits>(logits_params(n), {(float *)(ws + p.o_z), (int)g.T, (int)ld_logits()}, p.z, st);
+    }
+    hipError_t largest_magnitudes()
+    {
+        if (!p.split) return hipSuccess;
+        parts_h = cdiv(g.T, 4) > kMaxParts ? kMaxParts : cdiv(g.T, 4);
+        parts_w = cdiv(g.V, 4) > kMaxParts ? kMaxParts : cdiv(g.V, 4);
+        hipLaunchKernelGGL(top_kernel, dim3(parts_h + parts_w), dim3(256), 0, st, (const float *)H, g.ld_h, g.T, (const float *)W, g.ld_w, g.V, g.D,
+                           meta.counts, parts_h, meta.top);
+        return hipGetLastError();
+    }
+
+public:
+    Loss(const LossGeom &g_, const LossPlan &p_, const void *H_, const void *W_, const void *b_, const int64_t *labels, void *ws_, hipStream_t st_)
+        : g(g_), p(p_), H((const T *)H_), W((const T *)W_), b((const T *)b_), ws((char *)ws_), st(st_), meta(meta_at((char *)ws_ + p_.o_meta, g_.T))
+    {
+        meta.direct = p.direct;
+        meta.counts = Counts{labels, g.ignore, (int)g.V};
+    }
+
+    hipError_t forward(float *loss, float *lse)
+    {
+        hipError_t e = largest_magnitudes();
         if (e != hipSuccess) return e;
-        if (dW) {
-            Params d{};
-            d.a = G;
-            d.lda = ld_g;
-            d.b = ws + p.o_h;
-            d.ldb = p.row_bytes;
-            d.M = (int)n;
-            d.N = (int)g.D;
-            d.K = (int)g.T;
-            d.k_dev = meta.count;
-            d.batch = 1;
-            e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(d, {dW + v0 * g.D, meta}, p.w, st);
+        PackRows rows{};
+        rows.loss = loss;
+        rows.lse_out = lse;
+        float *part = (float *)(ws + p.o_part);
+        int part0 = 0;
+        for (long v0 = 0; v0 < g.V; v0 += p.piece) {
+            const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
+            if ((e = operands(v0, n, &rows)) != hipSuccess) return e;
+            if (p.z.slices > 1) { // (one piece)
+                if ((e = logits_in_slices(n)) != hipSuccess) return e;
+                hipLaunchKernelGGL(row_loss_kernel<T>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)(ws + p.o_z), g.T * ld_logits(),
+                                   (int)ld_logits(), p.z.slices, b, (int)g.V, loss, lse);
+                return hipGetLastError();
+            }
+            e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(logits_params(n), {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.z, st);
+            if (e != hipSuccess) return e;
+            part0 += (int)wave_columns(n, p.z.shape);
+        }
+        hipLaunchKernelGGL(join_kernel, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
+        return hipGetLastError();
+    }
+
+    hipError_t backward(const float *lse, const float *gloss, T *dH, T *dW, T *db)
+    {
+        hipError_t e = largest_magnitudes();
+        if (e != hipSuccess) return e;
+        meta.lse_in = lse;
+        meta.gloss = gloss;
+        PackRows rows{};
+        rows.lse = lse;
+        rows.gloss = gloss;
+        rows.dH = dH;
+        char *G = ws + p.o_g;
+        const long ld_g = (p.piece + 7) / 8 * 8 * (p.split ? 4 : 2);
+        float *sums = p.pieces > 1 || p.h.slices > 1 ? (float *)(ws + p.o_acc) : nullptr;
+        for (long v0 = 0; v0 < g.V; v0 += p.piece) {
+            const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
+            if ((e = operands(v0, n, &rows)) != hipSuccess) return e;
+            if (p.z.slices > 1) {
+                if ((e = logits_in_slices(n)) != hipSuccess) return e;
+                hipLaunchKernelGGL(row_grad_kernel<T>, dim3((unsigned)g.T, cdiv(g.V, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
+                                   g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g);
+                e = hipGetLastError();
+            } else {
+                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<T>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
+            }
+            if (e != hipSuccess) return e;
+            PairParams<T> q{};
+            q.w.a = G;
+            q.w.lda = ld_g;
+            q.w.b = h;
+            q.w.ldb = ld_h;
+            q.w.M = (int)n;
+            q.w.N = (int)g.D;
+            q.w.K = (int)g.T;
+            q.w.batch = 1;
+            if (p.direct) q.w.counts_k = meta.counts;
+            else q.w.k_dev = meta.count;
+            q.ew = {dW ? dW + v0 * g.D : nullptr, meta};
+            q.h.a = G;
+            q.h.lda = ld_g;
+            q.h.b = w;
+            q.h.ldb = ld_w;
+            q.h.M = (int)g.T;
+            q.h.N = (int)g.D;
+            q.h.K = (int)n;
+            q.h.batch = 1;
+            if (!p.direct) q.h.m_dev = meta.count;
+            q.eh = {dH, sums, g.T * g.D, v0 > 0, meta};
+            q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr};
+            const int bias_blocks = db ? cdiv(n, 64) : 0;
+            if (p.pair) {
+                q.slices_h = p.h.slices;
+                if (dW) q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
+                if (dH) q.blocks_h = place_tiles<Small>(&q.h, false, p.h.slices, kPass<P, Small::R>);
+                static const hipError_t attr =
+                    hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, Small::kLds);
+                if (attr != hipSuccess) return attr;
+                hipLaunchKernelGGL(pair_kernel<T>, dim3(q.blocks_w + q.blocks_h * q.slices_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
+                e = hipGetLastError();
+            } else {
+                if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(q.w, q.ew, p.w, st);
+                if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<T>>(q.h, q.eh, p.h, st);
+                if (db && e == hipSuccess) {
+                    hipLaunchKernelGGL(bias_kernel<T>, dim3(bias_blocks), dim3(256), 0, st, q.b);
+                    e = hipGetLastError();
+                }
+            }
             if (e != hipSuccess) return e;
         }
-        if (dH) {
-            Params d{};
-            d.a = G;
-            d.lda = ld_g;
-            d.b = w;
-            d.ldb = ld_w;
-            d.M = (int)g.T;
-            d.N = (int)g.D;
-            d.K = (int)n;
-            d.m_dev = meta.count;
-            d.batch = 1;
-            e = launch<P, Lay::kAlong, Lay::kDown, OutH<T>>(d, {dH, sums ? (float *)(ws + p.o_acc) : nullptr, g.T * g.D, v0 > 0, meta}, p.h, st);
-            if (e != hipSuccess) return e;
+        if (dH && sums) {
+            hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 1024)), dim3(256), 0, st, meta, (const float *)sums, g.T * g.D,
+                               p.h.slices, (int)g.D, dH);
+            e = hipGetLastError();
         }
-        if (db) {
-            hipLaunchKernelGGL(bias_kernel<T>, dim3(cdiv(n, 64)), dim3(256), 0, st, meta, (const char *)G, ld_g, (int)n, db + v0);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
+        return e;
     }
-    if (dH && sums) {
-        hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_acc), g.T * g.D,
-                           p.h.slices, (int)g.D, dH);
-        e = hipGetLastError();
-    }
-    return e;
-}
+};
 
 } // namespace
 
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            float *loss, float *lse, void *ws, hipStream_t st)
 {
-    if (g.dtype == CAC_F32) return forward(g, p, (const float *)H, (const float *)W, (const float *)b, labels, loss, lse, (char *)ws, st);
-    return forward(g, p, (const bf16_t *)H, (const bf16_t *)W, (const bf16_t *)b, labels, loss, lse, (char *)ws, st);
+    if (g.dtype == CAC_F32) return Loss<float>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    return Loss<bf16_t>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
 }
 
 hipError_t launch_loss_bwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            const float *lse, const float *gloss, void *dH, void *dW, void *db, void *ws, hipStream_t st)
 {
-    if (g.dtype == CAC_F32)
-        return backward(g, p, (const float *)H, (const float *)W, (const float *)b, labels, lse, gloss, (float *)dH, (float *)dW, (float *)db,
-                        (char *)ws, st);
-    return backward(g, p, (const bf16_t *)H, (const bf16_t *)W, (const bf16_t *)b, labels, lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db,
-                    (char *)ws, st);
+    if (g.dtype == CAC_F32) return Loss<float>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    return Loss<bf16_t>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
 }
 
 } // namespace cac

@@ -38,6 +38,19 @@ struct Split { static constexpr int kParts = 2; };
 
 constexpr uint32_t kNowhere = 0x80000000u; // an offset past every descriptor's range
 
+// Rows of H that count: whose label is a class and not the one that is ignored.
+struct Counts {
+    const int64_t *labels; // null: every row counts
+    int64_t ignore;
+    int classes;
+    __device__ __forceinline__ bool operator()(int row) const
+    {
+        if (!labels) return true;
+        const int64_t l = labels[row];
+        return l != ignore && l >= 0 && l < classes;
+    }
+};
+
 struct Params {
     const void *a, *b;
     long lda, ldb;             // bytes from a row of memory to the next, below 2^23
@@ -48,6 +61,7 @@ struct Params {
     int tiles;                 // of one matrix: tiles_m * tiles_n, or those on and above the diagonal
     int group;                 // tile rows that one XCD walks together
     int kt_slice;              // passes over K of one slice of the sum
+    Counts counts_m, counts_k; // rows of a (terms of b, of which there is one pass) that count: the others are zeros, whatever stands there
 };
 
 template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of the sum in one pass, R bytes of K to a row
@@ -83,7 +97,7 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
     int left;         // chunks (kAlong) or rows (kDown) of K from the pass to load next on
 
     // first: first row of C; count: rows of C in the matrix; K: terms; kt: first pass, kt1: behind the last
-    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane)
+    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts)
     {
         const int row0 = (wave * 64 + lane) / kChunks, slot = (wave * 64 + lane) % kChunks;
         const int columns = P::kParts * ((count + 7) / 8) - first / 8 * P::kParts; // kDown: chunks from the tile's first on
@@ -102,7 +116,8 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row);
-            const bool there = L == Lay::kAlong ? first + row < count : c < columns;
+            bool there = L == Lay::kAlong ? first + row < count : c < columns;
+            if (counts.labels && there) there = L == Lay::kAlong ? counts(first + row) : row < K && counts(row);
             off[i] = there ? (uint32_t)(row * (int)ld + c * 16) : kNowhere;
         }
     }
@@ -238,8 +253,8 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
 
     Stage<P, LA, TM, S::R, S::kWaves> sa;
     Stage<P, LB, TN, S::R, S::kWaves> sb;
-    sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane);
-    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane);
+    sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane, p.counts_m);
+    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane, p.counts_k);
     const int wm = wave / S::WN, wn = wave % S::WN;
     Frag<P, LA, TM, S::R> fa;
     Frag<P, LB, TN, S::R> fb;
@@ -346,11 +361,12 @@ inline long tiles_of(int shape, long M, long N, bool symmetric)
     return symmetric ? m * (m + 1) / 2 : m * n;
 }
 // The cheapest of them; more than one slice costs the writing and reading of that many sums of 32 bits, and a launch.
-inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetric, int max_slices)
+inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetric, int max_slices, bool small_only = false)
 {
     Choice best{kSmall, 1};
     double least = 1e30;
     for (int shape = 0; shape < kShapes; ++shape) {
+        if (small_only && shape != kSmall) break;
         if (shape == kWide && !split) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
         const long tiles = tiles_of(shape, M, N, symmetric) * batch;
         const int passes = cdiv(K, split ? 32 : 64);
@@ -370,7 +386,7 @@ inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetr
 // parts that a row's columns fall into, one to a wave
 inline long wave_columns(long N, int shape) { return (long)cdiv(N, kEdge[shape]) * wave_columns_of(shape); }
 
-// Fills in the tiles; returns the workgroups of one slice.
+// Fills in the tiles; returns the workgroups of one slice (a multiple of the XCDs).
 template <class S> inline unsigned place_tiles(Params *p, bool symmetric, int slices, int pass)
 {
     p->tiles_m = cdiv(p->M, S::TM);

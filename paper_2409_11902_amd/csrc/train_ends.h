@@ -16,14 +16,16 @@ struct LossGeom {
 };
 struct LossPlan {
     bool split;       // float: operands as two halves
+    bool direct;      // few rows: H is read where it lies, rows that do not count as zeros
     bool pack_w;      // the weights go through the workspace, piece by piece
+    bool pair;        // backward: dW, dH and db in one launch
     long dp;          // features, in whole chunks of 8
     long row_bytes;   // of a packed row
     long piece;       // classes in one piece
     int pieces;
     TileChoice z, w, h; // the logits' product, dW's, dH's
     long parts;       // forward: maximum and sum, this many for every row
-    size_t o_meta, o_h, o_w, o_part, o_g, o_acc, bytes;
+    size_t o_meta, o_h, o_w, o_part, o_z, o_g, o_acc, bytes;
 };
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p);
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
