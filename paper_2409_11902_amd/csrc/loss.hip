@@ -444,30 +444,32 @@ template <typename T> struct Grad {
         const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
         const float largest = e.meta.largest(p.lane);
         const int Np = (p.N + 7) & ~7;
+        typedef RowBlock<sizeof(T) == 4 ? Fmt::kSplit : Fmt::kBf16, NI> Block;
+        constexpr int kIn16 = sizeof(T) == 4 ? 32 : 16; // bytes that eight columns take
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const int m = p.m0 + i * 32 + (p.lane & 31);
-            if (m >= p.M) continue;
+            const int m0 = p.m0 + i * 32, m = min(m0 + (p.lane & 31), p.M - 1);
             const int label = e.meta.label_of(m) - e.v0;
             const bool in = label > Meta::kOut / 2;
             const float q_row = e.meta.q_of(m, largest), lse = e.meta.lse_of(m);
-            char *row = e.out + (long)m * e.ld;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (n >= Np) continue;
                     float bias[4], g[4];
                     load_bias(e.b, n, p.N, bias);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float z = (sizeof(T) == 4 ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
                         const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        g[k] = n + k < p.N && in ? x : 0.f;
+                        g[k] = n + k < p.N && in ? (sizeof(T) == 4 ? x * (float)(1 << kStoreG) : x) : 0.f;
                     }
-                    store_gradient(T(), row, n, g);
+                    Block::put(p.lds, p.lane, j, q, g);
                 }
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (m0 + row < p.M && p.n0 + at / kIn16 * 8 < Np) *(u32x4 *)(e.out + (long)(m0 + row) * e.ld + p.n0 / 8 * kIn16 + at) = x;
+            });
         }
     }
 };
@@ -486,6 +488,18 @@ template <typename T> __device__ __forceinline__ void store_four(T *o, int n, in
         if (n + k < N) Elem<T>::store(o + k, v[k]);
 }
 
+// 32 rows of a product, times s, into a wave's LDS
+template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x16 (&acc)[MI][NI], int i, float s, const Place &p)
+{
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {s * acc[i][j][q * 4], s * acc[i][j][q * 4 + 1], s * acc[i][j][q * 4 + 2], s * acc[i][j][q * 4 + 3]};
+            RowBlock<Fmt::kF32, NI>::put(p.lds, p.lane, j, q, v);
+        }
+}
+
 // dW of a piece
 template <typename T> struct OutW {
     static constexpr bool kSymmetric = false;
@@ -493,20 +507,17 @@ template <typename T> struct OutW {
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[0]) : e.meta.largest(p.lane);
+        typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (m >= p.M || n >= p.N) continue;
-                    float v[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = s * acc[i][j][q * 4 + k];
-                    store_four(e.out + (long)m * p.N + n, n, p.N, wide, v);
-                }
+        for (int i = 0; i < MI; ++i) {
+            const int m0 = p.m0 + i * 32;
+            put_scaled<MI, NI>(acc, i, s, p);
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                const int m = m0 + row, n = p.n0 + at / 4;
+                if (m < p.M && n < p.N) store_four(e.out + (long)m * p.N + n, n, p.N, wide, {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])});
+            });
+        }
     }
 };
 
@@ -517,32 +528,34 @@ template <typename T> struct OutH {
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
+        typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const int m = p.m0 + i * 32 + (p.lane & 31);
-            if (m >= p.M) continue;
-            const int row = e.sums ? m : e.meta.row_of(m);
+            const int m0 = p.m0 + i * 32;
+            put_scaled<MI, NI>(acc, i, s, p);
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                const int m = m0 + row, n = p.n0 + at / 4;
+                if (m >= p.M || n >= p.N) return;
+                float v[4] = {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])};
+                if (!e.sums) {
+                    store_four(e.out + (long)e.meta.row_of(m) * p.N + n, n, p.N, wide, v);
+                    return;
+                }
+                float *o = e.sums + p.slice * e.slice_stride + (long)m * p.N + n;
+                if (e.add) {
+                    if (wide) {
+                        const f32x4 old = *(const f32x4 *)o;
 #pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (n >= p.N) continue;
-                    float v[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = s * acc[i][j][q * 4 + k];
-                    if (!e.sums) {
-                        store_four(e.out + (long)row * p.N + n, n, p.N, wide, v);
-                        continue;
-                    }
-                    float *o = e.sums + p.slice * e.slice_stride + (long)m * p.N + n;
-                    if (e.add)
+                        for (int k = 0; k < 4; ++k) v[k] += old[k];
+                    } else {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (n + k < p.N) v[k] += o[k];
-                    store_four(o, n, p.N, wide, v);
+                    }
                 }
+                store_four(o, n, p.N, wide, v);
+            });
         }
     }
 };
@@ -657,17 +670,14 @@ struct Logits {
     struct Params { float *out; int T, ld; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
+        typedef RowBlock<Fmt::kF32, NI> Block;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const int m = p.m0 + i * 32 + (p.lane & 31);
-            float *row = e.out + ((long)p.slice * e.T + m) * e.ld;
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (m < p.M && n < e.ld) *(f32x4 *)(row + n) = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-                }
+            const int m0 = p.m0 + i * 32;
+            put_scaled<MI, NI>(acc, i, 1.f, p);
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (m0 + row < p.M && p.n0 + at / 4 < e.ld) *(u32x4 *)(e.out + ((long)p.slice * e.T + m0 + row) * e.ld + p.n0 + at / 4) = x;
+            });
         }
     }
 };

@@ -184,6 +184,86 @@ template <class P> __device__ __forceinline__ f32x16 product(s16x8 a, s16x8 b, f
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
 }
 
+// ---- a float as two halves
+__device__ __forceinline__ void split_float(float x, _Float16 *hi, _Float16 *lo)
+{
+    *hi = (_Float16)x;
+    *lo = (_Float16)(x - (float)*hi);
+}
+// four neighbours of a row (n a multiple of 4) to where a split matrix's row `row` holds them
+__device__ __forceinline__ void store_split(char *row, int n, const float (&v)[4])
+{
+    union { _Float16 h[4]; u32x2 u; } hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split_float(v[e], &hi.h[e], &lo.h[e]);
+    char *c = row + (n >> 3) * 32 + (n & 4) * 2;
+    *(u32x2 *)c = hi.u;
+    *(u32x2 *)(c + 16) = lo.u;
+}
+__device__ __forceinline__ void load_split(const char *row, int n, float (&v)[4])
+{
+    union { _Float16 h[4]; u32x2 u; } hi, lo;
+    const char *c = row + (n >> 3) * 32 + (n & 4) * 2;
+    hi.u = *(const u32x2 *)c;
+    lo.u = *(const u32x2 *)(c + 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)hi.h[e] + (float)lo.h[e];
+}
+
+// ---- 32 rows of a wave's part of C on their way to memory.  A lane holds four neighbours of a row, and a store of them touches 32 rows at
+// 8 or 16 bytes each; through LDS they become stores of 16 bytes a lane, whole lines side by side.
+enum class Fmt { kBf16, kF32, kSplit };
+template <Fmt F, int NI> struct RowBlock {
+    static constexpr int kRow = 32 * NI * (F == Fmt::kBf16 ? 2 : 4), kPitch = kRow + 16; // bytes
+    static __device__ __forceinline__ void put(unsigned char *lds, int lane, int j, int q, const float (&v)[4])
+    {
+        unsigned char *r = lds + (lane & 31) * kPitch;
+        const int n = j * 32 + q * 8 + (lane >> 5) * 4;
+        if (F == Fmt::kSplit) {
+            store_split((char *)r, n, v);
+        } else if (F == Fmt::kF32) {
+            *(f32x4 *)(r + n * 4) = f32x4{v[0], v[1], v[2], v[3]};
+        } else {
+            u32x2 u;
+            u[0] = f32x2_to_bf16x2(v[0], v[1]);
+            u[1] = f32x2_to_bf16x2(v[2], v[3]);
+            *(u32x2 *)(r + n * 2) = u;
+        }
+    }
+    // the mirror image of a block of 32 x 32, in rows of 32: a lane's four become four rows' (NI = 1)
+    static __device__ __forceinline__ void put_mirrored(unsigned char *lds, int lane, int q, const float (&v)[4])
+    {
+        const int n = q * 8 + (lane >> 5) * 4, m = lane & 31;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            _Float16 hi, lo;
+            split_float(v[e], &hi, &lo);
+            unsigned char *c = lds + (n + e) * kPitch + (m >> 3) * 32 + (m & 7) * 2;
+            *(_Float16 *)c = hi;
+            *(_Float16 *)(c + 16) = lo;
+        }
+    }
+    // store(row, byte offset in the row, 16 bytes) for all of it; the block's LDS is free afterwards
+    template <class Fn> static __device__ __forceinline__ void each(unsigned char *lds, int lane, Fn store)
+    {
+        asm volatile("" ::: "memory"); // (a wave's LDS accesses are in order; other lanes' stores are read here)
+        __builtin_amdgcn_wave_barrier();
+        u32x4 v[kRow / 32];
+#pragma unroll
+        for (int c = 0; c < kRow / 32; ++c) {
+            const int at = c * 64 + lane;
+            v[c] = *(const u32x4 *)(lds + at / (kRow / 16) * kPitch + at % (kRow / 16) * 16);
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < kRow / 32; ++c) {
+            const int at = c * 64 + lane;
+            store(at / (kRow / 16), at % (kRow / 16) * 16, v[c]);
+        }
+    }
+};
+
 // Where a wave's part of C lies.  acc[mi][ni][4 q + e] is C[m][n] of m = m0 + 32 mi + lane % 32 and
 // n = n0 + 32 ni + 8 q + 4 (lane / 32) + e: a lane holds four neighbours of a row of C.
 struct Place {
@@ -192,6 +272,7 @@ struct Place {
     int batch, slice;
     int tm, tn;         // the tile
     int part;           // the wave's place among the waves that share a row of C
+    unsigned char *lds; // the wave's own, free at the end
     int lane;
 };
 
@@ -321,6 +402,7 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
     at.tn = tn;
     at.part = tn * S::WN + wn;
     at.lane = lane;
+    at.lds = smem + wave * (S::kLds / S::kWaves / 16 * 16);
     Epi::template run<MI, NI>(e, acc, at);
 }
 
@@ -415,32 +497,6 @@ hipError_t launch(const Params &p, const typename Epi::Params &e, Choice c, hipS
         if (c.shape == kWide) return launch_shape<P, LA, LB, Wide, Epi>(p, e, c.slices, st);
     if (c.shape == kMiddle) return launch_shape<P, LA, LB, Middle, Epi>(p, e, c.slices, st);
     return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
-}
-
-// ---- a float as two halves
-__device__ __forceinline__ void split_float(float x, _Float16 *hi, _Float16 *lo)
-{
-    *hi = (_Float16)x;
-    *lo = (_Float16)(x - (float)*hi);
-}
-// four neighbours of a row (n a multiple of 4) to where a split matrix's row `row` holds them
-__device__ __forceinline__ void store_split(char *row, int n, const float (&v)[4])
-{
-    union { _Float16 h[4]; u32x2 u; } hi, lo;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) split_float(v[e], &hi.h[e], &lo.h[e]);
-    char *c = row + (n >> 3) * 32 + (n & 4) * 2;
-    *(u32x2 *)c = hi.u;
-    *(u32x2 *)(c + 16) = lo.u;
-}
-__device__ __forceinline__ void load_split(const char *row, int n, float (&v)[4])
-{
-    union { _Float16 h[4]; u32x2 u; } hi, lo;
-    const char *c = row + (n >> 3) * 32 + (n & 4) * 2;
-    hi.u = *(const u32x2 *)c;
-    lo.u = *(const u32x2 *)(c + 16);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)hi.h[e] + (float)lo.h[e];
 }
 
 } // namespace mm

@@ -52,46 +52,54 @@ __device__ __forceinline__ void store_symmetric(char *out, long ld, int m, int n
             *(_Float16 *)(c + 16) = lo;
         }
 }
-
-template <int MI, int NI> __device__ __forceinline__ void Gram::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+// a wave's part of a symmetric matrix, value(i, j, q, m, n, v) giving four of it
+template <int MI, int NI, class Fn> __device__ __forceinline__ void store_symmetric_part(char *out, long ld, const Place &p, Fn value)
 {
-    char *out = e.out + p.batch * e.stride;
     const int Np = (p.N + 7) & ~7;
-    const bool mirror = p.tm != p.tn;
+    typedef RowBlock<Fmt::kSplit, 1> Block;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j)
+        for (int j = 0; j < NI; ++j) {
+            const int m0 = p.m0 + i * 32, n0 = p.n0 + j * 32;
+            float v[4][4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k] * kTake;
-                store_symmetric(out, e.ld, m, n, p.M, Np, mirror, v);
+                value(i, j, q, m0 + (p.lane & 31), n0 + q * 8 + (p.lane >> 5) * 4, v[q]);
+                Block::put(p.lds, p.lane, 0, q, v[q]);
             }
+            // (16 bytes hold the hi or the lo of eight columns)
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (m0 + row < p.M && n0 + at / 32 * 8 < Np) *(u32x4 *)(out + (m0 + row) * ld + n0 * 4 + at) = x;
+            });
+            if (p.tm == p.tn) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) Block::put_mirrored(p.lds, p.lane, q, v[q]);
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (n0 + row < p.N && m0 + at / 32 * 8 < Np) *(u32x4 *)(out + (n0 + row) * ld + m0 * 4 + at) = x;
+            });
+        }
+}
+
+template <int MI, int NI> __device__ __forceinline__ void Gram::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+{
+    store_symmetric_part<MI, NI>(e.out + p.batch * e.stride, e.ld, p, [&](int i, int j, int q, int, int, float (&v)[4]) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k] * kTake;
+    });
 }
 
 template <int MI, int NI> __device__ __forceinline__ void Poly::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
 {
-    char *out = e.out + p.batch * e.stride;
     const char *a = e.a + p.batch * e.stride;
     const int Np = (p.N + 7) & ~7;
-    const bool mirror = p.tm != p.tn;
+    store_symmetric_part<MI, NI>(e.out + p.batch * e.stride, e.ld, p, [&](int i, int j, int q, int m, int n, float (&v)[4]) {
+        v[0] = v[1] = v[2] = v[3] = 0.f;
+        if (m < p.M && n < Np) load_split(a + m * e.ld, n, v);
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                float v[4] = {0.f, 0.f, 0.f, 0.f};
-                if (m < p.M && n < Np) load_split(a + m * e.ld, n, v);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    v[k] = kB * v[k] + (kC * kTake) * acc[i][j][q * 4 + k] + (m == n + k && m < p.M ? kA * kStore : 0.f);
-                store_symmetric(out, e.ld, m, n, p.M, Np, mirror, v);
-            }
+        for (int k = 0; k < 4; ++k)
+            v[k] = kB * v[k] + (kC * kTake) * acc[i][j][q * 4 + k] + (m == n + k && m < p.M ? kA * kStore : 0.f);
+    });
 }
 
 // a slice's part of S, in float, [slice][batch][r][ld]
@@ -101,16 +109,21 @@ struct GramPart {
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         float *out = e.out + ((long)p.slice * e.batch + p.batch) * p.N * e.ld;
+        typedef RowBlock<Fmt::kF32, NI> Block;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (m < p.M && n < e.ld)
-                        *(f32x4 *)(out + (long)m * e.ld + n) = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                    const float v[4] = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                    Block::put(p.lds, p.lane, j, q, v);
                 }
+            const int m0 = p.m0 + i * 32;
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (m0 + row < p.M && p.n0 + at / 4 < e.ld) *(u32x4 *)(out + (long)(m0 + row) * e.ld + p.n0 + at / 4) = x;
+            });
+        }
     }
 };
 // ... and S from the slices' parts: 32 x 32 of it to a block, of which a thread has four neighbours of a row
@@ -141,18 +154,23 @@ struct Next {
     {
         char *out = e.out + p.batch * e.stride;
         const int Np = (p.N + 7) & ~7;
+        typedef RowBlock<Fmt::kSplit, NI> Block;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
                     float v[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k] * kTake;
-                    if (m < p.M && n < Np) store_split(out + m * e.ld, n, v);
+                    Block::put(p.lds, p.lane, j, q, v);
                 }
+            const int m0 = p.m0 + i * 32;
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                if (m0 + row < p.M && p.n0 + at / 32 * 8 < Np) *(u32x4 *)(out + (m0 + row) * e.ld + p.n0 * 4 + at) = x;
+            });
+        }
     }
 };
 
@@ -163,35 +181,39 @@ template <typename T, bool UPDATE> struct Last {
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         T *out = e.out + (long)p.batch * p.M * p.N;
-        const bool wide = (p.N & 3) == 0; // rows in whole groups of four: one access for a lane's four
+        const bool wide = (p.N & 3) == 0; // rows in whole groups of four
+        typedef RowBlock<Fmt::kF32, NI> Block;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
+            const int m0 = p.m0 + i * 32;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int m = p.m0 + i * 32 + (p.lane & 31), n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    if (m >= p.M || n >= p.N) continue;
-                    T *o = out + (long)m * p.N + n;
-                    if (wide) {
-                        struct alignas(4 * sizeof(T)) Four { T v[4]; };
-                        Four f;
-                        if (UPDATE) f = *(const Four *)o;
+                    float v[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float x = e.scale * acc[i][j][q * 4 + k];
-                            Elem<T>::store(&f.v[k], UPDATE ? e.keep * Elem<T>::load(&f.v[k]) + x : x);
-                        }
-                        *(Four *)o = f;
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (n + k < p.N) {
-                                const float x = e.scale * acc[i][j][q * 4 + k];
-                                Elem<T>::store(o + k, UPDATE ? e.keep * Elem<T>::load(o + k) + x : x);
-                            }
-                    }
+                    for (int k = 0; k < 4; ++k) v[k] = e.scale * acc[i][j][q * 4 + k];
+                    Block::put(p.lds, p.lane, j, q, v);
                 }
+            // (float in LDS for both types: four numbers to a lane, neighbouring lanes side by side)
+            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                const int m = m0 + row, n = p.n0 + at / 4;
+                if (m >= p.M || n >= p.N) return;
+                T *o = out + (long)m * p.N + n;
+                struct alignas(4 * sizeof(T)) Four { T v[4]; } f;
+                if (wide) {
+                    if (UPDATE) f = *(const Four *)o;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        Elem<T>::store(&f.v[k], UPDATE ? e.keep * Elem<T>::load(&f.v[k]) + __uint_as_float(x[k]) : __uint_as_float(x[k]));
+                    *(Four *)o = f;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (n + k < p.N) Elem<T>::store(o + k, UPDATE ? e.keep * Elem<T>::load(o + k) + __uint_as_float(x[k]) : __uint_as_float(x[k]));
+                }
+            });
+        }
     }
 };
 
