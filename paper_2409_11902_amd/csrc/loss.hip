@@ -106,22 +106,36 @@ __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, l
         const float v = fabsf(x);
         m = v <= 3.4028235e38f ? fmaxf(m, v) : m;
     };
-    const bool wide = (((uintptr_t)x & 15) | (ld & 3) | (D & 3)) == 0;
-    for (long r = (long)block * 4 + wave; r < rows; r += blocks * 4) {
-        if (is_h && !counts((int)r)) continue;
-        const float *p = x + r * ld;
-        if (wide) {
-            for (long d = lane * 4; d < D; d += 1024) { // four accesses of 16 bytes on their way at a time
-                f32x4 v[4];
+    if (!is_h && ld == D) { // dense and all of it: no rows to tell apart
+        const long n4 = rows * D / 4, step = (long)blocks * 256;
+        for (long i = (long)block * 256 + threadIdx.x; i < n4; i += step * 8) { // eight accesses of 16 bytes on their way at a time
+            f32x4 v[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = d + e * 256 < D ? *(const f32x4 *)(p + d + e * 256) : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int e = 0; e < 8; ++e) v[e] = i + e * step < n4 ? ((const f32x4 *)x)[i + e * step] : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 8; ++e)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) see(v[e][k]);
+                for (int k = 0; k < 4; ++k) see(v[e][k]);
+        }
+        if (block == 0 && (long)threadIdx.x < rows * D - n4 * 4) see(x[n4 * 4 + threadIdx.x]);
+    } else {
+        for (long r = (long)block * 4 + wave; r < rows; r += blocks * 4) {
+            if (is_h && !counts((int)r)) continue;
+            const float *p = x + r * ld;
+            long d = lane;
+            if ((((uintptr_t)x & 15) | (ld & 3)) == 0) {
+                for (d = lane * 4; d + 3 < D; d += 2048) {
+                    f32x4 v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = d + e * 256 + 3 < D ? *(const f32x4 *)(p + d + e * 256) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) see(v[e][k]);
+                }
+                d = (D & ~3L) + lane;
             }
-        } else {
-            for (long d = lane; d < D; d += 512) {
+            for (; d < D; d += 512) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = d + e * 64 < D ? p[d + e * 64] : 0.f;
@@ -174,21 +188,39 @@ struct PackRows {
     void *dH;
 };
 
-// eight neighbours of a row of memory in float, zeros past its end
-template <typename T> __device__ __forceinline__ void load8(const T *p, int n, int D, bool aligned, float (&v)[8])
+// 512 numbers of a row of memory from n0 on in float, eight neighbours to a lane, zeros past the row's end.  A row that does not start
+// on 16 bytes is read side by side and dealt out through the wave's 2304 bytes of LDS.
+constexpr int kDeal = 576; // 512 floats, and 4 after every 32, which keeps the lanes' eights apart
+template <typename T> __device__ __forceinline__ void load8(const T *p, int n0, int D, bool aligned, int lane, float *deal, float (&v)[8])
 {
-    if (aligned && n + 8 <= D) {
+    const int n = n0 + lane * 8;
+    if (aligned) {
         struct alignas(16) Some { T v[16 / sizeof(T)]; };
+        if (n + 8 <= D) {
 #pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            const Some s = *(const Some *)(p + n + h * (16 / sizeof(T)));
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+                const Some s = *(const Some *)(p + n + h * (16 / sizeof(T)));
 #pragma unroll
-            for (int e = 0; e < (int)(16 / sizeof(T)); ++e) v[h * (16 / sizeof(T)) + e] = Elem<T>::load(&s.v[e]);
+                for (int e = 0; e < (int)(16 / sizeof(T)); ++e) v[h * (16 / sizeof(T)) + e] = Elem<T>::load(&s.v[e]);
+            }
+            return;
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = n + e < D ? Elem<T>::load(p + n + e) : 0.f;
         return;
     }
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = n + e < D ? Elem<T>::load(p + n + e) : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = n0 + e * 64 + lane < D ? Elem<T>::load(p + n0 + e * 64 + lane) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) deal[e * 72 + lane + lane / 32 * 4] = x[e];
+    asm volatile("" ::: "memory"); // (a wave's LDS accesses are in order; other lanes' stores are read here)
+    __builtin_amdgcn_wave_barrier();
+    const float *d = deal + lane * 8 + lane / 4 * 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = d[e];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
 }
 // ... and into a packed row (bfloat16: as they are; float: two halves, times `scale`)
 __device__ __forceinline__ void store8(bf16_t, char *row, int n, const float (&v)[8], float)
@@ -209,7 +241,7 @@ __device__ __forceinline__ void store8(float, char *row, int n, const float (&v)
 
 // Rows that count, one behind the other, and what is known about them.  A block takes a run of rows; where they go follows from the
 // labels before them.
-template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &p)
+template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &p, float *deal)
 {
     const Counts &counts = p.meta.counts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -274,10 +306,10 @@ template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &
                 const int jj = place + __popcll(mask & (((uint64_t)1 << k) - 1));
                 const T *h = (const T *)p.H + (long)row * p.ld_h;
                 char *o = p.out + (long)jj * p.row_bytes;
-                for (int n = lane * 8; n < p.D; n += 512) {
+                for (int n0 = 0; n0 < p.D; n0 += 512) {
                     float v[8];
-                    load8(h, n, p.D, aligned, v);
-                    store8(T(), o, n, v, scale);
+                    load8(h, n0, p.D, aligned, lane, deal, v);
+                    if (n0 + lane * 8 < p.D) store8(T(), o, n0 + lane * 8, v, scale);
                 }
             } else if (p.dH) {
                 T *o = (T *)p.dH + (long)row * p.D;
@@ -290,7 +322,7 @@ template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &
 }
 
 // A piece of the weights, its rows padded to whole chunks.
-template <typename T> __device__ __forceinline__ void pack_weights(const PackRows &p)
+template <typename T> __device__ __forceinline__ void pack_weights(const PackRows &p, float *deal)
 {
     const float s = sizeof(T) == 4 ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
     const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
@@ -298,17 +330,18 @@ template <typename T> __device__ __forceinline__ void pack_weights(const PackRow
     for (int row = 4 * (blockIdx.x - p.row_blocks) + (threadIdx.x >> 6); row < p.classes; row += rows) {
         const T *w = (const T *)p.W + row * p.ld_w;
         char *out = p.out_w + row * p.row_bytes;
-        for (int n = lane * 8; n < p.D; n += 512) {
+        for (int n0 = 0; n0 < p.D; n0 += 512) {
             float v[8];
-            load8(w, n, p.D, aligned, v);
-            store8(T(), out, n, v, s);
+            load8(w, n0, p.D, aligned, lane, deal, v);
+            if (n0 + lane * 8 < p.D) store8(T(), out, n0 + lane * 8, v, s);
         }
     }
 }
 template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const PackRows p)
 {
-    if ((int)blockIdx.x < p.row_blocks) pack_rows<T>(p);
-    else pack_weights<T>(p);
+    __shared__ float deal[4][kDeal];
+    if ((int)blockIdx.x < p.row_blocks) pack_rows<T>(p, deal[threadIdx.x >> 6]);
+    else pack_weights<T>(p, deal[threadIdx.x >> 6]);
 }
 
 // four neighbours of b from n on, zeros past its end
