@@ -146,8 +146,11 @@ int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
     MuonPlan p;
     plan_muon(g, &p);
-    snprintf(buf, buf_len, "%s, square products of %ld: tile %d in %d slices, then %d; tile %d", p.tall ? "X^T X" : "X X^T", p.r, tile_edge(p.gram),
-             p.gram.slices, tile_edge(p.poly), tile_edge(p.apply));
+    if (p.narrow)
+        snprintf(buf, buf_len, "narrow: %d workgroups of %d columns, %d launches", p.np.slices, p.np.width, p.np.slices == 1 ? 1 : g.steps + 1);
+    else
+        snprintf(buf, buf_len, "%s, square products of %ld: tile %d in %d slices, then %d; tile %d", p.tall ? "X^T X" : "X X^T", p.r, tile_edge(p.gram),
+                 p.gram.slices, tile_edge(p.poly), tile_edge(p.apply));
     return CAC_OK;
 }
 

@@ -184,9 +184,11 @@ template <class P> __device__ __forceinline__ f32x16 product(s16x8 a, s16x8 b, f
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
 }
 
-// ---- a float as two halves
+// ---- a float as two halves.  x is fixed first: left to itself the compiler takes hi from a product's rounded value and lo from the
+// product, and where those lie on two sides of a half-precision number's middle, hi + lo is off by a unit of hi.
 __device__ __forceinline__ void split_float(float x, _Float16 *hi, _Float16 *lo)
 {
+    asm("" : "+v"(x));
     *hi = (_Float16)x;
     *lo = (_Float16)(x - (float)*hi);
 }

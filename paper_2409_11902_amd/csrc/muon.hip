@@ -328,6 +328,11 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 void plan_muon(const MuonGeom &g, MuonPlan *p)
 {
+    p->narrow = plan_muon_narrow(g, &p->np);
+    if (p->narrow) {
+        p->bytes = p->np.bytes;
+        return;
+    }
     p->tall = g.rows > g.cols;
     p->r = p->tall ? g.cols : g.rows;
     p->ld_x = (g.cols + 31) / 32 * 128;
@@ -390,6 +395,7 @@ hipError_t launch_apply(const MuonGeom &g, const MuonPlan &p, const char *x, con
 hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, float *M, void *W, void *O, float momentum, float keep,
                        float lr, void *ws_, hipStream_t st)
 {
+    if (p.narrow) return launch_muon_narrow(g, p.np, G, M, W, O, momentum, keep, lr, ws_, st);
     char *ws = (char *)ws_;
     hipError_t e = g.grad_dtype == CAC_F32 ? launch_start(g, p, (const float *)G, M, momentum, ws, st)
                                            : launch_start(g, p, (const bf16_t *)G, M, momentum, ws, st);

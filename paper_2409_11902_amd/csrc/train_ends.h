@@ -39,7 +39,16 @@ struct MuonGeom {
     int batch, steps, dtype, grad_dtype;
     bool nesterov;
 };
+struct MuonNarrowPlan { // muon_narrow.hip: a shorter side of at most 64
+    int width, slices;  // columns to a workgroup, workgroups to a matrix
+    size_t o_x, o_part, o_exps, bytes;
+};
+bool plan_muon_narrow(const MuonGeom &g, MuonNarrowPlan *p);
+hipError_t launch_muon_narrow(const MuonGeom &g, const MuonNarrowPlan &p, const void *G, float *M, void *W, void *O, float momentum, float keep,
+                              float lr, void *ws, hipStream_t st);
 struct MuonPlan {
+    bool narrow;
+    MuonNarrowPlan np;
     bool tall;          // more rows than columns: X^T X in the place of X X^T
     long r;             // the shorter side
     long ld_x, ld_a;    // bytes of a row
