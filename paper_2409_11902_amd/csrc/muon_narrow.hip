@@ -128,30 +128,86 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
     };
 
     if (p.step < 0) {
-        // U, eight neighbouring columns of a row to a thread and turn; neighbouring threads take neighbours in memory
+        // U, eight neighbouring columns of a row to a thread and turn; neighbouring threads take neighbours in memory.  Everything is
+        // asked for before anything is stored, so that it is on its way together.
         float u[kOwn][8], top = 0.f;
         const TG *g = (const TG *)p.G + batch * size;
         float *m = p.M ? p.M + batch * size : nullptr;
+        auto where = [&](int c, int e) -> long { // of element e of turn c; -1 past the edge
+            const int at = c * 256 + tid, i = p.tall ? at & 63 : at / (W / 8), j = j0 + (p.tall ? at >> 6 : at % (W / 8)) * 8 + e;
+            if (i >= p.r || j >= p.n) return -1;
+            return p.tall ? (long)j * p.r + i : (long)i * p.n + j;
+        };
+        // (rows of whole groups of four, and a first column that is one of 64: four neighbours in one access)
+        const bool wide = !p.tall && (p.n & 3) == 0;
+        struct alignas(4 * sizeof(TG)) Four { TG v[4]; };
 #pragma unroll
         for (int c = 0; c < kOwn; ++c) {
-            const int at = c * 256 + tid, i = p.tall ? at & 63 : at / (W / 8), j = j0 + (p.tall ? at >> 6 : at % (W / 8)) * 8;
+            if (wide) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float v = 0.f;
-                if (i < p.r && j + e < p.n) {
-                    const long k = p.tall ? (long)(j + e) * p.r + i : (long)i * p.n + j + e;
-                    v = Elem<TG>::load(g + k);
-                    if (m) {
-                        const float mm = p.mu * m[k] + v;
-                        m[k] = mm;
-                        v = p.nesterov ? v + p.mu * mm : mm;
-                    }
+                for (int h = 0; h < 8; h += 4) {
+                    const long k = where(c, h);
+                    Four f;
+                    if (k >= 0) f = *(const Four *)(g + k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[c][h + e] = k >= 0 ? Elem<TG>::load(&f.v[e]) : 0.f;
                 }
-                u[c][e] = v;
-                const float a = fabsf(v);
-                top = a <= 3.4028235e38f ? fmaxf(top, a) : top;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const long k = where(c, e);
+                    u[c][e] = k >= 0 ? Elem<TG>::load(g + k) : 0.f;
+                }
             }
         }
+        if (m) {
+            float mm[kOwn][8];
+#pragma unroll
+            for (int c = 0; c < kOwn; ++c)
+                if (wide) {
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const long k = where(c, h);
+                        const f32x4 f = k >= 0 ? *(const f32x4 *)(m + k) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mm[c][h + e] = f[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const long k = where(c, e);
+                        mm[c][e] = k >= 0 ? m[k] : 0.f;
+                    }
+                }
+#pragma unroll
+            for (int c = 0; c < kOwn; ++c) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    mm[c][e] = p.mu * mm[c][e] + u[c][e];
+                    u[c][e] = p.nesterov ? u[c][e] + p.mu * mm[c][e] : mm[c][e];
+                }
+                if (wide) {
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const long k = where(c, h);
+                        if (k >= 0) *(f32x4 *)(m + k) = f32x4{mm[c][h], mm[c][h + 1], mm[c][h + 2], mm[c][h + 3]};
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const long k = where(c, e);
+                        if (k >= 0) m[k] = mm[c][e];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float a = fabsf(u[c][e]);
+                top = a <= 3.4028235e38f ? fmaxf(top, a) : top;
+            }
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
         if (lane == 0) red[wave] = top;
@@ -178,7 +234,11 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
             return;
         }
     } else {
-        for (int c = tid * 16; c < kCols; c += 4096) *(u32x4 *)(X + c) = *(const u32x4 *)(x_mine + c);
+        u32x4 x[kCols / 4096];
+#pragma unroll
+        for (int c = 0; c < kCols / 4096; ++c) x[c] = *(const u32x4 *)(x_mine + c * 4096 + tid * 16);
+#pragma unroll
+        for (int c = 0; c < kCols / 4096; ++c) *(u32x4 *)(X + c * 4096 + tid * 16) = x[c];
     }
 
     const int first = single ? 0 : p.step, last = single ? p.steps : p.step + 1;
@@ -206,17 +266,26 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
         } else {
             const float *part = p.part + ((long)(step & 1) * gridDim.y + batch) * p.slices * (kSide * kSide);
             const int *exps = p.exps + batch * p.slices;
-            int e_ref = 1 << 20;
-            if (step == 0) // (the slices' powers of two are brought to that of the largest numbers)
-                for (int k = 0; k < p.slices; ++k) e_ref = min(e_ref, exps[k]);
+            // the slices' powers of two are brought to that of the largest numbers (a lane knows one slice's: there are at most 32)
+            int e_ref = step == 0 ? exps[min(lane, p.slices - 1)] : 0;
+            const int e_lane = e_ref;
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) e_ref = min(e_ref, __shfl_xor(e_ref, off, 64));
             float v[4][4] = {};
-            for (int k = 0; k < p.slices; ++k) {
-                const float w = step == 0 ? ldexpf(1.f, 2 * (e_ref - exps[k])) : 1.f;
+            for (int k0 = 0; k0 < p.slices; k0 += 4) { // sixteen accesses on their way at a time
+                f32x4 x[4][4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const f32x4 x = *(const f32x4 *)(part + (long)k * (kSide * kSide) + c * 1024 + tid * 4);
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[c][e] += w * x[e];
+                    for (int c = 0; c < 4; ++c)
+                        x[k][c] = k0 + k < p.slices ? *(const f32x4 *)(part + (long)(k0 + k) * (kSide * kSide) + c * 1024 + tid * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float w = ldexpf(1.f, 2 * (e_ref - __shfl(e_lane, min(k0 + k, p.slices - 1), 64)));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[c][e] += w * x[k][c][e];
                 }
             }
             float take = kTake;
@@ -269,18 +338,53 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
             const float scale = (UPDATE ? -p.lr : 1.f) * kTake * kTake * ratio;
             TO *out = (TO *)p.out + batch * size;
             const int i = wm * 32 + (lane & 31);
+            auto where = [&](int b, int q, int k) -> long {
+                const int j = j0 + (b * 2 + wn) * 32 + q * 8 + (lane >> 5) * 4 + k;
+                if (i >= p.r || j >= p.n) return -1;
+                return p.tall ? (long)j * p.r + i : (long)i * p.n + j;
+            };
+            const bool wide = !p.tall && (p.n & 3) == 0;
+            struct alignas(4 * sizeof(TO)) Four { TO v[4]; };
 #pragma unroll
-            for (int b = 0; b < kJobs; ++b)
+            for (int b = 0; b < kJobs; ++b) {
+                float old[16] = {};
+                if (UPDATE) { // (asked for together, before the first store)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < 4; ++q)
+                        if (wide) {
+                            const long at = where(b, q, 0);
+                            Four f;
+                            if (at >= 0) f = *(const Four *)(out + at);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int j = j0 + (b * 2 + wn) * 32 + q * 8 + (lane >> 5) * 4 + k;
-                        if (i >= p.r || j >= p.n) continue;
-                        TO *o = out + (p.tall ? (long)j * p.r + i : (long)i * p.n + j);
-                        const float x = scale * y[b][q * 4 + k];
-                        Elem<TO>::store(o, UPDATE ? p.keep * Elem<TO>::load(o) + x : x);
+                            for (int k = 0; k < 4; ++k) old[q * 4 + k] = at >= 0 ? Elem<TO>::load(&f.v[k]) : 0.f;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const long at = where(b, q, k);
+                                old[q * 4 + k] = at >= 0 ? Elem<TO>::load(out + at) : 0.f;
+                            }
+                        }
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = UPDATE ? p.keep * old[q * 4 + k] + scale * y[b][q * 4 + k] : scale * y[b][q * 4 + k];
+                    if (wide) {
+                        const long at = where(b, q, 0);
+                        Four f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) Elem<TO>::store(&f.v[k], v[k]);
+                        if (at >= 0) *(Four *)(out + at) = f;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const long at = where(b, q, k);
+                            if (at >= 0) Elem<TO>::store(out + at, v[k]);
+                        }
                     }
+                }
+            }
             return;
         }
         __syncthreads(); // (every wave has read the columns that it multiplied)
