@@ -83,28 +83,36 @@ __device__ __forceinline__ f32x16 zeros()
     for (int r = 0; r < 16; ++r) z[r] = 0.f;
     return z;
 }
-// a value of every thread's, added up over the block in a fixed order (red: 4 floats)
-__device__ __forceinline__ float block_sum(float v, float *red)
+// a value of every thread's, added up over the block in a fixed order, or the largest (red: a float a wave that nobody else uses)
+template <bool LARGEST, int kWaves> __device__ __forceinline__ float over_block(float v, float *red)
 {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    for (int off = 32; off > 0; off >>= 1) v = LARGEST ? fmaxf(v, __shfl_xor(v, off, 64)) : v + __shfl_xor(v, off, 64);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    return ((red[0] + red[1]) + red[2]) + red[3];
+    v = red[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v = LARGEST ? fmaxf(v, red[w]) : v + red[w];
+    __syncthreads();
+    return v;
 }
 
-// W columns to a workgroup of four waves
-template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch_bounds__(256) narrow_kernel(const Args p)
+// W columns to a workgroup of KG groups of 2 x 2 waves, which share the terms of X X^T
+template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void __launch_bounds__(256 * KG) narrow_kernel(const Args p)
 {
+    constexpr int kWaves = 4 * KG, kThreads = 64 * kWaves;
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int RS = 4 * W, kCols = kSide * RS; // bytes
-    constexpr int kOwn = W / 32;                  // chunks of eight columns that a thread brings in
-    constexpr int kJobs = W / 64;                 // blocks of 32 x 32 that a wave multiplies
+    constexpr int kOwn = W * 8 / kThreads;        // chunks of eight columns that a thread brings in
+    constexpr int kApart = kWaves / 2, kJobs = W / 32 / kApart; // a wave multiplies every kApart-th block of 32 columns
+    constexpr int kCopies = kCols / (16 * kThreads), kSums = 1024 / kThreads;
     unsigned char *X = smem, *A = smem + kCols, *B = A + kSquare;
-    float *red = (float *)(B + kSquare);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    float *red = (float *)A;
+    const int tid = threadIdx.x, wave = tid >> 6, group = wave >> 2, wm = (wave >> 1) & 1, wn = wave & 1;
+    const int rb = (wave & 1) * 32, cb = wave >> 1; // the rows, and the first block of columns, of the polynomial's product
     const int slice = blockIdx.x, batch = blockIdx.y, j0 = slice * W;
+    int lane = tid & 63;
     const long size = (long)p.r * p.n;
     char *x_mine = p.x + ((long)batch * p.slices + slice) * kCols;
     const bool single = p.slices == 1;
@@ -113,118 +121,126 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
     float ratio = 1.f; // what X has to be multiplied by to be X times kStore
     f32x16 s = zeros();
 
-    auto gram = [&]() {
+    auto gram = [&]() { // into the first group's s; A is free
         s = zeros();
-#pragma unroll 4
-        for (int k = 0; k < W / 16; ++k)
+        if (W > 64) asm volatile("" : "+v"(lane));
+#pragma unroll 2
+        for (int kk = 0; kk < W / 16 / KG; ++kk) {
+            const int k = kk * KG + group;
             three(along(X, RS, wm * 32, k, 0, lane), along(X, RS, wm * 32, k, 1, lane), along(X, RS, wn * 32, k, 0, lane), along(X, RS, wn * 32, k, 1, lane), &s);
+        }
+        if (KG == 1) return;
+        f32x4 *sums = (f32x4 *)A + (wave & 3) * 256 + lane;
+        if (group == 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sums[q * 64] = f32x4{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 v = sums[q * 64];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[q * 4 + k] += v[k];
+            }
+        __syncthreads();
     };
     auto leave = [&](int parity) { // this workgroup's part of X X^T, and its columns
         float *o = p.part + ((((long)parity * gridDim.y + batch) * p.slices) + slice) * (kSide * kSide);
+        if (group == 0)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *(f32x4 *)(o + (wm * 32 + (lane & 31)) * kSide + wn * 32 + q * 8 + (lane >> 5) * 4) = f32x4{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
-        for (int c = tid * 16; c < kCols; c += 4096) *(u32x4 *)(x_mine + c) = *(const u32x4 *)(X + c);
+            for (int q = 0; q < 4; ++q)
+                *(f32x4 *)(o + (wm * 32 + (lane & 31)) * kSide + wn * 32 + q * 8 + (lane >> 5) * 4) = f32x4{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) *(u32x4 *)(x_mine + (c * kThreads + tid) * 16) = *(const u32x4 *)(X + (c * kThreads + tid) * 16);
     };
 
     if (p.step < 0) {
-        // U, eight neighbouring columns of a row to a thread and turn; neighbouring threads take neighbours in memory.  Everything is
-        // asked for before anything is stored, so that it is on its way together.
-        float u[kOwn][8], top = 0.f;
+        // U, eight neighbouring columns of a row to a thread and turn; neighbouring threads take neighbours in memory.  A few turns' numbers
+        // are asked for before any is stored, so that they are on their way together.  Until the largest number is known they wait as
+        // floats where their halves will be.
+        float top = 0.f;
         const TG *g = (const TG *)p.G + batch * size;
         float *m = p.M ? p.M + batch * size : nullptr;
-        auto where = [&](int c, int e) -> long { // of element e of turn c; -1 past the edge
-            const int at = c * 256 + tid, i = p.tall ? at & 63 : at / (W / 8), j = j0 + (p.tall ? at >> 6 : at % (W / 8)) * 8 + e;
-            if (i >= p.r || j >= p.n) return -1;
-            return p.tall ? (long)j * p.r + i : (long)i * p.n + j;
-        };
         // (rows of whole groups of four, and a first column that is one of 64: four neighbours in one access)
         const bool wide = !p.tall && (p.n & 3) == 0;
         struct alignas(4 * sizeof(TG)) Four { TG v[4]; };
+        constexpr int kTogether = kOwn <= 4 ? kOwn : 4;
+        auto row_of = [&](int c) { return p.tall ? (c * kThreads + tid) & 63 : (c * kThreads + tid) / (W / 8); };
+        auto col_of = [&](int c) { return (p.tall ? (c * kThreads + tid) >> 6 : (c * kThreads + tid) % (W / 8)) * 8; };
+#pragma unroll 1
+        for (int c0 = 0; c0 < kOwn; c0 += kTogether) {
+            float u[kTogether][8], mm[kTogether][8];
 #pragma unroll
-        for (int c = 0; c < kOwn; ++c) {
-            if (wide) {
+            for (int t = 0; t < kTogether; ++t) {
+                const int i = row_of(c0 + t), j = j0 + col_of(c0 + t);
+                const long at = p.tall ? (long)j * p.r + i : (long)i * p.n + j, step = p.tall ? p.r : 1;
+                const int left = i < p.r ? p.n - j : 0; // elements from the first on
 #pragma unroll
                 for (int h = 0; h < 8; h += 4) {
-                    const long k = where(c, h);
-                    Four f;
-                    if (k >= 0) f = *(const Four *)(g + k);
+                    if (wide) {
+                        Four f;
+                        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+                        if (h < left) f = *(const Four *)(g + at + h);
+                        if (h < left && m) o = *(const f32x4 *)(m + at + h);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[c][h + e] = k >= 0 ? Elem<TG>::load(&f.v[e]) : 0.f;
-                }
-            } else {
+                        for (int e = 0; e < 4; ++e) {
+                            u[t][h + e] = h < left ? Elem<TG>::load(&f.v[e]) : 0.f;
+                            mm[t][h + e] = o[e];
+                        }
+                    } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const long k = where(c, e);
-                    u[c][e] = k >= 0 ? Elem<TG>::load(g + k) : 0.f;
+                        for (int e = h; e < h + 4; ++e) {
+                            u[t][e] = e < left ? Elem<TG>::load(g + at + e * step) : 0.f;
+                            mm[t][e] = e < left && m ? m[at + e * step] : 0.f;
+                        }
+                    }
                 }
             }
-        }
-        if (m) {
-            float mm[kOwn][8];
 #pragma unroll
-            for (int c = 0; c < kOwn; ++c)
-                if (wide) {
-#pragma unroll
-                    for (int h = 0; h < 8; h += 4) {
-                        const long k = where(c, h);
-                        const f32x4 f = k >= 0 ? *(const f32x4 *)(m + k) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mm[c][h + e] = f[e];
-                    }
-                } else {
+            for (int t = 0; t < kTogether; ++t) {
+                const int i = row_of(c0 + t), jc = col_of(c0 + t), j = j0 + jc;
+                const long at = p.tall ? (long)j * p.r + i : (long)i * p.n + j, step = p.tall ? p.r : 1;
+                const int left = i < p.r ? p.n - j : 0;
+                if (m) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const long k = where(c, e);
-                        mm[c][e] = k >= 0 ? m[k] : 0.f;
+                        mm[t][e] = p.mu * mm[t][e] + u[t][e];
+                        u[t][e] = p.nesterov ? u[t][e] + p.mu * mm[t][e] : mm[t][e];
                     }
-                }
-#pragma unroll
-            for (int c = 0; c < kOwn; ++c) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    mm[c][e] = p.mu * mm[c][e] + u[c][e];
-                    u[c][e] = p.nesterov ? u[c][e] + p.mu * mm[c][e] : mm[c][e];
-                }
-                if (wide) {
 #pragma unroll
                     for (int h = 0; h < 8; h += 4) {
-                        const long k = where(c, h);
-                        if (k >= 0) *(f32x4 *)(m + k) = f32x4{mm[c][h], mm[c][h + 1], mm[c][h + 2], mm[c][h + 3]};
-                    }
-                } else {
+                        if (wide) {
+                            if (h < left) *(f32x4 *)(m + at + h) = f32x4{mm[t][h], mm[t][h + 1], mm[t][h + 2], mm[t][h + 3]};
+                        } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const long k = where(c, e);
-                        if (k >= 0) m[k] = mm[c][e];
+                            for (int e = h; e < h + 4; ++e)
+                                if (e < left) m[at + e * step] = mm[t][e];
+                        }
                     }
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a = fabsf(u[t][e]);
+                    top = a <= 3.4028235e38f ? fmaxf(top, a) : top;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *(f32x4 *)(X + place(i, (jc >> 3) * 2 + h, RS)) = f32x4{u[t][h * 4], u[t][h * 4 + 1], u[t][h * 4 + 2], u[t][h * 4 + 3]};
             }
         }
-#pragma unroll
-        for (int c = 0; c < kOwn; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float a = fabsf(u[c][e]);
-                top = a <= 3.4028235e38f ? fmaxf(top, a) : top;
-            }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        if (lane == 0) red[wave] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        top = over_block<true, kWaves>(top, red);
         if (top > 0.f) {
             frexpf(top, &e_mine);
             e_mine = 12 - e_mine; // the largest is stored as one below 2^12
         }
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < kOwn; ++c) {
-            const int at = c * 256 + tid, i = p.tall ? at & 63 : at / (W / 8), j = (p.tall ? at >> 6 : at % (W / 8)) * 8;
-#pragma unroll
-            for (int h = 0; h < 8; h += 4) {
-                const float v[4] = {ldexpf(u[c][h], e_mine), ldexpf(u[c][h + 1], e_mine), ldexpf(u[c][h + 2], e_mine), ldexpf(u[c][h + 3], e_mine)};
-                put(X, RS, i, j + h, v);
-            }
+            const int i = row_of(c), jc = col_of(c);
+            const f32x4 a = *(const f32x4 *)(X + place(i, (jc >> 3) * 2, RS)), b = *(const f32x4 *)(X + place(i, (jc >> 3) * 2 + 1, RS));
+            const float v[4] = {ldexpf(a[0], e_mine), ldexpf(a[1], e_mine), ldexpf(a[2], e_mine), ldexpf(a[3], e_mine)};
+            const float w[4] = {ldexpf(b[0], e_mine), ldexpf(b[1], e_mine), ldexpf(b[2], e_mine), ldexpf(b[3], e_mine)};
+            put(X, RS, i, jc, v);
+            put(X, RS, i, jc + 4, w);
         }
         __syncthreads();
         gram();
@@ -233,31 +249,27 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
             if (tid == 0) p.exps[batch * p.slices + slice] = e_mine;
             return;
         }
-    } else {
-        u32x4 x[kCols / 4096];
-#pragma unroll
-        for (int c = 0; c < kCols / 4096; ++c) x[c] = *(const u32x4 *)(x_mine + c * 4096 + tid * 16);
-#pragma unroll
-        for (int c = 0; c < kCols / 4096; ++c) *(u32x4 *)(X + c * 4096 + tid * 16) = x[c];
     }
 
     const int first = single ? 0 : p.step, last = single ? p.steps : p.step + 1;
     for (int step = first; step < last; ++step) {
+        if (W > 64) asm volatile("" : "+v"(lane)); // (places in LDS are worked out where they are used: kept from step to step they take all registers)
         // A times kStore, as two halves
         if (single) {
             float take = kTake;
             if (step == 0) {
                 float d = 0.f;
-                if (wm == wn)
+                if (group == 0 && wm == wn)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (q * 8 + (lane >> 5) * 4 + k == (lane & 31)) d += s[q * 4 + k];
-                const double norm = sqrt((double)block_sum(d, red)) + ldexp((double)kEps, e_mine); // in U's units times 2^e_mine
+                const double norm = sqrt((double)over_block<false, kWaves>(d, red)) + ldexp((double)kEps, e_mine); // in U's units times 2^e_mine
                 ratio = (float)((double)kStore / norm);
                 take = (float)((double)kStore / (norm * norm));
             }
+            if (group == 0)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float v[4] = {s[q * 4] * take, s[q * 4 + 1] * take, s[q * 4 + 2] * take, s[q * 4 + 3] * take};
@@ -271,75 +283,83 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
             const int e_lane = e_ref;
 #pragma unroll
             for (int off = 32; off > 0; off >>= 1) e_ref = min(e_ref, __shfl_xor(e_ref, off, 64));
-            float v[4][4] = {};
-            for (int k0 = 0; k0 < p.slices; k0 += 4) { // sixteen accesses on their way at a time
-                f32x4 x[4][4];
+            u32x4 mine[kCopies]; // (the columns are on their way while the parts are added up)
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+            for (int c = 0; c < kCopies; ++c) mine[c] = *(const u32x4 *)(x_mine + (c * kThreads + tid) * 16);
+            float v[kSums][4] = {};
+            for (int k0 = 0; k0 < p.slices; k0 += 16 / kSums) { // sixteen accesses on their way at a time
+                f32x4 x[16 / kSums][kSums];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        x[k][c] = k0 + k < p.slices ? *(const f32x4 *)(part + (long)(k0 + k) * (kSide * kSide) + c * 1024 + tid * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int k = 0; k < 16 / kSums; ++k)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                    for (int c = 0; c < kSums; ++c)
+                        x[k][c] = k0 + k < p.slices ? *(const f32x4 *)(part + (long)(k0 + k) * (kSide * kSide) + (c * kThreads + tid) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < 16 / kSums; ++k) {
                     const float w = ldexpf(1.f, 2 * (e_ref - __shfl(e_lane, min(k0 + k, p.slices - 1), 64)));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < kSums; ++c)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[c][e] += w * x[k][c][e];
                 }
             }
+#pragma unroll
+            for (int c = 0; c < kCopies; ++c) *(u32x4 *)(X + (c * kThreads + tid) * 16) = mine[c];
             float take = kTake;
             if (step == 0) {
                 float d = 0.f;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < kSums; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if ((tid & 15) * 4 + e == c * 16 + (tid >> 4)) d += v[c][e];
-                const double norm = sqrt((double)block_sum(d, red)) + ldexp((double)kEps, e_ref);
+                        if ((tid & 15) * 4 + e == c * (kThreads / 16) + (tid >> 4)) d += v[c][e];
+                const double norm = sqrt((double)over_block<false, kWaves>(d, red)) + ldexp((double)kEps, e_ref);
                 ratio = (float)(ldexp((double)kStore, e_ref - exps[slice]) / norm);
                 take = (float)((double)kStore / (norm * norm));
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < kSums; ++c) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[c][e] *= take;
-                put(A, 256, c * 16 + (tid >> 4), (tid & 15) * 4, v[c]);
+                put(A, 256, c * (kThreads / 16) + (tid >> 4), (tid & 15) * 4, v[c]);
             }
         }
         __syncthreads();
-        // a I + b A + c A A
-        f32x16 acc = zeros();
+        // a I + b A + c A A, by the first group
+        if (group == 0) {
+            f32x16 acc = zeros();
 #pragma unroll
-        for (int k = 0; k < kSide / 16; ++k)
-            three(along(A, 256, wm * 32, k, 0, lane), along(A, 256, wm * 32, k, 1, lane), along(A, 256, wn * 32, k, 0, lane), along(A, 256, wn * 32, k, 1, lane), &acc);
+            for (int k = 0; k < kSide / 16; ++k)
+                three(along(A, 256, wm * 32, k, 0, lane), along(A, 256, wm * 32, k, 1, lane), along(A, 256, wn * 32, k, 0, lane), along(A, 256, wn * 32, k, 1, lane), &acc);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int i = wm * 32 + (lane & 31), j = wn * 32 + q * 8 + (lane >> 5) * 4;
-            float v[4];
-            get(A, 256, i, j, v);
+            for (int q = 0; q < 4; ++q) {
+                const int i = wm * 32 + (lane & 31), j = wn * 32 + q * 8 + (lane >> 5) * 4;
+                float v[4];
+                get(A, 256, i, j, v);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = kB * v[k] + (kC * kTake) * acc[q * 4 + k] + (i == j + k ? kA * kStore : 0.f);
-            put(B, 256, i, j, v);
+                for (int k = 0; k < 4; ++k) v[k] = kB * v[k] + (kC * kTake) * acc[q * 4 + k] + (i == j + k ? kA * kStore : 0.f);
+                put(B, 256, i, j, v);
+            }
         }
         __syncthreads();
-        // ... times X: rows wm * 32 on, every other block of columns
+        // ... times X: 32 rows, every kApart-th block of columns
+        if (W > 64) asm volatile("" : "+v"(lane));
         f32x16 y[kJobs];
 #pragma unroll
         for (int b = 0; b < kJobs; ++b) y[b] = zeros();
 #pragma unroll
         for (int k = 0; k < kSide / 16; ++k) {
-            const s16x8 bh = along(B, 256, wm * 32, k, 0, lane), bl = along(B, 256, wm * 32, k, 1, lane);
+            const s16x8 ph = along(B, 256, rb, k, 0, lane), pl = along(B, 256, rb, k, 1, lane);
 #pragma unroll
             for (int b = 0; b < kJobs; ++b)
-                three(bh, bl, down(X, RS, (b * 2 + wn) * 32, k, 0, lane), down(X, RS, (b * 2 + wn) * 32, k, 1, lane), &y[b]);
+                three(ph, pl, down(X, RS, (cb + b * kApart) * 32, k, 0, lane), down(X, RS, (cb + b * kApart) * 32, k, 1, lane), &y[b]);
         }
         if (step + 1 == p.steps) {
             const float scale = (UPDATE ? -p.lr : 1.f) * kTake * kTake * ratio;
             TO *out = (TO *)p.out + batch * size;
-            const int i = wm * 32 + (lane & 31);
+            const int i = rb + (lane & 31);
             auto where = [&](int b, int q, int k) -> long {
-                const int j = j0 + (b * 2 + wn) * 32 + q * 8 + (lane >> 5) * 4 + k;
+                const int j = j0 + (cb + b * kApart) * 32 + q * 8 + (lane >> 5) * 4 + k;
                 if (i >= p.r || j >= p.n) return -1;
                 return p.tall ? (long)j * p.r + i : (long)i * p.n + j;
             };
@@ -388,6 +408,7 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
             return;
         }
         __syncthreads(); // (every wave has read the columns that it multiplied)
+        if (W > 64) asm volatile("" : "+v"(lane));
 #pragma unroll
         for (int b = 0; b < kJobs; ++b)
 #pragma unroll
@@ -395,7 +416,7 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = y[b][q * 4 + k] * (kTake * ratio);
-                put(X, RS, wm * 32 + (lane & 31), (b * 2 + wn) * 32 + q * 8 + (lane >> 5) * 4, v);
+                put(X, RS, rb + (lane & 31), (cb + b * kApart) * 32 + q * 8 + (lane >> 5) * 4, v);
             }
         ratio = 1.f;
         __syncthreads();
@@ -406,15 +427,15 @@ template <typename TG, typename TO, bool UPDATE, int W> __global__ void __launch
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-template <typename TG, typename TO, bool UPDATE, int W> hipError_t launch(Args a, int batch, hipStream_t st)
+template <typename TG, typename TO, bool UPDATE, int W, int KG> hipError_t launch(Args a, int batch, hipStream_t st)
 {
-    constexpr int lds = kSide * 4 * W + 2 * kSquare + 64;
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(narrow_kernel<TG, TO, UPDATE, W>),
+    constexpr int lds = kSide * 4 * W + 2 * kSquare;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(narrow_kernel<TG, TO, UPDATE, W, KG>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
     for (int step = -1; step < (a.slices == 1 ? 0 : a.steps); ++step) {
         a.step = step;
-        hipLaunchKernelGGL((narrow_kernel<TG, TO, UPDATE, W>), dim3(a.slices, batch), dim3(256), lds, st, a);
+        hipLaunchKernelGGL((narrow_kernel<TG, TO, UPDATE, W, KG>), dim3(a.slices, batch), dim3(256 * KG), lds, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -422,9 +443,9 @@ template <typename TG, typename TO, bool UPDATE, int W> hipError_t launch(Args a
 }
 template <typename TG, typename TO, bool UPDATE> hipError_t launch(const Args &a, int width, int batch, hipStream_t st)
 {
-    if (width == 64) return launch<TG, TO, UPDATE, 64>(a, batch, st);
-    if (width == 128) return launch<TG, TO, UPDATE, 128>(a, batch, st);
-    return launch<TG, TO, UPDATE, 256>(a, batch, st);
+    if (width == 64) return launch<TG, TO, UPDATE, 64, 1>(a, batch, st);
+    if (width == 128) return launch<TG, TO, UPDATE, 128, 1>(a, batch, st);
+    return launch<TG, TO, UPDATE, 256, 2>(a, batch, st);
 }
 template <typename TG> hipError_t launch(const Args &a, int width, int batch, int dtype, bool update, hipStream_t st)
 {
@@ -439,7 +460,7 @@ bool plan_muon_narrow(const MuonGeom &g, MuonNarrowPlan *p)
     const long r = g.rows < g.cols ? g.rows : g.cols, n = g.rows < g.cols ? g.cols : g.rows;
     // every workgroup reads all of its matrix' parts: not more than 32 of them
     if (r > kSide || n > 8192) return false;
-    p->width = n <= 64 ? 64 : n <= 128 || (n > 256 && n <= 2048) ? 128 : 256;
+    p->width = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : n <= 2048 ? 128 : 256;
     p->slices = (int)((n + p->width - 1) / p->width);
     size_t o = 0;
     p->o_x = o;
