@@ -676,8 +676,7 @@ template <typename T> struct PairParams {
     typename OutW<T>::Params ew;
     typename OutH<T>::Params eh;
     Bias<T> b;
-    unsigned blocks_w, blocks_h; // of dW; of one of dH's slices
-    int slices_h;
+    unsigned blocks_w, blocks_h;
 };
 template <typename T> __global__ void __launch_bounds__(Small::kThreads, Small::kPerSimd) pair_kernel(const PairParams<T> p)
 {
@@ -685,16 +684,12 @@ template <typename T> __global__ void __launch_bounds__(Small::kThreads, Small::
     typedef typename FormatOf<T>::type P;
     unsigned block = blockIdx.x;
     if (block < p.blocks_w) {
-        mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, 0, smem);
+        mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, smem);
         return;
     }
     block -= p.blocks_w;
-    if (block < p.blocks_h * p.slices_h) {
-        const unsigned slice = block / p.blocks_h;
-        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block - slice * p.blocks_h, slice, smem);
-        return;
-    }
-    bias_sums(p.b, block - p.blocks_h * p.slices_h, (float(*)[64])smem);
+    if (block < p.blocks_h) mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block, smem);
+    else bias_sums(p.b, block - p.blocks_h, (float(*)[64])smem);
 }
 
 // a slice's part of the logits' products, [slice][T][ld]
@@ -1001,13 +996,12 @@ public:
             q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr};
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
-                q.slices_h = p.h.slices;
                 if (dW) q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
                 if (dH) q.blocks_h = place_tiles<Small>(&q.h, false, p.h.slices, kPass<P, Small::R>);
                 static const hipError_t attr =
                     hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, Small::kLds);
                 if (attr != hipSuccess) return attr;
-                hipLaunchKernelGGL(pair_kernel<T>, dim3(q.blocks_w + q.blocks_h * q.slices_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
+                hipLaunchKernelGGL(pair_kernel<T>, dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
                 e = hipGetLastError();
             } else {
                 if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(q.w, q.ew, p.w, st);

@@ -57,8 +57,8 @@ struct Params {
     long a_batch, b_batch;     // bytes from a matrix to the next
     int M, N, K;
     const int *m_dev, *k_dev;  // where set: the rows (the terms) that there really are, at most M (K)
-    int tiles_m, tiles_n, batch;
-    int tiles;                 // of one matrix: tiles_m * tiles_n, or those on and above the diagonal
+    int tiles_n, tiles;        // tiles in a row of them, and of one matrix: all, or those on and above the diagonal
+    int batch, slices;         // matrices; parts that each sum is formed in
     int group;                 // tile rows that one XCD walks together
     int kt_slice;              // passes over K of one slice of the sum
     Counts counts_m, counts_k; // rows of a (terms of b, of which there is one pass) that count: the others are zeros, whatever stands there
@@ -295,9 +295,9 @@ template <int N> __device__ __forceinline__ void meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// One workgroup's tile, as workgroup `block` of the product; slice: which part of the sum.
+// One workgroup's tile, as workgroup `block` of the product.
 template <class P, Lay LA, Lay LB, class S, class Epi>
-__device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Params &e, int block, int slice, unsigned char *smem)
+__device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Params &e, int block, unsigned char *smem)
 {
     constexpr int MI = S::MI, NI = S::NI, TM = S::TM, TN = S::TN;
     constexpr int kSteps = S::R / 32 / P::kParts; // of 16 terms, in a pass
@@ -305,23 +305,25 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = p.m_dev ? min(p.M, *p.m_dev) : p.M, K = p.k_dev ? min(p.K, *p.k_dev) : p.K;
 
-    // Workgroups go round the eight XCDs: each XCD gets a run of neighbouring tiles, and walks it in groups of `group` tile rows.
-    const int per = (p.tiles * p.batch + 7) / 8;
-    const int t = (block & 7) * per + (block >> 3);
-    if ((block >> 3) >= per || t >= p.tiles * p.batch) return;
-    const int batch = t / p.tiles, tt = t - batch * p.tiles;
+    // Workgroups go round the eight XCDs, each with an L2 of its own: an XCD gets a run of neighbouring tiles of the rows that there
+    // really are, slice after slice (a slice's tiles share its terms and no other's), and walks it in groups of `group` tile rows.
+    const int tiles_m = (M + TM - 1) / TM, tiles = Epi::kSymmetric ? p.tiles : tiles_m * p.tiles_n, all = tiles * p.slices * p.batch;
+    const int per = (all + 7) / 8, t = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || t >= all) return;
+    // (said to be uniform, which quotients of uniform numbers are not seen to be)
+    const int batch = __builtin_amdgcn_readfirstlane(t / (tiles * p.slices));
+    const int slice = __builtin_amdgcn_readfirstlane(t / tiles) - batch * p.slices, tt = t - (batch * p.slices + slice) * tiles;
     int tm, tn;
     if (Epi::kSymmetric) { // the tiles on and above the diagonal, row by row: row i has tiles_m - i
-        tm = (int)(p.tiles_m + 0.5f - sqrtf((p.tiles_m + 0.5f) * (p.tiles_m + 0.5f) - 2.f * tt));
-        while (tm > 0 && tm * p.tiles_m - tm * (tm - 1) / 2 > tt) --tm;
-        while ((tm + 1) * p.tiles_m - (tm + 1) * tm / 2 <= tt) ++tm;
-        tn = tt - (tm * p.tiles_m - tm * (tm - 1) / 2) + tm;
+        tm = __builtin_amdgcn_readfirstlane((int)(tiles_m + 0.5f - sqrtf((tiles_m + 0.5f) * (tiles_m + 0.5f) - 2.f * tt)));
+        while (tm > 0 && tm * tiles_m - tm * (tm - 1) / 2 > tt) --tm;
+        while ((tm + 1) * tiles_m - (tm + 1) * tm / 2 <= tt) ++tm;
+        tn = tt - (tm * tiles_m - tm * (tm - 1) / 2) + tm;
     } else {
-        const int g0 = tt / (p.group * p.tiles_n) * p.group, gr = min(p.group, p.tiles_m - g0), gi = tt - g0 * p.tiles_n;
-        tm = g0 + gi % gr;
-        tn = gi / gr;
+        const int g0 = __builtin_amdgcn_readfirstlane(tt / (p.group * p.tiles_n)) * p.group, gr = min(p.group, tiles_m - g0), gi = tt - g0 * p.tiles_n;
+        tn = __builtin_amdgcn_readfirstlane(gi / gr);
+        tm = g0 + gi - tn * gr;
     }
-    if (tm * TM >= M) return;
 
     const int passes = (K + kPass<P, S::R> - 1) / kPass<P, S::R>;
     const int kt0 = slice * p.kt_slice, kt1 = min(passes, kt0 + p.kt_slice);
@@ -412,7 +414,7 @@ template <class P, Lay LA, Lay LB, class S, class Epi>
 __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Params p, const typename Epi::Params e)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    mm_tile<P, LA, LB, S, Epi>(p, e, blockIdx.x, blockIdx.y, smem);
+    mm_tile<P, LA, LB, S, Epi>(p, e, blockIdx.x, smem);
 }
 
 // ---- host
@@ -470,15 +472,16 @@ inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetr
 // parts that a row's columns fall into, one to a wave
 inline long wave_columns(long N, int shape) { return (long)cdiv(N, kEdge[shape]) * wave_columns_of(shape); }
 
-// Fills in the tiles; returns the workgroups of one slice (a multiple of the XCDs).
+// Fills in the tiles; returns the workgroups (a multiple of the XCDs).
 template <class S> inline unsigned place_tiles(Params *p, bool symmetric, int slices, int pass)
 {
-    p->tiles_m = cdiv(p->M, S::TM);
+    const int tiles_m = cdiv(p->M, S::TM);
     p->tiles_n = cdiv(p->N, S::TN);
-    p->tiles = symmetric ? p->tiles_m * (p->tiles_m + 1) / 2 : p->tiles_m * p->tiles_n;
+    p->tiles = symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * p->tiles_n;
     p->group = 8;
+    p->slices = slices;
     p->kt_slice = cdiv(cdiv(p->K, pass), slices);
-    return (unsigned)(8 * (((long)p->tiles * p->batch + 7) / 8));
+    return (unsigned)(8 * (((long)p->tiles * p->batch * slices + 7) / 8));
 }
 template <class P, Lay LA, Lay LB, class S, class Epi>
 hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hipStream_t st)
@@ -487,7 +490,7 @@ hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hip
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
     if (attr != hipSuccess) return attr;
     const unsigned blocks = place_tiles<S>(&p, Epi::kSymmetric, slices, kPass<P, S::R>);
-    hipLaunchKernelGGL((mm_kernel<P, LA, LB, S, Epi>), dim3(blocks, slices), dim3(S::kThreads), S::kLds, st, p, e);
+    hipLaunchKernelGGL((mm_kernel<P, LA, LB, S, Epi>), dim3(blocks), dim3(S::kThreads), S::kLds, st, p, e);
     return hipGetLastError();
 }
 
