@@ -212,6 +212,18 @@ __device__ __forceinline__ void load_split(const char *row, int n, float (&v)[4]
     for (int e = 0; e < 4; ++e) v[e] = (float)hi.h[e] + (float)lo.h[e];
 }
 
+// ---- Newton-Schulz products (muon.hip, muon_narrow.hip)
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f, kNsEps = 1e-7f;
+constexpr float kNsStore = 4096.f, kNsTake = 1.f / 4096.f; // what X, A and the polynomial are stored times
+// A matrix whose norm is little beside kNsEps starts, and a few steps at 3.4445 apiece later ends, with small numbers: its X is
+// stored times 2^lift too, by as much as the last step leaves room for.
+__device__ __forceinline__ int ns_lift(double norm, int steps)
+{
+    const double last = norm / (norm + (double)kNsEps) * pow((double)kNsA, (double)steps);
+    if (!(last > 0.0 && last < 1.0)) return 0;
+    return -ilogb(last) - 1;
+}
+
 // ---- 32 rows of a wave's part of C on their way to memory.  A lane holds four neighbours of a row, and a store of them touches 32 rows at
 // 8 or 16 bytes each; through LDS they become stores of 16 bytes a lane, whole lines side by side.
 enum class Fmt { kBf16, kF32, kSplit };

@@ -18,15 +18,14 @@ namespace {
 
 using namespace mm;
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
-constexpr float kStore = 4096.f, kTake = 1.f / 4096.f; // what X, A and the polynomial are stored times
+constexpr float kA = kNsA, kB = kNsB, kC = kNsC, kTake = kNsTake, kStore = kNsStore;
 constexpr int kMaxSumBlocks = 256;
 
 // ---- endings of the products
 // S = acc / 4096, symmetric: the tiles above the diagonal are computed and written twice
 struct Gram {
     static constexpr bool kSymmetric = true;
-    struct Params { char *out; long ld, stride; };
+    struct Params { char *out; long ld, stride; const int *lift; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p);
 };
 // a I + b A + c A A
@@ -83,9 +82,10 @@ template <int MI, int NI, class Fn> __device__ __forceinline__ void store_symmet
 
 template <int MI, int NI> __device__ __forceinline__ void Gram::run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
 {
+    const float take = ldexpf(kTake, -2 * e.lift[p.batch]);
     store_symmetric_part<MI, NI>(e.out + p.batch * e.stride, e.ld, p, [&](int i, int j, int q, int, int, float (&v)[4]) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k] * kTake;
+        for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k] * take;
     });
 }
 
@@ -128,7 +128,7 @@ struct GramPart {
 };
 // ... and S from the slices' parts: 32 x 32 of it to a block, of which a thread has four neighbours of a row
 __global__ void __launch_bounds__(256) join_gram_kernel(const float *__restrict__ part, int r, int ld, int batches, int slices, int tile,
-                                                        char *__restrict__ out, long ld_out)
+                                                        char *__restrict__ out, long ld_out, const int *__restrict__ lift)
 {
     if (blockIdx.x * 32 / tile < blockIdx.y * 32 / tile) return; // (below the diagonal's tiles: written as the mirror image)
     const bool mirror = blockIdx.x * 32 / tile != blockIdx.y * 32 / tile;
@@ -141,8 +141,9 @@ __global__ void __launch_bounds__(256) join_gram_kernel(const float *__restrict_
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] += x[e];
         }
+    const float take = ldexpf(kTake, -2 * lift[blockIdx.z]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= kTake;
+    for (int e = 0; e < 4; ++e) v[e] *= take;
     store_symmetric(out + blockIdx.z * r * ld_out, ld_out, m, n, r, (r + 7) & ~7, mirror, v);
 }
 
@@ -177,11 +178,12 @@ struct Next {
 // the result, or the weights' update: out = keep * out + scale * acc
 template <typename T, bool UPDATE> struct Last {
     static constexpr bool kSymmetric = false;
-    struct Params { T *out; float keep, scale; };
+    struct Params { T *out; float keep, scale; const int *lift; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         T *out = e.out + (long)p.batch * p.M * p.N;
         const bool wide = (p.N & 3) == 0; // rows in whole groups of four
+        const float scale = ldexpf(e.scale, -e.lift[p.batch]);
         typedef RowBlock<Fmt::kF32, NI> Block;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -192,7 +194,7 @@ template <typename T, bool UPDATE> struct Last {
                 for (int q = 0; q < 4; ++q) {
                     float v[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = e.scale * acc[i][j][q * 4 + k];
+                    for (int k = 0; k < 4; ++k) v[k] = scale * acc[i][j][q * 4 + k];
                     Block::put(p.lds, p.lane, j, q, v);
                 }
             // (float in LDS for both types: four numbers to a lane, neighbouring lanes side by side)
@@ -272,7 +274,7 @@ momentum_kernel(const TG *__restrict__ G, float *__restrict__ M, long size, floa
 // X_0, split; a thread takes eight neighbours of a row
 template <typename TG> __global__ void __launch_bounds__(256)
 normalise_kernel(const TG *__restrict__ G, const float *__restrict__ M, int rows, int cols, float mu, int nesterov,
-                 const double *__restrict__ part, int nparts, char *__restrict__ X, long ld)
+                 const double *__restrict__ part, int nparts, char *__restrict__ X, long ld, int steps, int *__restrict__ lifts)
 {
     const int batch = blockIdx.y;
     __shared__ double red[4];
@@ -281,8 +283,10 @@ normalise_kernel(const TG *__restrict__ G, const float *__restrict__ M, int rows
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
     // (divided in double: a norm that float does not hold, of a gradient that it does, still has a quotient)
-    const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]) + (double)kEps;
-    const double scale = (double)kStore / norm;
+    const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
+    const int lift = ns_lift(norm, steps);
+    if (blockIdx.x == 0 && threadIdx.x == 0) lifts[batch] = lift;
+    const double scale = ldexp((double)kStore, lift) / (norm + (double)kNsEps);
     const long size = (long)rows * cols;
     const TG *g = G + batch * size;
     const float *m = M ? M + batch * size : nullptr;
@@ -345,6 +349,8 @@ void plan_muon(const MuonGeom &g, MuonPlan *p)
     size_t o = 0;
     p->o_sum = o;
     o += up(sizeof(double) * g.batch * p->sum_blocks);
+    p->o_lift = o;
+    o += up(sizeof(int) * g.batch);
     for (int i = 0; i < 2; ++i) {
         p->o_x[i] = o;
         o += up((size_t)g.batch * g.rows * p->ld_x);
@@ -367,7 +373,7 @@ hipError_t launch_start(const MuonGeom &g, const MuonPlan &p, const TG *G, float
     hipLaunchKernelGGL(momentum_kernel<TG>, dim3(p.sum_blocks, g.batch), dim3(256), 0, st, G, M, g.rows * g.cols, mu, (int)g.nesterov, part);
     const long chunks = g.rows * ((g.cols + 7) / 8);
     hipLaunchKernelGGL(normalise_kernel<TG>, dim3((unsigned)(chunks > 256 * 2048 ? 2048 : (chunks + 255) / 256), g.batch), dim3(256), 0, st, G, M,
-                       (int)g.rows, (int)g.cols, mu, (int)g.nesterov, (const double *)part, p.sum_blocks, ws + p.o_x[0], p.ld_x);
+                       (int)g.rows, (int)g.cols, mu, (int)g.nesterov, (const double *)part, p.sum_blocks, ws + p.o_x[0], p.ld_x, g.steps, (int *)(ws + p.o_lift));
     return hipGetLastError();
 }
 
@@ -402,6 +408,7 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
     if (e != hipSuccess) return e;
     const long sx = g.rows * p.ld_x, sa = p.r * p.ld_a;
     char *a = ws + p.o_a, *b = ws + p.o_b;
+    const int *lift = (const int *)(ws + p.o_lift);
     for (int s = 0; s < g.steps; ++s) {
         char *x = ws + p.o_x[s & 1];
         Params m{};
@@ -412,7 +419,7 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
         m.K = (int)(p.tall ? g.rows : g.cols);
         m.batch = g.batch;
         if (p.gram.slices == 1) {
-            const Gram::Params eg{a, p.ld_a, sa};
+            const Gram::Params eg{a, p.ld_a, sa, lift};
             e = p.tall ? launch<Split, Lay::kDown, Lay::kDown, Gram>(m, eg, p.gram, st) : launch<Split, Lay::kAlong, Lay::kAlong, Gram>(m, eg, p.gram, st);
         } else {
             float *part = (float *)(ws + p.o_part);
@@ -422,7 +429,7 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
                        : launch<Split, Lay::kAlong, Lay::kAlong, GramPart>(m, eg, p.gram, st);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL(join_gram_kernel, dim3(cdiv(p.r, 32), cdiv(p.r, 32), g.batch), dim3(256), 0, st, (const float *)part, (int)p.r, ld, g.batch,
-                               p.gram.slices, kEdge[p.gram.shape], a, p.ld_a);
+                               p.gram.slices, kEdge[p.gram.shape], a, p.ld_a, lift);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return e;
@@ -436,11 +443,11 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
             e = launch_apply<Next>(g, p, x, b, Next::Params{ws + p.o_x[(s + 1) & 1], p.ld_x, sx}, st);
         } else if (W) {
             const float scale = -lr * kTake * kTake;
-            e = g.dtype == CAC_F32 ? launch_apply<Last<float, true>>(g, p, x, b, {(float *)W, keep, scale}, st)
-                                   : launch_apply<Last<bf16_t, true>>(g, p, x, b, {(bf16_t *)W, keep, scale}, st);
+            e = g.dtype == CAC_F32 ? launch_apply<Last<float, true>>(g, p, x, b, {(float *)W, keep, scale, lift}, st)
+                                   : launch_apply<Last<bf16_t, true>>(g, p, x, b, {(bf16_t *)W, keep, scale, lift}, st);
         } else {
-            e = g.dtype == CAC_F32 ? launch_apply<Last<float, false>>(g, p, x, b, {(float *)O, 0.f, kTake * kTake}, st)
-                                   : launch_apply<Last<bf16_t, false>>(g, p, x, b, {(bf16_t *)O, 0.f, kTake * kTake}, st);
+            e = g.dtype == CAC_F32 ? launch_apply<Last<float, false>>(g, p, x, b, {(float *)O, 0.f, kTake * kTake, lift}, st)
+                                   : launch_apply<Last<bf16_t, false>>(g, p, x, b, {(bf16_t *)O, 0.f, kTake * kTake, lift}, st);
         }
         if (e != hipSuccess) return e;
     }

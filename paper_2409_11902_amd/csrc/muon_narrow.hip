@@ -13,8 +13,7 @@ namespace {
 
 using namespace mm;
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
-constexpr float kStore = 4096.f, kTake = 1.f / 4096.f; // what X, A and the polynomial are stored times
+constexpr float kA = kNsA, kB = kNsB, kC = kNsC, kTake = kNsTake, kStore = kNsStore;
 constexpr int kSide = 64, kSquare = kSide * 256;       // bytes of a square matrix in LDS
 
 struct Args {
@@ -28,6 +27,7 @@ struct Args {
     char *x;           // [batch][slices][kSide][4 W]: the columns as they lie in LDS
     float *part;       // [2][batch][slices][kSide][kSide], by the step's parity
     int *exps;         // [batch][slices]
+    int *lifts;        // [batch]
     int step;          // -1: the first launch; else a step (more than one slice)
 };
 
@@ -117,7 +117,7 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
     char *x_mine = p.x + ((long)batch * p.slices + slice) * kCols;
     const bool single = p.slices == 1;
 
-    int e_mine = 0;
+    int e_mine = 0, lift = 0;
     float ratio = 1.f; // what X has to be multiplied by to be X times kStore
     f32x16 s = zeros();
 
@@ -256,7 +256,7 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
         if (W > 64) asm volatile("" : "+v"(lane)); // (places in LDS are worked out where they are used: kept from step to step they take all registers)
         // A times kStore, as two halves
         if (single) {
-            float take = kTake;
+            float take = ldexpf(kTake, -2 * lift);
             if (step == 0) {
                 float d = 0.f;
                 if (group == 0 && wm == wn)
@@ -265,8 +265,9 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
                             if (q * 8 + (lane >> 5) * 4 + k == (lane & 31)) d += s[q * 4 + k];
-                const double norm = sqrt((double)over_block<false, kWaves>(d, red)) + ldexp((double)kEps, e_mine); // in U's units times 2^e_mine
-                ratio = (float)((double)kStore / norm);
+                const double size = sqrt((double)over_block<false, kWaves>(d, red)), norm = size + ldexp((double)kNsEps, e_mine); // times 2^e_mine
+                lift = ns_lift(ldexp(size, -e_mine), p.steps);
+                ratio = (float)(ldexp((double)kStore, lift) / norm);
                 take = (float)((double)kStore / (norm * norm));
             }
             if (group == 0)
@@ -305,7 +306,8 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
             }
 #pragma unroll
             for (int c = 0; c < kCopies; ++c) *(u32x4 *)(X + (c * kThreads + tid) * 16) = mine[c];
-            float take = kTake;
+            if (step > 0) lift = p.lifts[batch];
+            float take = ldexpf(kTake, -2 * lift);
             if (step == 0) {
                 float d = 0.f;
 #pragma unroll
@@ -313,8 +315,10 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if ((tid & 15) * 4 + e == c * (kThreads / 16) + (tid >> 4)) d += v[c][e];
-                const double norm = sqrt((double)over_block<false, kWaves>(d, red)) + ldexp((double)kEps, e_ref);
-                ratio = (float)(ldexp((double)kStore, e_ref - exps[slice]) / norm);
+                const double size = sqrt((double)over_block<false, kWaves>(d, red)), norm = size + ldexp((double)kNsEps, e_ref); // times 2^e_ref
+                lift = ns_lift(ldexp(size, -e_ref), p.steps);
+                if (slice == 0 && tid == 0) p.lifts[batch] = lift;
+                ratio = (float)(ldexp((double)kStore, e_ref - exps[slice] + lift) / norm);
                 take = (float)((double)kStore / (norm * norm));
             }
 #pragma unroll
@@ -355,7 +359,7 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
                 three(ph, pl, down(X, RS, (cb + b * kApart) * 32, k, 0, lane), down(X, RS, (cb + b * kApart) * 32, k, 1, lane), &y[b]);
         }
         if (step + 1 == p.steps) {
-            const float scale = (UPDATE ? -p.lr : 1.f) * kTake * kTake * ratio;
+            const float scale = ldexpf((UPDATE ? -p.lr : 1.f) * kTake * kTake * ratio, -lift);
             TO *out = (TO *)p.out + batch * size;
             const int i = rb + (lane & 31);
             auto where = [&](int b, int q, int k) -> long {
@@ -468,7 +472,7 @@ bool plan_muon_narrow(const MuonGeom &g, MuonNarrowPlan *p)
     p->o_part = o;
     if (p->slices > 1) o += up((size_t)2 * g.batch * p->slices * kSide * kSide * 4);
     p->o_exps = o;
-    if (p->slices > 1) o += up((size_t)g.batch * p->slices * 4);
+    if (p->slices > 1) o += up((size_t)g.batch * (p->slices + 1) * 4);
     p->bytes = o;
     return true;
 }
@@ -493,6 +497,7 @@ hipError_t launch_muon_narrow(const MuonGeom &g, const MuonNarrowPlan &p, const 
     a.x = ws + p.o_x;
     a.part = (float *)(ws + p.o_part);
     a.exps = (int *)(ws + p.o_exps);
+    a.lifts = a.exps + (size_t)g.batch * p.slices;
     if (g.grad_dtype == CAC_F32) return launch<float>(a, p.width, g.batch, g.dtype, W != nullptr, st);
     return launch<bf16_t>(a, p.width, g.batch, g.dtype, W != nullptr, st);
 }

@@ -54,7 +54,7 @@ struct MuonPlan {
     long ld_x, ld_a;    // bytes of a row
     TileChoice gram, poly, apply;
     int sum_blocks;     // partial sums of squares of one matrix
-    size_t o_sum, o_x[2], o_a, o_b, o_part, bytes;
+    size_t o_sum, o_lift, o_x[2], o_a, o_b, o_part, bytes;
 };
 void plan_muon(const MuonGeom &g, MuonPlan *p);
 // M, W: null where only O is asked for; O: null where the weights are updated

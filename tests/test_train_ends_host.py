@@ -1,0 +1,118 @@
+"""Host-only checks of the entry points at the two ends of a training step (the classifier's loss, the
+orthogonalised update): descriptors as the header has them, refusals before any launch, plans and workspaces."""
+import ctypes
+import os
+import re
+
+import pytest
+
+from paper_2409_11902_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("name", ["cac_loss_desc", "cac_muon_desc"])
+def test_descriptor_layout_matches_header(name):
+    hdr = open(os.path.join(ROOT, "include", "cac.h")).read()
+    body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (name, name), hdr, flags=re.S).group(1)
+    body = re.sub(r"/\*.*?\*/", "", body, flags=re.S)
+    names = []
+    for decl in body.split(";"):
+        if decl.strip():
+            names += [n.strip() for n in decl.strip().split(None, 1)[1].split(",")]
+    cls = getattr(B, name)
+    assert names == [f[0] for f in cls._fields_]
+    assert ctypes.sizeof(cls) == 4 * len(names)
+
+
+def _expect(code, fn, *a):
+    with pytest.raises(B.CacError) as e:
+        fn(*a)
+    assert e.value.code == code, str(e.value)
+    assert len(str(e.value)) > 20
+
+
+def test_loss_descriptors_are_refused():
+    good = dict(T=8, D=16, V=10)
+    for bad in (dict(T=0), dict(D=-1), dict(V=0), dict(dtype=5), dict(ld_h=15), dict(ld_w=8)):
+        _expect(B.ERR_INVALID_ARG, B.cac_loss_workspace_size, B.make_loss_desc(**{**good, **bad}), B.LOSS_FWD)
+    for bad in (dict(T=(1 << 22) + 1), dict(V=(1 << 24) + 1), dict(D=(1 << 18) + 1), dict(ld_w=(1 << 20) + 1)):
+        _expect(B.ERR_UNSUPPORTED, B.cac_loss_workspace_size, B.make_loss_desc(**{**good, **bad}), B.LOSS_BWD)
+    d = B.make_loss_desc(**good)
+    _expect(B.ERR_INVALID_ARG, B.cac_loss_workspace_size, d, 2)
+    _expect(B.ERR_INVALID_ARG, B.cac_loss_describe_plan, d, -1)
+    d.size = 8
+    _expect(B.ERR_INVALID_ARG, B.cac_loss_workspace_size, d, B.LOSS_FWD)
+    assert B.lib().cac_loss_workspace_size(None, 0, None) == B.ERR_INVALID_ARG
+
+
+def test_muon_descriptors_are_refused():
+    good = dict(rows=8, cols=16)
+    for bad in (dict(rows=0), dict(cols=-3), dict(batch=0), dict(dtype=2), dict(grad_dtype=-1), dict(steps=0), dict(steps=33)):
+        _expect(B.ERR_INVALID_ARG, B.cac_muon_workspace_size, B.make_muon_desc(**{**good, **bad}), B.MUON_STEP)
+    for bad in (dict(rows=(1 << 18) + 1), dict(cols=(1 << 18) + 1), dict(batch=65536), dict(rows=1 << 18, cols=1 << 18, batch=128)):
+        _expect(B.ERR_UNSUPPORTED, B.cac_muon_workspace_size, B.make_muon_desc(**{**good, **bad}), B.MUON_ORTHOGONALISE)
+    d = B.make_muon_desc(**good)
+    _expect(B.ERR_INVALID_ARG, B.cac_muon_workspace_size, d, 7)
+    d.size += 4
+    _expect(B.ERR_INVALID_ARG, B.cac_muon_describe_plan, d, B.MUON_STEP)
+
+
+def test_pointers_and_workspaces_are_checked_before_any_launch():
+    """These calls would touch the GPU if a check let them through."""
+    L, ok, odd = B.lib(), 1 << 20, (1 << 20) + 8
+    d = B.make_loss_desc(8, 16, 10, has_bias=1)
+    need = B.cac_loss_workspace_size(d, B.LOSS_FWD)
+    args = [ok, ok, ok, ok, ok, ok]                       # H, W, b, labels, loss, lse
+    for i in range(6):
+        for bad, code in ((None, B.ERR_INVALID_ARG), (odd, B.ERR_ALIGNMENT)):
+            a = list(args)
+            a[i] = bad
+            assert L.cac_loss_fwd(d, *a, ok, need, None) == code
+    assert L.cac_loss_fwd(d, *args, ok, need - 1, None) == B.ERR_WORKSPACE_TOO_SMALL
+    assert L.cac_loss_fwd(d, *args, None, need, None) == B.ERR_WORKSPACE_TOO_SMALL
+    assert L.cac_loss_fwd(d, *args, odd, need, None) == B.ERR_ALIGNMENT
+    need = B.cac_loss_workspace_size(d, B.LOSS_BWD)
+    args = [ok, ok, ok, ok, ok, ok]                       # H, W, b, labels, lse, gloss
+    for i in range(6):
+        a = list(args)
+        a[i] = None
+        assert L.cac_loss_bwd(d, *a, ok, ok, ok, ok, need, None) == B.ERR_INVALID_ARG
+    assert L.cac_loss_bwd(d, *args, None, None, None, ok, need, None) == B.ERR_INVALID_ARG   # nothing asked for
+    for i in range(3):
+        out = [None, None, None]
+        out[i] = odd
+        assert L.cac_loss_bwd(d, *args, *out, ok, need, None) == B.ERR_ALIGNMENT
+    assert L.cac_loss_bwd(d, *args, ok, ok, ok, ok, need - 1, None) == B.ERR_WORKSPACE_TOO_SMALL
+    for shape in ((100, 300), (64, 4000)):
+        d = B.make_muon_desc(*shape)
+        need = B.cac_muon_workspace_size(d, B.MUON_STEP)
+        assert need > 0
+        for i in range(3):
+            for bad, code in ((None, B.ERR_INVALID_ARG), (odd, B.ERR_ALIGNMENT)):
+                a = [ok, ok, ok]
+                a[i] = bad
+                assert L.cac_muon_step(d, *a, 0.9, 1.0, 0.1, ok, need, None) == code
+        assert L.cac_muon_step(d, ok, ok, ok, 0.9, 1.0, 0.1, ok, need - 1, None) == B.ERR_WORKSPACE_TOO_SMALL
+        assert L.cac_orthogonalise(d, ok, None, ok, need, None) == B.ERR_INVALID_ARG
+        assert L.cac_orthogonalise(d, ok, ok, None, 0, None) == B.ERR_WORKSPACE_TOO_SMALL
+    assert "workspace" in L.cac_last_error().decode()
+
+
+def test_logits_are_not_kept():
+    """The workspace of a large class set is a fraction of what its logits would take."""
+    T, D, V = 8192, 1024, 1 << 20
+    for dtype in (B.BF16, B.F32):
+        for op in (B.LOSS_FWD, B.LOSS_BWD):
+            d = B.make_loss_desc(T, D, V, dtype=dtype)
+            assert B.cac_loss_workspace_size(d, op) < T * V * 4 // 20
+            assert "pieces" in B.cac_loss_describe_plan(d, op)
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (64, 64), (64, 256), (8192, 33), (64, 8193), (65, 65), (512, 4608), (2048, 512), (4096, 4096)])
+def test_muon_plans_are_described(shape):
+    d = B.make_muon_desc(*shape, batch=2)
+    plan = B.cac_muon_describe_plan(d, B.MUON_STEP)
+    assert ("narrow" in plan) == (min(shape) <= 64 and max(shape) <= 8192)
+    if "narrow" not in plan:
+        assert ("X^T X" in plan) == (shape[0] > shape[1])
