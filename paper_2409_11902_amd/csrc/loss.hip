@@ -326,7 +326,31 @@ template <typename T> __device__ __forceinline__ void pack_weights(const PackRow
 {
     const float s = sizeof(T) == 4 ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
     const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
-    const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks); // a wave to a row
+    const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks);
+    if (p.D <= 256) { // a thread to eight numbers, wherever they are
+        const unsigned per_row = (p.D + 7) / 8, all = p.classes * per_row; // (2^24 at most)
+        for (unsigned c = (blockIdx.x - p.row_blocks) * 256 + threadIdx.x; c < all; c += rows * 64) {
+            const unsigned row = c / per_row;
+            const int n = (c - row * per_row) * 8;
+            const T *w = (const T *)p.W + row * p.ld_w + n;
+            float v[8];
+            if (aligned && n + 8 <= p.D) {
+                struct alignas(16) Some { T v[16 / sizeof(T)]; };
+#pragma unroll
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+                    const Some x = *(const Some *)(w + h * (16 / sizeof(T)));
+#pragma unroll
+                    for (int e = 0; e < (int)(16 / sizeof(T)); ++e) v[h * (16 / sizeof(T)) + e] = Elem<T>::load(&x.v[e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = n + e < p.D ? Elem<T>::load(w + e) : 0.f;
+            }
+            store8(T(), p.out_w + row * p.row_bytes, n, v, s);
+        }
+        return;
+    }
+    // a wave to a row
     for (int row = 4 * (blockIdx.x - p.row_blocks) + (threadIdx.x >> 6); row < p.classes; row += rows) {
         const T *w = (const T *)p.W + row * p.ld_w;
         char *out = p.out_w + row * p.row_bytes;
@@ -401,20 +425,21 @@ template <typename T> struct Stats {
     }
 };
 
-// lse and loss of a compact row from its parts: 16 rows to a block, 16 threads to a row
-__global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float *__restrict__ part, int parts, long T_rows, float *__restrict__ loss,
-                                                   float *__restrict__ lse)
+// lse and loss of a compact row from its parts: ROWS rows to a block, 256 / ROWS threads to a row
+template <int ROWS> __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float *__restrict__ part, int parts, long T_rows,
+                                                                       float *__restrict__ loss, float *__restrict__ lse)
 {
+    constexpr int kThreads = 256 / ROWS;
     const int count = meta.rows();
-    const int r = threadIdx.x & 15, s = threadIdx.x >> 4;
-    const int j = blockIdx.x * 16 + r;
+    const int r = threadIdx.x % ROWS, s = threadIdx.x / ROWS;
+    const int j = blockIdx.x * ROWS + r;
     float top = -INFINITY, sum = 0.f;
     if (j < count)
-        for (int k0 = s; k0 < parts; k0 += 128) { // eight parts on their way at a time
+        for (int k0 = s; k0 < parts; k0 += 8 * kThreads) { // eight parts on their way at a time
             float t[8], u[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int k = k0 + e * 16;
+                const int k = k0 + e * kThreads;
                 t[e] = k < parts ? part[2L * k * T_rows + j] : -INFINITY;
                 u[e] = k < parts ? part[(2L * k + 1) * T_rows + j] : 0.f;
             }
@@ -427,16 +452,24 @@ __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float 
             for (int e = 0; e < 8; ++e) sum += u[e] * __builtin_amdgcn_exp2f((t[e] - shift) * kLog2e);
             top = m;
         }
-    __shared__ float tops[16][17], sums[16][17];
-    tops[s][r] = top;
-    sums[s][r] = sum;
+    // the threads of a row, in halves
+    __shared__ float tops[256], sums[256];
+    tops[threadIdx.x] = top;
+    sums[threadIdx.x] = sum;
     __syncthreads();
+#pragma unroll
+    for (int n = kThreads / 2; n > 0; n >>= 1) {
+        if (s < n) {
+            const int other = threadIdx.x + n * ROWS;
+            const float m = fmaxf(tops[threadIdx.x], tops[other]), shift = m == -INFINITY ? 0.f : m;
+            sums[threadIdx.x] = sums[threadIdx.x] * __builtin_amdgcn_exp2f((tops[threadIdx.x] - shift) * kLog2e) +
+                                sums[other] * __builtin_amdgcn_exp2f((tops[other] - shift) * kLog2e);
+            tops[threadIdx.x] = m;
+        }
+        __syncthreads();
+    }
     if (s == 0 && j < count) {
-        for (int k = 1; k < 16; ++k) top = fmaxf(top, tops[k][r]);
-        const float shift = top == -INFINITY ? 0.f : top;
-        float total = 0.f;
-        for (int k = 0; k < 16; ++k) total += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - shift) * kLog2e);
-        const float l = top + logf(total);
+        const float l = tops[r] + logf(sums[r]);
         const int t = meta.row_of(j);
         if (meta.label_of(j) == Meta::kOut) {
             loss[t] = lse[t] = 0.f;
@@ -593,28 +626,44 @@ template <typename T> struct OutH {
     }
 };
 
-// dH from the slices' sums; a block takes 1024 numbers of a compact row
+// dH from the slices' sums; a block takes 256 numbers of a compact row, four to a thread, and its waves take turns over the slices
 template <typename T> __global__ void __launch_bounds__(256)
 finish_rows_kernel(const Meta meta, const float *__restrict__ sums, long slice_stride, int slices, int D, T *__restrict__ dH)
 {
     if ((int)blockIdx.x >= meta.rows()) return;
-    const int n = blockIdx.y * 1024 + threadIdx.x * 4;
-    if (n >= D) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * 256 + lane * 4;
     const long at = (long)blockIdx.x * D + n;
     const bool wide = (D & 3) == 0;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < slices; ++s) {
-        const float *p = sums + s * slice_stride + at;
-        if (wide) {
-            const f32x4 x = *(const f32x4 *)p;
+    if (n < D)
+        for (int s0 = wave; s0 < slices; s0 += 16) { // four slices on their way at a time
+            float x[4][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += x[k];
-        } else {
+            for (int e = 0; e < 4; ++e) {
+                const int s = s0 + e * 4;
+                const float *p = sums + s * slice_stride + at;
+                if (wide) {
+                    const f32x4 y = s < slices ? *(const f32x4 *)p : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (n + k < D) v[k] += p[k];
+                    for (int k = 0; k < 4; ++k) x[e][k] = y[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[e][k] = s < slices && n + k < D ? p[k] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += x[e][k];
         }
-    }
+    __shared__ f32x4 red[3][64];
+    if (wave > 0) red[wave - 1][lane] = f32x4{v[0], v[1], v[2], v[3]};
+    __syncthreads();
+    if (wave > 0 || n >= D) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] += red[w][lane][k];
     store_four(dH + (long)meta.row_of(blockIdx.x) * D + n, n, D, wide, v);
 }
 
@@ -683,13 +732,13 @@ template <typename T> __global__ void __launch_bounds__(Small::kThreads, Small::
     extern __shared__ __align__(1024) unsigned char smem[];
     typedef typename FormatOf<T>::type P;
     unsigned block = blockIdx.x;
-    if (block < p.blocks_w) {
-        mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, smem);
+    if (block < p.blocks_h) { // (dH's sums are the longer ones: they begin first)
+        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block, smem);
         return;
     }
-    block -= p.blocks_w;
-    if (block < p.blocks_h) mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block, smem);
-    else bias_sums(p.b, block - p.blocks_h, (float(*)[64])smem);
+    block -= p.blocks_h;
+    if (block < p.blocks_w) mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, smem);
+    else bias_sums(p.b, block - p.blocks_w, (float(*)[64])smem);
 }
 
 // a slice's part of the logits' products, [slice][T][ld]
@@ -715,7 +764,13 @@ template <typename T> __device__ __forceinline__ void join_logits(const float *p
     float bias[4];
     load_bias(b, n, V, bias);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < slices; ++k) s += *(const f32x4 *)(part + k * slice_stride + n);
+    for (int k0 = 0; k0 < slices; k0 += 8) { // eight slices on their way at a time
+        f32x4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = k0 + k < slices ? *(const f32x4 *)(part + (k0 + k) * slice_stride + n) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += x[k];
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = n + e < V ? (sizeof(T) == 4 ? ldexpf(s[e], ze) : s[e]) + bias[e] : -INFINITY;
 }
@@ -812,13 +867,13 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
     p->z = choose(p->split, g.T, piece, 1, g.D, false, p->pieces > 1 || logits * 16 > 32L << 20 ? 1 : 16);
     p->w = choose(p->split, piece, g.D, 1, g.T, false, 1);
-    p->h = choose(p->split, g.T, g.D, 1, piece, false, 16);
+    p->h = choose(p->split, g.T, g.D, 1, piece, false, 128);
     // dW and dH together where both would take the smallest tiles anyway, or are over before a launch is
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
     p->pair = backward && (work < 4e9 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
-        p->h = choose(p->split, g.T, g.D, 1, piece, false, 16, true);
+        p->h = choose(p->split, g.T, g.D, 1, piece, false, 128, true);
     }
     p->parts = 0;
     for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->z.shape);
@@ -878,7 +933,8 @@ template <typename T> class Loss {
         rows->out_w = ws + p.o_w;
         rows->row_bytes = p.row_bytes;
         rows->meta = meta;
-        const long weight_blocks = !p.pack_w ? 0 : n > 4 * 4096 ? 4096 : (n + 3) / 4;
+        const long waves = g.D <= 256 ? (n * ((g.D + 7) / 8) + 63) / 64 : n; // with something to do
+        const long weight_blocks = !p.pack_w ? 0 : waves > 4 * 4096 ? 4096 : (waves + 3) / 4;
         hipLaunchKernelGGL(pack_kernel<T>, dim3((unsigned)(rows->row_blocks + weight_blocks)), dim3(256), 0, st, *rows);
         return hipGetLastError();
     }
@@ -942,7 +998,9 @@ public:
             if (e != hipSuccess) return e;
             part0 += (int)wave_columns(n, p.z.shape);
         }
-        hipLaunchKernelGGL(join_kernel, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
+        // (few rows: a block to a row, with the parts' reads apart; many: sixteen, side by side)
+        if (g.T < 1024) hipLaunchKernelGGL(join_kernel<1>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
+        else hipLaunchKernelGGL(join_kernel<16>, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
         return hipGetLastError();
     }
 
@@ -1014,7 +1072,7 @@ public:
             if (e != hipSuccess) return e;
         }
         if (dH && sums) {
-            hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 1024)), dim3(256), 0, st, meta, (const float *)sums, g.T * g.D,
+            hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 256)), dim3(256), 0, st, meta, (const float *)sums, g.T * g.D,
                                p.h.slices, (int)g.D, dH);
             e = hipGetLastError();
         }

@@ -468,7 +468,7 @@ inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetr
         if (shape == kWide && !split) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
         const long tiles = tiles_of(shape, M, N, symmetric) * batch;
         const int passes = cdiv(K, split ? 32 : 64);
-        for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices < 8 ? 2 : 4) {
+        for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices / 4 * 2) {
             if (slices > 1 && passes / slices < 4) break;
             if (slices > 1 && tiles * slices > 2048) break;
             double us = product_us(shape, split, tiles, passes, slices);

@@ -136,10 +136,15 @@ __global__ void __launch_bounds__(256) join_gram_kernel(const float *__restrict_
     const int m = blockIdx.y * 32 + (threadIdx.x & 31), n = blockIdx.x * 32 + (threadIdx.x >> 5) * 4;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (m < r && n < ld)
-        for (int s = 0; s < slices; ++s) {
-            const f32x4 x = *(const f32x4 *)(part + (((long)s * batches + blockIdx.z) * r + m) * ld + n);
+        for (int s0 = 0; s0 < slices; s0 += 8) { // eight slices on their way at a time
+            f32x4 x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += x[e];
+            for (int s = 0; s < 8; ++s)
+                x[s] = s0 + s < slices ? *(const f32x4 *)(part + (((long)(s0 + s) * batches + blockIdx.z) * r + m) * ld + n) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += x[s][e];
         }
     const float take = ldexpf(kTake, -2 * lift[blockIdx.z]);
 #pragma unroll

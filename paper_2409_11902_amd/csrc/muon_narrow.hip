@@ -294,7 +294,7 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
                 for (int k = 0; k < 16 / kSums; ++k)
 #pragma unroll
                     for (int c = 0; c < kSums; ++c)
-                        x[k][c] = k0 + k < p.slices ? *(const f32x4 *)(part + (long)(k0 + k) * (kSide * kSide) + (c * kThreads + tid) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+                        x[k][c] = k0 + k < p.slices && c * (kThreads / 16) + (tid >> 4) < p.r ? *(const f32x4 *)(part + (long)(k0 + k) * (kSide * kSide) + (c * kThreads + tid) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < 16 / kSums; ++k) {
                     const float w = ldexpf(1.f, 2 * (e_ref - __shfl(e_lane, min(k0 + k, p.slices - 1), 64)));
