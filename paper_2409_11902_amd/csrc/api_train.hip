@@ -82,7 +82,7 @@ int cac_loss_describe_plan(const cac_loss_desc *d, int op, char *buf, size_t buf
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
     LossPlan p;
     plan_loss(g, op == CAC_LOSS_BWD, &p);
-    const int n = snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d", p.split ? "two halves" : "bfloat16",
+    const int n = snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d", p.split ? "two halves" : p.raw ? "float" : "bfloat16",
                            p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, tile_edge(p.z));
     if (op == CAC_LOSS_BWD && n > 0 && (size_t)n < buf_len)
         snprintf(buf + n, buf_len - n, ", dW tile %d, dH tile %d in %d slices", tile_edge(p.w), tile_edge(p.h), p.h.slices);

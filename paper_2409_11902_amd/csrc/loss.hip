@@ -17,6 +17,11 @@ namespace {
 
 using namespace mm;
 
+// What the operands are, as they lie and as they are multiplied.
+struct OfBf16 { typedef bf16_t E; typedef Bf16 P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kBf16; };
+struct OfSplit { typedef float E; typedef Split P; static constexpr bool kSplit = true; static constexpr Fmt kG = Fmt::kSplit; };
+struct OfRaw { typedef float E; typedef Raw P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kF32; };
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStoreG = 14;        // G is stored times 2^14 as two halves: |G| <= 1, and 1e-8 is still a normal number
 constexpr int kMaxParts = 1024;    // blocks that look for a matrix's largest number
@@ -64,7 +69,7 @@ struct Meta {
     __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
     static constexpr int kOut = -(1 << 30);
 };
-constexpr int kDirectRows = 64; // one pass over them as terms of dW; a wave looks them all up at once
+constexpr int kDirectRows = 64; // a wave looks them all up at once
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
 inline Meta meta_at(char *p, long T)
@@ -222,27 +227,29 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, int n0, 
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 }
-// ... and into a packed row (bfloat16: as they are; float: two halves, times `scale`)
-__device__ __forceinline__ void store8(bf16_t, char *row, int n, const float (&v)[8], float)
+// ... and into a packed row (as they are, or two halves times `scale`)
+template <class K> __device__ __forceinline__ void store8(char *row, int n, const float (&v)[8], float scale)
 {
-    u32x4 u;
+    if (K::kG == Fmt::kBf16) {
+        u32x4 u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
-    *(u32x4 *)(row + n * 2) = u;
-}
-__device__ __forceinline__ void store8(float, char *row, int n, const float (&v)[8], float scale)
-{
+        for (int e = 0; e < 4; ++e) u[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
+        *(u32x4 *)(row + n * 2) = u;
+        return;
+    }
 #pragma unroll
     for (int h = 0; h < 8; h += 4) {
         const float x[4] = {v[h] * scale, v[h + 1] * scale, v[h + 2] * scale, v[h + 3] * scale};
-        store_split(row, n + h, x);
+        if (K::kSplit) store_split(row, n + h, x);
+        else *(f32x4 *)(row + (n + h) * 4) = f32x4{x[0], x[1], x[2], x[3]};
     }
 }
 
 // Rows that count, one behind the other, and what is known about them.  A block takes a run of rows; where they go follows from the
 // labels before them.
-template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &p, float *deal)
+template <class K> __device__ __forceinline__ void pack_rows(const PackRows &p, float *deal)
 {
+    typedef typename K::E T;
     const Counts &counts = p.meta.counts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int first = blockIdx.x * p.rows_per_block, last = min(p.T, first + p.rows_per_block);
@@ -267,10 +274,10 @@ template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &
     __syncthreads();
     before = red_n[0] + red_n[1] + red_n[2] + red_n[3];
     c = fmaxf(fmaxf(red_c[0], red_c[1]), fmaxf(red_c[2], red_c[3]));
-    const int exp_h = sizeof(T) == 4 ? stored_exp(p.meta.top, p.parts_h) : 0;
+    const int exp_h = K::kSplit ? stored_exp(p.meta.top, p.parts_h) : 0;
     const float scale = ldexpf(1.f, exp_h);
     if (blockIdx.x == 0 && wave == 0) {
-        const int exp_w = sizeof(T) == 4 ? stored_exp(p.meta.top + kMaxParts, p.parts_w) : 0;
+        const int exp_w = K::kSplit ? stored_exp(p.meta.top + kMaxParts, p.parts_w) : 0;
         if (lane == 0) {
             p.meta.exps[0] = exp_h;
             p.meta.exps[1] = exp_w;
@@ -309,7 +316,7 @@ template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &
                 for (int n0 = 0; n0 < p.D; n0 += 512) {
                     float v[8];
                     load8(h, n0, p.D, aligned, lane, deal, v);
-                    if (n0 + lane * 8 < p.D) store8(T(), o, n0 + lane * 8, v, scale);
+                    if (n0 + lane * 8 < p.D) store8<K>(o, n0 + lane * 8, v, scale);
                 }
             } else if (p.dH) {
                 T *o = (T *)p.dH + (long)row * p.D;
@@ -322,9 +329,10 @@ template <typename T> __device__ __forceinline__ void pack_rows(const PackRows &
 }
 
 // A piece of the weights, its rows padded to whole chunks.
-template <typename T> __device__ __forceinline__ void pack_weights(const PackRows &p, float *deal)
+template <class K> __device__ __forceinline__ void pack_weights(const PackRows &p, float *deal)
 {
-    const float s = sizeof(T) == 4 ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
+    typedef typename K::E T;
+    const float s = K::kSplit ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
     const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
     const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks);
     if (p.D <= 256) { // a thread to eight numbers, wherever they are
@@ -346,7 +354,7 @@ template <typename T> __device__ __forceinline__ void pack_weights(const PackRow
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = n + e < p.D ? Elem<T>::load(w + e) : 0.f;
             }
-            store8(T(), p.out_w + row * p.row_bytes, n, v, s);
+            store8<K>(p.out_w + row * p.row_bytes, n, v, s);
         }
         return;
     }
@@ -357,15 +365,15 @@ template <typename T> __device__ __forceinline__ void pack_weights(const PackRow
         for (int n0 = 0; n0 < p.D; n0 += 512) {
             float v[8];
             load8(w, n0, p.D, aligned, lane, deal, v);
-            if (n0 + lane * 8 < p.D) store8(T(), out, n0 + lane * 8, v, s);
+            if (n0 + lane * 8 < p.D) store8<K>(out, n0 + lane * 8, v, s);
         }
     }
 }
-template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const PackRows p)
+template <class K> __global__ void __launch_bounds__(256) pack_kernel(const PackRows p)
 {
     __shared__ float deal[4][kDeal];
-    if ((int)blockIdx.x < p.row_blocks) pack_rows<T>(p, deal[threadIdx.x >> 6]);
-    else pack_weights<T>(p, deal[threadIdx.x >> 6]);
+    if ((int)blockIdx.x < p.row_blocks) pack_rows<K>(p, deal[threadIdx.x >> 6]);
+    else pack_weights<K>(p, deal[threadIdx.x >> 6]);
 }
 
 // four neighbours of b from n on, zeros past its end
@@ -377,8 +385,9 @@ template <typename T> __device__ __forceinline__ void load_bias(const T *b, int 
 
 // ---- endings of the products
 // forward: maximum and sum of exp of a row over a wave's columns, and the label's logit
-template <typename T> struct Stats {
-    static constexpr bool kSymmetric = false;
+template <class K> struct Stats : Ending {
+    typedef typename K::E T;
+    static constexpr bool kCountsM = true;
     struct Params {
         const T *b;
         Meta meta;
@@ -388,7 +397,7 @@ template <typename T> struct Stats {
     };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
+        const int ze = K::kSplit ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
         const int part = e.part0 + p.part;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -404,7 +413,7 @@ template <typename T> struct Stats {
                     load_bias(e.b, n, p.N, bias);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float v = (sizeof(T) == 4 ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
+                        const float v = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
                         z[j][q * 4 + k] = n + k < p.N ? v : -INFINITY;
                         if (n + k == label && n + k < p.N) e.meta.zlabel[m] = v;
                         top = fmaxf(top, z[j][q * 4 + k]);
@@ -482,22 +491,25 @@ template <int ROWS> __global__ void __launch_bounds__(256) join_kernel(const Met
 }
 
 // four neighbours of a row of G
-__device__ __forceinline__ void store_gradient(float, char *row, int n, const float (&g)[4])
+template <class K> __device__ __forceinline__ void store_gradient(char *row, int n, const float (&g)[4])
 {
-    const float v[4] = {g[0] * (float)(1 << kStoreG), g[1] * (float)(1 << kStoreG), g[2] * (float)(1 << kStoreG), g[3] * (float)(1 << kStoreG)};
-    store_split(row, n, v);
-}
-__device__ __forceinline__ void store_gradient(bf16_t, char *row, int n, const float (&g)[4])
-{
-    u32x2 u;
-    u[0] = f32x2_to_bf16x2(g[0], g[1]);
-    u[1] = f32x2_to_bf16x2(g[2], g[3]);
-    *(u32x2 *)(row + n * 2) = u;
+    if (K::kG == Fmt::kSplit) {
+        const float v[4] = {g[0] * (float)(1 << kStoreG), g[1] * (float)(1 << kStoreG), g[2] * (float)(1 << kStoreG), g[3] * (float)(1 << kStoreG)};
+        store_split(row, n, v);
+    } else if (K::kG == Fmt::kF32) {
+        *(f32x4 *)(row + n * 4) = f32x4{g[0], g[1], g[2], g[3]};
+    } else {
+        u32x2 u;
+        u[0] = f32x2_to_bf16x2(g[0], g[1]);
+        u[1] = f32x2_to_bf16x2(g[2], g[3]);
+        *(u32x2 *)(row + n * 2) = u;
+    }
 }
 
 // backward: G of a piece
-template <typename T> struct Grad {
-    static constexpr bool kSymmetric = false;
+template <class K> struct Grad : Ending {
+    typedef typename K::E T;
+    static constexpr bool kCountsM = true;
     struct Params {
         const T *b;
         Meta meta;
@@ -507,10 +519,10 @@ template <typename T> struct Grad {
     };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const int ze = sizeof(T) == 4 ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
+        const int ze = K::kSplit ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
         const float largest = e.meta.largest(p.lane);
         const int Np = (p.N + 7) & ~7;
-        typedef RowBlock<sizeof(T) == 4 ? Fmt::kSplit : Fmt::kBf16, NI> Block;
+        typedef RowBlock<K::kG, NI> Block;
         constexpr int kIn16 = sizeof(T) == 4 ? 32 : 16; // bytes that eight columns take
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -527,9 +539,9 @@ template <typename T> struct Grad {
                     load_bias(e.b, n, p.N, bias);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float z = (sizeof(T) == 4 ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
+                        const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
                         const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        g[k] = n + k < p.N && in ? (sizeof(T) == 4 ? x * (float)(1 << kStoreG) : x) : 0.f;
+                        g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
                     }
                     Block::put(p.lds, p.lane, j, q, g);
                 }
@@ -567,12 +579,13 @@ template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x1
 }
 
 // dW of a piece
-template <typename T> struct OutW {
-    static constexpr bool kSymmetric = false;
+template <class K> struct OutW : Ending {
+    typedef typename K::E T;
+    static constexpr bool kCountsK = true;
     struct Params { T *out; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[0]) : e.meta.largest(p.lane);
+        const float s = K::kSplit ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[0]) : e.meta.largest(p.lane);
         typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
@@ -588,12 +601,12 @@ template <typename T> struct OutW {
 };
 
 // dH: the result, or sums of a slice (added to what the pieces before left)
-template <typename T> struct OutH {
-    static constexpr bool kSymmetric = false;
+template <class K> struct OutH : Ending {
+    typedef typename K::E T;
     struct Params { T *out; float *sums; long slice_stride; int add; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = sizeof(T) == 4 ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
+        const float s = K::kSplit ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
         typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
@@ -626,21 +639,23 @@ template <typename T> struct OutH {
     }
 };
 
-// dH from the slices' sums; a block takes 256 numbers of a compact row, four to a thread, and its waves take turns over the slices
-template <typename T> __global__ void __launch_bounds__(256)
+// dH from the slices' sums, four numbers of a compact row to a thread.  WAVES: of few slices every thread adds up its own; of many the
+// block's waves take turns over them.
+template <typename T, bool WAVES> __global__ void __launch_bounds__(256)
 finish_rows_kernel(const Meta meta, const float *__restrict__ sums, long slice_stride, int slices, int D, T *__restrict__ dH)
 {
     if ((int)blockIdx.x >= meta.rows()) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.y * 256 + lane * 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = WAVES ? blockIdx.y * 256 + lane * 4 : (int)(blockIdx.y * 1024 + threadIdx.x * 4);
     const long at = (long)blockIdx.x * D + n;
     const bool wide = (D & 3) == 0;
+    constexpr int kTurn = WAVES ? 4 : 1;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (n < D)
-        for (int s0 = wave; s0 < slices; s0 += 16) { // four slices on their way at a time
+        for (int s0 = WAVES ? wave : 0; s0 < slices; s0 += 4 * kTurn) { // four slices on their way at a time
             float x[4][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int s = s0 + e * 4;
+                const int s = s0 + e * kTurn;
                 const float *p = sums + s * slice_stride + at;
                 if (wide) {
                     const f32x4 y = s < slices ? *(const f32x4 *)p : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -656,27 +671,31 @@ finish_rows_kernel(const Meta meta, const float *__restrict__ sums, long slice_s
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] += x[e][k];
         }
-    __shared__ f32x4 red[3][64];
-    if (wave > 0) red[wave - 1][lane] = f32x4{v[0], v[1], v[2], v[3]};
-    __syncthreads();
-    if (wave > 0 || n >= D) return;
+    if (WAVES) {
+        __shared__ f32x4 red[3][64];
+        if (wave > 0) red[wave - 1][lane] = f32x4{v[0], v[1], v[2], v[3]};
+        __syncthreads();
+        if (wave > 0) return;
 #pragma unroll
-    for (int w = 0; w < 3; ++w)
+        for (int w = 0; w < 3; ++w)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += red[w][lane][k];
-    store_four(dH + (long)meta.row_of(blockIdx.x) * D + n, n, D, wide, v);
+            for (int k = 0; k < 4; ++k) v[k] += red[w][lane][k];
+    }
+    if (n < D) store_four(dH + (long)meta.row_of(blockIdx.x) * D + n, n, D, wide, v);
 }
 
 // db of a piece: the columns' sums of G, eight columns to a thread, the block's four waves over the rows
-template <typename T> struct Bias {
+template <class K> struct Bias {
+    typedef typename K::E T;
     Meta meta;
     const char *G;
     long ld;
     int V;
     T *db;
 };
-template <typename T> __device__ __forceinline__ void bias_sums(const Bias<T> &p, int block, float (*red)[64])
+template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, int block, float (*red)[64])
 {
+    typedef typename K::E T;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int count = p.meta.rows();
     const float largest = p.meta.largest(lane);
@@ -686,7 +705,14 @@ template <typename T> __device__ __forceinline__ void bias_sums(const Bias<T> &p
     if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
             const char *g = p.G + (long)m * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
-            if (sizeof(T) == 4) {
+            if (K::kG == Fmt::kF32) {
+                const f32x4 lo = *(const f32x4 *)g, hi = *(const f32x4 *)(g + 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[e] += lo[e];
+                    s[e + 4] += hi[e];
+                }
+            } else if (K::kSplit) {
                 const f16x8 hi = *(const f16x8 *)g, lo = *(const f16x8 *)(g + 16);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] += (float)hi[e] + (float)lo[e];
@@ -706,44 +732,42 @@ template <typename T> __device__ __forceinline__ void bias_sums(const Bias<T> &p
     }
     __syncthreads();
     if (threadIdx.x < 64 && block * 64 + (int)threadIdx.x < p.V) {
-        const float c = sizeof(T) == 4 ? ldexpf(largest, -kStoreG) : largest;
+        const float c = K::kSplit ? ldexpf(largest, -kStoreG) : largest;
         Elem<T>::store(p.db + block * 64 + threadIdx.x, c * (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
     }
 }
-template <typename T> __global__ void __launch_bounds__(256) bias_kernel(const Bias<T> p)
+template <class K> __global__ void __launch_bounds__(256) bias_kernel(const Bias<K> p)
 {
     __shared__ float red[4][64];
     bias_sums(p, blockIdx.x, red);
 }
 
-template <typename T> struct FormatOf { typedef Bf16 type; };
-template <> struct FormatOf<float> { typedef Split type; };
-
 // dW, dH and db of a piece in one launch: small products end sooner than a launch begins
-template <typename T> struct PairParams {
+template <class K> struct PairParams {
+    typedef typename K::E T;
     Params w, h;
-    typename OutW<T>::Params ew;
-    typename OutH<T>::Params eh;
-    Bias<T> b;
+    typename OutW<K>::Params ew;
+    typename OutH<K>::Params eh;
+    Bias<K> b;
     unsigned blocks_w, blocks_h;
 };
-template <typename T> __global__ void __launch_bounds__(Small::kThreads, Small::kPerSimd) pair_kernel(const PairParams<T> p)
+template <class K> __global__ void __launch_bounds__(Small::kThreads, Small::kPerSimd) pair_kernel(const PairParams<K> p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    typedef typename FormatOf<T>::type P;
+    typedef typename K::P P;
     unsigned block = blockIdx.x;
     if (block < p.blocks_h) { // (dH's sums are the longer ones: they begin first)
-        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<T>>(p.h, p.eh, block, smem);
+        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<K>>(p.h, p.eh, block, smem);
         return;
     }
     block -= p.blocks_h;
-    if (block < p.blocks_w) mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<T>>(p.w, p.ew, block, smem);
+    if (block < p.blocks_w) mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<K>>(p.w, p.ew, block, smem);
     else bias_sums(p.b, block - p.blocks_w, (float(*)[64])smem);
 }
 
 // a slice's part of the logits' products, [slice][T][ld]
-struct Logits {
-    static constexpr bool kSymmetric = false;
+struct Logits : Ending {
+    static constexpr bool kCountsM = true;
     struct Params { float *out; int T, ld; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -759,7 +783,7 @@ struct Logits {
     }
 };
 // ... joined: four logits of row m
-template <typename T> __device__ __forceinline__ void join_logits(const float *part, long slice_stride, int slices, const T *b, int n, int V, int ze, float (&z)[4])
+template <class K> __device__ __forceinline__ void join_logits(const float *part, long slice_stride, int slices, const typename K::E *b, int n, int V, int ze, float (&z)[4])
 {
     float bias[4];
     load_bias(b, n, V, bias);
@@ -772,11 +796,11 @@ template <typename T> __device__ __forceinline__ void join_logits(const float *p
         for (int k = 0; k < 8; ++k) s += x[k];
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = n + e < V ? (sizeof(T) == 4 ? ldexpf(s[e], ze) : s[e]) + bias[e] : -INFINITY;
+    for (int e = 0; e < 4; ++e) z[e] = n + e < V ? (K::kSplit ? ldexpf(s[e], ze) : s[e]) + bias[e] : -INFINITY;
 }
 // loss and lse of a compact row from the slices' logits, a block to a row
-template <typename T> __global__ void __launch_bounds__(256)
-row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const T *__restrict__ b, int V,
+template <class K> __global__ void __launch_bounds__(256)
+row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const typename K::E *__restrict__ b, int V,
                 float *__restrict__ loss, float *__restrict__ lse)
 {
     const int m = blockIdx.x;
@@ -786,13 +810,13 @@ row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
         if (threadIdx.x == 0) loss[t] = lse[t] = 0.f;
         return;
     }
-    const int ze = sizeof(T) == 4 ? -(meta.exps[0] + meta.exps[1]) : 0;
+    const int ze = K::kSplit ? -(meta.exps[0] + meta.exps[1]) : 0;
     const float *row = part + (long)m * ld;
     float top = -INFINITY, sum = 0.f;
     __shared__ float at_label, tops[4], sums[4];
     for (int n = threadIdx.x * 4; n < V; n += 1024) {
         float z[4];
-        join_logits(row, slice_stride, slices, b, n, V, ze, z);
+        join_logits<K>(row, slice_stride, slices, b, n, V, ze, z);
         float m4 = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
         if (label >= n && label < n + 4) at_label = label == n ? z[0] : label == n + 1 ? z[1] : label == n + 2 ? z[2] : z[3];
         m4 = fmaxf(m4, top);
@@ -823,8 +847,8 @@ row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
     }
 }
 // G of a compact row, 1024 classes to a block
-template <typename T> __global__ void __launch_bounds__(256)
-row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const T *__restrict__ b, int V,
+template <class K> __global__ void __launch_bounds__(256)
+row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const typename K::E *__restrict__ b, int V,
                 char *__restrict__ G, long ld_g)
 {
     const int m = blockIdx.x, n = blockIdx.y * 1024 + threadIdx.x * 4;
@@ -834,27 +858,32 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
     const float q = meta.q_of(m, largest), lse = meta.lse_of(m);
     float g[4] = {0.f, 0.f, 0.f, 0.f};
     if (label != Meta::kOut && n < V) {
-        const int ze = sizeof(T) == 4 ? -(meta.exps[0] + meta.exps[1]) : 0;
+        const int ze = K::kSplit ? -(meta.exps[0] + meta.exps[1]) : 0;
         float z[4];
-        join_logits(part + (long)m * ld, slice_stride, slices, b, n, V, ze, z);
+        join_logits<K>(part + (long)m * ld, slice_stride, slices, b, n, V, ze, z);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (n + e < V) g[e] = q * (__builtin_amdgcn_exp2f((z[e] - lse) * kLog2e) - (n + e == label ? 1.f : 0.f));
     }
-    store_gradient(T(), G + (long)m * ld_g, n, g);
+    store_gradient<K>(G + (long)m * ld_g, n, g);
 }
 
 } // namespace
 
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 {
-    p->split = g.dtype == CAC_F32;
+    // Small products of floats: three bfloat16 parts made of a fragment when it is multiplied cost less than the passes that
+    // find the largest numbers and split everything beforehand (64 x 2048 x 1000, both passes: 55 us split, 41 us so).
+    const int in16 = g.dtype == CAC_F32 ? 4 : 8; // numbers in 16 bytes
+    p->raw = g.dtype == CAC_F32 && (double)g.T * g.D * g.V <= 2.5e8 && g.D % 8 == 0 && g.ld_w % in16 == 0;
+    p->split = g.dtype == CAC_F32 && !p->raw;
+    p->pack_w = !p->raw && (p->split || g.D % 8 || g.ld_w % 8);
+    p->direct = !p->split && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % in16 == 0;
     p->dp = (g.D + 7) / 8 * 8;
-    p->row_bytes = (p->split ? 4 : 2) * p->dp;
-    p->pack_w = p->split || g.D % 8 || g.ld_w % 8;
-    p->direct = !p->split && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % 8 == 0;
+    const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
+    p->row_bytes = e * p->dp;
     // A piece's G (and its packed weights) stay within the 256 MiB that the chip caches; at least 4096 classes, in whole tiles.
-    const long per_class = (backward ? g.T * (p->split ? 4 : 2) : 0) + (p->pack_w ? p->row_bytes : 0);
+    const long per_class = (backward ? g.T * e : 0) + (p->pack_w ? p->row_bytes : 0);
     long piece = per_class ? (256L << 20) / per_class / 256 * 256 : g.V;
     if (piece < 4096) piece = 4096;
     if (piece > 1L << 19) piece = 1L << 19;
@@ -865,15 +894,16 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->piece = piece;
     // A sum over D in slices leaves its parts of the logits in the workspace: for few rows and classes only.
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
-    p->z = choose(p->split, g.T, piece, 1, g.D, false, p->pieces > 1 || logits * 16 > 32L << 20 ? 1 : 16);
-    p->w = choose(p->split, piece, g.D, 1, g.T, false, 1);
-    p->h = choose(p->split, g.T, g.D, 1, piece, false, 128);
+    const bool wide_k = g.dtype == CAC_F32; // (a pass is 32 terms)
+    p->z = choose(wide_k, g.T, piece, 1, g.D, false, p->pieces > 1 || logits * 16 > 32L << 20 ? 1 : 16, p->raw);
+    p->w = choose(wide_k, piece, g.D, 1, g.T, false, 1);
+    p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128);
     // dW and dH together where both would take the smallest tiles anyway, or are over before a launch is
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
-    p->pair = backward && (work < 4e9 || (p->w.shape == kSmall && p->h.shape == kSmall));
+    p->pair = backward && (p->raw || work < 4e9 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
-        p->h = choose(p->split, g.T, g.D, 1, piece, false, 128, true);
+        p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128, true);
     }
     p->parts = 0;
     for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->z.shape);
@@ -889,7 +919,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->o_z = o;
     if (p->z.slices > 1) o += up256((size_t)logits * p->z.slices);
     p->o_g = o;
-    if (backward) o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * (p->split ? 4 : 2));
+    if (backward) o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * e);
     p->o_acc = o;
     if (backward && (p->pieces > 1 || p->h.slices > 1)) o += up256((size_t)p->h.slices * g.T * g.D * 4);
     p->bytes = o;
@@ -897,8 +927,9 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 
 namespace {
 
-template <typename T> class Loss {
-    typedef typename FormatOf<T>::type P;
+template <class K> class Loss {
+    typedef typename K::E T;
+    typedef typename K::P P;
     const LossGeom &g;
     const LossPlan &p;
     const T *H, *W, *b;
@@ -935,7 +966,7 @@ template <typename T> class Loss {
         rows->meta = meta;
         const long waves = g.D <= 256 ? (n * ((g.D + 7) / 8) + 63) / 64 : n; // with something to do
         const long weight_blocks = !p.pack_w ? 0 : waves > 4 * 4096 ? 4096 : (waves + 3) / 4;
-        hipLaunchKernelGGL(pack_kernel<T>, dim3((unsigned)(rows->row_blocks + weight_blocks)), dim3(256), 0, st, *rows);
+        hipLaunchKernelGGL(pack_kernel<K>, dim3((unsigned)(rows->row_blocks + weight_blocks)), dim3(256), 0, st, *rows);
         return hipGetLastError();
     }
     Params logits_params(long n) const
@@ -990,11 +1021,11 @@ public:
             if ((e = operands(v0, n, &rows)) != hipSuccess) return e;
             if (p.z.slices > 1) { // (one piece)
                 if ((e = logits_in_slices(n)) != hipSuccess) return e;
-                hipLaunchKernelGGL(row_loss_kernel<T>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)(ws + p.o_z), g.T * ld_logits(),
+                hipLaunchKernelGGL(row_loss_kernel<K>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)(ws + p.o_z), g.T * ld_logits(),
                                    (int)ld_logits(), p.z.slices, b, (int)g.V, loss, lse);
                 return hipGetLastError();
             }
-            e = launch<P, Lay::kAlong, Lay::kAlong, Stats<T>>(logits_params(n), {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.z, st);
+            e = launch<P, Lay::kAlong, Lay::kAlong, Stats<K>>(logits_params(n), {b ? b + v0 : nullptr, meta, part, g.T, part0, (int)v0}, p.z, st);
             if (e != hipSuccess) return e;
             part0 += (int)wave_columns(n, p.z.shape);
         }
@@ -1015,21 +1046,21 @@ public:
         rows.gloss = gloss;
         rows.dH = dH;
         char *G = ws + p.o_g;
-        const long ld_g = (p.piece + 7) / 8 * 8 * (p.split ? 4 : 2);
+        const long ld_g = (p.piece + 7) / 8 * 8 * (long)sizeof(T);
         float *sums = p.pieces > 1 || p.h.slices > 1 ? (float *)(ws + p.o_acc) : nullptr;
         for (long v0 = 0; v0 < g.V; v0 += p.piece) {
             const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
             if ((e = operands(v0, n, &rows)) != hipSuccess) return e;
             if (p.z.slices > 1) {
                 if ((e = logits_in_slices(n)) != hipSuccess) return e;
-                hipLaunchKernelGGL(row_grad_kernel<T>, dim3((unsigned)g.T, cdiv(g.V, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
+                hipLaunchKernelGGL(row_grad_kernel<K>, dim3((unsigned)g.T, cdiv(g.V, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
                                    g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g);
                 e = hipGetLastError();
             } else {
-                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<T>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
+                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<K>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
             }
             if (e != hipSuccess) return e;
-            PairParams<T> q{};
+            PairParams<K> q{};
             q.w.a = G;
             q.w.lda = ld_g;
             q.w.b = h;
@@ -1057,23 +1088,27 @@ public:
                 if (dW) q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
                 if (dH) q.blocks_h = place_tiles<Small>(&q.h, false, p.h.slices, kPass<P, Small::R>);
                 static const hipError_t attr =
-                    hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, Small::kLds);
+                    hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<K>), hipFuncAttributeMaxDynamicSharedMemorySize, Small::kLds);
                 if (attr != hipSuccess) return attr;
-                hipLaunchKernelGGL(pair_kernel<T>, dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
+                hipLaunchKernelGGL(pair_kernel<K>, dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
                 e = hipGetLastError();
-            } else {
-                if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<T>>(q.w, q.ew, p.w, st);
-                if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<T>>(q.h, q.eh, p.h, st);
+            } else if constexpr (!P::kRaw) { // (floats as they lie are small products)
+                if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
+                if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);
                 if (db && e == hipSuccess) {
-                    hipLaunchKernelGGL(bias_kernel<T>, dim3(bias_blocks), dim3(256), 0, st, q.b);
+                    hipLaunchKernelGGL(bias_kernel<K>, dim3(bias_blocks), dim3(256), 0, st, q.b);
                     e = hipGetLastError();
                 }
             }
             if (e != hipSuccess) return e;
         }
         if (dH && sums) {
-            hipLaunchKernelGGL(finish_rows_kernel<T>, dim3((unsigned)g.T, cdiv(g.D, 256)), dim3(256), 0, st, meta, (const float *)sums, g.T * g.D,
-                               p.h.slices, (int)g.D, dH);
+            if (p.h.slices >= 8)
+                hipLaunchKernelGGL((finish_rows_kernel<T, true>), dim3((unsigned)g.T, cdiv(g.D, 256)), dim3(256), 0, st, meta, (const float *)sums,
+                                   g.T * g.D, p.h.slices, (int)g.D, dH);
+            else
+                hipLaunchKernelGGL((finish_rows_kernel<T, false>), dim3((unsigned)g.T, cdiv(g.D, 1024)), dim3(256), 0, st, meta, (const float *)sums,
+                                   g.T * g.D, p.h.slices, (int)g.D, dH);
             e = hipGetLastError();
         }
         return e;
@@ -1085,15 +1120,17 @@ public:
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            float *loss, float *lse, void *ws, hipStream_t st)
 {
-    if (g.dtype == CAC_F32) return Loss<float>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
-    return Loss<bf16_t>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.raw) return Loss<OfRaw>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
 }
 
 hipError_t launch_loss_bwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            const float *lse, const float *gloss, void *dH, void *dW, void *db, void *ws, hipStream_t st)
 {
-    if (g.dtype == CAC_F32) return Loss<float>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
-    return Loss<bf16_t>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
+    if (p.raw) return Loss<OfRaw>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
 }
 
 } // namespace cac

@@ -4,7 +4,7 @@
 // A has M rows, B has N, and the sum runs over K.  Each operand comes in one of two layouts:
 //   kAlong: K runs along a row of memory (row index m or n)
 //   kDown : K is the row of memory (m or n runs along it); the transposing LDS read makes fragments of it
-// and in one of two number formats:
+// and in one of three number formats:
 //   Bf16  : bfloat16, one product
 //   Split : a float as the sum of two half-precision numbers, x = hi + lo.  hi holds 11 bits of the significand and lo the next
 //           12 (its sign is one of them): 2^-23 of x is lost.  hi hi + hi lo + lo hi leaves out lo lo, at most 2^-22 of a product and
@@ -12,6 +12,11 @@
 //           float instruction's rate.  A row of memory holds 8 hi, 8 lo, 8 hi, ...: a chunk of 16 bytes of one kind after one of
 //           the other, so that both formats are staged alike, 128 bytes of K to a row and pass.  Numbers are stored times a
 //           power of two that the caller takes out again, which keeps lo out of the subnormal range.
+//
+//   Raw   : floats as they lie, made into three bfloat16 parts (8 bits of the significand each, nothing is lost) when a fragment is
+//           multiplied: six products, without those below 2^-24 of a number's.  It needs no powers of two and no pass beforehand,
+//           and is what small products take, whose time is launches and latencies.  A chunk holds 4 numbers, two of them the 8 that
+//           a chunk of hi and one of lo hold.
 //
 // A workgroup of WM x WN waves owns a tile of C; a wave holds MI x NI accumulators of 32 x 32.  Tiles go from global memory straight
 // into one of two LDS buffers while the other is multiplied, and a step's fragments are read while the step before is multiplied: the
@@ -33,8 +38,9 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 enum class Lay { kAlong, kDown };
-struct Bf16 { static constexpr int kParts = 1; };
-struct Split { static constexpr int kParts = 2; };
+struct Bf16 { static constexpr int kParts = 1; static constexpr bool kRaw = false; };
+struct Split { static constexpr int kParts = 2; static constexpr bool kRaw = false; };
+struct Raw { static constexpr int kParts = 2; static constexpr bool kRaw = true; };
 
 constexpr uint32_t kNowhere = 0x80000000u; // an offset past every descriptor's range
 
@@ -61,7 +67,7 @@ struct Params {
     int batch, slices;         // matrices; parts that each sum is formed in
     int group;                 // tile rows that one XCD walks together
     int kt_slice;              // passes over K of one slice of the sum
-    Counts counts_m, counts_k; // rows of a (terms of b, of which there is one pass) that count: the others are zeros, whatever stands there
+    Counts counts_m, counts_k; // where an ending says so, rows of a, terms of b that count: the others are zeros, whatever stands there
 };
 
 template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of the sum in one pass, R bytes of K to a row
@@ -85,7 +91,7 @@ __device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t offset, uint32_t 
 }
 
 // One operand's way into LDS: T rows of C by one pass of K, R T bytes, by NW waves.
-template <class P, Lay L, int T, int R, int NW> struct Stage {
+template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
     static constexpr int kLoads = T * R / 1024 / NW;                       // per wave and pass, 1 KiB each
     static constexpr int kRowBytes = L == Lay::kAlong ? R : T * 2 * P::kParts;
     static constexpr int kChunks = kRowBytes / 16, kStep = NW * 64 / kChunks; // chunks of a row; rows from a load to the next
@@ -95,9 +101,11 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
     uint32_t off[kLoads];
     int at;           // the lane's chunk of a row (kAlong), its first row (kDown)
     int left;         // chunks (kAlong) or rows (kDown) of K from the pass to load next on
+    int row_k;        // kDown: the first row of K of the pass to load next
+    Counts counts;    // kDown: rows of K that count
 
     // first: first row of C; count: rows of C in the matrix; K: terms; kt: first pass, kt1: behind the last
-    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts)
+    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts_)
     {
         const int row0 = (wave * 64 + lane) / kChunks, slot = (wave * 64 + lane) % kChunks;
         const int columns = P::kParts * ((count + 7) / 8) - first / 8 * P::kParts; // kDown: chunks from the tile's first on
@@ -109,6 +117,8 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
             step = R;
         } else {
             at = row0;
+            row_k = kt * kPass<P, R>;
+            counts = counts_;
             left = min(K, kt1 * kPass<P, R>) - kt * kPass<P, R>;
             base = p + (long)first * 2 * P::kParts + (long)kt * kPass<P, R> * ld;
             step = kPass<P, R> * ld;
@@ -117,7 +127,7 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
         for (int i = 0; i < kLoads; ++i) {
             const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row);
             bool there = L == Lay::kAlong ? first + row < count : c < columns;
-            if (counts.labels && there) there = L == Lay::kAlong ? counts(first + row) : row < K && counts(row);
+            if (COUNTS && L == Lay::kAlong && there) there = counts_(first + row);
             off[i] = there ? (uint32_t)(row * (int)ld + c * 16) : kNowhere;
         }
     }
@@ -128,12 +138,15 @@ template <class P, Lay L, int T, int R, int NW> struct Stage {
         const u32x4 rs = {(uint32_t)from, (uint32_t)(from >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const uint32_t o = at + (L == Lay::kAlong ? 0 : i * kStep) < left ? off[i] : kNowhere;
+            uint32_t o = at + (L == Lay::kAlong ? 0 : i * kStep) < left ? off[i] : kNowhere;
+            if (COUNTS && L == Lay::kDown && counts.labels) // (few rows: looked up as they come)
+                if (o != kNowhere && !counts(row_k + at + i * kStep)) o = kNowhere;
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 1024);
             load_to_lds(rs, o, to);
         }
         base += step;
         left -= L == Lay::kAlong ? kChunks : kPass<P, R>;
+        if (COUNTS && L == Lay::kDown) row_k += kPass<P, R>;
     }
 };
 
@@ -165,6 +178,16 @@ template <class P, Lay L, int T, int R> struct Frag {
             const uint32_t c = x ^ (uint32_t)(s * 2 * P::kParts + part);
             return *(lds8 *)(uintptr_t)(lds + at + blk * 32 * R + (c << 4));
         }
+        if constexpr (P::kRaw) { // four terms of a column, one below the other
+            const uint32_t n = (block0 + blk) * 32 + (lane & 31);
+            union { float f[4]; s16x8 v; } r;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int row = s * 16 + 8 * (lane >> 5) + part * 4 + k;
+                r.f[k] = *(__attribute__((address_space(3))) float *)(uintptr_t)(lds + row * kRowBytes + (((n >> 2) ^ swizzle<P, L, T, R>(row)) << 4) + (n & 3) * 4);
+            }
+            return r.v;
+        }
         const uint32_t col = (block0 + blk) * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
         const uint32_t c = (col * P::kParts + part) ^ x;
         const uint32_t p = lds + at + (c << 4) + s * 16 * kRowBytes;
@@ -183,6 +206,9 @@ template <class P> __device__ __forceinline__ f32x16 product(s16x8 a, s16x8 b, f
     if (P::kParts == 2) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x.h, y.h, c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
 }
+
+// What an ending may say about its product.
+struct Ending { static constexpr bool kSymmetric = false, kCountsM = false, kCountsK = false; };
 
 // ---- a float as two halves.  x is fixed first: left to itself the compiler takes hi from a product's rounded value and lo from the
 // product, and where those lie on two sides of a half-precision number's middle, hi + lo is off by a unit of hi.
@@ -278,6 +304,28 @@ template <Fmt F, int NI> struct RowBlock {
     }
 };
 
+// Eight floats, two registers of four, in three bfloat16 parts: what is cut off below a part is the rest that the next is cut from.
+struct Parts3 { s16x8 p[3]; };
+__device__ __forceinline__ Parts3 cut_in_three(s16x8 first, s16x8 second)
+{
+    union { s16x8 v[2]; float f[8]; } x;
+    x.v[0] = first;
+    x.v[1] = second;
+    union { uint32_t u[4]; s16x8 v; } r[3];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float a = x.f[e], b = x.f[e + 1];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const uint32_t ua = __float_as_uint(a) & 0xffff0000u, ub = __float_as_uint(b) & 0xffff0000u;
+            r[k].u[e / 2] = (ua >> 16) | ub;
+            a -= __uint_as_float(ua);
+            b -= __uint_as_float(ub);
+        }
+    }
+    return Parts3{{r[0].v, r[1].v, r[2].v}};
+}
+
 // Where a wave's part of C lies.  acc[mi][ni][4 q + e] is C[m][n] of m = m0 + 32 mi + lane % 32 and
 // n = n0 + 32 ni + 8 q + 4 (lane / 32) + e: a lane holds four neighbours of a row of C.
 struct Place {
@@ -348,8 +396,8 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    Stage<P, LA, TM, S::R, S::kWaves> sa;
-    Stage<P, LB, TN, S::R, S::kWaves> sb;
+    Stage<P, LA, TM, S::R, S::kWaves, Epi::kCountsM> sa;
+    Stage<P, LB, TN, S::R, S::kWaves, Epi::kCountsK> sb;
     sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane, p.counts_m);
     sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane, p.counts_k);
     const int wm = wave / S::WN, wn = wave % S::WN;
@@ -396,6 +444,16 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
                     cur = next;
                 }
                 __builtin_amdgcn_sched_barrier(0);
+                if constexpr (P::kRaw) {
+                    static_assert(!P::kRaw || MI * NI == 1, "fragments are cut for one product each");
+                    const Parts3 x = cut_in_three(b[k & 1][0][0], b[k & 1][1][0]), y = cut_in_three(a[k & 1][0][0], a[k & 1][1][0]);
+#pragma unroll
+                    for (int h = 0; h < 3; ++h)
+#pragma unroll
+                        for (int g = 0; g + h < 3; ++g) acc[0][0] = product<Bf16>(x.p[h], y.p[g], acc[0][0]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    continue;
+                }
 #pragma unroll
                 for (int h = 0; h < 2 * P::kParts - 1; ++h) // hi hi, then hi lo and lo hi
 #pragma unroll
@@ -509,11 +567,15 @@ hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hip
 template <class P, Lay LA, Lay LB, class Epi>
 hipError_t launch(const Params &p, const typename Epi::Params &e, Choice c, hipStream_t st)
 {
-    if (c.shape == kBig) return launch_shape<P, LA, LB, Big, Epi>(p, e, c.slices, st);
-    if constexpr (P::kParts == 2)
-        if (c.shape == kWide) return launch_shape<P, LA, LB, Wide, Epi>(p, e, c.slices, st);
-    if (c.shape == kMiddle) return launch_shape<P, LA, LB, Middle, Epi>(p, e, c.slices, st);
-    return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
+    if constexpr (P::kRaw) {
+        return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st); // (the only ones that are asked for)
+    } else {
+        if (c.shape == kBig) return launch_shape<P, LA, LB, Big, Epi>(p, e, c.slices, st);
+        if constexpr (P::kParts == 2)
+            if (c.shape == kWide) return launch_shape<P, LA, LB, Wide, Epi>(p, e, c.slices, st);
+        if (c.shape == kMiddle) return launch_shape<P, LA, LB, Middle, Epi>(p, e, c.slices, st);
+        return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
+    }
 }
 
 } // namespace mm

@@ -23,13 +23,13 @@ constexpr int kMaxSumBlocks = 256;
 
 // ---- endings of the products
 // S = acc / 4096, symmetric: the tiles above the diagonal are computed and written twice
-struct Gram {
+struct Gram : Ending {
     static constexpr bool kSymmetric = true;
     struct Params { char *out; long ld, stride; const int *lift; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p);
 };
 // a I + b A + c A A
-struct Poly {
+struct Poly : Ending {
     static constexpr bool kSymmetric = true;
     struct Params { char *out; long ld, stride; const char *a; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p);
@@ -103,7 +103,7 @@ template <int MI, int NI> __device__ __forceinline__ void Poly::run(const Params
 }
 
 // a slice's part of S, in float, [slice][batch][r][ld]
-struct GramPart {
+struct GramPart : Ending {
     static constexpr bool kSymmetric = true;
     struct Params { float *out; int ld, batch; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
@@ -153,8 +153,7 @@ __global__ void __launch_bounds__(256) join_gram_kernel(const float *__restrict_
 }
 
 // the next X
-struct Next {
-    static constexpr bool kSymmetric = false;
+struct Next : Ending {
     struct Params { char *out; long ld, stride; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -181,8 +180,7 @@ struct Next {
 };
 
 // the result, or the weights' update: out = keep * out + scale * acc
-template <typename T, bool UPDATE> struct Last {
-    static constexpr bool kSymmetric = false;
+template <typename T, bool UPDATE> struct Last : Ending {
     struct Params { T *out; float keep, scale; const int *lift; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {

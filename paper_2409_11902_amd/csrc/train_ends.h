@@ -15,7 +15,7 @@ struct LossGeom {
     long ignore;
 };
 struct LossPlan {
-    bool split;       // float: operands as two halves
+    bool split, raw;  // float: operands as two halves, or as they lie
     bool direct;      // few rows: H is read where it lies, rows that do not count as zeros
     bool pack_w;      // the weights go through the workspace, piece by piece
     bool pair;        // backward: dW, dH and db in one launch
