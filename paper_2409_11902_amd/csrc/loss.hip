@@ -195,6 +195,7 @@ struct PackRows {
 
 // 512 numbers of a row of memory from n0 on in float, eight neighbours to a lane, zeros past the row's end.  A row that does not start
 // on 16 bytes is read side by side and dealt out through the wave's 2304 bytes of LDS.
+constexpr int kShortRow = 128;
 constexpr int kDeal = 576; // 512 floats, and 4 after every 32, which keeps the lanes' eights apart
 template <typename T> __device__ __forceinline__ void load8(const T *p, int n0, int D, bool aligned, int lane, float *deal, float (&v)[8])
 {
@@ -230,7 +231,7 @@ template <typename T> __device__ __forceinline__ void load8(const T *p, int n0, 
 // ... and into a packed row (as they are, or two halves times `scale`)
 template <class K> __device__ __forceinline__ void store8(char *row, int n, const float (&v)[8], float scale)
 {
-    if (K::kG == Fmt::kBf16) {
+    if (!K::kSplit) {
         u32x4 u;
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = f32x2_to_bf16x2(v[2 * e], v[2 * e + 1]);
@@ -240,8 +241,7 @@ template <class K> __device__ __forceinline__ void store8(char *row, int n, cons
 #pragma unroll
     for (int h = 0; h < 8; h += 4) {
         const float x[4] = {v[h] * scale, v[h + 1] * scale, v[h + 2] * scale, v[h + 3] * scale};
-        if (K::kSplit) store_split(row, n + h, x);
-        else *(f32x4 *)(row + (n + h) * 4) = f32x4{x[0], x[1], x[2], x[3]};
+        store_split(row, n + h, x);
     }
 }
 
@@ -335,7 +335,9 @@ template <class K> __device__ __forceinline__ void pack_weights(const PackRows &
     const float s = K::kSplit ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
     const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
     const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks);
-    if (p.D <= 256) { // a thread to eight numbers, wherever they are
+    // Short rows: a thread to eight numbers, wherever they are (100 x 100 x 60000 float forward: 53 us with a wave to a row, 43 so;
+    // of 16 x 252 x 60000 bfloat16 40 and 43).
+    if (p.D <= kShortRow) {
         const unsigned per_row = (p.D + 7) / 8, all = p.classes * per_row; // (2^24 at most)
         for (unsigned c = (blockIdx.x - p.row_blocks) * 256 + threadIdx.x; c < all; c += rows * 64) {
             const unsigned row = c / per_row;
@@ -872,19 +874,24 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
 
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 {
-    // Small products of floats: three bfloat16 parts made of a fragment when it is multiplied cost less than the passes that
-    // find the largest numbers and split everything beforehand (64 x 2048 x 1000, both passes: 55 us split, 41 us so).
+    // Few rows: everything is read where it lies, and floats are made into three bfloat16 parts when they are multiplied.  With more
+    // of them the six products cost more than the passes that compact rows, find the largest numbers and split everything
+    // beforehand.  Both passes, packed beforehand and as they lie:
+    //   bfloat16  1 x 512 x 1000  29 and 23 us    64 x 2048 x 8000  74 and 66 us
+    //   float     64 x 64 x 512   37 and 31 us    16 x 1024 x 100000  961 and 521 us    96 x 2048 x 600  51 and 53 us    256 x 512 x 800  49 and 62 us
     const int in16 = g.dtype == CAC_F32 ? 4 : 8; // numbers in 16 bytes
-    p->raw = g.dtype == CAC_F32 && (double)g.T * g.D * g.V <= 2.5e8 && g.D % 8 == 0 && g.ld_w % in16 == 0;
+    p->direct = g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % in16 == 0 && (g.dtype == CAC_BF16 || g.ld_w % in16 == 0);
+    p->raw = g.dtype == CAC_F32 && p->direct;
     p->split = g.dtype == CAC_F32 && !p->raw;
     p->pack_w = !p->raw && (p->split || g.D % 8 || g.ld_w % 8);
-    p->direct = !p->split && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % in16 == 0;
     p->dp = (g.D + 7) / 8 * 8;
     const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
     p->row_bytes = e * p->dp;
-    // A piece's G (and its packed weights) stay within the 256 MiB that the chip caches; at least 4096 classes, in whole tiles.
+    // A piece's G and packed weights take 1 GiB at most, the weights alone half of that, or 4096 classes.  Smaller pieces cost more ends
+    // of launches and more sums of dH to add to: 4096 x 1024 x 32000 float 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one;
+    // 2048 x 1024 x 200000 float forward 2.88 ms of 256 MiB, 2.75 of 512, 2.66 in one.
     const long per_class = (backward ? g.T * e : 0) + (p->pack_w ? p->row_bytes : 0);
-    long piece = per_class ? (256L << 20) / per_class / 256 * 256 : g.V;
+    long piece = per_class ? ((backward ? 1024L : 512L) << 20) / per_class / 256 * 256 : g.V;
     if (piece < 4096) piece = 4096;
     if (piece > 1L << 19) piece = 1L << 19;
     if (piece >= g.V) piece = g.V;
@@ -892,15 +899,17 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     if (p->pieces > 1) piece = ((g.V + p->pieces - 1) / p->pieces + 255) / 256 * 256;
     p->pieces = (int)((g.V + piece - 1) / piece);
     p->piece = piece;
-    // A sum over D in slices leaves its parts of the logits in the workspace: for few rows and classes only.
+    // A sum over D in slices leaves its parts of the logits in the workspace (256 x 8192 x 2000 float forward: 107 us in one, 82 so).
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
     const bool wide_k = g.dtype == CAC_F32; // (a pass is 32 terms)
-    p->z = choose(wide_k, g.T, piece, 1, g.D, false, p->pieces > 1 || logits * 16 > 32L << 20 ? 1 : 16, p->raw);
+    p->z = choose(wide_k, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw);
     p->w = choose(wide_k, piece, g.D, 1, g.T, false, 1);
     p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128);
-    // dW and dH together where both would take the smallest tiles anyway, or are over before a launch is
+    // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
+    // end where compute units run out of work (512 x 512 x 1500 float 75 us apart, 61 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
+    // 1024 x 2048 x 16000 341 and 379).
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
-    p->pair = backward && (p->raw || work < 4e9 || (p->w.shape == kSmall && p->h.shape == kSmall));
+    p->pair = backward && (p->raw || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
         p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128, true);
@@ -948,7 +957,11 @@ template <class K> class Loss {
         ld_h = p.direct ? g.ld_h * (long)sizeof(T) : p.row_bytes;
         w = p.pack_w ? (const void *)(ws + p.o_w) : W + v0 * g.ld_w;
         ld_w = p.pack_w ? p.row_bytes : g.ld_w * (long)sizeof(T);
-        if (!pack_h && !p.pack_w) return hipSuccess;
+        if constexpr (P::kRaw) return hipSuccess; // (everything lies where it is)
+        else return !pack_h && !p.pack_w ? hipSuccess : pack(v0, n, pack_h, rows);
+    }
+    hipError_t pack(long v0, long n, bool pack_h, PackRows *rows)
+    {
         rows->H = H;
         rows->W = W + v0 * g.ld_w;
         rows->ld_h = g.ld_h;
@@ -964,7 +977,7 @@ template <class K> class Loss {
         rows->out_w = ws + p.o_w;
         rows->row_bytes = p.row_bytes;
         rows->meta = meta;
-        const long waves = g.D <= 256 ? (n * ((g.D + 7) / 8) + 63) / 64 : n; // with something to do
+        const long waves = g.D <= kShortRow ? (n * ((g.D + 7) / 8) + 63) / 64 : n; // with something to do
         const long weight_blocks = !p.pack_w ? 0 : waves > 4 * 4096 ? 4096 : (waves + 3) / 4;
         hipLaunchKernelGGL(pack_kernel<K>, dim3((unsigned)(rows->row_blocks + weight_blocks)), dim3(256), 0, st, *rows);
         return hipGetLastError();
@@ -1029,8 +1042,9 @@ public:
             if (e != hipSuccess) return e;
             part0 += (int)wave_columns(n, p.z.shape);
         }
-        // (few rows: a block to a row, with the parts' reads apart; many: sixteen, side by side)
-        if (g.T < 1024) hipLaunchKernelGGL(join_kernel<1>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
+        // Few rows of many parts: a block to a row; else sixteen rows, whose parts lie side by side (forward, in blocks of one row and of
+        // sixteen: 64 x 256 x 50000 20 and 25 us, 64 x 256 x 4000 9.9 and 9.3, 1024 x 256 x 50000 99 and 88).
+        if (g.T <= 256 && p.parts > 128) hipLaunchKernelGGL(join_kernel<1>, dim3((unsigned)g.T), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
         else hipLaunchKernelGGL(join_kernel<16>, dim3(cdiv(g.T, 16)), dim3(256), 0, st, meta, (const float *)part, (int)p.parts, g.T, loss, lse);
         return hipGetLastError();
     }
@@ -1103,6 +1117,8 @@ public:
             if (e != hipSuccess) return e;
         }
         if (dH && sums) {
+            // (1 x 512 x 21841: 51 us where every thread adds up all of its slices, 46 where waves share them; one slice of 8192 x 4096:
+            // 7.95 and 8.05 ms of the whole)
             if (p.h.slices >= 8)
                 hipLaunchKernelGGL((finish_rows_kernel<T, true>), dim3((unsigned)g.T, cdiv(g.D, 256)), dim3(256), 0, st, meta, (const float *)sums,
                                    g.T * g.D, p.h.slices, (int)g.D, dH);

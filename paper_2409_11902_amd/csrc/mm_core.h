@@ -76,7 +76,8 @@ template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of t
 // wave reads 4 rows together at 32 neighbouring columns (of every other chunk where a row has two parts).
 template <class P, Lay L, int T, int R> __device__ __forceinline__ int swizzle(int row)
 {
-    if (L == Lay::kAlong) return R == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+    static_assert(R == 128, "eight chunks to a row");
+    if (L == Lay::kAlong) return (row >> 1) & 7;
     if (P::kParts == 2) return ((row & 1) << 3) ^ ((row >> 1) & 1);
     if (T == 64) return (row & 2) << 1;
     return (row & 3) << 2;
@@ -361,7 +362,7 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
 {
     constexpr int MI = S::MI, NI = S::NI, TM = S::TM, TN = S::TN;
     constexpr int kSteps = S::R / 32 / P::kParts; // of 16 terms, in a pass
-    constexpr int kTurn = kSteps % 2 ? 2 : 1;     // passes after which the fragments' registers are the same again
+    static_assert(kSteps % 2 == 0, "a pass ends with the fragments' registers that it began with");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int M = p.m_dev ? min(p.M, *p.m_dev) : p.M, K = p.k_dev ? min(p.K, *p.k_dev) : p.K;
 
@@ -430,23 +431,22 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
         meet<kAhead>();
         load(lds_end - S::kBuffer);
         read(0, lds, 0);
-        for (int kt = kt0; kt < kt1; kt += kTurn) { // (a pass behind the last is zeros)
+        for (int kt = kt0; kt < kt1; ++kt) {
 #pragma unroll
-            for (int k = 0; k < kTurn * kSteps; ++k) {
-                const int s = k % kSteps;
+            for (int s = 0; s < kSteps; ++s) {
                 if (s + 1 < kSteps) {
-                    read((k + 1) & 1, cur, s + 1);
+                    read((s + 1) & 1, cur, s + 1);
                 } else {
                     const uint32_t next = cur + S::kBuffer == lds_end ? lds : cur + S::kBuffer;
                     meet<kAhead>(); // the next pass has arrived; this one's last fragments are in registers
                     load(cur);
-                    read((k + 1) & 1, next, 0);
+                    read((s + 1) & 1, next, 0);
                     cur = next;
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (P::kRaw) {
                     static_assert(!P::kRaw || MI * NI == 1, "fragments are cut for one product each");
-                    const Parts3 x = cut_in_three(b[k & 1][0][0], b[k & 1][1][0]), y = cut_in_three(a[k & 1][0][0], a[k & 1][1][0]);
+                    const Parts3 x = cut_in_three(b[s & 1][0][0], b[s & 1][1][0]), y = cut_in_three(a[s & 1][0][0], a[s & 1][1][0]);
 #pragma unroll
                     for (int h = 0; h < 3; ++h)
 #pragma unroll
@@ -459,7 +459,7 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
 #pragma unroll
                     for (int i = 0; i < MI; ++i)
 #pragma unroll
-                        for (int j = 0; j < NI; ++j) acc[i][j] = product<P>(b[k & 1][h & 1][j], a[k & 1][h >> 1][i], acc[i][j]);
+                        for (int j = 0; j < NI; ++j) acc[i][j] = product<P>(b[s & 1][h & 1][j], a[s & 1][h >> 1][i], acc[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }

@@ -279,7 +279,7 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
         } else {
             const float *part = p.part + ((long)(step & 1) * gridDim.y + batch) * p.slices * (kSide * kSide);
             const int *exps = p.exps + batch * p.slices;
-            // the slices' powers of two are brought to that of the largest numbers (a lane knows one slice's: there are at most 32)
+            // the slices' powers of two are brought to that of the largest numbers (a lane knows one slice's: there are at most 64)
             int e_ref = step == 0 ? exps[min(lane, p.slices - 1)] : 0;
             const int e_lane = e_ref;
 #pragma unroll
@@ -462,9 +462,12 @@ template <typename TG> hipError_t launch(const Args &a, int width, int batch, in
 bool plan_muon_narrow(const MuonGeom &g, MuonNarrowPlan *p)
 {
     const long r = g.rows < g.cols ? g.rows : g.cols, n = g.rows < g.cols ? g.cols : g.rows;
-    // every workgroup reads all of its matrix' parts: not more than 32 of them
-    if (r > kSide || n > 8192) return false;
-    p->width = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : n <= 2048 ? 128 : 256;
+    // Every workgroup reads all of its matrix' parts, and a lane knows one part's power of two: not more than 64 of them (64 x 16384: 108 us
+    // here, 148 with muon.hip's launches; 64 x 2048 60 and 93).
+    if (r > kSide || n > 16384) return false;
+    // The narrowest that holds a matrix in one launch; else more workgroups while their parts are few (a step of 64 x 576 in columns of 64,
+    // 128 and 256: 55, 52 and 57 us, of 64 x 2048 81, 64 and 60, of 64 x 8192 -, 128 and 80).
+    p->width = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : n <= 1024 ? 128 : 256;
     p->slices = (int)((n + p->width - 1) / p->width);
     size_t o = 0;
     p->o_x = o;

@@ -64,7 +64,7 @@ def rel(a, b):
 
 SHAPES = [
     (1, 1, 1), (1, 1, 9), (2, 5, 1), (1, 3, 5), (2, 17, 40), (3, 64, 64), (2, 64, 65), (2, 64, 128), (1, 40, 129), (2, 200, 64), (2, 64, 256),
-    (1, 257, 33), (4, 64, 576), (2, 1001, 50), (1, 64, 2049), (1, 33, 8192), (1, 64, 8200), (2, 65, 65), (1, 100, 300), (3, 130, 67),
+    (1, 257, 33), (4, 64, 576), (2, 1001, 50), (1, 64, 2049), (1, 33, 8192), (1, 64, 8200), (2, 12000, 20), (1, 64, 16384), (1, 64, 16400), (2, 65, 65), (1, 100, 300), (3, 130, 67),
     (1, 129, 1152), (2, 300, 700), (3, 512, 512), (1, 1000, 513), (1, 700, 2049), (1, 2048, 256), (1, 1030, 1030),
 ]
 

@@ -109,10 +109,10 @@ def test_logits_are_not_kept():
             assert "pieces" in B.cac_loss_describe_plan(d, op)
 
 
-@pytest.mark.parametrize("shape", [(1, 1), (64, 64), (64, 256), (8192, 33), (64, 8193), (65, 65), (512, 4608), (2048, 512), (4096, 4096)])
+@pytest.mark.parametrize("shape", [(1, 1), (64, 64), (64, 256), (8192, 33), (64, 8193), (16384, 64), (64, 16385), (65, 65), (512, 4608), (2048, 512), (4096, 4096)])
 def test_muon_plans_are_described(shape):
     d = B.make_muon_desc(*shape, batch=2)
     plan = B.cac_muon_describe_plan(d, B.MUON_STEP)
-    assert ("narrow" in plan) == (min(shape) <= 64 and max(shape) <= 8192)
+    assert ("narrow" in plan) == (min(shape) <= 64 and max(shape) <= 16384)
     if "narrow" not in plan:
         assert ("X^T X" in plan) == (shape[0] > shape[1])
