@@ -6,7 +6,11 @@
 
 namespace cac {
 
-static int tile_edge(const TileChoice &c) { return 64 * (c.shape + 1); }
+static const char *tile_name(const TileChoice &c)
+{
+    static const char *const names[] = {"64", "128", "192", "256", "32 x 128"};
+    return names[c.shape];
+}
 
 static int make_loss_geom(const cac_loss_desc *d, LossGeom *g)
 {
@@ -82,10 +86,10 @@ int cac_loss_describe_plan(const cac_loss_desc *d, int op, char *buf, size_t buf
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
     LossPlan p;
     plan_loss(g, op == CAC_LOSS_BWD, &p);
-    const int n = snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %d", p.split ? "two halves" : p.raw ? "float" : "bfloat16",
-                           p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, tile_edge(p.z));
+    const int n = snprintf(buf, buf_len, "%s operands, weights %s, %d pieces of %ld classes, logits tile %s", p.split ? "two halves" : p.raw ? "float" : "bfloat16",
+                           p.pack_w ? "packed" : "as they lie", p.pieces, p.piece, tile_name(p.z));
     if (op == CAC_LOSS_BWD && n > 0 && (size_t)n < buf_len)
-        snprintf(buf + n, buf_len - n, ", dW tile %d, dH tile %d in %d slices", tile_edge(p.w), tile_edge(p.h), p.h.slices);
+        snprintf(buf + n, buf_len - n, ", dW tile %s, dH tile %s in %d slices", tile_name(p.w), tile_name(p.h), p.h.slices);
     return CAC_OK;
 }
 
@@ -149,8 +153,8 @@ int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf
     if (p.narrow)
         snprintf(buf, buf_len, "narrow: %d workgroups of %d columns, %d launches", p.np.slices, p.np.width, p.np.slices == 1 ? 1 : g.steps + 1);
     else
-        snprintf(buf, buf_len, "%s, square products of %ld: tile %d in %d slices, then %d; tile %d", p.tall ? "X^T X" : "X X^T", p.r, tile_edge(p.gram),
-                 p.gram.slices, tile_edge(p.poly), tile_edge(p.apply));
+        snprintf(buf, buf_len, "%s, square products of %ld: tile %s in %d slices, then %s; tile %s", p.tall ? "X^T X" : "X X^T", p.r, tile_name(p.gram),
+                 p.gram.slices, tile_name(p.poly), tile_name(p.apply));
     return CAC_OK;
 }
 

@@ -20,7 +20,7 @@ using namespace mm;
 // What the operands are, as they lie and as they are multiplied.
 struct OfBf16 { typedef bf16_t E; typedef Bf16 P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kBf16; };
 struct OfSplit { typedef float E; typedef Split P; static constexpr bool kSplit = true; static constexpr Fmt kG = Fmt::kSplit; };
-struct OfRaw { typedef float E; typedef Raw P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kF32; };
+template <class R> struct OfRaw { typedef float E; typedef R P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kF32; }; // (Raw, RawOdd)
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStoreG = 14;        // G is stored times 2^14 as two halves: |G| <= 1, and 1e-8 is still a normal number
@@ -63,13 +63,17 @@ struct Meta {
     __device__ __forceinline__ float largest(int lane) const
     {
         if (!direct) return *c;
-        const float g = lane < T && counts(lane) ? fabsf(gloss[lane]) : 0.f;
-        return wave_max(g <= 3.4028235e38f ? g : 0.f);
+        float m = 0.f;
+        for (int t = lane; t < T; t += 64) {
+            const float g = counts(t) ? fabsf(gloss[t]) : 0.f;
+            m = g <= 3.4028235e38f ? fmaxf(m, g) : m;
+        }
+        return wave_max(m);
     }
     __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
     static constexpr int kOut = -(1 << 30);
 };
-constexpr int kDirectRows = 64; // a wave looks them all up at once
+constexpr int kDirectRows = 64, kRawRows = 64; // of bfloat16, of float
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
 inline Meta meta_at(char *p, long T)
@@ -753,13 +757,14 @@ template <class K> struct PairParams {
     Bias<K> b;
     unsigned blocks_w, blocks_h;
 };
-template <class K> __global__ void __launch_bounds__(Small::kThreads, Small::kPerSimd) pair_kernel(const PairParams<K> p)
+template <class K, class SH> __global__ void __launch_bounds__(Small::kThreads, SH::kPerSimd) pair_kernel(const PairParams<K> p)
 {
+    static_assert(SH::kThreads == Small::kThreads, "one kernel");
     extern __shared__ __align__(1024) unsigned char smem[];
     typedef typename K::P P;
     unsigned block = blockIdx.x;
     if (block < p.blocks_h) { // (dH's sums are the longer ones: they begin first)
-        mm_tile<P, Lay::kAlong, Lay::kDown, Small, OutH<K>>(p.h, p.eh, block, smem);
+        mm_tile<P, Lay::kAlong, Lay::kDown, SH, OutH<K>>(p.h, p.eh, block, smem);
         return;
     }
     block -= p.blocks_h;
@@ -874,15 +879,14 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
 
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 {
-    // Few rows: everything is read where it lies, and floats are made into three bfloat16 parts when they are multiplied.  With more
-    // of them the six products cost more than the passes that compact rows, find the largest numbers and split everything
-    // beforehand.  Both passes, packed beforehand and as they lie:
+    // Few rows: everything is read where it lies.  With more of them the float instruction costs more than the passes that compact rows,
+    // find the largest numbers and split everything beforehand.  Both passes, packed beforehand and as they lie:
     //   bfloat16  1 x 512 x 1000  29 and 23 us    64 x 2048 x 8000  74 and 66 us
-    //   float     64 x 64 x 512   37 and 31 us    16 x 1024 x 100000  961 and 521 us    96 x 2048 x 600  51 and 53 us    256 x 512 x 800  49 and 62 us
-    const int in16 = g.dtype == CAC_F32 ? 4 : 8; // numbers in 16 bytes
-    p->direct = g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % in16 == 0 && (g.dtype == CAC_BF16 || g.ld_w % in16 == 0);
-    p->raw = g.dtype == CAC_F32 && p->direct;
+    //   float     64 x 64 x 512   37 and 31 us    16 x 1024 x 100000  961 and 570 us
+    p->raw = g.dtype == CAC_F32 && g.T <= kRawRows;
+    p->odd = p->raw && (g.D % 4 || g.ld_h % 4 || g.ld_w % 4);
     p->split = g.dtype == CAC_F32 && !p->raw;
+    p->direct = p->raw || (g.dtype == CAC_BF16 && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % 8 == 0);
     p->pack_w = !p->raw && (p->split || g.D % 8 || g.ld_w % 8);
     p->dp = (g.D + 7) / 8 * 8;
     const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
@@ -901,10 +905,10 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->piece = piece;
     // A sum over D in slices leaves its parts of the logits in the workspace (256 x 8192 x 2000 float forward: 107 us in one, 82 so).
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
-    const bool wide_k = g.dtype == CAC_F32; // (a pass is 32 terms)
-    p->z = choose(wide_k, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw);
-    p->w = choose(wide_k, piece, g.D, 1, g.T, false, 1);
-    p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128);
+    const Format f = p->raw ? kRaw : p->split ? kSplit : kBf16;
+    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw);
+    p->w = choose(f, piece, g.D, 1, g.T, false, 1);
+    p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
     // end where compute units run out of work (512 x 512 x 1500 float 75 us apart, 61 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
     // 1024 x 2048 x 16000 341 and 379).
@@ -912,7 +916,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->pair = backward && (p->raw || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
-        p->h = choose(wide_k, g.T, g.D, 1, piece, false, 128, true);
+        p->h = choose(f, g.T, g.D, 1, piece, false, 128, true);
     }
     p->parts = 0;
     for (int k = 0; k < p->pieces; ++k) p->parts += wave_columns(k + 1 < p->pieces ? piece : g.V - (p->pieces - 1) * piece, p->z.shape);
@@ -1001,6 +1005,15 @@ template <class K> class Loss {
     hipError_t logits_in_slices(long n)
     {
         return launch<P, Lay::kAlong, Lay::kAlong, Logits>(logits_params(n), {(float *)(ws + p.o_z), (int)g.T, (int)ld_logits()}, p.z, st);
+    }
+    template <class SH> hipError_t launch_pair(PairParams<K> &q, bool want_h, int bias_blocks)
+    {
+        constexpr int lds = SH::kLds > Small::kLds ? SH::kLds : Small::kLds;
+        if (want_h) q.blocks_h = place_tiles<SH>(&q.h, false, p.h.slices, kPass<P, SH::R>);
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<K, SH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (attr != hipSuccess) return attr;
+        hipLaunchKernelGGL((pair_kernel<K, SH>), dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), lds, st, q);
+        return hipGetLastError();
     }
     hipError_t largest_magnitudes()
     {
@@ -1100,12 +1113,8 @@ public:
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
                 if (dW) q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
-                if (dH) q.blocks_h = place_tiles<Small>(&q.h, false, p.h.slices, kPass<P, Small::R>);
-                static const hipError_t attr =
-                    hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<K>), hipFuncAttributeMaxDynamicSharedMemorySize, Small::kLds);
-                if (attr != hipSuccess) return attr;
-                hipLaunchKernelGGL(pair_kernel<K>, dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), Small::kLds, st, q);
-                e = hipGetLastError();
+                if constexpr (P::kRaw) e = p.h.shape == kLow ? launch_pair<Low>(q, dH, bias_blocks) : launch_pair<Small>(q, dH, bias_blocks);
+                else e = launch_pair<Small>(q, dH, bias_blocks);
             } else if constexpr (!P::kRaw) { // (floats as they lie are small products)
                 if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
                 if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);
@@ -1136,7 +1145,8 @@ public:
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            float *loss, float *lse, void *ws, hipStream_t st)
 {
-    if (p.raw) return Loss<OfRaw>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.raw) return Loss<OfRaw<Raw>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
     if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
     return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
 }
@@ -1144,7 +1154,8 @@ hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, 
 hipError_t launch_loss_bwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            const float *lse, const float *gloss, void *dH, void *dW, void *db, void *ws, hipStream_t st)
 {
-    if (p.raw) return Loss<OfRaw>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    if (p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    if (p.raw) return Loss<OfRaw<Raw>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
     if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
     return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
 }

@@ -13,10 +13,10 @@
 //           the other, so that both formats are staged alike, 128 bytes of K to a row and pass.  Numbers are stored times a
 //           power of two that the caller takes out again, which keeps lo out of the subnormal range.
 //
-//   Raw   : floats as they lie, made into three bfloat16 parts (8 bits of the significand each, nothing is lost) when a fragment is
-//           multiplied: six products, without those below 2^-24 of a number's.  It needs no powers of two and no pass beforehand,
-//           and is what small products take, whose time is launches and latencies.  A chunk holds 4 numbers, two of them the 8 that
-//           a chunk of hi and one of lo hold.
+//   Raw   : floats as they lie, by the float instruction.  It needs no powers of two and no pass beforehand, and is what products of few
+//           rows take, whose time is that of reading the other operand once.  A chunk holds 4 numbers, two of them the 8 that a
+//           chunk of hi and one of lo hold.
+//   RawOdd: the same of rows that do not start on 16 bytes: 4 bytes to a lane and load in the place of 16.
 //
 // A workgroup of WM x WN waves owns a tile of C; a wave holds MI x NI accumulators of 32 x 32.  Tiles go from global memory straight
 // into one of two LDS buffers while the other is multiplied, and a step's fragments are read while the step before is multiplied: the
@@ -38,9 +38,12 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 enum class Lay { kAlong, kDown };
-struct Bf16 { static constexpr int kParts = 1; static constexpr bool kRaw = false; };
-struct Split { static constexpr int kParts = 2; static constexpr bool kRaw = false; };
-struct Raw { static constexpr int kParts = 2; static constexpr bool kRaw = true; };
+struct Bf16 { static constexpr int kParts = 1, kUnit = 16; static constexpr bool kRaw = false; }; // (kUnit: bytes to a lane and load)
+struct Split { static constexpr int kParts = 2, kUnit = 16; static constexpr bool kRaw = false; };
+struct Raw { static constexpr int kParts = 2, kUnit = 16; static constexpr bool kRaw = true; };
+struct RawOdd { static constexpr int kParts = 2, kUnit = 4; static constexpr bool kRaw = true; };
+// units that n numbers of a row take: whole eights, of raw floats no more than there are
+template <class P> __host__ __device__ constexpr int units(int n) { return P::kRaw ? (n * 4 + P::kUnit - 1) / P::kUnit : P::kParts * ((n + 7) / 8); }
 
 constexpr uint32_t kNowhere = 0x80000000u; // an offset past every descriptor's range
 
@@ -83,37 +86,39 @@ template <class P, Lay L, int T, int R> __device__ __forceinline__ int swizzle(i
     return (row & 3) << 2;
 }
 
-// 16 bytes a lane from `offset` in `rs` to LDS, side by side from the uniform address `to` on.  Written out, because the compiler makes
+// 16 (4) bytes a lane from `offset` in `rs` to LDS, side by side from the uniform address `to` on.  Written out, because the compiler makes
 // every transposing LDS read that follows one of its own wait for all of them; meet() says when they have arrived.  No register is
 // written, so there is nothing that could be overwritten under way.
-__device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t offset, uint32_t to)
+template <int UNIT> __device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory"); // (m0 has no other use in these kernels)
+    if (UNIT == 4) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory"); // (m0 has no other use in these kernels)
 }
 
 // One operand's way into LDS: T rows of C by one pass of K, R T bytes, by NW waves.
 template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
-    static constexpr int kLoads = T * R / 1024 / NW;                       // per wave and pass, 1 KiB each
+    static constexpr int kUnit = P::kUnit, kOf16 = 16 / kUnit;             // bytes to a lane and load; units in a chunk
+    static constexpr int kLoads = T * R / (64 * kUnit) / NW;               // per wave and pass
     static constexpr int kRowBytes = L == Lay::kAlong ? R : T * 2 * P::kParts;
-    static constexpr int kChunks = kRowBytes / 16, kStep = NW * 64 / kChunks; // chunks of a row; rows from a load to the next
-    static_assert(kLoads * 1024 * NW == T * R && kStep * kChunks == NW * 64, "whole loads");
+    static constexpr int kUnits = kRowBytes / kUnit, kStep = NW * 64 / kUnits; // units of a row; rows from a load to the next
+    static_assert(kLoads * 64 * kUnit * NW == T * R && kStep * kUnits == NW * 64, "whole loads");
     const char *base; // of the pass to load next
     long step;        // bytes from a pass to the next
     uint32_t off[kLoads];
-    int at;           // the lane's chunk of a row (kAlong), its first row (kDown)
-    int left;         // chunks (kAlong) or rows (kDown) of K from the pass to load next on
+    int at;           // the lane's unit of a row in even loads (kAlong), its first row (kDown)
+    int left;         // units (kAlong) or rows (kDown) of K from the pass to load next on
     int row_k;        // kDown: the first row of K of the pass to load next
     Counts counts;    // kDown: rows of K that count
 
     // first: first row of C; count: rows of C in the matrix; K: terms; kt: first pass, kt1: behind the last
     __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts_)
     {
-        const int row0 = (wave * 64 + lane) / kChunks, slot = (wave * 64 + lane) % kChunks;
-        const int columns = P::kParts * ((count + 7) / 8) - first / 8 * P::kParts; // kDown: chunks from the tile's first on
+        const int row0 = (wave * 64 + lane) / kUnits, slot = (wave * 64 + lane) % kUnits;
+        const int columns = units<P>(count) - units<P>(first); // kDown: units from the tile's first on
         if (L == Lay::kAlong) {
-            static_assert(L != Lay::kAlong || kStep % 16 == 0, "a lane's chunk is the same in every load");
-            at = slot ^ swizzle<P, L, T, R>(row0);
-            left = min(P::kParts * ((K + 7) / 8), kt1 * kChunks) - kt * kChunks;
+            static_assert(L != Lay::kAlong || kStep % 16 == 0 || kStep == 8, "a lane's unit is the same in every load, or every other");
+            at = slot ^ swizzle<P, L, T, R>(row0) * kOf16;
+            left = min(units<P>(K), kt1 * kUnits) - kt * kUnits;
             base = p + (long)first * ld + (long)kt * R;
             step = R;
         } else {
@@ -126,10 +131,10 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row);
+            const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row) * kOf16;
             bool there = L == Lay::kAlong ? first + row < count : c < columns;
             if (COUNTS && L == Lay::kAlong && there) there = counts_(first + row);
-            off[i] = there ? (uint32_t)(row * (int)ld + c * 16) : kNowhere;
+            off[i] = there ? (uint32_t)(row * (int)ld + c * kUnit) : kNowhere;
         }
     }
     // the next pass into LDS at byte address `lds`; behind the last that is zeros
@@ -139,14 +144,15 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
         const u32x4 rs = {(uint32_t)from, (uint32_t)(from >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            uint32_t o = at + (L == Lay::kAlong ? 0 : i * kStep) < left ? off[i] : kNowhere;
+            const int here = L == Lay::kDown ? at + i * kStep : kStep == 8 && i % 2 ? at ^ 4 * kOf16 : at; // (8 rows on: four chunks apart)
+            uint32_t o = here < left ? off[i] : kNowhere;
             if (COUNTS && L == Lay::kDown && counts.labels) // (few rows: looked up as they come)
                 if (o != kNowhere && !counts(row_k + at + i * kStep)) o = kNowhere;
-            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 1024);
-            load_to_lds(rs, o, to);
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 64 * kUnit);
+            load_to_lds<kUnit>(rs, o, to);
         }
         base += step;
-        left -= L == Lay::kAlong ? kChunks : kPass<P, R>;
+        left -= L == Lay::kAlong ? kUnits : kPass<P, R>;
         if (COUNTS && L == Lay::kDown) row_k += kPass<P, R>;
     }
 };
@@ -206,6 +212,13 @@ template <class P> __device__ __forceinline__ f32x16 product(s16x8 a, s16x8 b, f
     y.s = b;
     if (P::kParts == 2) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x.h, y.h, c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.b, y.b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x4 as_floats(s16x8 v)
+{
+    union { s16x8 s; f32x4 f; } x;
+    x.s = v;
+    return x.f;
 }
 
 // What an ending may say about its product.
@@ -305,28 +318,6 @@ template <Fmt F, int NI> struct RowBlock {
     }
 };
 
-// Eight floats, two registers of four, in three bfloat16 parts: what is cut off below a part is the rest that the next is cut from.
-struct Parts3 { s16x8 p[3]; };
-__device__ __forceinline__ Parts3 cut_in_three(s16x8 first, s16x8 second)
-{
-    union { s16x8 v[2]; float f[8]; } x;
-    x.v[0] = first;
-    x.v[1] = second;
-    union { uint32_t u[4]; s16x8 v; } r[3];
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        float a = x.f[e], b = x.f[e + 1];
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            const uint32_t ua = __float_as_uint(a) & 0xffff0000u, ub = __float_as_uint(b) & 0xffff0000u;
-            r[k].u[e / 2] = (ua >> 16) | ub;
-            a -= __uint_as_float(ua);
-            b -= __uint_as_float(ub);
-        }
-    }
-    return Parts3{{r[0].v, r[1].v, r[2].v}};
-}
-
 // Where a wave's part of C lies.  acc[mi][ni][4 q + e] is C[m][n] of m = m0 + 32 mi + lane % 32 and
 // n = n0 + 32 ni + 8 q + 4 (lane / 32) + e: a lane holds four neighbours of a row of C.
 struct Place {
@@ -349,6 +340,7 @@ typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256
 typedef Shape<2, 6, 3, 1, 128, 3, 1> Wide;   // 192 x 192
 typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128
 typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64
+typedef Shape<1, 4, 1, 1, 128, 3, 2> Low;    // 32 x 128
 
 // All but the N youngest loads have arrived, the fragments asked for are in registers, and every wave of the workgroup says so.
 template <int N> __device__ __forceinline__ void meet()
@@ -444,22 +436,24 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
                     cur = next;
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (P::kRaw) {
-                    static_assert(!P::kRaw || MI * NI == 1, "fragments are cut for one product each");
-                    const Parts3 x = cut_in_three(b[s & 1][0][0], b[s & 1][1][0]), y = cut_in_three(a[s & 1][0][0], a[s & 1][1][0]);
+                if constexpr (P::kRaw) { // (term e of a lane's eight: one of the first 8 with one of the second)
 #pragma unroll
-                    for (int h = 0; h < 3; ++h)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int g = 0; g + h < 3; ++g) acc[0][0] = product<Bf16>(x.p[h], y.p[g], acc[0][0]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    continue;
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                                for (int j = 0; j < NI; ++j)
+                                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(as_floats(b[s & 1][h][j])[e], as_floats(a[s & 1][h][i])[e], acc[i][j], 0, 0, 0);
+                } else {
+#pragma unroll
+                        for (int h = 0; h < 2 * P::kParts - 1; ++h) // hi hi, then hi lo and lo hi
+#pragma unroll
+                        for (int i = 0; i < MI; ++i)
+#pragma unroll
+                            for (int j = 0; j < NI; ++j) acc[i][j] = product<P>(b[s & 1][h & 1][j], a[s & 1][h >> 1][i], acc[i][j]);
                 }
-#pragma unroll
-                for (int h = 0; h < 2 * P::kParts - 1; ++h) // hi hi, then hi lo and lo hi
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-#pragma unroll
-                        for (int j = 0; j < NI; ++j) acc[i][j] = product<P>(b[s & 1][h & 1][j], a[s & 1][h >> 1][i], acc[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -491,46 +485,51 @@ __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) mm_kernel(const Para
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
 // Which tile a product takes, and in how many slices its sum is formed.
-enum { kSmall, kMiddle, kWide, kBig, kShapes };
+enum { kSmall, kMiddle, kWide, kBig, kLow, kShapes };
+enum Format { kBf16, kSplit, kRaw };
 typedef TileChoice Choice;
-constexpr int kEdge[kShapes] = {64, 128, 192, 256};
-inline int wave_columns_of(int shape) { return shape == kSmall ? Small::WN : shape == kMiddle ? Middle::WN : shape == kWide ? Wide::WN : Big::WN; }
+constexpr int kRows[kShapes] = {64, 128, 192, 256, 32}, kColumns[kShapes] = {64, 128, 192, 256, 128}; // of a tile
+constexpr int kWaveColumns[kShapes] = {Small::WN, Middle::WN, Wide::WN, Big::WN, Low::WN};            // waves that a tile's columns fall to
+constexpr int kTerms[] = {64, 32, 32};                                                                // of the sum, in a pass
 
 // Microseconds of a product, from what a pass measured: on a compute unit with one workgroup, and with as many as it holds.
-inline double product_us(int shape, bool split, long tiles, int passes, int slices)
+inline double product_us(int shape, Format f, long tiles, int passes, int slices)
 {
-    static const int kHolds[kShapes] = {3, 2, 1, 1};
-    static const double kAlone[kShapes][2] = {{0.27, 0.27}, {0.77, 0.80}, {1.4, 1.75}, {1.95, 2.85}}, kFull[kShapes][2] = {{0.62, 0.95}, {1.12, 1.5}, {1.4, 1.75}, {1.95, 2.85}},
-                        kOnce[kShapes] = {2.5, 3.5, 5.0, 6.0};
+    static const int kHolds[kShapes] = {3, 2, 1, 1, 2};
+    static const double kAlone[kShapes][3] = {{0.27, 0.27, 0.5}, {0.77, 0.80}, {0, 1.75}, {1.95, 2.85}, {0, 0, 0.5}},
+                        kFull[kShapes][3] = {{0.62, 0.95, 1.4}, {1.12, 1.5}, {0, 1.75}, {1.95, 2.85}, {0, 0, 1.0}},
+                        kOnce[kShapes] = {2.5, 3.5, 5.0, 6.0, 2.5};
     const long wgs = tiles * slices, round = 256L * kHolds[shape];
     const double n = cdiv(passes, slices), rest = (double)(wgs % round);
-    double us = (wgs / round) * (kFull[shape][split] * n + kOnce[shape]);
+    double us = (wgs / round) * (kFull[shape][f] * n + kOnce[shape]);
     if (rest > 0) {
         const double share = rest <= 256 ? 0.0 : (rest - 256) / (round - 256);
-        us += (kAlone[shape][split] + share * (kFull[shape][split] - kAlone[shape][split])) * n + kOnce[shape];
+        us += (kAlone[shape][f] + share * (kFull[shape][f] - kAlone[shape][f])) * n + kOnce[shape];
     }
     return us;
 }
 inline long tiles_of(int shape, long M, long N, bool symmetric)
 {
-    const long m = cdiv(M, kEdge[shape]), n = cdiv(N, kEdge[shape]);
+    const long m = cdiv(M, kRows[shape]), n = cdiv(N, kColumns[shape]);
     return symmetric ? m * (m + 1) / 2 : m * n;
 }
-// The cheapest of them; more than one slice costs the writing and reading of that many sums of 32 bits, and a launch.
-inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetric, int max_slices, bool small_only = false)
+// The cheapest of them; more than one slice costs the writing and reading of that many sums of 32 bits, and a launch.  (Over 150 products of 16
+// to 6000 rows, columns and terms the one that this takes is 0.7 % (Split; Bf16 1.1 %) slower in the mean than the fastest of the four.)
+inline Choice choose(Format f, long M, long N, int batch, long K, bool symmetric, int max_slices, bool small_only = false)
 {
     Choice best{kSmall, 1};
     double least = 1e30;
     for (int shape = 0; shape < kShapes; ++shape) {
-        if (small_only && shape != kSmall) break;
-        if (shape == kWide && !split) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
+        if (small_only && shape != kSmall && shape != kLow) continue;
+        if (shape == kWide && f != kSplit) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
+        if ((shape == kLow) != (f == kRaw && M <= kRows[kLow])) continue;
         const long tiles = tiles_of(shape, M, N, symmetric) * batch;
-        const int passes = cdiv(K, split ? 32 : 64);
+        const int passes = cdiv(K, kTerms[f]);
         for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices / 4 * 2) {
             if (slices > 1 && passes / slices < 4) break;
             if (slices > 1 && tiles * slices > 2048) break;
-            double us = product_us(shape, split, tiles, passes, slices);
-            if (slices > 1) us += 4.0 + 8e-6 / 2.5 * slices * tiles * kEdge[shape] * kEdge[shape];
+            double us = product_us(shape, f, tiles, passes, slices);
+            if (slices > 1) us += 4.0 + 8e-6 / 2.5 * slices * tiles * kRows[shape] * kColumns[shape];
             if (us < least) {
                 least = us;
                 best = Choice{shape, slices};
@@ -540,7 +539,7 @@ inline Choice choose(bool split, long M, long N, int batch, long K, bool symmetr
     return best;
 }
 // parts that a row's columns fall into, one to a wave
-inline long wave_columns(long N, int shape) { return (long)cdiv(N, kEdge[shape]) * wave_columns_of(shape); }
+inline long wave_columns(long N, int shape) { return (long)cdiv(N, kColumns[shape]) * kWaveColumns[shape]; }
 
 // Fills in the tiles; returns the workgroups (a multiple of the XCDs).
 template <class S> inline unsigned place_tiles(Params *p, bool symmetric, int slices, int pass)
@@ -567,8 +566,9 @@ hipError_t launch_shape(Params p, const typename Epi::Params &e, int slices, hip
 template <class P, Lay LA, Lay LB, class Epi>
 hipError_t launch(const Params &p, const typename Epi::Params &e, Choice c, hipStream_t st)
 {
-    if constexpr (P::kRaw) {
-        return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st); // (the only ones that are asked for)
+    if constexpr (P::kRaw) { // (the only ones that are asked for)
+        if (c.shape == kLow) return launch_shape<P, LA, LB, Low, Epi>(p, e, c.slices, st);
+        return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
     } else {
         if (c.shape == kBig) return launch_shape<P, LA, LB, Big, Epi>(p, e, c.slices, st);
         if constexpr (P::kParts == 2)

@@ -344,9 +344,9 @@ void plan_muon(const MuonGeom &g, MuonPlan *p)
     p->r = p->tall ? g.cols : g.rows;
     p->ld_x = (g.cols + 31) / 32 * 128;
     p->ld_a = (p->r + 31) / 32 * 128;
-    p->gram = choose(true, p->r, p->r, g.batch, p->tall ? g.rows : g.cols, true, 16);
-    p->poly = choose(true, p->r, p->r, g.batch, p->r, true, 1);
-    p->apply = choose(true, g.rows, g.cols, g.batch, p->r, false, 1);
+    p->gram = choose(kSplit, p->r, p->r, g.batch, p->tall ? g.rows : g.cols, true, 16);
+    p->poly = choose(kSplit, p->r, p->r, g.batch, p->r, true, 1);
+    p->apply = choose(kSplit, g.rows, g.cols, g.batch, p->r, false, 1);
     const long size = g.rows * g.cols;
     p->sum_blocks = (int)(size / 8192 < 1 ? 1 : size / 8192 > kMaxSumBlocks ? kMaxSumBlocks : size / 8192);
     size_t o = 0;
@@ -432,7 +432,7 @@ hipError_t launch_muon(const MuonGeom &g, const MuonPlan &p, const void *G, floa
                        : launch<Split, Lay::kAlong, Lay::kAlong, GramPart>(m, eg, p.gram, st);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL(join_gram_kernel, dim3(cdiv(p.r, 32), cdiv(p.r, 32), g.batch), dim3(256), 0, st, (const float *)part, (int)p.r, ld, g.batch,
-                               p.gram.slices, kEdge[p.gram.shape], a, p.ld_a, lift);
+                               p.gram.slices, kRows[p.gram.shape], a, p.ld_a, lift);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return e;

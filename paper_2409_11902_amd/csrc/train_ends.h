@@ -16,6 +16,7 @@ struct LossGeom {
 };
 struct LossPlan {
     bool split, raw;  // float: operands as two halves, or as they lie
+    bool odd;         // ... whose rows do not all start on 16 bytes
     bool direct;      // few rows: H is read where it lies, rows that do not count as zeros
     bool pack_w;      // the weights go through the workspace, piece by piece
     bool pair;        // backward: dW, dH and db in one launch
