@@ -587,7 +587,6 @@ template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x1
 // dW of a piece
 template <class K> struct OutW : Ending {
     typedef typename K::E T;
-    static constexpr bool kCountsK = true;
     struct Params { T *out; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -748,6 +747,132 @@ template <class K> __global__ void __launch_bounds__(256) bias_kernel(const Bias
     bias_sums(p, blockIdx.x, red);
 }
 
+// dW of few rows: a wave holds G of 32 classes in registers and passes over columns of H, which needs neither LDS nor a meeting; the
+// stores of dW are what takes time.  ROWS: T or more, a power of two.
+template <class K> struct Few {
+    typedef typename K::E T;
+    Meta meta;
+    const char *G;
+    const T *H;
+    long ld_g, ld_h;   // bytes, elements
+    int V, D;
+    T *out;
+    int runs, run;     // runs of columns that D is cut into; blocks of columns in one
+};
+// Columns of a block: a lane has one of float, two neighbours of bfloat16.
+template <class K> constexpr int kFewColumns = sizeof(typename K::E) == 4 ? 32 : 64;
+template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<K> &p, unsigned block)
+{
+    typedef typename K::E T;
+    constexpr bool kFloat = sizeof(T) == 4;
+    constexpr int kHave = ROWS < 32 ? ROWS / 2 : 16; // rows of H that a lane has at a time, and as many under way
+    const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+    const unsigned job = __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6));
+    const int v0 = __builtin_amdgcn_readfirstlane(job / p.runs) * 32, first = (int)(job % p.runs) * p.run * kFewColumns<K>;
+    if (v0 >= p.V) return;
+    const int last = min(p.D, first + p.run * kFewColumns<K>), rows = p.meta.T;
+    // the lane's k-th row of H and G: 2 k + half of float, 8 neighbours of every 16 for bfloat16
+    constexpr int kHalf = kFloat ? 1 : 8;
+    auto row = [&](int k) { return (kFloat ? 2 * k : k / 8 * 16 + k % 8) + half * kHalf; };
+    // rows that count, from the lane's first on
+    const uint64_t all = __ballot(lane < rows && p.meta.counts(lane)), mine64 = all >> (half * kHalf);
+    const uint32_t there[2] = {(uint32_t)mine64, (uint32_t)(mine64 >> 32)};
+    const bool whole = all == ~0ull >> (64 - ROWS);
+    auto counts = [&](int k) {
+        const int b = kFloat ? 2 * k : k / 8 * 16 + k % 8;
+        return (there[b / 32] >> b % 32 & 1) != 0;
+    };
+    const float scale = p.meta.largest(lane);
+    const int gv = min(v0 + c, (p.V + 7) / 8 * 8 - 1);
+    uint32_t g[kFloat ? ROWS / 2 : ROWS / 4], h[2][kHave];
+#pragma unroll
+    for (int k = 0; k < ROWS / 2; ++k) {
+        const char *r = p.G + min(row(k), rows - 1) * p.ld_g;
+        if (kFloat) {
+            g[k] = ((const uint32_t *)r)[gv];
+            g[k] = counts(k) ? g[k] : 0u;
+        } else {
+            uint32_t v = ((const uint16_t *)r)[gv];
+            v = counts(k) ? v : 0u;
+            if (k % 2) g[k / 2] |= v << 16;
+            else g[k / 2] = v;
+        }
+    }
+    const uint32_t ld = p.ld_h * sizeof(T), end = (rows - 1) * ld; // (bytes: 64 rows are less than 2^32)
+    auto read = [&](int b, int n0, int k0) {
+        uint32_t mine = row(0) * ld;
+        asm volatile("" : "+v"(mine)); // (the rows' places are worked out again: kept they take half of the registers)
+        const uint32_t n = min(n0 + c * (kFloat ? 1 : 2), p.D - (kFloat ? 1 : 2)) * sizeof(T);
+#pragma unroll
+        for (int k = 0; k < kHave; ++k) {
+            const uint32_t r = min(mine + (uint32_t)(row(k0 + k) - row(0)) * ld, end);
+            h[b][k] = *(const uint32_t *)((const char *)p.H + (r + n));
+        }
+    };
+    constexpr int kSets = kFloat ? 1 : 2; // (the even and the odd columns of bfloat16)
+    f32x16 acc[kSets];
+    auto multiply = [&](int b, int k0) {
+        if (k0 == 0)
+#pragma unroll
+            for (int s = 0; s < kSets; ++s)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[s][r] = 0.f;
+        if (!whole) // whatever stands in a row that does not count
+#pragma unroll
+            for (int k = 0; k < kHave; ++k) h[b][k] = counts(k0 + k) ? h[b][k] : 0u;
+        if constexpr (kFloat) {
+#pragma unroll
+            for (int k = 0; k < kHave; ++k) acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(g[k0 + k]), __uint_as_float(h[b][k]), acc[0], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kHave; k += 8) {
+                union { uint32_t u[4]; s16x8 v; } a, even, odd;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    a.u[e] = g[(k0 + k) / 2 + e];
+                    even.u[e] = __builtin_amdgcn_perm(h[b][k + 2 * e + 1], h[b][k + 2 * e], 0x05040100u);
+                    odd.u[e] = __builtin_amdgcn_perm(h[b][k + 2 * e + 1], h[b][k + 2 * e], 0x07060302u);
+                }
+                acc[0] = product<Bf16>(a.v, even.v, acc[0]);
+                acc[kSets - 1] = product<Bf16>(a.v, odd.v, acc[kSets - 1]);
+            }
+        }
+    };
+    auto write = [&](int n0) {
+        const int n = n0 + c * (kFloat ? 1 : 2);
+        T *o = p.out + (long)v0 * p.D + n;
+        if (n < p.D)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int v = r / 4 * 8 + half * 4 + r % 4;
+                if (v0 + v >= p.V) continue;
+                if constexpr (kFloat) o[v * p.D] = scale * acc[0][r];
+                else *(uint32_t *)(o + v * p.D) = f32x2_to_bf16x2(scale * acc[0][r], scale * acc[kSets - 1][r]);
+            }
+    };
+    constexpr int kCols = kFewColumns<K>;
+    read(0, first, 0);
+    if constexpr (ROWS > 32) {
+        for (int n0 = first; n0 < last; n0 += kCols) {
+            read(1, n0, kHave);
+            multiply(0, 0);
+            if (n0 + kCols < last) read(0, n0 + kCols, 0);
+            multiply(1, kHave);
+            write(n0);
+        }
+    } else {
+        for (int n0 = first; n0 < last; n0 += 2 * kCols) {
+            if (n0 + kCols < last) read(1, n0 + kCols, 0);
+            multiply(0, 0);
+            write(n0);
+            if (n0 + kCols >= last) break;
+            if (n0 + 2 * kCols < last) read(0, n0 + 2 * kCols, 0);
+            multiply(1, 0);
+            write(n0 + kCols);
+        }
+    }
+}
+
 // dW, dH and db of a piece in one launch: small products end sooner than a launch begins
 template <class K> struct PairParams {
     typedef typename K::E T;
@@ -755,9 +880,11 @@ template <class K> struct PairParams {
     typename OutW<K>::Params ew;
     typename OutH<K>::Params eh;
     Bias<K> b;
+    Few<K> few;
     unsigned blocks_w, blocks_h;
 };
-template <class K, class SH> __global__ void __launch_bounds__(Small::kThreads, SH::kPerSimd) pair_kernel(const PairParams<K> p)
+// SH: dH's tile.  ROWS: 0, or few rows' dW
+template <class K, class SH, int ROWS> __global__ void __launch_bounds__(Small::kThreads, SH::kPerSimd) pair_kernel(const PairParams<K> p)
 {
     static_assert(SH::kThreads == Small::kThreads, "one kernel");
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -768,8 +895,12 @@ template <class K, class SH> __global__ void __launch_bounds__(Small::kThreads, 
         return;
     }
     block -= p.blocks_h;
-    if (block < p.blocks_w) mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<K>>(p.w, p.ew, block, smem);
-    else bias_sums(p.b, block - p.blocks_w, (float(*)[64])smem);
+    if (block < p.blocks_w) {
+        if constexpr (ROWS > 0) few_rows<K, ROWS>(p.few, block);
+        else mm_tile<P, Lay::kDown, Lay::kDown, Small, OutW<K>>(p.w, p.ew, block, smem);
+    } else {
+        bias_sums(p.b, block - p.blocks_w, (float(*)[64])smem);
+    }
 }
 
 // a slice's part of the logits' products, [slice][T][ld]
@@ -913,7 +1044,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // end where compute units run out of work (512 x 512 x 1500 float 75 us apart, 61 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
     // 1024 x 2048 x 16000 341 and 379).
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
-    p->pair = backward && (p->raw || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
+    p->pair = backward && (p->direct || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
         p->h = choose(f, g.T, g.D, 1, piece, false, 128, true);
@@ -1006,14 +1137,36 @@ template <class K> class Loss {
     {
         return launch<P, Lay::kAlong, Lay::kAlong, Logits>(logits_params(n), {(float *)(ws + p.o_z), (int)g.T, (int)ld_logits()}, p.z, st);
     }
-    template <class SH> hipError_t launch_pair(PairParams<K> &q, bool want_h, int bias_blocks)
+    template <class SH, int ROWS> hipError_t launch_pair(PairParams<K> &q, bool want_h, int bias_blocks)
     {
         constexpr int lds = SH::kLds > Small::kLds ? SH::kLds : Small::kLds;
+        if (!q.ew.out) {
+            q.blocks_w = 0;
+        } else if (ROWS) {
+            const long blocks = cdiv(g.D, kFewColumns<K>), all = cdiv(q.few.V, 32) * blocks;
+            const long run = all / 4096 < 1 ? 1 : all / 4096 > 16 ? 16 : all / 4096;
+            q.few.run = (int)run;
+            q.few.runs = cdiv(blocks, run);
+            q.blocks_w = (unsigned)cdiv((long)cdiv(q.few.V, 32) * q.few.runs, 4);
+        } else {
+            q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
+        }
         if (want_h) q.blocks_h = place_tiles<SH>(&q.h, false, p.h.slices, kPass<P, SH::R>);
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<K, SH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        static const hipError_t attr =
+            hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<K, SH, ROWS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (attr != hipSuccess) return attr;
-        hipLaunchKernelGGL((pair_kernel<K, SH>), dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), lds, st, q);
+        hipLaunchKernelGGL((pair_kernel<K, SH, ROWS>), dim3(q.blocks_w + q.blocks_h + bias_blocks), dim3(Small::kThreads), lds, st, q);
         return hipGetLastError();
+    }
+    template <class SH> hipError_t launch_few(PairParams<K> &q, bool want_h, int bias_blocks)
+    {
+        constexpr bool any = !P::kRaw, low = SH::TM == 32; // (float: the low tile is that of 32 rows)
+        if constexpr (any || low) {
+            if (g.T <= 16) return launch_pair<SH, 16>(q, want_h, bias_blocks);
+            if (g.T <= 32) return launch_pair<SH, 32>(q, want_h, bias_blocks);
+        }
+        if constexpr (!low) return launch_pair<SH, 64>(q, want_h, bias_blocks);
+        return hipErrorInvalidValue;
     }
     hipError_t largest_magnitudes()
     {
@@ -1096,8 +1249,7 @@ public:
             q.w.N = (int)g.D;
             q.w.K = (int)g.T;
             q.w.batch = 1;
-            if (p.direct) q.w.counts_k = meta.counts;
-            else q.w.k_dev = meta.count;
+            q.w.k_dev = meta.count;
             q.ew = {dW ? dW + v0 * g.D : nullptr, meta};
             q.h.a = G;
             q.h.lda = ld_g;
@@ -1112,9 +1264,15 @@ public:
             q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr};
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
-                if (dW) q.blocks_w = place_tiles<Small>(&q.w, false, 1, kPass<P, Small::R>);
-                if constexpr (P::kRaw) e = p.h.shape == kLow ? launch_pair<Low>(q, dH, bias_blocks) : launch_pair<Small>(q, dH, bias_blocks);
-                else e = launch_pair<Small>(q, dH, bias_blocks);
+                if constexpr (K::kSplit) {
+                    e = launch_pair<Small, 0>(q, dH, bias_blocks);
+                } else if (!p.direct) {
+                    if constexpr (!P::kRaw) e = launch_pair<Small, 0>(q, dH, bias_blocks);
+                } else {
+                    q.few = {meta, G, H, ld_g, g.ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
+                    if constexpr (P::kRaw) e = p.h.shape == kLow ? launch_few<Low>(q, dH, bias_blocks) : launch_few<Small>(q, dH, bias_blocks);
+                    else e = launch_few<Small>(q, dH, bias_blocks);
+                }
             } else if constexpr (!P::kRaw) { // (floats as they lie are small products)
                 if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
                 if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);

@@ -70,7 +70,7 @@ struct Params {
     int batch, slices;         // matrices; parts that each sum is formed in
     int group;                 // tile rows that one XCD walks together
     int kt_slice;              // passes over K of one slice of the sum
-    Counts counts_m, counts_k; // where an ending says so, rows of a, terms of b that count: the others are zeros, whatever stands there
+    Counts counts_m;           // where an ending says so, rows of a that count: the others are zeros, whatever stands there
 };
 
 template <class P, int R> constexpr int kPass = R / 2 / P::kParts; // terms of the sum in one pass, R bytes of K to a row
@@ -107,11 +107,9 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
     uint32_t off[kLoads];
     int at;           // the lane's unit of a row in even loads (kAlong), its first row (kDown)
     int left;         // units (kAlong) or rows (kDown) of K from the pass to load next on
-    int row_k;        // kDown: the first row of K of the pass to load next
-    Counts counts;    // kDown: rows of K that count
 
     // first: first row of C; count: rows of C in the matrix; K: terms; kt: first pass, kt1: behind the last
-    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts_)
+    __device__ __forceinline__ void init(const char *p, long ld, int first, int count, int K, int kt, int kt1, int wave, int lane, const Counts &counts)
     {
         const int row0 = (wave * 64 + lane) / kUnits, slot = (wave * 64 + lane) % kUnits;
         const int columns = units<P>(count) - units<P>(first); // kDown: units from the tile's first on
@@ -123,8 +121,6 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
             step = R;
         } else {
             at = row0;
-            row_k = kt * kPass<P, R>;
-            counts = counts_;
             left = min(K, kt1 * kPass<P, R>) - kt * kPass<P, R>;
             base = p + (long)first * 2 * P::kParts + (long)kt * kPass<P, R> * ld;
             step = kPass<P, R> * ld;
@@ -133,7 +129,7 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
         for (int i = 0; i < kLoads; ++i) {
             const int row = row0 + i * kStep, c = slot ^ swizzle<P, L, T, R>(row) * kOf16;
             bool there = L == Lay::kAlong ? first + row < count : c < columns;
-            if (COUNTS && L == Lay::kAlong && there) there = counts_(first + row);
+            if (COUNTS && there) there = counts(first + row);
             off[i] = there ? (uint32_t)(row * (int)ld + c * kUnit) : kNowhere;
         }
     }
@@ -145,15 +141,12 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int here = L == Lay::kDown ? at + i * kStep : kStep == 8 && i % 2 ? at ^ 4 * kOf16 : at; // (8 rows on: four chunks apart)
-            uint32_t o = here < left ? off[i] : kNowhere;
-            if (COUNTS && L == Lay::kDown && counts.labels) // (few rows: looked up as they come)
-                if (o != kNowhere && !counts(row_k + at + i * kStep)) o = kNowhere;
+            const uint32_t o = here < left ? off[i] : kNowhere;
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 64 * kUnit);
             load_to_lds<kUnit>(rs, o, to);
         }
         base += step;
         left -= L == Lay::kAlong ? kUnits : kPass<P, R>;
-        if (COUNTS && L == Lay::kDown) row_k += kPass<P, R>;
     }
 };
 
@@ -222,7 +215,7 @@ __device__ __forceinline__ f32x4 as_floats(s16x8 v)
 }
 
 // What an ending may say about its product.
-struct Ending { static constexpr bool kSymmetric = false, kCountsM = false, kCountsK = false; };
+struct Ending { static constexpr bool kSymmetric = false, kCountsM = false; };
 
 // ---- a float as two halves.  x is fixed first: left to itself the compiler takes hi from a product's rounded value and lo from the
 // product, and where those lie on two sides of a half-precision number's middle, hi + lo is off by a unit of hi.
@@ -390,9 +383,9 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
     Stage<P, LA, TM, S::R, S::kWaves, Epi::kCountsM> sa;
-    Stage<P, LB, TN, S::R, S::kWaves, Epi::kCountsK> sb;
+    Stage<P, LB, TN, S::R, S::kWaves, false> sb;
     sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane, p.counts_m);
-    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane, p.counts_k);
+    sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane, p.counts_m);
     const int wm = wave / S::WN, wn = wave % S::WN;
     Frag<P, LA, TM, S::R> fa;
     Frag<P, LB, TN, S::R> fb;
