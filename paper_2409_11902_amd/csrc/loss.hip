@@ -8,6 +8,8 @@
 // Rows that are left out (label equal to ignore_index, or no class) are taken out of H when it is copied into the workspace: no
 // product reads them, whatever stands there, and the products get shorter by them.
 // Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float.
+// Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the rounding took away is kept as 32 further rows
+// of G: a tile has room for 64 rows, so that products of them cost nothing.
 #include "mm_core.h"
 #include "train_ends.h"
 
@@ -18,7 +20,7 @@ namespace {
 using namespace mm;
 
 // What the operands are, as they lie and as they are multiplied.
-struct OfBf16 { typedef bf16_t E; typedef Bf16 P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kBf16; };
+template <class B> struct OfBf16 { typedef bf16_t E; typedef B P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kBf16; }; // (Bf16, Bf16Odd)
 struct OfSplit { typedef float E; typedef Split P; static constexpr bool kSplit = true; static constexpr Fmt kG = Fmt::kSplit; };
 template <class R> struct OfRaw { typedef float E; typedef R P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kF32; }; // (Raw, RawOdd)
 
@@ -73,7 +75,8 @@ struct Meta {
     __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
     static constexpr int kOut = -(1 << 30);
 };
-constexpr int kDirectRows = 64, kRawRows = 64; // of bfloat16, of float
+constexpr int kFewRows = 64; // a wave looks them all up at once
+constexpr int kLoRow = 32;   // the row of G that the first row's rest is, where rests are kept
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
 inline Meta meta_at(char *p, long T)
@@ -314,7 +317,7 @@ template <class K> __device__ __forceinline__ void pack_rows(const PackRows &p, 
         for (int k = wave; k < min(64, last - r0); k += 4) {
             const int row = r0 + k;
             if (mask >> k & 1) {
-                const int jj = place + __popcll(mask & (((uint64_t)1 << k) - 1));
+                const int jj = p.meta.direct ? row : place + __popcll(mask & (((uint64_t)1 << k) - 1));
                 const T *h = (const T *)p.H + (long)row * p.ld_h;
                 char *o = p.out + (long)jj * p.row_bytes;
                 for (int n0 = 0; n0 < p.D; n0 += 512) {
@@ -512,6 +515,13 @@ template <class K> __device__ __forceinline__ void store_gradient(char *row, int
     }
 }
 
+// what rounding to bfloat16 takes away
+__device__ __forceinline__ float rest_of(float g)
+{
+    const float r = g - bf16_to_f32(f32_to_bf16(g));
+    return g - g == 0.f ? r : 0.f; // (an infinite or undefined one has none)
+}
+
 // backward: G of a piece
 template <class K> struct Grad : Ending {
     typedef typename K::E T;
@@ -522,6 +532,7 @@ template <class K> struct Grad : Ending {
         char *out;
         long ld;
         int v0;
+        bool rests;
     };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -536,24 +547,30 @@ template <class K> struct Grad : Ending {
             const int label = e.meta.label_of(m) - e.v0;
             const bool in = label > Meta::kOut / 2;
             const float q_row = e.meta.q_of(m, largest), lse = e.meta.lse_of(m);
+            auto fill = [&](bool rest) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j)
+                for (int j = 0; j < NI; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                    float bias[4], g[4];
-                    load_bias(e.b, n, p.N, bias);
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
+                        float bias[4], g[4];
+                        load_bias(e.b, n, p.N, bias);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
-                        const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
+                        for (int k = 0; k < 4; ++k) {
+                            const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
+                            const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
+                            g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
+                            if (rest) g[k] = rest_of(g[k]);
+                        }
+                        Block::put(p.lds, p.lane, j, q, g);
                     }
-                    Block::put(p.lds, p.lane, j, q, g);
-                }
-            Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
-                if (m0 + row < p.M && p.n0 + at / kIn16 * 8 < Np) *(u32x4 *)(e.out + (long)(m0 + row) * e.ld + p.n0 / 8 * kIn16 + at) = x;
-            });
+                char *out = e.out + (rest ? kLoRow * e.ld : 0);
+                Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
+                    if (m0 + row < p.M && p.n0 + at / kIn16 * 8 < Np) *(u32x4 *)(out + (long)(m0 + row) * e.ld + p.n0 / 8 * kIn16 + at) = x;
+                });
+            };
+            fill(false);
+            if (K::kG == Fmt::kBf16 && e.rests) fill(true);
         }
     }
 };
@@ -608,7 +625,7 @@ template <class K> struct OutW : Ending {
 // dH: the result, or sums of a slice (added to what the pieces before left)
 template <class K> struct OutH : Ending {
     typedef typename K::E T;
-    struct Params { T *out; float *sums; long slice_stride; int add; Meta meta; };
+    struct Params { T *out; float *sums; long slice_stride; int add; bool rests; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const float s = K::kSplit ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
@@ -618,10 +635,20 @@ template <class K> struct OutH : Ending {
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
             put_scaled<MI, NI>(acc, i, s, p);
+            const bool rests = K::kG == Fmt::kBf16 && e.rests; // (32 rows and their rests: neighbouring waves of one tile)
+            if (rests) {
+                __syncthreads();
+                if (m0 >= kLoRow) return;
+            }
             Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
                 const int m = m0 + row, n = p.n0 + at / 4;
-                if (m >= p.M || n >= p.N) return;
+                if (m >= (rests ? e.meta.T : p.M) || n >= p.N) return;
                 float v[4] = {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])};
+                if (rests) {
+                    const f32x4 r = *(const f32x4 *)(p.lds + p.lds_rows + row * Block::kPitch + at);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] += r[k];
+                }
                 if (!e.sums) {
                     store_four(e.out + (long)e.meta.row_of(m) * p.N + n, n, p.N, wide, v);
                     return;
@@ -697,19 +724,20 @@ template <class K> struct Bias {
     long ld;
     int V;
     T *db;
+    bool rests;
 };
 template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, int block, float (*red)[64])
 {
     typedef typename K::E T;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int count = p.meta.rows();
+    const int rows = p.meta.rows(), count = K::kG == Fmt::kBf16 && p.rests ? 2 * rows : rows;
     const float largest = p.meta.largest(lane);
     // 8 chunks of columns by 8 rows to a wave
     const int chunk = block * 8 + (lane & 7), n = chunk * 8;
     float s[8] = {};
     if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
-            const char *g = p.G + (long)m * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
+            const char *g = p.G + (long)(m < rows ? m : m - rows + kLoRow) * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
             if (K::kG == Fmt::kF32) {
                 const f32x4 lo = *(const f32x4 *)g, hi = *(const f32x4 *)(g + 16);
 #pragma unroll
@@ -754,7 +782,7 @@ template <class K> struct Few {
     Meta meta;
     const char *G;
     const T *H;
-    long ld_g, ld_h;   // bytes, elements
+    long ld_g, ld_h;   // bytes
     int V, D;
     T *out;
     int runs, run;     // runs of columns that D is cut into; blocks of columns in one
@@ -785,6 +813,8 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
     const float scale = p.meta.largest(lane);
     const int gv = min(v0 + c, (p.V + 7) / 8 * 8 - 1);
     uint32_t g[kFloat ? ROWS / 2 : ROWS / 4], h[2][kHave];
+    constexpr bool kRests = !kFloat && ROWS <= kLoRow;
+    uint32_t low[kRests ? ROWS / 4 : 1];
 #pragma unroll
     for (int k = 0; k < ROWS / 2; ++k) {
         const char *r = p.G + min(row(k), rows - 1) * p.ld_g;
@@ -796,13 +826,19 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
             v = counts(k) ? v : 0u;
             if (k % 2) g[k / 2] |= v << 16;
             else g[k / 2] = v;
+            if constexpr (kRests) {
+                v = ((const uint16_t *)(r + kLoRow * p.ld_g))[gv];
+                v = counts(k) ? v : 0u;
+                if (k % 2) low[k / 2] |= v << 16;
+                else low[k / 2] = v;
+            }
         }
     }
-    const uint32_t ld = p.ld_h * sizeof(T), end = (rows - 1) * ld; // (bytes: 64 rows are less than 2^32)
+    const uint32_t ld = p.ld_h, end = (rows - 1) * ld; // (bytes: 64 rows are less than 2^32)
     auto read = [&](int b, int n0, int k0) {
         uint32_t mine = row(0) * ld;
         asm volatile("" : "+v"(mine)); // (the rows' places are worked out again: kept they take half of the registers)
-        const uint32_t n = min(n0 + c * (kFloat ? 1 : 2), p.D - (kFloat ? 1 : 2)) * sizeof(T);
+        const uint32_t n = min(n0 + c * (kFloat ? 1 : 2), (p.D - 1) & (kFloat ? ~0 : ~1)) * sizeof(T);
 #pragma unroll
         for (int k = 0; k < kHave; ++k) {
             const uint32_t r = min(mine + (uint32_t)(row(k0 + k) - row(0)) * ld, end);
@@ -835,6 +871,12 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
                 }
                 acc[0] = product<Bf16>(a.v, even.v, acc[0]);
                 acc[kSets - 1] = product<Bf16>(a.v, odd.v, acc[kSets - 1]);
+                if constexpr (kRests) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a.u[e] = low[(k0 + k) / 2 + e];
+                    acc[0] = product<Bf16>(a.v, even.v, acc[0]);
+                    acc[kSets - 1] = product<Bf16>(a.v, odd.v, acc[kSets - 1]);
+                }
             }
         }
     };
@@ -847,7 +889,11 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
                 const int v = r / 4 * 8 + half * 4 + r % 4;
                 if (v0 + v >= p.V) continue;
                 if constexpr (kFloat) o[v * p.D] = scale * acc[0][r];
-                else *(uint32_t *)(o + v * p.D) = f32x2_to_bf16x2(scale * acc[0][r], scale * acc[kSets - 1][r]);
+                else if (p.D % 2 == 0) *(uint32_t *)(o + v * p.D) = f32x2_to_bf16x2(scale * acc[0][r], scale * acc[kSets - 1][r]);
+                else {
+                    o[v * p.D] = f32_to_bf16(scale * acc[0][r]);
+                    if (n + 1 < p.D) o[v * p.D + 1] = f32_to_bf16(scale * acc[kSets - 1][r]);
+                }
             }
     };
     constexpr int kCols = kFewColumns<K>;
@@ -987,7 +1033,7 @@ row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
 // G of a compact row, 1024 classes to a block
 template <class K> __global__ void __launch_bounds__(256)
 row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const typename K::E *__restrict__ b, int V,
-                char *__restrict__ G, long ld_g)
+                char *__restrict__ G, long ld_g, bool rests)
 {
     const int m = blockIdx.x, n = blockIdx.y * 1024 + threadIdx.x * 4;
     const float largest = meta.largest(threadIdx.x & 63);
@@ -1004,6 +1050,10 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
             if (n + e < V) g[e] = q * (__builtin_amdgcn_exp2f((z[e] - lse) * kLog2e) - (n + e == label ? 1.f : 0.f));
     }
     store_gradient<K>(G + (long)m * ld_g, n, g);
+    if (K::kG == Fmt::kBf16 && rests) {
+        const float r[4] = {rest_of(g[0]), rest_of(g[1]), rest_of(g[2]), rest_of(g[3])};
+        store_gradient<K>(G + (long)(m + kLoRow) * ld_g, n, r);
+    }
 }
 
 } // namespace
@@ -1014,11 +1064,14 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // find the largest numbers and split everything beforehand.  Both passes, packed beforehand and as they lie:
     //   bfloat16  1 x 512 x 1000  29 and 23 us    64 x 2048 x 8000  74 and 66 us
     //   float     64 x 64 x 512   37 and 31 us    16 x 1024 x 100000  961 and 570 us
-    p->raw = g.dtype == CAC_F32 && g.T <= kRawRows;
-    p->odd = p->raw && (g.D % 4 || g.ld_h % 4 || g.ld_w % 4);
+    const int in4 = g.dtype == CAC_F32 ? 1 : 2; // numbers in 4 bytes
+    p->few = g.T <= kFewRows;
+    p->direct = p->few && g.D % in4 == 0 && g.ld_h % in4 == 0 && g.ld_w % in4 == 0;
+    p->odd = p->direct && (g.D % (4 * in4) || g.ld_h % (4 * in4) || g.ld_w % (4 * in4));
+    p->raw = g.dtype == CAC_F32 && p->few;
+    p->rests = p->few && !p->raw && g.T <= kLoRow;
     p->split = g.dtype == CAC_F32 && !p->raw;
-    p->direct = p->raw || (g.dtype == CAC_BF16 && g.T <= kDirectRows && g.D % 8 == 0 && g.ld_h % 8 == 0);
-    p->pack_w = !p->raw && (p->split || g.D % 8 || g.ld_w % 8);
+    p->pack_w = !p->direct && (p->split || g.D % 8 || g.ld_w % 8);
     p->dp = (g.D + 7) / 8 * 8;
     const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
     p->row_bytes = e * p->dp;
@@ -1037,14 +1090,14 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // A sum over D in slices leaves its parts of the logits in the workspace (256 x 8192 x 2000 float forward: 107 us in one, 82 so).
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
     const Format f = p->raw ? kRaw : p->split ? kSplit : kBf16;
-    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw);
+    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw || p->odd);
     p->w = choose(f, piece, g.D, 1, g.T, false, 1);
     p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
     // end where compute units run out of work (512 x 512 x 1500 float 75 us apart, 61 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
     // 1024 x 2048 x 16000 341 and 379).
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
-    p->pair = backward && (p->direct || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
+    p->pair = backward && (p->few || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
     if (p->pair) {
         p->w = Choice{kSmall, 1};
         p->h = choose(f, g.T, g.D, 1, piece, false, 128, true);
@@ -1063,7 +1116,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->o_z = o;
     if (p->z.slices > 1) o += up256((size_t)logits * p->z.slices);
     p->o_g = o;
-    if (backward) o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * e);
+    if (backward) o += up256((size_t)(g.T + (p->rests ? kLoRow : 0)) * ((piece + 7) / 8 * 8) * e);
     p->o_acc = o;
     if (backward && (p->pieces > 1 || p->h.slices > 1)) o += up256((size_t)p->h.slices * g.T * g.D * 4);
     p->bytes = o;
@@ -1074,6 +1127,7 @@ namespace {
 template <class K> class Loss {
     typedef typename K::E T;
     typedef typename K::P P;
+    static constexpr bool kDirect = P::kRaw || P::kUnit == 4; // always few rows
     const LossGeom &g;
     const LossPlan &p;
     const T *H, *W, *b;
@@ -1092,7 +1146,7 @@ template <class K> class Loss {
         ld_h = p.direct ? g.ld_h * (long)sizeof(T) : p.row_bytes;
         w = p.pack_w ? (const void *)(ws + p.o_w) : W + v0 * g.ld_w;
         ld_w = p.pack_w ? p.row_bytes : g.ld_w * (long)sizeof(T);
-        if constexpr (P::kRaw) return hipSuccess; // (everything lies where it is)
+        if constexpr (kDirect) return hipSuccess; // (everything lies where it is)
         else return !pack_h && !p.pack_w ? hipSuccess : pack(v0, n, pack_h, rows);
     }
     hipError_t pack(long v0, long n, bool pack_h, PackRows *rows)
@@ -1128,7 +1182,7 @@ template <class K> class Loss {
         m.N = (int)n;
         m.K = (int)g.D;
         m.batch = 1;
-        if (p.direct) m.counts_m = meta.counts;
+        if (p.few) m.counts_m = meta.counts;
         else m.m_dev = meta.count;
         return m;
     }
@@ -1182,7 +1236,7 @@ public:
     Loss(const LossGeom &g_, const LossPlan &p_, const void *H_, const void *W_, const void *b_, const int64_t *labels, void *ws_, hipStream_t st_)
         : g(g_), p(p_), H((const T *)H_), W((const T *)W_), b((const T *)b_), ws((char *)ws_), st(st_), meta(meta_at((char *)ws_ + p_.o_meta, g_.T))
     {
-        meta.direct = p.direct;
+        meta.direct = p.few;
         meta.counts = Counts{labels, g.ignore, (int)g.V};
     }
 
@@ -1224,7 +1278,7 @@ public:
         PackRows rows{};
         rows.lse = lse;
         rows.gloss = gloss;
-        rows.dH = dH;
+        rows.dH = p.few ? nullptr : dH;
         char *G = ws + p.o_g;
         const long ld_g = (p.piece + 7) / 8 * 8 * (long)sizeof(T);
         float *sums = p.pieces > 1 || p.h.slices > 1 ? (float *)(ws + p.o_acc) : nullptr;
@@ -1234,10 +1288,10 @@ public:
             if (p.z.slices > 1) {
                 if ((e = logits_in_slices(n)) != hipSuccess) return e;
                 hipLaunchKernelGGL(row_grad_kernel<K>, dim3((unsigned)g.T, cdiv(g.V, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
-                                   g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g);
+                                   g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g, p.rests);
                 e = hipGetLastError();
             } else {
-                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<K>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0}, p.z, st);
+                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<K>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0, p.rests}, p.z, st);
             }
             if (e != hipSuccess) return e;
             PairParams<K> q{};
@@ -1255,25 +1309,25 @@ public:
             q.h.lda = ld_g;
             q.h.b = w;
             q.h.ldb = ld_w;
-            q.h.M = (int)g.T;
+            q.h.M = (int)g.T + (p.rests ? kLoRow : 0);
             q.h.N = (int)g.D;
             q.h.K = (int)n;
             q.h.batch = 1;
-            if (!p.direct) q.h.m_dev = meta.count;
-            q.eh = {dH, sums, g.T * g.D, v0 > 0, meta};
-            q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr};
+            if (!p.few) q.h.m_dev = meta.count;
+            q.eh = {dH, sums, g.T * g.D, v0 > 0, p.rests, meta};
+            q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr, p.rests};
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
                 if constexpr (K::kSplit) {
                     e = launch_pair<Small, 0>(q, dH, bias_blocks);
-                } else if (!p.direct) {
-                    if constexpr (!P::kRaw) e = launch_pair<Small, 0>(q, dH, bias_blocks);
+                } else if (!p.few) {
+                    if constexpr (!kDirect) e = launch_pair<Small, 0>(q, dH, bias_blocks);
                 } else {
-                    q.few = {meta, G, H, ld_g, g.ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
+                    q.few = {meta, G, (const T *)h, ld_g, ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
                     if constexpr (P::kRaw) e = p.h.shape == kLow ? launch_few<Low>(q, dH, bias_blocks) : launch_few<Small>(q, dH, bias_blocks);
                     else e = launch_few<Small>(q, dH, bias_blocks);
                 }
-            } else if constexpr (!P::kRaw) { // (floats as they lie are small products)
+            } else if constexpr (!kDirect) {
                 if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
                 if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);
                 if (db && e == hipSuccess) {
@@ -1303,19 +1357,21 @@ public:
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            float *loss, float *lse, void *ws, hipStream_t st)
 {
-    if (p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.raw && p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
     if (p.raw) return Loss<OfRaw<Raw>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
     if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
-    return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    if (p.odd) return Loss<OfBf16<Bf16Odd>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
+    return Loss<OfBf16<Bf16>>(g, p, H, W, b, labels, ws, st).forward(loss, lse);
 }
 
 hipError_t launch_loss_bwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,
                            const float *lse, const float *gloss, void *dH, void *dW, void *db, void *ws, hipStream_t st)
 {
-    if (p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
+    if (p.raw && p.odd) return Loss<OfRaw<RawOdd>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
     if (p.raw) return Loss<OfRaw<Raw>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
     if (p.split) return Loss<OfSplit>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (float *)dH, (float *)dW, (float *)db);
-    return Loss<OfBf16>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
+    if (p.odd) return Loss<OfBf16<Bf16Odd>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
+    return Loss<OfBf16<Bf16>>(g, p, H, W, b, labels, ws, st).backward(lse, gloss, (bf16_t *)dH, (bf16_t *)dW, (bf16_t *)db);
 }
 
 } // namespace cac

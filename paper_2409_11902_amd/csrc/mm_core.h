@@ -16,7 +16,7 @@
 //   Raw   : floats as they lie, by the float instruction.  It needs no powers of two and no pass beforehand, and is what products of few
 //           rows take, whose time is that of reading the other operand once.  A chunk holds 4 numbers, two of them the 8 that a
 //           chunk of hi and one of lo hold.
-//   RawOdd: the same of rows that do not start on 16 bytes: 4 bytes to a lane and load in the place of 16.
+//   Bf16Odd, RawOdd: the same of rows that start on 4 bytes and not on 16: 4 bytes to a lane and load in the place of 16.
 //
 // A workgroup of WM x WN waves owns a tile of C; a wave holds MI x NI accumulators of 32 x 32.  Tiles go from global memory straight
 // into one of two LDS buffers while the other is multiplied, and a step's fragments are read while the step before is multiplied: the
@@ -39,11 +39,15 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 enum class Lay { kAlong, kDown };
 struct Bf16 { static constexpr int kParts = 1, kUnit = 16; static constexpr bool kRaw = false; }; // (kUnit: bytes to a lane and load)
+struct Bf16Odd { static constexpr int kParts = 1, kUnit = 4; static constexpr bool kRaw = false; };
 struct Split { static constexpr int kParts = 2, kUnit = 16; static constexpr bool kRaw = false; };
 struct Raw { static constexpr int kParts = 2, kUnit = 16; static constexpr bool kRaw = true; };
 struct RawOdd { static constexpr int kParts = 2, kUnit = 4; static constexpr bool kRaw = true; };
-// units that n numbers of a row take: whole eights, of raw floats no more than there are
-template <class P> __host__ __device__ constexpr int units(int n) { return P::kRaw ? (n * 4 + P::kUnit - 1) / P::kUnit : P::kParts * ((n + 7) / 8); }
+// units that n numbers of a row take: whole eights where rows are padded to them, else no more than there are
+template <class P> __host__ __device__ constexpr int units(int n)
+{
+    return P::kRaw || P::kUnit == 4 ? (n * (P::kRaw ? 4 : 2) + P::kUnit - 1) / P::kUnit : P::kParts * ((n + 7) / 8);
+}
 
 constexpr uint32_t kNowhere = 0x80000000u; // an offset past every descriptor's range
 
@@ -320,6 +324,7 @@ struct Place {
     int tm, tn;         // the tile
     int part;           // the wave's place among the waves that share a row of C
     unsigned char *lds; // the wave's own, free at the end
+    int lds_rows;       // from there to that of the wave with the rows that follow
     int lane;
 };
 
@@ -464,6 +469,7 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
     at.part = tn * S::WN + wn;
     at.lane = lane;
     at.lds = smem + wave * (S::kLds / S::kWaves / 16 * 16);
+    at.lds_rows = S::WN * (S::kLds / S::kWaves / 16 * 16);
     Epi::template run<MI, NI>(e, acc, at);
 }
 
@@ -561,6 +567,8 @@ hipError_t launch(const Params &p, const typename Epi::Params &e, Choice c, hipS
 {
     if constexpr (P::kRaw) { // (the only ones that are asked for)
         if (c.shape == kLow) return launch_shape<P, LA, LB, Low, Epi>(p, e, c.slices, st);
+        return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
+    } else if constexpr (P::kUnit == 4) {
         return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
     } else {
         if (c.shape == kBig) return launch_shape<P, LA, LB, Big, Epi>(p, e, c.slices, st);

@@ -15,9 +15,11 @@ struct LossGeom {
     long ignore;
 };
 struct LossPlan {
-    bool split, raw;  // float: operands as two halves, or as they lie
-    bool odd;         // ... whose rows do not all start on 16 bytes
-    bool direct;      // few rows: H is read where it lies, rows that do not count as zeros
+    bool few;         // few rows: row m of the products is row m of H, zeros where it does not count
+    bool direct;      // ... and all is read where it lies
+    bool odd;         // ... which does not all start on 16 bytes
+    bool split, raw;  // float: operands as two halves, or (few rows) as they lie
+    bool rests;       // G's rounding errors are kept as rows of their own
     bool pack_w;      // the weights go through the workspace, piece by piece
     bool pair;        // backward: dW, dH and db in one launch
     long dp;          // features, in whole chunks of 8
