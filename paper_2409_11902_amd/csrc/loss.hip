@@ -547,30 +547,39 @@ template <class K> struct Grad : Ending {
             const int label = e.meta.label_of(m) - e.v0;
             const bool in = label > Meta::kOut / 2;
             const float q_row = e.meta.q_of(m, largest), lse = e.meta.lse_of(m);
-            auto fill = [&](bool rest) {
+            constexpr bool kRests = K::kG == Fmt::kBf16 && MI * NI == 1; // (few rows take the smallest tiles)
+            float kept[kRests ? 16 : 1];
 #pragma unroll
-                for (int j = 0; j < NI; ++j)
+            for (int j = 0; j < NI; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
-                        float bias[4], g[4];
-                        load_bias(e.b, n, p.N, bias);
+                for (int q = 0; q < 4; ++q) {
+                    const int n = p.n0 + j * 32 + q * 8 + (p.lane >> 5) * 4;
+                    float bias[4], g[4];
+                    load_bias(e.b, n, p.N, bias);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
-                            const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                            g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
-                            if (rest) g[k] = rest_of(g[k]);
-                        }
-                        Block::put(p.lds, p.lane, j, q, g);
+                    for (int k = 0; k < 4; ++k) {
+                        const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
+                        const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
+                        g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
+                        if constexpr (kRests) kept[q * 4 + k] = g[k];
                     }
-                char *out = e.out + (rest ? kLoRow * e.ld : 0);
+                    Block::put(p.lds, p.lane, j, q, g);
+                }
+            auto store = [&](char *out) {
                 Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
                     if (m0 + row < p.M && p.n0 + at / kIn16 * 8 < Np) *(u32x4 *)(out + (long)(m0 + row) * e.ld + p.n0 / 8 * kIn16 + at) = x;
                 });
             };
-            fill(false);
-            if (K::kG == Fmt::kBf16 && e.rests) fill(true);
+            store(e.out);
+            if constexpr (kRests) {
+                if (!e.rests) continue;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float r[4] = {rest_of(kept[q * 4]), rest_of(kept[q * 4 + 1]), rest_of(kept[q * 4 + 2]), rest_of(kept[q * 4 + 3])};
+                    Block::put(p.lds, p.lane, 0, q, r);
+                }
+                store(e.out + kLoRow * e.ld);
+            }
         }
     }
 };
@@ -1090,7 +1099,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // A sum over D in slices leaves its parts of the logits in the workspace (256 x 8192 x 2000 float forward: 107 us in one, 82 so).
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
     const Format f = p->raw ? kRaw : p->split ? kSplit : kBf16;
-    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw || p->odd);
+    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->few);
     p->w = choose(f, piece, g.D, 1, g.T, false, 1);
     p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
