@@ -104,7 +104,8 @@ __device__ __forceinline__ int wave_add(int v)
     return v;
 }
 
-// Largest finite magnitude of H (rows that count) and of W, a part from every block.
+// Largest finite magnitude of H (rows that count) and of W, a part from every block.  Bound by reading: 1531 x 1001 and 50257 x 1001
+// float, 207 MB, in 43 us (4.8 TB/s).
 __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, long ld_h, long T, const float *__restrict__ W, long ld_w, long V,
                                                   long D, const Counts counts, int blocks_h, float *__restrict__ top)
 {
@@ -253,7 +254,7 @@ template <class K> __device__ __forceinline__ void store8(char *row, int n, cons
 }
 
 // Rows that count, one behind the other, and what is known about them.  A block takes a run of rows; where they go follows from the
-// labels before them.
+// labels before them.  With the weights (below) 1531 x 1001 and 50257 x 1001 float in 78 us, 414 MB in and out (5.3 TB/s).
 template <class K> __device__ __forceinline__ void pack_rows(const PackRows &p, float *deal)
 {
     typedef typename K::E T;
@@ -443,7 +444,7 @@ template <class K> struct Stats : Ending {
     }
 };
 
-// lse and loss of a compact row from its parts: ROWS rows to a block, 256 / ROWS threads to a row
+// lse and loss of a compact row from its parts: ROWS rows to a block, 256 / ROWS threads to a row.  4096 rows of 500 parts in 8 us.
 template <int ROWS> __global__ void __launch_bounds__(256) join_kernel(const Meta meta, const float *__restrict__ part, int parts, long T_rows,
                                                                        float *__restrict__ loss, float *__restrict__ lse)
 {
@@ -785,7 +786,8 @@ template <class K> __global__ void __launch_bounds__(256) bias_kernel(const Bias
 }
 
 // dW of few rows: a wave holds G of 32 classes in registers and passes over columns of H, which needs neither LDS nor a meeting; the
-// stores of dW are what takes time.  ROWS: T or more, a power of two.
+// stores of dW are what takes time: with dH, which reads W, 16 x 1024 x 100000 in 162 us of float and 69 of bfloat16 (820 and 410 MB in
+// and out, 5.1 and 5.9 TB/s, some of it cached; as tiles of a product 324 and 169).  ROWS: T or more, a power of two.
 template <class K> struct Few {
     typedef typename K::E T;
     Meta meta;
