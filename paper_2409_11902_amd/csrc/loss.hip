@@ -75,7 +75,7 @@ struct Meta {
     __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
     static constexpr int kOut = -(1 << 30);
 };
-constexpr int kFewRows = 64; // a wave looks them all up at once
+constexpr int kFewRows = 64, kFewFloatRows = 128;
 constexpr int kLoRow = 32;   // the row of G that the first row's rest is, where rests are kept
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
@@ -813,10 +813,16 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
     // the lane's k-th row of H and G: 2 k + half of float, 8 neighbours of every 16 for bfloat16
     constexpr int kHalf = kFloat ? 1 : 8;
     auto row = [&](int k) { return (kFloat ? 2 * k : k / 8 * 16 + k % 8) + half * kHalf; };
-    // rows that count, from the lane's first on
-    const uint64_t all = __ballot(lane < rows && p.meta.counts(lane)), mine64 = all >> (half * kHalf);
-    const uint32_t there[2] = {(uint32_t)mine64, (uint32_t)(mine64 >> 32)};
-    const bool whole = all == ~0ull >> (64 - ROWS);
+    // rows that count, from the lane's first on (64 to a pair of words)
+    uint32_t there[4];
+    bool whole = true;
+#pragma unroll
+    for (int w = 0; w < (ROWS > 64 ? 2 : 1); ++w) {
+        const uint64_t all = __ballot(w * 64 + lane < rows && p.meta.counts(w * 64 + lane)), mine = all >> (half * kHalf);
+        there[2 * w] = (uint32_t)mine;
+        there[2 * w + 1] = (uint32_t)(mine >> 32);
+        whole = whole && all == ~0ull >> (ROWS < 64 ? 64 - ROWS : 0);
+    }
     auto counts = [&](int k) {
         const int b = kFloat ? 2 * k : k / 8 * 16 + k % 8;
         return (there[b / 32] >> b % 32 & 1) != 0;
@@ -845,7 +851,7 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
             }
         }
     }
-    const uint32_t ld = p.ld_h, end = (rows - 1) * ld; // (bytes: 64 rows are less than 2^32)
+    const uint32_t ld = p.ld_h, end = (rows - 1) * ld; // (bytes: 128 rows are less than 2^32)
     auto read = [&](int b, int n0, int k0) {
         uint32_t mine = row(0) * ld;
         asm volatile("" : "+v"(mine)); // (the rows' places are worked out again: kept they take half of the registers)
@@ -910,11 +916,14 @@ template <class K, int ROWS> __device__ __forceinline__ void few_rows(const Few<
     constexpr int kCols = kFewColumns<K>;
     read(0, first, 0);
     if constexpr (ROWS > 32) {
+        constexpr int kTimes = ROWS / 2 / kHave; // (even: a block ends with the registers that it began with)
         for (int n0 = first; n0 < last; n0 += kCols) {
-            read(1, n0, kHave);
-            multiply(0, 0);
-            if (n0 + kCols < last) read(0, n0 + kCols, 0);
-            multiply(1, kHave);
+#pragma unroll
+            for (int t = 0; t < kTimes; ++t) {
+                if (t + 1 < kTimes) read((t + 1) & 1, n0, (t + 1) * kHave);
+                else if (n0 + kCols < last) read(0, n0 + kCols, 0);
+                multiply(t & 1, t * kHave);
+            }
             write(n0);
         }
     } else {
@@ -1072,11 +1081,13 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 {
     // Few rows: everything is read where it lies.  With more of them the float instruction costs more than the passes that compact rows,
-    // find the largest numbers and split everything beforehand.  Both passes, packed beforehand and as they lie:
-    //   bfloat16  1 x 512 x 1000  29 and 23 us    64 x 2048 x 8000  74 and 66 us
-    //   float     64 x 64 x 512   37 and 31 us    16 x 1024 x 100000  961 and 570 us
+    // find the largest numbers and split everything beforehand.  Packed beforehand and as they lie, both passes:
+    //   bfloat16  16 x 256 x 300  28 and 23 us    64 x 700 x 5000  53 and 40 us    64 x 2048 x 30000  152 and 106 us
+    //   float     40 x 256 x 300  39 and 34 us    64 x 2048 x 600  52 and 38 us    64 x 2048 x 30000  564 and 365 us
+    //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  77 and 81 us   128 x 1001 x 20000  240 and 281 us
+    // and the forward pass of float alone: 128 x 2048 x 600  22 and 14 us, 128 x 2048 x 30000  234 and 151 us.
     const int in4 = g.dtype == CAC_F32 ? 1 : 2; // numbers in 4 bytes
-    p->few = g.T <= kFewRows;
+    p->few = g.T <= kFewRows || (g.dtype == CAC_F32 && g.T <= kFewFloatRows && (!backward || (double)g.D * g.V <= 2e6));
     p->direct = p->few && g.D % in4 == 0 && g.ld_h % in4 == 0 && g.ld_w % in4 == 0;
     p->odd = p->direct && (g.D % (4 * in4) || g.ld_h % (4 * in4) || g.ld_w % (4 * in4));
     p->raw = g.dtype == CAC_F32 && p->few;
@@ -1230,7 +1241,10 @@ template <class K> class Loss {
             if (g.T <= 16) return launch_pair<SH, 16>(q, want_h, bias_blocks);
             if (g.T <= 32) return launch_pair<SH, 32>(q, want_h, bias_blocks);
         }
-        if constexpr (!low) return launch_pair<SH, 64>(q, want_h, bias_blocks);
+        if constexpr (!low) {
+            if (g.T <= 64) return launch_pair<SH, 64>(q, want_h, bias_blocks);
+            if constexpr (P::kRaw) return launch_pair<SH, 128>(q, want_h, bias_blocks);
+        }
         return hipErrorInvalidValue;
     }
     hipError_t largest_magnitudes()
