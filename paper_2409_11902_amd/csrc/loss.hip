@@ -6,9 +6,10 @@
 //             and G is rounded once.
 //
 // Rows that are left out (label equal to ignore_index, or no class) are taken out of H when it is copied into the workspace: no
-// product reads them, whatever stands there, and the products get shorter by them.
-// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float.
-// Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the rounding took away is kept as 32 further rows
+// product reads them, whatever stands there, and the products get shorter by them.  Few rows stay where they are: those that are left
+// out are loaded as zeros.
+// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float, or
+// as floats where there are few rows.  Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the rounding took away is kept as 32 further rows
 // of G: a tile has room for 64 rows, so that products of them cost nothing.
 #include "mm_core.h"
 #include "train_ends.h"
@@ -75,7 +76,7 @@ struct Meta {
     __device__ __forceinline__ float q_of(int m, float largest) const { return direct ? (largest > 0.f ? gloss[m] / largest : gloss[m]) : q[m]; }
     static constexpr int kOut = -(1 << 30);
 };
-constexpr int kFewRows = 64, kFewFloatRows = 128;
+constexpr int kFewRows = 64, kFewFloatRows = 128; // (the plan says when)
 constexpr int kLoRow = 32;   // the row of G that the first row's rest is, where rests are kept
 __host__ __device__ inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 __host__ __device__ inline size_t meta_bytes(long T) { return 256 + up256(2 * kMaxParts * 4) + 5 * up256(4 * (size_t)T); }
@@ -1236,8 +1237,8 @@ template <class K> class Loss {
     }
     template <class SH> hipError_t launch_few(PairParams<K> &q, bool want_h, int bias_blocks)
     {
-        constexpr bool any = !P::kRaw, low = SH::TM == 32; // (float: the low tile is that of 32 rows)
-        if constexpr (any || low) {
+        constexpr bool low = SH::TM == 32; // (float: the tile of up to 32 rows, and of no more)
+        if constexpr (!P::kRaw || low) {
             if (g.T <= 16) return launch_pair<SH, 16>(q, want_h, bias_blocks);
             if (g.T <= 32) return launch_pair<SH, 32>(q, want_h, bias_blocks);
         }

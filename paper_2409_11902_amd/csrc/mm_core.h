@@ -4,7 +4,7 @@
 // A has M rows, B has N, and the sum runs over K.  Each operand comes in one of two layouts:
 //   kAlong: K runs along a row of memory (row index m or n)
 //   kDown : K is the row of memory (m or n runs along it); the transposing LDS read makes fragments of it
-// and in one of three number formats:
+// and in one of these number formats:
 //   Bf16  : bfloat16, one product
 //   Split : a float as the sum of two half-precision numbers, x = hi + lo.  hi holds 11 bits of the significand and lo the next
 //           12 (its sign is one of them): 2^-23 of x is lost.  hi hi + hi lo + lo hi leaves out lo lo, at most 2^-22 of a product and
@@ -340,7 +340,7 @@ typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256: power.  8192 x 131072
 typedef Shape<2, 6, 3, 1, 128, 3, 1> Wide;   // 192 x 192: as Big, where its tiles fill the compute units better.  4096 cubed, symmetric, Split 0.31
 typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128: what a compute unit takes in, 35 to 50 KB a us.  512 x 4608 x 512, three of them, Split 0.25
 typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64: latency.  A pass takes 0.27 us alone and 0.2 to 0.3 with two others beside it
-typedef Shape<1, 4, 1, 1, 128, 3, 2> Low;    // 32 x 128, for few rows of floats: reading b.  16 x 100000 x 1024 3.4 TB/s
+typedef Shape<1, 4, 1, 1, 128, 3, 2> Low;    // 32 x 128, for few rows of floats: reading b.  16 x 100000 x 1024 3.0 to 3.7 TB/s
 
 // All but the N youngest loads have arrived, the fragments asked for are in registers, and every wave of the workgroup says so.
 template <int N> __device__ __forceinline__ void meet()
