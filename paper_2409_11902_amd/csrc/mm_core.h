@@ -336,7 +336,7 @@ template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU> struc
 };
 // Measured, with what bounds them (a library's product of 8192 cubed reaches 1.23 PFLOP/s in bfloat16 and 1.33 in half precision on the same
 // card, 1.33 / 3 = 0.44 for three of them; bare matrix instructions 1.7):
-typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256: power.  8192 x 131072 x 4096 bfloat16 1.18 PFLOP/s; 4096 cubed Split 0.36
+typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256: power.  7373 x 131072 x 4096 bfloat16 1.07 PFLOP/s; 4096 cubed Split 0.36
 typedef Shape<2, 6, 3, 1, 128, 3, 1> Wide;   // 192 x 192: as Big, where its tiles fill the compute units better.  4096 cubed, symmetric, Split 0.31
 typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128: what a compute unit takes in, 35 to 50 KB a us.  512 x 4608 x 512, three of them, Split 0.25
 typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64: latency.  A pass takes 0.27 us alone and 0.2 to 0.3 with two others beside it
