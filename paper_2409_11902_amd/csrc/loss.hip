@@ -1087,8 +1087,11 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     //   float     40 x 256 x 300  39 and 34 us    64 x 2048 x 600  52 and 38 us    64 x 2048 x 30000  564 and 365 us
     //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  77 and 81 us   128 x 1001 x 20000  240 and 281 us
     // and the forward pass of float alone: 128 x 2048 x 600  22 and 14 us, 128 x 2048 x 30000  234 and 151 us.
+    // A short forward pass of bfloat16 saves the launch that packs, though rows that are left out are multiplied then (512 x 1024 x 8000
+    // 28 and 21 us, with half of them left out 26 and 21; 256 x 512 x 21841  28 and 25, 22 and 24).
     const int in4 = g.dtype == CAC_F32 ? 1 : 2; // numbers in 4 bytes
-    p->few = g.T <= kFewRows || (g.dtype == CAC_F32 && g.T <= kFewFloatRows && (!backward || (double)g.D * g.V <= 2e6));
+    p->few = g.T <= kFewRows || (g.dtype == CAC_F32 && g.T <= kFewFloatRows && (!backward || (double)g.D * g.V <= 2e6)) ||
+             (g.dtype == CAC_BF16 && !backward && g.D % 8 == 0 && g.ld_h % 8 == 0 && g.ld_w % 8 == 0 && (double)g.T * g.D * g.V <= 5e9);
     p->direct = p->few && g.D % in4 == 0 && g.ld_h % in4 == 0 && g.ld_w % in4 == 0;
     p->odd = p->direct && (g.D % (4 * in4) || g.ld_h % (4 * in4) || g.ld_w % (4 * in4));
     p->raw = g.dtype == CAC_F32 && p->few;
@@ -1113,7 +1116,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // A sum over D in slices leaves its parts of the logits in the workspace (256 x 8192 x 2000 float forward: 107 us in one, 82 so).
     const long logits = g.T * ((piece + 3) & ~3L) * 4;
     const Format f = p->raw ? kRaw : p->split ? kSplit : kBf16;
-    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->few);
+    p->z = choose(f, g.T, piece, 1, g.D, false, p->pieces > 1 ? 1 : 16, p->raw || g.T <= kFewRows);
     p->w = choose(f, piece, g.D, 1, g.T, false, 1);
     p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
