@@ -6,11 +6,11 @@
 //             and G is rounded once.
 //
 // Rows that are left out (label equal to ignore_index, or no class) are taken out of H when it is copied into the workspace: no
-// product reads them, whatever stands there, and the products get shorter by them.  Few rows stay where they are: those that are left
-// out are loaded as zeros.
-// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float, or
-// as floats where there are few rows.  Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the rounding took away is kept as 32 further rows
-// of G: a tile has room for 64 rows, so that products of them cost nothing.
+// product reads them, whatever stands there, and the products get shorter by them.  Few rows, and short forward passes, stay where
+// they are: rows that are left out are loaded as zeros.
+// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float,
+// or as floats where there are few rows.  Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the
+// rounding took away is kept as 32 further rows of G: a tile has room for 64 rows, so that products of them cost nothing.
 #include "mm_core.h"
 #include "train_ends.h"
 
@@ -1081,17 +1081,20 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
 
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
 {
-    // Few rows: everything is read where it lies.  With more of them the float instruction costs more than the passes that compact rows,
-    // find the largest numbers and split everything beforehand.  Packed beforehand and as they lie, both passes:
+    // Few rows (and short forward passes): everything is read where it lies.  With more of them the float instruction costs more than the
+    // passes that compact rows, find the largest numbers and split everything beforehand.  Packed beforehand and as they lie, both passes:
     //   bfloat16  16 x 256 x 300  28 and 23 us    64 x 700 x 5000  53 and 40 us    64 x 2048 x 30000  152 and 106 us
     //   float     40 x 256 x 300  39 and 34 us    64 x 2048 x 600  52 and 38 us    64 x 2048 x 30000  564 and 365 us
     //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  77 and 81 us   128 x 1001 x 20000  240 and 281 us
-    // and the forward pass of float alone: 128 x 2048 x 600  22 and 14 us, 128 x 2048 x 30000  234 and 151 us.
-    // A short forward pass of bfloat16 saves the launch that packs, though rows that are left out are multiplied then (512 x 1024 x 8000
+    // Forward passes of float read a large operand once so, where the other has few rows, and small ones save two launches: 128 x 2048 x
+    // 30000  234 and 151 us, 12000 x 4000 x 64  193 and 88, 300 x 256 x 300  18 and 13, 1000 x 512 x 1000  25 and 19, 2000 x 1000 x 1000  44 and 47.
+    // Short ones of bfloat16 save the launch that packs, though rows that are left out are multiplied then (512 x 1024 x 8000
     // 28 and 21 us, with half of them left out 26 and 21; 256 x 512 x 21841  28 and 25, 22 and 24).
+    const double volume = (double)g.T * g.D * g.V;
     const int in4 = g.dtype == CAC_F32 ? 1 : 2; // numbers in 4 bytes
-    p->few = g.T <= kFewRows || (g.dtype == CAC_F32 && g.T <= kFewFloatRows && (!backward || (double)g.D * g.V <= 2e6)) ||
-             (g.dtype == CAC_BF16 && !backward && g.D % 8 == 0 && g.ld_h % 8 == 0 && g.ld_w % 8 == 0 && (double)g.T * g.D * g.V <= 5e9);
+    if (backward) p->few = g.T <= kFewRows || (g.dtype == CAC_F32 && g.T <= kFewFloatRows && (double)g.D * g.V <= 2e6);
+    else if (g.dtype == CAC_F32) p->few = g.T <= kFewFloatRows || g.V <= kFewFloatRows || volume <= 1e9;
+    else p->few = g.T <= kFewRows || (volume <= 5e9 && g.D % 8 == 0 && g.ld_h % 8 == 0 && g.ld_w % 8 == 0);
     p->direct = p->few && g.D % in4 == 0 && g.ld_h % in4 == 0 && g.ld_w % in4 == 0;
     p->odd = p->direct && (g.D % (4 * in4) || g.ld_h % (4 * in4) || g.ld_w % (4 * in4));
     p->raw = g.dtype == CAC_F32 && p->few;

@@ -15,7 +15,7 @@ struct LossGeom {
     long ignore;
 };
 struct LossPlan {
-    bool few;         // few rows: row m of the products is row m of H, zeros where it does not count
+    bool few;         // few rows, short forward passes: row m of the products is row m of H, zeros where it does not count
     bool direct;      // ... and all is read where it lies
     bool odd;         // ... which does not all start on 16 bytes
     bool split, raw;  // float: operands as two halves, or (few rows) as they lie

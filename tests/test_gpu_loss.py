@@ -128,7 +128,7 @@ def test_classes_in_pieces(dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("T", [1, 15, 17, 31, 33, 48, 64, 65, 100, 127, 128])
+@pytest.mark.parametrize("T", [1, 15, 17, 31, 33, 48, 64, 65, 100, 127, 128, 300])
 @pytest.mark.parametrize("D,ld_h,ld_w", [(96, 0, 0), (98, 0, 0), (99, 0, 0), (96, 98, 100), (130, 131, 0), (128, 0, 129), (1, 0, 0), (2, 3, 4), (514, 516, 520)])
 def test_few_rows_of_any_stride(T, D, ld_h, ld_w, dtype):
     t = make(T, D, 333, dtype, bias=D % 2, out=0.3 if T > 15 else 0.0, seed=T + D, ld_h=ld_h, ld_w=ld_w)
