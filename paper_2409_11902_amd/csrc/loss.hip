@@ -600,14 +600,16 @@ template <typename T> __device__ __forceinline__ void store_four(T *o, int n, in
         if (n + k < N) Elem<T>::store(o + k, v[k]);
 }
 
-// 32 rows of a product, times s, into a wave's LDS
-template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x16 (&acc)[MI][NI], int i, float s, const Place &p)
+// 32 rows of a product, times s, into a wave's LDS; zeros where the lane's row is left out
+template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x16 (&acc)[MI][NI], int i, float s, const Place &p, bool out = false)
 {
 #pragma unroll
     for (int j = 0; j < NI; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float v[4] = {s * acc[i][j][q * 4], s * acc[i][j][q * 4 + 1], s * acc[i][j][q * 4 + 2], s * acc[i][j][q * 4 + 3]};
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = out ? 0.f : s * acc[i][j][q * 4 + k];
             RowBlock<Fmt::kF32, NI>::put(p.lds, p.lane, j, q, v);
         }
 }
@@ -645,8 +647,10 @@ template <class K> struct OutH : Ending {
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
-            put_scaled<MI, NI>(acc, i, s, p);
             const bool rests = K::kG == Fmt::kBf16 && e.rests; // (32 rows and their rests: neighbouring waves of one tile)
+            // a row that is left out has zeros in G where nothing is compacted, and a zero times an infinite weight is none
+            const int m = m0 + (p.lane & 31), row = rests && m >= kLoRow ? m - kLoRow : m;
+            put_scaled<MI, NI>(acc, i, s, p, e.meta.direct && row < e.meta.T && e.meta.label_of(row) == Meta::kOut);
             if (rests) {
                 __syncthreads();
                 if (m0 >= kLoRow) return;
