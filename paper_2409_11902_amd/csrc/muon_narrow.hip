@@ -17,6 +17,8 @@ using namespace mm;
 
 constexpr float kA = kNsA, kB = kNsB, kC = kNsC, kTake = kNsTake, kStore = kNsStore;
 constexpr int kSide = 64, kSquare = kSide * 256;       // bytes of a square matrix in LDS
+// The power of two of columns that hold zeros alone, above every other's (which are 12 + 148 at most): the smallest is what all slices are brought to.
+constexpr int kNone = 256;
 
 struct Args {
     const void *G;
@@ -234,6 +236,8 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
         if (top > 0.f) {
             frexpf(top, &e_mine);
             e_mine = 12 - e_mine; // the largest is stored as one below 2^12
+        } else {
+            e_mine = kNone;
         }
 #pragma unroll 1
         for (int c = 0; c < kOwn; ++c) {
