@@ -293,7 +293,8 @@ int cac_grad_cosine(const cac_desc *d, const void *dW_a, const void *dW_b, void 
  *     2^-28 of their matrix's largest keep fewer.  An infinity or NaN in H or W comes out as NaN in every row and
  *     gradient that it meets.  Few rows, and short forward passes, are multiplied as floats.  dtype CAC_BF16: the logits' gradients are rounded
  *     to bfloat16 (times the row's gradient over the largest row's) before they are multiplied with H and W, of up to 32
- *     rows to two such numbers.  Sums are float in both; loss, lse and gloss are float. */
+ *     rows to two such numbers.  Sums are float in both; loss, lse and gloss are float.
+ * What is written shares no memory with anything else that a call is given, but for dH, which may take the place of dense H. */
 typedef enum cac_loss_op { CAC_LOSS_FWD = 0, CAC_LOSS_BWD = 1 } cac_loss_op;
 
 typedef struct cac_loss_desc {

@@ -98,7 +98,7 @@ int check_ptr(const void *p, const char *name)
     return CAC_OK;
 }
 
-static bool share_memory(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+bool share_memory(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
 {
     return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }

@@ -8,6 +8,7 @@ namespace cac {
 int fail(int code, const char *fmt, ...);
 int check_ptr(const void *p, const char *name);
 int check_ws(size_t need, const void *ws, size_t ws_bytes);
+bool share_memory(const void *a, size_t a_bytes, const void *b, size_t b_bytes);
 int launched(hipError_t e, const char *what);
 
 } // namespace cac

@@ -12,6 +12,25 @@ static const char *tile_name(const TileChoice &c)
     return names[c.shape];
 }
 
+// A call's buffers: the first `outputs` are written, the others are read or are workspace.  No output may share memory with another
+// buffer (null ones are left out).
+struct Buffer {
+    const void *p;
+    size_t bytes;
+    const char *name;
+};
+static int check_apart(const Buffer *b, int outputs, int all)
+{
+    for (int i = 0; i < outputs; ++i)
+        for (int k = i + 1; k < all; ++k)
+            if (b[i].p && b[k].p && share_memory(b[i].p, b[i].bytes, b[k].p, b[k].bytes))
+                return fail(CAC_ERR_INVALID_ARG, "%s shares memory with %s", b[i].name, b[k].name);
+    return CAC_OK;
+}
+
+// from the first number of a matrix to behind its last
+static size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
+
 static int make_loss_geom(const cac_loss_desc *d, LossGeom *g)
 {
     if (!d) return fail(CAC_ERR_INVALID_ARG, "descriptor is NULL");
@@ -106,6 +125,11 @@ int cac_loss_fwd(const cac_loss_desc *d, const void *H, const void *W, const voi
     LossPlan p;
     plan_loss(g, false, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
+    const size_t e = g.dtype == CAC_F32 ? 4 : 2;
+    const Buffer buffers[] = {{loss, 4 * (size_t)g.T, "loss"}, {lse, 4 * (size_t)g.T, "lse"}, {H, rows_bytes(g.T, g.D, g.ld_h, e), "H"},
+                              {W, rows_bytes(g.V, g.D, g.ld_w, e), "W"}, {g.bias ? b : nullptr, g.V * e, "b"}, {labels, 8 * (size_t)g.T, "labels"},
+                              {ws, p.bytes, "the workspace"}};
+    if ((rc = check_apart(buffers, 2, 7))) return rc;
     return launched(launch_loss_fwd(g, p, H, W, g.bias ? b : nullptr, labels, loss, lse, ws, (hipStream_t)stream), "cross entropy");
 }
 
@@ -124,6 +148,13 @@ int cac_loss_bwd(const cac_loss_desc *d, const void *H, const void *W, const voi
     LossPlan p;
     plan_loss(g, true, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
+    const size_t e = g.dtype == CAC_F32 ? 4 : 2;
+    const bool in_place = dH == H && g.ld_h == g.D;
+    const Buffer buffers[] = {{dH, g.T * g.D * e, "dH"}, {dW, g.V * g.D * e, "dW"}, {db, g.V * e, "db"},
+                              {in_place ? nullptr : H, rows_bytes(g.T, g.D, g.ld_h, e), "H"}, {W, rows_bytes(g.V, g.D, g.ld_w, e), "W"},
+                              {g.bias ? b : nullptr, g.V * e, "b"}, {labels, 8 * (size_t)g.T, "labels"}, {lse, 4 * (size_t)g.T, "lse"},
+                              {gloss, 4 * (size_t)g.T, "gloss"}, {ws, p.bytes, "the workspace"}};
+    if ((rc = check_apart(buffers, 3, 10))) return rc;
     return launched(launch_loss_bwd(g, p, H, W, g.bias ? b : nullptr, labels, lse, gloss, dH, dW, db, ws, (hipStream_t)stream),
                     "cross entropy backward");
 }

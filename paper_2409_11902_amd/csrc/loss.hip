@@ -1258,6 +1258,18 @@ template <class K> class Loss {
         }
         return hipErrorInvalidValue;
     }
+    hipError_t launch_together(PairParams<K> &q, bool want_h, int bias_blocks)
+    {
+        if constexpr (K::kSplit) {
+            return launch_pair<Small, 0>(q, want_h, bias_blocks);
+        } else {
+            if constexpr (!kDirect)
+                if (!p.few) return launch_pair<Small, 0>(q, want_h, bias_blocks);
+            if constexpr (P::kRaw)
+                if (p.h.shape == kLow) return launch_few<Low>(q, want_h, bias_blocks);
+            return launch_few<Small>(q, want_h, bias_blocks);
+        }
+    }
     hipError_t largest_magnitudes()
     {
         if (!p.split) return hipSuccess;
@@ -1354,14 +1366,14 @@ public:
             q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr, p.rests};
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
-                if constexpr (K::kSplit) {
-                    e = launch_pair<Small, 0>(q, dH, bias_blocks);
-                } else if (!p.few) {
-                    if constexpr (!kDirect) e = launch_pair<Small, 0>(q, dH, bias_blocks);
+                q.few = {meta, G, (const T *)h, ld_g, ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
+                // dH may take the place of H; where H is read as it lies dW has to be done with it by then
+                if (p.direct && (const T *)dH == H && (dW || db)) {
+                    e = launch_together(q, false, bias_blocks);
+                    q.ew.out = nullptr;
+                    if (e == hipSuccess) e = launch_together(q, true, 0);
                 } else {
-                    q.few = {meta, G, (const T *)h, ld_g, ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
-                    if constexpr (P::kRaw) e = p.h.shape == kLow ? launch_few<Low>(q, dH, bias_blocks) : launch_few<Small>(q, dH, bias_blocks);
-                    else e = launch_few<Small>(q, dH, bias_blocks);
+                    e = launch_together(q, dH, bias_blocks);
                 }
             } else if constexpr (!kDirect) {
                 if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
