@@ -340,12 +340,12 @@ typedef struct cac_muon_desc {
 int cac_muon_workspace_size(const cac_muon_desc *d, int op, size_t *bytes);
 int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf_len);
 
-/* O = the orthogonalised G.  O may be G where their types are the same. */
+/* O = the orthogonalised G.  O may be G where their types are the same, and shares no memory with anything else of the call. */
 int cac_orthogonalise(const cac_muon_desc *d, const void *G, void *O, void *ws, size_t ws_bytes, void *stream);
 
 /* The optimiser's step, in place:  M <- momentum * M + G,  U = G + momentum * M (U = M without nesterov),
  * W <- keep * W - lr * orthogonalised U.  M is float; keep is 1 - lr * weight decay, and lr takes any factor for the
- * matrix's shape with it. */
+ * matrix's shape with it.  M and W share no memory with G, the workspace or each other. */
 int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, float momentum, float keep, float lr, void *ws,
                   size_t ws_bytes, void *stream);
 

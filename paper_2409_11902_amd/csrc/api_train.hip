@@ -13,7 +13,7 @@ static const char *tile_name(const TileChoice &c)
 }
 
 // A call's buffers: the first `outputs` are written, the others are read or are workspace.  No output may share memory with another
-// buffer (null ones are left out).
+// buffer (null and empty ones are left out).
 struct Buffer {
     const void *p;
     size_t bytes;
@@ -23,11 +23,12 @@ static int check_apart(const Buffer *b, int outputs, int all)
 {
     for (int i = 0; i < outputs; ++i)
         for (int k = i + 1; k < all; ++k)
-            if (b[i].p && b[k].p && share_memory(b[i].p, b[i].bytes, b[k].p, b[k].bytes))
+            if (b[i].p && b[k].p && b[k].bytes && share_memory(b[i].p, b[i].bytes, b[k].p, b[k].bytes))
                 return fail(CAC_ERR_INVALID_ARG, "%s shares memory with %s", b[i].name, b[k].name);
     return CAC_OK;
 }
 
+static size_t bytes_of(int dtype) { return dtype == CAC_F32 ? 4 : 2; }
 // from the first number of a matrix to behind its last
 static size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
 
@@ -125,7 +126,7 @@ int cac_loss_fwd(const cac_loss_desc *d, const void *H, const void *W, const voi
     LossPlan p;
     plan_loss(g, false, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
-    const size_t e = g.dtype == CAC_F32 ? 4 : 2;
+    const size_t e = bytes_of(g.dtype);
     const Buffer buffers[] = {{loss, 4 * (size_t)g.T, "loss"}, {lse, 4 * (size_t)g.T, "lse"}, {H, rows_bytes(g.T, g.D, g.ld_h, e), "H"},
                               {W, rows_bytes(g.V, g.D, g.ld_w, e), "W"}, {g.bias ? b : nullptr, g.V * e, "b"}, {labels, 8 * (size_t)g.T, "labels"},
                               {ws, p.bytes, "the workspace"}};
@@ -148,7 +149,7 @@ int cac_loss_bwd(const cac_loss_desc *d, const void *H, const void *W, const voi
     LossPlan p;
     plan_loss(g, true, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
-    const size_t e = g.dtype == CAC_F32 ? 4 : 2;
+    const size_t e = bytes_of(g.dtype);
     const bool in_place = dH == H && g.ld_h == g.D;
     const Buffer buffers[] = {{dH, g.T * g.D * e, "dH"}, {dW, g.V * g.D * e, "dW"}, {db, g.V * e, "db"},
                               {in_place ? nullptr : H, rows_bytes(g.T, g.D, g.ld_h, e), "H"}, {W, rows_bytes(g.V, g.D, g.ld_w, e), "W"},
@@ -198,6 +199,10 @@ int cac_orthogonalise(const cac_muon_desc *d, const void *G, void *O, void *ws, 
     MuonPlan p;
     plan_muon(g, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
+    const size_t n = (size_t)g.batch * g.rows * g.cols;
+    const bool in_place = O == G && g.dtype == g.grad_dtype;
+    const Buffer buffers[] = {{O, n * bytes_of(g.dtype), "O"}, {in_place ? nullptr : G, n * bytes_of(g.grad_dtype), "G"}, {ws, p.bytes, "the workspace"}};
+    if ((rc = check_apart(buffers, 1, 3))) return rc;
     return launched(launch_muon(g, p, G, nullptr, nullptr, O, 0.f, 0.f, 0.f, ws, (hipStream_t)stream), "orthogonalise");
 }
 
@@ -211,6 +216,9 @@ int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, floa
     MuonPlan p;
     plan_muon(g, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
+    const size_t n = (size_t)g.batch * g.rows * g.cols;
+    const Buffer buffers[] = {{M, n * 4, "M"}, {W, n * bytes_of(g.dtype), "W"}, {G, n * bytes_of(g.grad_dtype), "G"}, {ws, p.bytes, "the workspace"}};
+    if ((rc = check_apart(buffers, 2, 4))) return rc;
     return launched(launch_muon(g, p, G, M, W, nullptr, momentum, keep, lr, ws, (hipStream_t)stream), "momentum and orthogonalised update");
 }
 
