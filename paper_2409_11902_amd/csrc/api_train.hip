@@ -55,7 +55,7 @@ static int make_loss_geom(const cac_loss_desc *d, LossGeom *g)
     return CAC_OK;
 }
 
-static int make_muon_geom(const cac_muon_desc *d, MuonGeom *g)
+static int make_muon_geom(const cac_muon_desc *d, MuonGeom *g, MuonPlan *p)
 {
     if (!d) return fail(CAC_ERR_INVALID_ARG, "descriptor is NULL");
     if (d->size != sizeof(cac_muon_desc))
@@ -73,8 +73,8 @@ static int make_muon_geom(const cac_muon_desc *d, MuonGeom *g)
     g->dtype = d->dtype;
     g->grad_dtype = d->grad_dtype;
     g->nesterov = d->nesterov != 0;
-    const long tiles = ((g->rows + 63) / 64) * ((g->cols + 63) / 64);
-    if (tiles * g->batch >= 1L << 30) return fail(CAC_ERR_UNSUPPORTED, "batch of matrices too large for one grid");
+    plan_muon(*g, p);
+    if (!p->fits) return fail(CAC_ERR_UNSUPPORTED, "batch of matrices too large for one grid");
     return CAC_OK;
 }
 
@@ -163,12 +163,11 @@ int cac_loss_bwd(const cac_loss_desc *d, const void *H, const void *W, const voi
 int cac_muon_workspace_size(const cac_muon_desc *d, int op, size_t *bytes)
 {
     MuonGeom g;
-    int rc = make_muon_geom(d, &g);
+    MuonPlan p;
+    int rc = make_muon_geom(d, &g, &p);
     if (rc) return rc;
     if (op != CAC_MUON_ORTHOGONALISE && op != CAC_MUON_STEP) return fail(CAC_ERR_INVALID_ARG, "unknown op %d", op);
     if (!bytes) return fail(CAC_ERR_INVALID_ARG, "bytes is NULL");
-    MuonPlan p;
-    plan_muon(g, &p);
     *bytes = p.bytes;
     return CAC_OK;
 }
@@ -176,12 +175,11 @@ int cac_muon_workspace_size(const cac_muon_desc *d, int op, size_t *bytes)
 int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf_len)
 {
     MuonGeom g;
-    int rc = make_muon_geom(d, &g);
+    MuonPlan p;
+    int rc = make_muon_geom(d, &g, &p);
     if (rc) return rc;
     if (op != CAC_MUON_ORTHOGONALISE && op != CAC_MUON_STEP) return fail(CAC_ERR_INVALID_ARG, "unknown op %d", op);
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
-    MuonPlan p;
-    plan_muon(g, &p);
     if (p.narrow)
         snprintf(buf, buf_len, "narrow: %d workgroups of %d columns, %d launches", p.np.slices, p.np.width, p.np.slices == 1 ? 1 : g.steps + 1);
     else
@@ -193,11 +191,10 @@ int cac_muon_describe_plan(const cac_muon_desc *d, int op, char *buf, size_t buf
 int cac_orthogonalise(const cac_muon_desc *d, const void *G, void *O, void *ws, size_t ws_bytes, void *stream)
 {
     MuonGeom g;
-    int rc = make_muon_geom(d, &g);
+    MuonPlan p;
+    int rc = make_muon_geom(d, &g, &p);
     if (rc) return rc;
     if ((rc = check_ptr(G, "G")) || (rc = check_ptr(O, "O"))) return rc;
-    MuonPlan p;
-    plan_muon(g, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
     const size_t n = (size_t)g.batch * g.rows * g.cols;
     const bool in_place = O == G && g.dtype == g.grad_dtype;
@@ -210,11 +207,10 @@ int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, floa
                   void *stream)
 {
     MuonGeom g;
-    int rc = make_muon_geom(d, &g);
+    MuonPlan p;
+    int rc = make_muon_geom(d, &g, &p);
     if (rc) return rc;
     if ((rc = check_ptr(G, "G")) || (rc = check_ptr(M, "M")) || (rc = check_ptr(W, "W"))) return rc;
-    MuonPlan p;
-    plan_muon(g, &p);
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
     const size_t n = (size_t)g.batch * g.rows * g.cols;
     const Buffer buffers[] = {{M, n * 4, "M"}, {W, n * bytes_of(g.dtype), "W"}, {G, n * bytes_of(g.grad_dtype), "G"}, {ws, p.bytes, "the workspace"}};

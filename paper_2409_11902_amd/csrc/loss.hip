@@ -1116,6 +1116,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     if (piece < 4096) piece = 4096;
     if (piece > 1L << 19) piece = 1L << 19;
     if (piece >= g.V) piece = g.V;
+    while (!fits_grid(kBig, tiles_of(kBig, g.T, piece, false))) piece /= 2; // (millions of rows)
     p->pieces = (int)((g.V + piece - 1) / piece);
     if (p->pieces > 1) piece = ((g.V + p->pieces - 1) / p->pieces + 255) / 256 * 256;
     p->pieces = (int)((g.V + piece - 1) / piece);

@@ -509,6 +509,12 @@ inline double product_us(int shape, Format f, long tiles, int passes, int slices
     }
     return us;
 }
+// A launch has fewer than 2^32 threads, its workgroups rounded up to the XCDs.
+inline bool fits_grid(int shape, long workgroups)
+{
+    static const int kThreads[kShapes] = {Small::kThreads, Middle::kThreads, Wide::kThreads, Big::kThreads, Low::kThreads};
+    return (workgroups + 7) / 8 * 8 * kThreads[shape] < 1L << 32;
+}
 inline long tiles_of(int shape, long M, long N, bool symmetric)
 {
     const long m = cdiv(M, kRows[shape]), n = cdiv(N, kColumns[shape]);
@@ -529,6 +535,7 @@ inline Choice choose(Format f, long M, long N, int batch, long K, bool symmetric
         for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices / 4 * 2) {
             if (slices > 1 && passes / slices < 4) break;
             if (slices > 1 && tiles * slices > 2048) break;
+            if (!fits_grid(shape, tiles)) break; // (where none does the caller has to do with less at a time)
             double us = product_us(shape, f, tiles, passes, slices);
             if (slices > 1) us += 4.0 + 8e-6 / 2.5 * slices * tiles * kRows[shape] * kColumns[shape];
             if (us < least) {

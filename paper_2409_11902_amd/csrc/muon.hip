@@ -339,7 +339,7 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 void plan_muon(const MuonGeom &g, MuonPlan *p)
 {
-    p->narrow = plan_muon_narrow(g, &p->np);
+    p->narrow = p->fits = plan_muon_narrow(g, &p->np);
     if (p->narrow) {
         p->bytes = p->np.bytes;
         return;
@@ -351,6 +351,9 @@ void plan_muon(const MuonGeom &g, MuonPlan *p)
     p->gram = choose(kSplit, p->r, p->r, g.batch, p->tall ? g.rows : g.cols, true, 16);
     p->poly = choose(kSplit, p->r, p->r, g.batch, p->r, true, 1);
     p->apply = choose(kSplit, g.rows, g.cols, g.batch, p->r, false, 1);
+    p->fits = fits_grid(p->gram.shape, tiles_of(p->gram.shape, p->r, p->r, true) * p->gram.slices * g.batch) &&
+              fits_grid(p->poly.shape, tiles_of(p->poly.shape, p->r, p->r, true) * g.batch) &&
+              fits_grid(p->apply.shape, tiles_of(p->apply.shape, g.rows, g.cols, false) * g.batch);
     const long size = g.rows * g.cols;
     p->sum_blocks = (int)(size / 8192 < 1 ? 1 : size / 8192 > kMaxSumBlocks ? kMaxSumBlocks : size / 8192);
     size_t o = 0;

@@ -56,6 +56,7 @@ struct MuonPlan {
     long r;             // the shorter side
     long ld_x, ld_a;    // bytes of a row
     TileChoice gram, poly, apply;
+    bool fits;          // every launch's grid is one that there is
     int sum_blocks;     // partial sums of squares of one matrix
     size_t o_sum, o_lift, o_x[2], o_a, o_b, o_part, bytes;
 };
