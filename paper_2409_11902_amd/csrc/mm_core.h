@@ -497,7 +497,7 @@ constexpr int kTerms[] = {64, 32, 32};                                          
 inline double product_us(int shape, Format f, long tiles, int passes, int slices)
 {
     static const int kHolds[kShapes] = {3, 2, 1, 1, 2};
-    static const double kAlone[kShapes][3] = {{0.27, 0.27, 0.5}, {0.77, 0.80}, {0, 1.75}, {1.95, 2.85}, {0, 0, 0.5}},
+    static const double kAlone[kShapes][3] = {{0.27, 0.27, 0.5}, {0.77, 0.80}, {0, 1.75}, {1.95, 2.85}, {0, 0, 0.5}}, // (0: no such kernel)
                         kFull[kShapes][3] = {{0.62, 0.95, 1.4}, {1.12, 1.5}, {0, 1.75}, {1.95, 2.85}, {0, 0, 1.0}},
                         kOnce[kShapes] = {2.5, 3.5, 5.0, 6.0, 2.5};
     const long wgs = tiles * slices, round = 256L * kHolds[shape];
@@ -530,6 +530,7 @@ inline Choice choose(Format f, long M, long N, int batch, long K, bool symmetric
         if (small_only && shape != kSmall && shape != kLow) continue;
         if (shape == kWide && f != kSplit) continue; // (192 columns of bfloat16 are no whole number of swizzled chunks)
         if ((shape == kLow) != (f == kRaw && M <= kRows[kLow])) continue;
+        if (f == kRaw && shape != kSmall && shape != kLow) continue; // (there are no others)
         const long tiles = tiles_of(shape, M, N, symmetric) * batch;
         const int passes = cdiv(K, kTerms[f]);
         for (int slices = 1; slices <= max_slices; slices += slices < 4 ? 1 : slices / 4 * 2) {
