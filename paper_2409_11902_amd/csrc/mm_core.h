@@ -95,8 +95,8 @@ template <class P, Lay L, int T, int R> __device__ __forceinline__ int swizzle(i
 // written, so there is nothing that could be overwritten under way.
 template <int UNIT> __device__ __forceinline__ void load_to_lds(u32x4 rs, uint32_t offset, uint32_t to)
 {
-    if (UNIT == 4) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory", "m0");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory", "m0");
+    if (UNIT == 4) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(rs) : "memory"); // (m0 has no other use in these kernels)
 }
 
 // One operand's way into LDS: T rows of C by one pass of K, R T bytes, by NW waves.
