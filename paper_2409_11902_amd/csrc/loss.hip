@@ -600,8 +600,23 @@ template <typename T> __device__ __forceinline__ void store_four(T *o, int n, in
         if (n + k < N) Elem<T>::store(o + k, v[k]);
 }
 
+// What a product is multiplied by on its way out: a float, and of two halves a power of two beside it (one float would have to hold what the
+// operands were stored times, which the product still is: results that float holds would meet a factor that it does not).
+template <bool SPLIT> struct Factor {
+    float f;
+    int e;
+    __device__ __forceinline__ Factor(float largest, int exponent) : f(largest), e(0)
+    {
+        if (SPLIT) {
+            f = frexpf(largest, &e);
+            e += exponent;
+        }
+    }
+    __device__ __forceinline__ float operator()(float v) const { return SPLIT ? ldexpf(f * v, e) : f * v; }
+};
+
 // 32 rows of a product, times s, into a wave's LDS; zeros where the lane's row is left out
-template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x16 (&acc)[MI][NI], int i, float s, const Place &p, bool out = false)
+template <class S, int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x16 (&acc)[MI][NI], int i, S s, const Place &p, bool out = false)
 {
 #pragma unroll
     for (int j = 0; j < NI; ++j)
@@ -609,7 +624,7 @@ template <int MI, int NI> __device__ __forceinline__ void put_scaled(const f32x1
         for (int q = 0; q < 4; ++q) {
             float v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = out ? 0.f : s * acc[i][j][q * 4 + k];
+            for (int k = 0; k < 4; ++k) v[k] = out ? 0.f : s(acc[i][j][q * 4 + k]);
             RowBlock<Fmt::kF32, NI>::put(p.lds, p.lane, j, q, v);
         }
 }
@@ -620,13 +635,13 @@ template <class K> struct OutW : Ending {
     struct Params { T *out; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = K::kSplit ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[0]) : e.meta.largest(p.lane);
+        const Factor<K::kSplit> s(e.meta.largest(p.lane), K::kSplit ? -kStoreG - e.meta.exps[0] : 0);
         typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
-            put_scaled<MI, NI>(acc, i, s, p);
+            put_scaled(acc, i, s, p);
             Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
                 const int m = m0 + row, n = p.n0 + at / 4;
                 if (m < p.M && n < p.N) store_four(e.out + (long)m * p.N + n, n, p.N, wide, {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])});
@@ -641,7 +656,7 @@ template <class K> struct OutH : Ending {
     struct Params { T *out; float *sums; long slice_stride; int add; bool rests; Meta meta; };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
-        const float s = K::kSplit ? ldexpf(e.meta.largest(p.lane), -kStoreG - e.meta.exps[1]) : e.meta.largest(p.lane);
+        const Factor<K::kSplit> s(e.meta.largest(p.lane), K::kSplit ? -kStoreG - e.meta.exps[1] : 0);
         typedef RowBlock<Fmt::kF32, NI> Block;
         const bool wide = (p.N & 3) == 0;
 #pragma unroll
@@ -650,7 +665,7 @@ template <class K> struct OutH : Ending {
             const bool rests = K::kG == Fmt::kBf16 && e.rests; // (32 rows and their rests: neighbouring waves of one tile)
             // a row that is left out has zeros in G where nothing is compacted, and a zero times an infinite weight is none
             const int m = m0 + (p.lane & 31), row = rests && m >= kLoRow ? m - kLoRow : m;
-            put_scaled<MI, NI>(acc, i, s, p, e.meta.direct && row < e.meta.T && e.meta.label_of(row) == Meta::kOut);
+            put_scaled(acc, i, s, p, e.meta.direct && row < e.meta.T && e.meta.label_of(row) == Meta::kOut);
             if (rests) {
                 __syncthreads();
                 if (m0 >= kLoRow) return;
@@ -780,8 +795,8 @@ template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, i
     }
     __syncthreads();
     if (threadIdx.x < 64 && block * 64 + (int)threadIdx.x < p.V) {
-        const float c = K::kSplit ? ldexpf(largest, -kStoreG) : largest;
-        Elem<T>::store(p.db + block * 64 + threadIdx.x, c * (((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
+        const Factor<K::kSplit> c(largest, -kStoreG);
+        Elem<T>::store(p.db + block * 64 + threadIdx.x, c(((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
     }
 }
 template <class K> __global__ void __launch_bounds__(256) bias_kernel(const Bias<K> p)
@@ -984,7 +999,7 @@ struct Logits : Ending {
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
-            put_scaled<MI, NI>(acc, i, 1.f, p);
+            put_scaled(acc, i, Factor<false>(1.f, 0), p);
             Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
                 if (m0 + row < p.M && p.n0 + at / 4 < e.ld) *(u32x4 *)(e.out + ((long)p.slice * e.T + m0 + row) * e.ld + p.n0 + at / 4) = x;
             });
