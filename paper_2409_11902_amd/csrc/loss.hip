@@ -26,7 +26,8 @@ struct OfSplit { typedef float E; typedef Split P; static constexpr bool kSplit 
 template <class R> struct OfRaw { typedef float E; typedef R P; static constexpr bool kSplit = false; static constexpr Fmt kG = Fmt::kF32; }; // (Raw, RawOdd)
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kStoreG = 14;        // G is stored times 2^14 as two halves: |G| <= 1, and 1e-8 is still a normal number
+// G is stored times 2^14 as two halves, |G| <= 1, which keeps its 23 bits down to 2^-16; below that they end at 2^-39.
+constexpr int kStoreG = 14;
 constexpr int kMaxParts = 1024;    // blocks that look for a matrix's largest number
 
 __device__ __forceinline__ float wave_max(float v)
@@ -191,6 +192,7 @@ struct PackRows {
     int rows_per_block, row_blocks; // the blocks behind the row blocks pack weights
     int classes;                    // of the weights, from W on
     char *out_w;
+    uint32_t *peak;                 // backward: of the classes, to be cleared
     int parts_h, parts_w;  // of the largest magnitudes (float)
     char *out;
     long row_bytes;
@@ -344,6 +346,8 @@ template <class K> __device__ __forceinline__ void pack_weights(const PackRows &
     const float s = K::kSplit ? ldexpf(1.f, stored_exp(p.meta.top + kMaxParts, p.parts_w)) : 1.f;
     const bool aligned = ((uintptr_t)p.W & 15) == 0 && (p.ld_w * sizeof(T)) % 16 == 0;
     const int lane = threadIdx.x & 63, rows = 4 * (gridDim.x - p.row_blocks);
+    if (K::kSplit && p.peak)
+        for (int c = (blockIdx.x - p.row_blocks) * 256 + threadIdx.x; c < p.classes; c += rows * 64) p.peak[c] = 0u;
     // Short rows: a thread to eight numbers, wherever they are (100 x 100 x 60000 float forward: 53 us with a wave to a row, 43 so;
     // of 16 x 252 x 60000 bfloat16 40 and 43).
     if (p.D <= kShortRow) {
@@ -524,10 +528,58 @@ __device__ __forceinline__ float rest_of(float g)
     return g - g == 0.f ? r : 0.f; // (an infinite or undefined one has none)
 }
 
-// backward: G of a piece
-template <class K> struct Grad : Ending {
+// ---- Classes that no row thinks probable.  dW and db of a class are sums of its own G, so what 2^-39 of the largest G does not hold would
+// be all of a class whose G lies down there.  The pass that forms G as two halves leaves every class's largest |G|; where that is below 2^-16, the
+// class's G is formed once more, times a power of two of its own, for dW and db (dH has G as it was first: there a row's G are added
+// up, improbable beside probable ones).  Tiles without such a class end at once.  Both passes of 512 x 512 x 1500 and 1000 x 1001 x 50257:
+// 51 and 1610 us without all this, 58 and 1640 where no class is improbable, 65 and 1950 where all tiles are formed again.
+constexpr float kSmallPeak = 0x1p-16f;
+__device__ __forceinline__ bool small_peak(uint32_t peak)
+{
+    const float m = __uint_as_float(peak);
+    return m > 0.f && m < kSmallPeak;
+}
+// a class's G are below 2^peak_exp (and stored times 2^-peak_exp)
+__device__ __forceinline__ int peak_exp(uint32_t peak)
+{
+    int e = 0;
+    if (small_peak(peak)) frexpf(__uint_as_float(peak), &e);
+    return e;
+}
+// of `count` classes, asked by a whole wave
+__device__ __forceinline__ bool any_small_peak(const uint32_t *peak, int first, int count, int lane)
+{
+    bool any = false;
+    for (int k = lane; k < count; k += 64) any = any || small_peak(peak[first + k]);
+    return __any(any);
+}
+// (numbers are not negative, so that they are ordered as their bits are; the largest does not depend on the order of arrival)
+__device__ __forceinline__ void raise_peak(uint32_t *peak, float v)
+{
+    const uint32_t bits = __float_as_uint(v);
+    if (bits > __hip_atomic_load(peak, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(peak, bits);
+}
+// of a wave's 32 NI columns: v[j][4 q + k] as C lies, largest of the wave's blocks of rows.  Lanes that hold rows of the same columns share the numbers out.
+template <int NI> __device__ __forceinline__ void raise_peaks(uint32_t *peak, float (&v)[NI][16], const Place &p)
+{
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+#pragma unroll
+        for (int n = 8; n > 0; n >>= 1) {
+            const bool up = p.lane & 2 * n;
+#pragma unroll
+            for (int k = 0; k < n; ++k) v[j][k] = fmaxf(up ? v[j][k + n] : v[j][k], __shfl_xor(up ? v[j][k] : v[j][k + n], 2 * n, 64));
+        }
+        const float top = fmaxf(v[j][0], __shfl_xor(v[j][0], 1, 64));
+        const int at = p.lane >> 1 & 15, n = p.n0 + j * 32 + (at >> 2) * 8 + (p.lane >> 5) * 4 + (at & 3);
+        if (!(p.lane & 1) && n < p.N) raise_peak(peak + n, top);
+    }
+}
+
+// backward: G of a piece.  AGAIN: of two halves, of tiles with a class whose G are small, every class times its power of two.
+template <class K, bool AGAIN = false> struct Grad : Ending {
     typedef typename K::E T;
-    static constexpr bool kCountsM = true;
+    static constexpr bool kCountsM = true, kGated = AGAIN;
     struct Params {
         const T *b;
         Meta meta;
@@ -535,7 +587,9 @@ template <class K> struct Grad : Ending {
         long ld;
         int v0;
         bool rests;
+        uint32_t *peak;   // of two halves: [classes], raised (AGAIN: read)
     };
+    static __device__ __forceinline__ bool wanted(const Params &e, int first, int count, int lane) { return any_small_peak(e.peak, first, count, lane); }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const int ze = K::kSplit ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
@@ -543,6 +597,8 @@ template <class K> struct Grad : Ending {
         const int Np = (p.N + 7) & ~7;
         typedef RowBlock<K::kG, NI> Block;
         constexpr int kIn16 = sizeof(T) == 4 ? 32 : 16; // bytes that eight columns take
+        constexpr bool kPeaks = K::kSplit && !AGAIN;
+        float peaks[kPeaks ? NI : 1][16] = {};
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32, m = min(m0 + (p.lane & 31), p.M - 1);
@@ -562,7 +618,9 @@ template <class K> struct Grad : Ending {
                     for (int k = 0; k < 4; ++k) {
                         const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
                         const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        g[k] = n + k < p.N && in ? (K::kSplit ? x * (float)(1 << kStoreG) : x) : 0.f;
+                        const float stored = AGAIN ? ldexpf(x, kStoreG - peak_exp(e.peak[min(n + k, p.N - 1)])) : K::kSplit ? x * (float)(1 << kStoreG) : x;
+                        g[k] = n + k < p.N && in ? stored : 0.f;
+                        if constexpr (kPeaks) peaks[j][q * 4 + k] = fmaxf(peaks[j][q * 4 + k], fabsf(x));
                         if constexpr (kRests) kept[q * 4 + k] = g[k];
                     }
                     Block::put(p.lds, p.lane, j, q, g);
@@ -583,6 +641,7 @@ template <class K> struct Grad : Ending {
                 store(e.out + kLoRow * e.ld);
             }
         }
+        if constexpr (kPeaks) raise_peaks<NI>(e.peak, peaks, p);
     }
 };
 
@@ -632,7 +691,17 @@ template <class S, int MI, int NI> __device__ __forceinline__ void put_scaled(co
 // dW of a piece
 template <class K> struct OutW : Ending {
     typedef typename K::E T;
-    struct Params { T *out; Meta meta; };
+    static constexpr bool kOther = K::kSplit;
+    struct Params {
+        T *out;
+        Meta meta;
+        const uint32_t *peak; // of two halves, and where G lies that was formed again, if it is elsewhere
+        const char *again;
+    };
+    static __device__ __forceinline__ const void *operand_a(const Params &e, const void *a, int first, int count, int lane)
+    {
+        return e.again && any_small_peak(e.peak, first, count, lane) ? e.again : a;
+    }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const Factor<K::kSplit> s(e.meta.largest(p.lane), K::kSplit ? -kStoreG - e.meta.exps[0] : 0);
@@ -641,7 +710,9 @@ template <class K> struct OutW : Ending {
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
-            put_scaled(acc, i, s, p);
+            Factor<K::kSplit> of_class = s;
+            if (K::kSplit) of_class.e += peak_exp(e.peak[min(m0 + (p.lane & 31), p.M - 1)]);
+            put_scaled(acc, i, of_class, p);
             Block::each(p.lds, p.lane, [&](int row, int at, u32x4 x) {
                 const int m = m0 + row, n = p.n0 + at / 4;
                 if (m < p.M && n < p.N) store_four(e.out + (long)m * p.N + n, n, p.N, wide, {__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3])});
@@ -755,6 +826,8 @@ template <class K> struct Bias {
     int V;
     T *db;
     bool rests;
+    const uint32_t *peak; // as OutW's
+    const char *again;
 };
 template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, int block, float (*red)[64])
 {
@@ -764,10 +837,11 @@ template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, i
     const float largest = p.meta.largest(lane);
     // 8 chunks of columns by 8 rows to a wave
     const int chunk = block * 8 + (lane & 7), n = chunk * 8;
+    const char *G = K::kSplit && p.again && any_small_peak(p.peak, block * 64, min(p.V - block * 64, 64), lane) ? p.again : p.G;
     float s[8] = {};
     if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
-            const char *g = p.G + (long)(m < rows ? m : m - rows + kLoRow) * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
+            const char *g = G + (long)(m < rows ? m : m - rows + kLoRow) * p.ld + (long)chunk * (sizeof(T) == 4 ? 32 : 16);
             if (K::kG == Fmt::kF32) {
                 const f32x4 lo = *(const f32x4 *)g, hi = *(const f32x4 *)(g + 16);
 #pragma unroll
@@ -795,7 +869,7 @@ template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, i
     }
     __syncthreads();
     if (threadIdx.x < 64 && block * 64 + (int)threadIdx.x < p.V) {
-        const Factor<K::kSplit> c(largest, -kStoreG);
+        const Factor<K::kSplit> c(largest, K::kSplit ? peak_exp(p.peak[block * 64 + threadIdx.x]) - kStoreG : 0);
         Elem<T>::store(p.db + block * 64 + threadIdx.x, c(((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
     }
 }
@@ -1070,29 +1144,52 @@ row_loss_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
         loss[t] = at_label == -INFINITY ? INFINITY : l - at_label;
     }
 }
-// G of a compact row, 1024 classes to a block
-template <class K> __global__ void __launch_bounds__(256)
+// G, four neighbours to a thread: of two halves 16 rows by 64 classes to a block, which has a largest number for each, else 1024 of a row.  AGAIN: as Grad's
+template <class K> constexpr int kGradRows = K::kSplit ? 16 : 1;
+template <class K, bool AGAIN> __global__ void __launch_bounds__(256)
 row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stride, int ld, int slices, const typename K::E *__restrict__ b, int V,
-                char *__restrict__ G, long ld_g, bool rests)
+                char *__restrict__ G, long ld_g, bool rests, uint32_t *__restrict__ peak)
 {
-    const int m = blockIdx.x, n = blockIdx.y * 1024 + threadIdx.x * 4;
-    const float largest = meta.largest(threadIdx.x & 63);
-    if (m >= meta.rows() || n >= ((V + 7) & ~7)) return;
-    const int label = meta.label_of(m);
-    const float q = meta.q_of(m, largest), lse = meta.lse_of(m);
+    constexpr int kThreads = 256 / kGradRows<K>; // of a row
+    const int lane = threadIdx.x & 63, m = blockIdx.x * kGradRows<K> + threadIdx.x / kThreads, n = (blockIdx.y * kThreads + threadIdx.x % kThreads) * 4;
+    const float largest = meta.largest(lane);
+    if (AGAIN && !any_small_peak(peak, blockIdx.y * 64, min(V - (int)blockIdx.y * 64, 64), lane)) return;
     float g[4] = {0.f, 0.f, 0.f, 0.f};
-    if (label != Meta::kOut && n < V) {
-        const int ze = K::kSplit ? -(meta.exps[0] + meta.exps[1]) : 0;
-        float z[4];
-        join_logits<K>(part + (long)m * ld, slice_stride, slices, b, n, V, ze, z);
+    if (m < meta.rows() && n < ((V + 7) & ~7)) {
+        const int label = meta.label_of(m);
+        const float q = meta.q_of(m, largest), lse = meta.lse_of(m);
+        if (label != Meta::kOut && n < V) {
+            const int ze = K::kSplit ? -(meta.exps[0] + meta.exps[1]) : 0;
+            float z[4];
+            join_logits<K>(part + (long)m * ld, slice_stride, slices, b, n, V, ze, z);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (n + e < V) g[e] = q * (__builtin_amdgcn_exp2f((z[e] - lse) * kLog2e) - (n + e == label ? 1.f : 0.f));
+            for (int e = 0; e < 4; ++e)
+                if (n + e < V) g[e] = q * (__builtin_amdgcn_exp2f((z[e] - lse) * kLog2e) - (n + e == label ? 1.f : 0.f));
+        }
+        if (AGAIN) {
+            const float v[4] = {ldexpf(g[0], -peak_exp(peak[min(n, V - 1)])), ldexpf(g[1], -peak_exp(peak[min(n + 1, V - 1)])),
+                                ldexpf(g[2], -peak_exp(peak[min(n + 2, V - 1)])), ldexpf(g[3], -peak_exp(peak[min(n + 3, V - 1)]))};
+            store_gradient<K>(G + (long)m * ld_g, n, v);
+        } else {
+            store_gradient<K>(G + (long)m * ld_g, n, g);
+        }
+        if (K::kG == Fmt::kBf16 && rests) {
+            const float r[4] = {rest_of(g[0]), rest_of(g[1]), rest_of(g[2]), rest_of(g[3])};
+            store_gradient<K>(G + (long)(m + kLoRow) * ld_g, n, r);
+        }
     }
-    store_gradient<K>(G + (long)m * ld_g, n, g);
-    if (K::kG == Fmt::kBf16 && rests) {
-        const float r[4] = {rest_of(g[0]), rest_of(g[1]), rest_of(g[2]), rest_of(g[3])};
-        store_gradient<K>(G + (long)(m + kLoRow) * ld_g, n, r);
+    if constexpr (K::kSplit && !AGAIN) { // the classes' largest of the block's rows
+        __shared__ float tops[4][64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v = fabsf(g[e]);
+            v = fmaxf(v, __shfl_xor(v, 16, 64));
+            v = fmaxf(v, __shfl_xor(v, 32, 64));
+            if (lane < 16) tops[threadIdx.x >> 6][lane * 4 + e] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x < 64 && (int)(blockIdx.y * 64 + threadIdx.x) < V)
+            raise_peak(peak + blockIdx.y * 64 + threadIdx.x, fmaxf(fmaxf(tops[0][lane], tops[1][lane]), fmaxf(tops[2][lane], tops[3][lane])));
     }
 }
 
@@ -1166,6 +1263,14 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     if (p->z.slices > 1) o += up256((size_t)logits * p->z.slices);
     p->o_g = o;
     if (backward) o += up256((size_t)(g.T + (p->rests ? kLoRow : 0)) * ((piece + 7) / 8 * 8) * e);
+    // (two halves: what classes with small G are formed again with; dW and dH of one launch read both)
+    p->o_peak = o;
+    if (backward && p->split) o += up256((size_t)piece * 4);
+    p->o_again = p->o_g;
+    if (p->split && p->pair) {
+        p->o_again = o;
+        o += up256((size_t)g.T * ((piece + 7) / 8 * 8) * e);
+    }
     p->o_acc = o;
     if (backward && (p->pieces > 1 || p->h.slices > 1)) o += up256((size_t)p->h.slices * g.T * g.D * 4);
     p->bytes = o;
@@ -1274,6 +1379,24 @@ template <class K> class Loss {
         }
         return hipErrorInvalidValue;
     }
+    // G of classes v0 .. v0 + n; AGAIN: of those with small G
+    template <bool AGAIN> hipError_t gradients(long v0, long n, char *G, long ld_g)
+    {
+        if constexpr (AGAIN && !K::kSplit) {
+            return hipSuccess;
+        } else {
+            uint32_t *peak = p.split ? (uint32_t *)(ws + p.o_peak) : nullptr;
+            if (p.z.slices == 1)
+                return launch<P, Lay::kAlong, Lay::kAlong, Grad<K, AGAIN>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0, p.rests, peak}, p.z, st);
+            if (!AGAIN) { // (one piece; the logits stay where they are)
+                const hipError_t e = logits_in_slices(n);
+                if (e != hipSuccess) return e;
+            }
+            hipLaunchKernelGGL((row_grad_kernel<K, AGAIN>), dim3(cdiv(g.T, kGradRows<K>), cdiv(g.V, 1024 / kGradRows<K>)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
+                               g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g, p.rests, peak);
+            return hipGetLastError();
+        }
+    }
     hipError_t launch_together(PairParams<K> &q, bool want_h, int bias_blocks)
     {
         if constexpr (K::kSplit) {
@@ -1343,21 +1466,15 @@ public:
         rows.lse = lse;
         rows.gloss = gloss;
         rows.dH = p.few ? nullptr : dH;
-        char *G = ws + p.o_g;
+        rows.peak = p.split ? (uint32_t *)(ws + p.o_peak) : nullptr;
+        char *const G = ws + p.o_g, *const again = ws + p.o_again;
+        const uint32_t *const peak = rows.peak;
         const long ld_g = (p.piece + 7) / 8 * 8 * (long)sizeof(T);
         float *sums = p.pieces > 1 || p.h.slices > 1 ? (float *)(ws + p.o_acc) : nullptr;
         for (long v0 = 0; v0 < g.V; v0 += p.piece) {
             const long n = v0 + p.piece < g.V ? p.piece : g.V - v0;
             if ((e = operands(v0, n, &rows)) != hipSuccess) return e;
-            if (p.z.slices > 1) {
-                if ((e = logits_in_slices(n)) != hipSuccess) return e;
-                hipLaunchKernelGGL(row_grad_kernel<K>, dim3((unsigned)g.T, cdiv(g.V, 1024)), dim3(256), 0, st, meta, (const float *)(ws + p.o_z),
-                                   g.T * ld_logits(), (int)ld_logits(), p.z.slices, b, (int)g.V, G, ld_g, p.rests);
-                e = hipGetLastError();
-            } else {
-                e = launch<P, Lay::kAlong, Lay::kAlong, Grad<K>>(logits_params(n), {b ? b + v0 : nullptr, meta, G, ld_g, (int)v0, p.rests}, p.z, st);
-            }
-            if (e != hipSuccess) return e;
+            if ((e = gradients<false>(v0, n, G, ld_g)) != hipSuccess) return e;
             PairParams<K> q{};
             q.w.a = G;
             q.w.lda = ld_g;
@@ -1368,7 +1485,7 @@ public:
             q.w.K = (int)g.T;
             q.w.batch = 1;
             q.w.k_dev = meta.count;
-            q.ew = {dW ? dW + v0 * g.D : nullptr, meta};
+            q.ew = {dW ? dW + v0 * g.D : nullptr, meta, peak, again == G ? nullptr : again};
             q.h.a = G;
             q.h.lda = ld_g;
             q.h.b = w;
@@ -1379,9 +1496,10 @@ public:
             q.h.batch = 1;
             if (!p.few) q.h.m_dev = meta.count;
             q.eh = {dH, sums, g.T * g.D, v0 > 0, p.rests, meta};
-            q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr, p.rests};
+            q.b = {meta, G, ld_g, (int)n, db ? db + v0 : nullptr, p.rests, peak, q.ew.again};
             const int bias_blocks = db ? cdiv(n, 64) : 0;
             if (p.pair) {
+                if (K::kSplit && (dW || db) && (e = gradients<true>(v0, n, again, ld_g)) != hipSuccess) return e;
                 q.few = {meta, G, (const T *)h, ld_g, ld_h, (int)n, (int)g.D, q.ew.out, 0, 0};
                 // dH may take the place of H; where H is read as it lies dW has to be done with it by then
                 if (p.direct && (const T *)dH == H && (dW || db)) {
@@ -1392,8 +1510,10 @@ public:
                     e = launch_together(q, dH, bias_blocks);
                 }
             } else if constexpr (!kDirect) {
-                if (dW) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
-                if (dH && e == hipSuccess) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);
+                // (G of two halves as it is formed first is what dH takes, as it is formed again what dW does)
+                if (dH) e = launch<P, Lay::kAlong, Lay::kDown, OutH<K>>(q.h, q.eh, p.h, st);
+                if (K::kSplit && (dW || db) && e == hipSuccess) e = gradients<true>(v0, n, G, ld_g);
+                if (dW && e == hipSuccess) e = launch<P, Lay::kDown, Lay::kDown, OutW<K>>(q.w, q.ew, p.w, st);
                 if (db && e == hipSuccess) {
                     hipLaunchKernelGGL(bias_kernel<K>, dim3(bias_blocks), dim3(256), 0, st, q.b);
                     e = hipGetLastError();

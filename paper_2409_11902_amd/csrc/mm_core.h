@@ -219,7 +219,8 @@ __device__ __forceinline__ f32x4 as_floats(s16x8 v)
 }
 
 // What an ending may say about its product.
-struct Ending { static constexpr bool kSymmetric = false, kCountsM = false; };
+struct Ending { static constexpr bool kSymmetric = false, kCountsM = false, kGated = false, kOther = false; };
+// (kGated: only tiles whose columns an ending's wanted() asks for; kOther: its operand_a() says where a tile's rows of a lie)
 
 // ---- a float as two halves.  x is fixed first: left to itself the compiler takes hi from a product's rounded value and lo from the
 // product, and where those lie on two sides of a half-precision number's middle, hi + lo is off by a unit of hi.
@@ -378,6 +379,11 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
         tm = g0 + gi - tn * gr;
     }
 
+    if constexpr (Epi::kGated)
+        if (!Epi::wanted(e, tn * TN, min(p.N - tn * TN, TN), lane)) return;
+    const void *from_a = p.a;
+    if constexpr (Epi::kOther) from_a = Epi::operand_a(e, p.a, tm * TM, min(M - tm * TM, TM), lane);
+
     const int passes = (K + kPass<P, S::R> - 1) / kPass<P, S::R>;
     const int kt0 = slice * p.kt_slice, kt1 = min(passes, kt0 + p.kt_slice);
 
@@ -391,7 +397,7 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
 
     Stage<P, LA, TM, S::R, S::kWaves, Epi::kCountsM> sa;
     Stage<P, LB, TN, S::R, S::kWaves, false> sb;
-    sa.init((const char *)p.a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane, p.counts_m);
+    sa.init((const char *)from_a + batch * p.a_batch, p.lda, tm * TM, M, K, kt0, kt1, wave, lane, p.counts_m);
     sb.init((const char *)p.b + batch * p.b_batch, p.ldb, tn * TN, p.N, K, kt0, kt1, wave, lane, p.counts_m);
     const int wm = wave / S::WN, wn = wave % S::WN;
     Frag<P, LA, TM, S::R> fa;

@@ -28,7 +28,7 @@ struct LossPlan {
     int pieces;
     TileChoice z, w, h; // the logits' product, dW's, dH's
     long parts;       // forward: maximum and sum, this many for every row
-    size_t o_meta, o_h, o_w, o_part, o_z, o_g, o_acc, bytes;
+    size_t o_meta, o_h, o_w, o_part, o_z, o_g, o_peak, o_again, o_acc, bytes;
 };
 void plan_loss(const LossGeom &g, bool backward, LossPlan *p);
 hipError_t launch_loss_fwd(const LossGeom &g, const LossPlan &p, const void *H, const void *W, const void *b, const int64_t *labels,

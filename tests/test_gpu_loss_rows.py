@@ -1,0 +1,86 @@
+"""The classifier's loss row by row: what a norm over a whole matrix does not show.
+
+Tolerances.  A logit's error is that of float arithmetic: sums of D products in steps of 16 terms lose some roundings of 2^-24 of
+the largest partial sum (eight are allowed), lse is stored with one, the difference and its factor log2 e add three of the
+difference.  A probability is off by that much of itself, and a label's gradient, probability - 1, by a rounding of 1 as well; a
+row's result by at most the sum of what its terms are off by, and by 2^-22 of its terms for the product."""
+import pytest
+import torch
+
+from paper_2409_11902_amd import binding as B
+from test_gpu_loss import DEV, make, reference, run
+
+pytestmark = pytest.mark.gpu
+
+
+def allowed(t):
+    """What G, [T, V], may be off by (every row counts)."""
+    d = t["desc"]
+    h, w = t["H"][:, :d.D].double(), t["W"][:, :d.D].double()
+    z = h @ w.t()
+    if t["b"] is not None:
+        z = z + t["b"].double()
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    fine = z > -1e30
+    zmax, dmax = float(z[fine].abs().max()), float((z - lse)[fine].abs().clamp(max=110).max())
+    part = 2.0 ** -24 * (8 * zmax + 2 * float(lse.abs().max()) + 3 * dmax)
+    p = (z - lse).exp()
+    at = torch.arange(d.T, device=DEV)
+    g, off = p.clone(), part * p
+    g[at, t["labels"]] -= 1
+    off[at, t["labels"]] += 2.0 ** -23
+    return (off + 2.0 ** -22 * g.abs()) * t["gloss"].double().abs().unsqueeze(1)
+
+
+def gradients(t, want):
+    """Those that are named, from a backward pass that is asked for no others."""
+    d, td = t["desc"], t["H"].dtype
+    loss, lse = torch.empty(d.T, device=DEV), torch.empty(d.T, device=DEV)
+    out = {"dH": (d.T, d.D), "dW": (d.V, d.D), "db": (d.V,)}
+    out = {k: torch.full(out[k], torch.nan, dtype=td, device=DEV) if k in want else None for k in out}
+    ws = torch.empty(max(B.cac_loss_workspace_size(d, op) for op in (B.LOSS_FWD, B.LOSS_BWD)), dtype=torch.uint8, device=DEV)
+    B.cac_loss_fwd(d, t["H"], t["W"], t["b"], t["labels"], loss, lse, ws)
+    B.cac_loss_bwd(d, t["H"], t["W"], t["b"], t["labels"], lse, t["gloss"], out["dH"], out["dW"], out["db"], ws)
+    return out
+
+
+def check_rows(t, got, names=("dH", "dW", "db")):
+    want, off = reference(t), allowed(t)
+    d = t["desc"]
+    h, w = t["H"][:, :d.D].double().abs(), t["W"][:, :d.D].double().abs()
+    bound = {"dH": (off @ w).norm(dim=1), "dW": (off.t() @ h).norm(dim=1), "db": off.sum(0)}
+    for k in names:
+        a = got[k].double() - want[k]
+        a = a.norm(dim=1) if a.dim() == 2 else a.abs()
+        assert bool(torch.isfinite(a).all()), k
+        # (below float's smallest normal number there is nothing to ask for)
+        size = want[k].norm(dim=1) if want[k].dim() == 2 else want[k].abs()
+        tiny = 2.0 ** -126 * (1 if k == "db" else float(h.max() if k == "dW" else w.max())) * d.T * d.D ** 0.5
+        worst = ((a - tiny).clamp(min=0) / bound[k].clamp(min=1e-300)).max()
+        row = int(((a - tiny) / bound[k].clamp(min=1e-300)).argmax())
+        assert float(worst) <= 1.0, (k, row, float(a[row]), float(bound[k][row]), float(size[row]))
+
+
+@pytest.mark.parametrize("spread", [2, 12, 16])
+@pytest.mark.parametrize("shape", [(40, 256, 900), (100, 256, 9000), (300, 256, 4000), (300, 1024, 700), (700, 72, 333), (1500, 512, 12000)])
+def test_classes_that_no_row_thinks_probable(shape, spread):
+    t = make(*shape, B.F32, seed=spread)
+    t["W"] *= spread / 2
+    check_rows(t, run(t))
+    for want in (("dW",), ("dW", "db"), ("db",)):
+        check_rows(t, gradients(t, want), want)
+
+
+@pytest.mark.parametrize("shape", [(40, 64, 300), (200, 64, 300), (1000, 256, 5000), (1200, 640, 12000)])
+def test_classes_kept_down_by_their_bias(shape):
+    """Probabilities down to 1e-34, a few classes and tiles of them, beside classes that are masked altogether."""
+    t = make(*shape, B.F32, seed=7)
+    V = shape[2]
+    b = torch.zeros(V, device=DEV)
+    b[V // 2:V // 2 + 100] = torch.linspace(-5, -75, 100, device=DEV)
+    b[-3:] = -torch.inf
+    t["b"] = b
+    t["labels"] %= V // 2
+    got = run(t)
+    check_rows(t, got)
+    assert bool((got["dW"][-3:] == 0).all()) and bool((got["db"][-3:] == 0).all())
