@@ -47,6 +47,7 @@ struct Meta {
     int *count;       // [0]: rows that count
     int *exps;        // H and W are stored times 2^exps[0] and 2^exps[1] as two halves
     float *c;         // [0]: the largest of the rows' gradients
+    int *uneven;      // [0]: some row's gradient is small beside it (row_exp)
     int *row;         // compact row -> row of H
     int *label;
     float *q, *lse;
@@ -89,6 +90,7 @@ inline Meta meta_at(char *p, long T)
     m.count = (int *)p;
     m.exps = (int *)(p + 64);
     m.c = (float *)(p + 128);
+    m.uneven = (int *)(p + 192);
     m.top = (float *)(p + 256);
     p += 256 + up256(2 * kMaxParts * 4);
     m.row = (int *)p;
@@ -106,11 +108,22 @@ __device__ __forceinline__ int wave_add(int v)
     return v;
 }
 
+// A row whose gradient q (over the largest row's) is small has its G as two halves times 2^-row_exp(q) as well, for dH: a row of dH is a sum of
+// its own G.  dW and db, whose sums run over the rows, take G as it is formed again then (small_peak).
+constexpr float kSmallRow = 0x1p-8f; // (beside q of 1 and with 2^-39 of it lost: 2^-31 of a row's largest)
+__device__ __forceinline__ int row_exp(float q)
+{
+    int e = 0;
+    if (q != 0.f && fabsf(q) < kSmallRow) frexpf(q, &e);
+    return e;
+}
+
 // Largest finite magnitude of H (rows that count) and of W, a part from every block.  Bound by reading: 1531 x 1001 and 50257 x 1001
 // float, 207 MB, in 43 us (4.8 TB/s).
 __global__ void __launch_bounds__(256) top_kernel(const float *__restrict__ H, long ld_h, long T, const float *__restrict__ W, long ld_w, long V,
-                                                  long D, const Counts counts, int blocks_h, float *__restrict__ top)
+                                                  long D, const Counts counts, int blocks_h, float *__restrict__ top, int *__restrict__ uneven)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *uneven = 0;
     const bool is_h = (int)blockIdx.x < blocks_h;
     const int block = is_h ? blockIdx.x : blockIdx.x - blocks_h, blocks = is_h ? blocks_h : gridDim.x - blocks_h;
     const float *x = is_h ? H : W;
@@ -309,7 +322,9 @@ template <class K> __device__ __forceinline__ void pack_rows(const PackRows &p, 
                 p.meta.label[j] = (int)counts.labels[t];
                 if (p.gloss) {
                     const float l = p.lse[t];
-                    p.meta.q[j] = c > 0.f ? p.gloss[t] / c : p.gloss[t];
+                    const float q = c > 0.f ? p.gloss[t] / c : p.gloss[t];
+                    p.meta.q[j] = q;
+                    if (K::kSplit && row_exp(q) != 0) *p.meta.uneven = 1;
                     // a row whose classes are all masked has no distribution: its probabilities are zeros
                     p.meta.lse[j] = l == -INFINITY ? INFINITY : l;
                 }
@@ -531,7 +546,7 @@ __device__ __forceinline__ float rest_of(float g)
 // ---- Classes that no row thinks probable.  dW and db of a class are sums of its own G, so what 2^-39 of the largest G does not hold would
 // be all of a class whose G lies down there.  The pass that forms G as two halves leaves every class's largest |G|; where that is below 2^-16, the
 // class's G is formed once more, times a power of two of its own, for dW and db (dH has G as it was first: there a row's G are added
-// up, improbable beside probable ones).  Tiles without such a class end at once.  Both passes of 512 x 512 x 1500 and 1000 x 1001 x 50257:
+// up, improbable beside probable ones).  So is all of G where rows' gradients differ much (row_exp).  Tiles without such a class end at once.  Both passes of 512 x 512 x 1500 and 1000 x 1001 x 50257:
 // 51 and 1610 us without all this, 58 and 1640 where no class is improbable, 65 and 1950 where all tiles are formed again.
 constexpr float kSmallPeak = 0x1p-16f;
 __device__ __forceinline__ bool small_peak(uint32_t peak)
@@ -589,7 +604,10 @@ template <class K, bool AGAIN = false> struct Grad : Ending {
         bool rests;
         uint32_t *peak;   // of two halves: [classes], raised (AGAIN: read)
     };
-    static __device__ __forceinline__ bool wanted(const Params &e, int first, int count, int lane) { return any_small_peak(e.peak, first, count, lane); }
+    static __device__ __forceinline__ bool wanted(const Params &e, int first, int count, int lane)
+    {
+        return *e.meta.uneven || any_small_peak(e.peak, first, count, lane);
+    }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
         const int ze = K::kSplit ? -(e.meta.exps[0] + e.meta.exps[1]) : 0;
@@ -605,6 +623,8 @@ template <class K, bool AGAIN = false> struct Grad : Ending {
             const int label = e.meta.label_of(m) - e.v0;
             const bool in = label > Meta::kOut / 2;
             const float q_row = e.meta.q_of(m, largest), lse = e.meta.lse_of(m);
+            const int q_exp = kPeaks ? row_exp(q_row) : 0;
+            const float q_stored = kPeaks ? ldexpf(q_row, kStoreG - q_exp) : q_row;
             constexpr bool kRests = K::kG == Fmt::kBf16 && MI * NI == 1; // (few rows take the smallest tiles)
             float kept[kRests ? 16 : 1];
 #pragma unroll
@@ -617,10 +637,10 @@ template <class K, bool AGAIN = false> struct Grad : Ending {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float z = (K::kSplit ? ldexpf(acc[i][j][q * 4 + k], ze) : acc[i][j][q * 4 + k]) + bias[k];
-                        const float x = q_row * (__builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f));
-                        const float stored = AGAIN ? ldexpf(x, kStoreG - peak_exp(e.peak[min(n + k, p.N - 1)])) : K::kSplit ? x * (float)(1 << kStoreG) : x;
+                        const float x = __builtin_amdgcn_exp2f((z - lse) * kLog2e) - (n + k == label ? 1.f : 0.f);
+                        const float stored = AGAIN ? ldexpf(q_row * x, kStoreG - peak_exp(e.peak[min(n + k, p.N - 1)])) : q_stored * x;
                         g[k] = n + k < p.N && in ? stored : 0.f;
-                        if constexpr (kPeaks) peaks[j][q * 4 + k] = fmaxf(peaks[j][q * 4 + k], fabsf(x));
+                        if constexpr (kPeaks) peaks[j][q * 4 + k] = fmaxf(peaks[j][q * 4 + k], fabsf(q_row * x));
                         if constexpr (kRests) kept[q * 4 + k] = g[k];
                     }
                     Block::put(p.lds, p.lane, j, q, g);
@@ -700,7 +720,7 @@ template <class K> struct OutW : Ending {
     };
     static __device__ __forceinline__ const void *operand_a(const Params &e, const void *a, int first, int count, int lane)
     {
-        return e.again && any_small_peak(e.peak, first, count, lane) ? e.again : a;
+        return e.again && (*e.meta.uneven || any_small_peak(e.peak, first, count, lane)) ? e.again : a;
     }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -736,7 +756,9 @@ template <class K> struct OutH : Ending {
             const bool rests = K::kG == Fmt::kBf16 && e.rests; // (32 rows and their rests: neighbouring waves of one tile)
             // a row that is left out has zeros in G where nothing is compacted, and a zero times an infinite weight is none
             const int m = m0 + (p.lane & 31), row = rests && m >= kLoRow ? m - kLoRow : m;
-            put_scaled(acc, i, s, p, e.meta.direct && row < e.meta.T && e.meta.label_of(row) == Meta::kOut);
+            Factor<K::kSplit> of_row = s;
+            if (K::kSplit) of_row.e += row_exp(e.meta.q[min(m, p.M - 1)]);
+            put_scaled(acc, i, of_row, p, e.meta.direct && row < e.meta.T && e.meta.label_of(row) == Meta::kOut);
             if (rests) {
                 __syncthreads();
                 if (m0 >= kLoRow) return;
@@ -837,7 +859,7 @@ template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, i
     const float largest = p.meta.largest(lane);
     // 8 chunks of columns by 8 rows to a wave
     const int chunk = block * 8 + (lane & 7), n = chunk * 8;
-    const char *G = K::kSplit && p.again && any_small_peak(p.peak, block * 64, min(p.V - block * 64, 64), lane) ? p.again : p.G;
+    const char *G = K::kSplit && p.again && (*p.meta.uneven || any_small_peak(p.peak, block * 64, min(p.V - block * 64, 64), lane)) ? p.again : p.G;
     float s[8] = {};
     if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
@@ -1153,7 +1175,7 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
     constexpr int kThreads = 256 / kGradRows<K>; // of a row
     const int lane = threadIdx.x & 63, m = blockIdx.x * kGradRows<K> + threadIdx.x / kThreads, n = (blockIdx.y * kThreads + threadIdx.x % kThreads) * 4;
     const float largest = meta.largest(lane);
-    if (AGAIN && !any_small_peak(peak, blockIdx.y * 64, min(V - (int)blockIdx.y * 64, 64), lane)) return;
+    if (AGAIN && !*meta.uneven && !any_small_peak(peak, blockIdx.y * 64, min(V - (int)blockIdx.y * 64, 64), lane)) return;
     float g[4] = {0.f, 0.f, 0.f, 0.f};
     if (m < meta.rows() && n < ((V + 7) & ~7)) {
         const int label = meta.label_of(m);
@@ -1169,6 +1191,10 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
         if (AGAIN) {
             const float v[4] = {ldexpf(g[0], -peak_exp(peak[min(n, V - 1)])), ldexpf(g[1], -peak_exp(peak[min(n + 1, V - 1)])),
                                 ldexpf(g[2], -peak_exp(peak[min(n + 2, V - 1)])), ldexpf(g[3], -peak_exp(peak[min(n + 3, V - 1)]))};
+            store_gradient<K>(G + (long)m * ld_g, n, v);
+        } else if (K::kSplit) {
+            const int e = -row_exp(q);
+            const float v[4] = {ldexpf(g[0], e), ldexpf(g[1], e), ldexpf(g[2], e), ldexpf(g[3], e)};
             store_gradient<K>(G + (long)m * ld_g, n, v);
         } else {
             store_gradient<K>(G + (long)m * ld_g, n, g);
@@ -1415,7 +1441,7 @@ template <class K> class Loss {
         parts_h = cdiv(g.T, 4) > kMaxParts ? kMaxParts : cdiv(g.T, 4);
         parts_w = cdiv(g.V, 4) > kMaxParts ? kMaxParts : cdiv(g.V, 4);
         hipLaunchKernelGGL(top_kernel, dim3(parts_h + parts_w), dim3(256), 0, st, (const float *)H, g.ld_h, g.T, (const float *)W, g.ld_w, g.V, g.D,
-                           meta.counts, parts_h, meta.top);
+                           meta.counts, parts_h, meta.top, meta.uneven);
         return hipGetLastError();
     }
 

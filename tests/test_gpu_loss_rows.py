@@ -84,3 +84,37 @@ def test_classes_kept_down_by_their_bias(shape):
     got = run(t)
     check_rows(t, got)
     assert bool((got["dW"][-3:] == 0).all()) and bool((got["db"][-3:] == 0).all())
+
+
+@pytest.mark.parametrize("shape", [(40, 64, 300), (200, 64, 300), (200, 2048, 700), (1000, 256, 5000), (1200, 640, 12000)])
+def test_gradients_of_rows_over_twelve_orders(shape):
+    """dH row by row: a row's own gradient scales its row, whatever the others' are."""
+    t = make(*shape, B.F32, seed=11)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    order = torch.randperm(shape[0], generator=g, device=DEV)
+    t["gloss"] = (10.0 ** torch.linspace(-12, 0, shape[0], device=DEV))[order] * (torch.randint(0, 2, (shape[0],), generator=g, device=DEV) * 2 - 1)
+    t["gloss"][3] = 0
+    check_rows(t, run(t))
+    for want in (("dH",), ("dH", "db"), ("dW",)):
+        check_rows(t, gradients(t, want), want)
+
+
+def test_rows_and_classes_in_pieces():
+    t = make(2048, 64, 140000, B.F32, seed=3)
+    assert " 1 pieces" not in B.cac_loss_describe_plan(t["desc"], B.LOSS_BWD)
+    t["b"][70000:70400] = -40
+    t["b"][139000:] = -40
+    t["labels"] %= 70000
+    t["gloss"][5] = 1e-9
+    t["gloss"][77] = 1e-6
+    got, want = run(t), reference(t)
+    low = torch.cat([torch.arange(70000, 70400), torch.arange(139000, 140000)]).to(DEV)
+    for k in ("dW", "db"):
+        for some in (low, torch.arange(0, 70000, 7, device=DEV)):
+            a, b = got[k][some].double(), want[k][some]
+            # (probabilities off by 2^-24 of 8 logits of up to 10, an lse of 12 and 3 differences of up to 62)
+            part = 2.0 ** -24 * (8 * 12 + 2 * 15 + 3 * 62)
+            assert float(((a - b).reshape(len(some), -1).norm(dim=1) / b.reshape(len(some), -1).norm(dim=1)).max()) <= 16 * part, k
+    for row in (5, 77, 1000):
+        assert float((got["dH"][row].double() - want["dH"][row]).norm() / want["dH"][row].norm()) <= 2e-5, row
