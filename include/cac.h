@@ -283,17 +283,19 @@ int cac_grad_cosine(const cac_desc *d, const void *dW_a, const void *dW_b, void 
 /* Softmax cross entropy of a linear classifier: z = H W^T + b, H [T, D] (a row for every image, pixel or token),
  * W [V, D] (a row for every class), b [V];
  *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,labels[t].
- * The logits are never kept: they pass through registers, and in the backward pass their gradients through the
- * workspace, a piece of the classes at a time.
+ * The logits are never kept: they pass through registers, and in the backward pass, which forms them once more, their gradients
+ * through the workspace, a piece of the classes at a time (of up to 1 GiB: all of them where they take no more).
  *   - A row whose label is ignore_index, or is no class (below 0, V or more), is left out: its loss and lse are 0, its
  *     gradient is 0, and its H is not read into any sum, whatever it holds.
  *   - A class can be masked by b = -infinity.  The loss of a row whose label is masked is +infinity (its gradient is
  *     that of the formula, probability 0 - 1); a row whose classes are all masked has probabilities of 0.
- *   - dtype CAC_F32: operands are multiplied as pairs of half-precision numbers, which keep 23 bits; numbers below
- *     2^-28 of their matrix's largest keep fewer.  An infinity or NaN in H or W comes out as NaN in every row and
- *     gradient that it meets.  Few rows, and short forward passes, are multiplied as floats.  dtype CAC_BF16: the logits' gradients are rounded
- *     to bfloat16 (times the row's gradient over the largest row's) before they are multiplied with H and W, of up to 32
- *     rows to two such numbers.  Sums are float in both; loss, lse and gloss are float.
+ *   - dtype CAC_F32: H and W are multiplied as pairs of half-precision numbers.  A pair keeps 23 bits of a number down to 2^-15 of
+ *     its matrix's largest; below that it is off by up to 2^-38 of the largest.  (The gradients of the logits are held so too, each
+ *     row's for dH and each class's for dW and db beside the largest of its own.)  An infinity or NaN in H or W comes out as NaN in every
+ *     row and gradient that it meets.  Few rows, and short forward passes, are multiplied as floats.
+ *   - dtype CAC_BF16: the logits' gradients are rounded to bfloat16 (times the row's gradient over the largest row's) before they
+ *     are multiplied with H and W and summed for db, of up to 32 rows to two such numbers.
+ *   - Sums are float in both; loss, lse and gloss are float.
  * What is written shares no memory with anything else that a call is given, but for dH, which may take the place of dense H. */
 typedef enum cac_loss_op { CAC_LOSS_FWD = 0, CAC_LOSS_BWD = 1 } cac_loss_op;
 
@@ -323,8 +325,8 @@ int cac_loss_bwd(const cac_loss_desc *d, const void *H, const void *W, const voi
  * convolution's dW as [C_out][C_in * R * S].  From X = U / (|U|_F + 1e-7), `steps` times:
  *   A = X X^T,  X <- a X + (b A + c A A) X,   (a, b, c) = (3.4445, -4.7750, 2.0315),
  * which brings every singular value near 1 and keeps the singular vectors.  Both dtypes are computed as pairs of
- * half-precision numbers (23 bits) with float sums; CAC_BF16 rounds the result once.  A matrix of zeros stays zero;
- * an infinity or NaN comes out as NaN in the matrix that it stands in. */
+ * half-precision numbers (23 bits of numbers down to 2^-14 of |U|_F, those below it off by up to 2^-37 of it) with float sums; CAC_BF16
+ * rounds the result once.  A matrix of zeros stays zero; an infinity or NaN comes out as NaN in the matrix that it stands in. */
 typedef enum cac_muon_op { CAC_MUON_ORTHOGONALISE = 0, CAC_MUON_STEP = 1 } cac_muon_op;
 
 typedef struct cac_muon_desc {

@@ -2,6 +2,7 @@
 
 The tolerance is that of the loss's float gradients elsewhere: sums of products of 22 bits and more."""
 import pytest
+import torch
 
 from paper_2409_11902_amd import binding as B
 from test_gpu_loss import make, reference, run
@@ -21,3 +22,21 @@ def test_results_far_from_one_keep_their_bits(T):
         for k, s in (("dW", scale_h * scale_g), ("dH", scale_w * scale_g), ("db", scale_g)):
             a, b = got[k].double() / s, want[k] / s
             assert float((a - b).norm() / b.norm()) <= 2e-5, (k, scale_h, scale_w, scale_g)
+
+
+@pytest.mark.parametrize("large", [2.0 ** 10, 2.0 ** 20, 2.0 ** 30])
+def test_operands_beside_a_large_one(large):
+    """Numbers of H and W are off by 2^-24 of themselves and, held as two halves, by 2^-38 of their matrix's largest."""
+    t = make(200, 512, 20000, B.F32, seed=6)
+    t["H"][7] *= large
+    t["W"][11] *= large
+    t["labels"] = torch.where(t["labels"] == 11, 12, t["labels"])
+    t["b"][11] = -torch.inf
+    got, want = run(t), reference(t)
+    h, w = t["H"].double().abs(), t["W"].double().abs()
+    rows = torch.arange(200, device=h.device) != 7
+    classes = torch.arange(20000, device=h.device) != 11
+    z = 2.0 ** -38 * (h.max() * w[classes].sum(1).max() + w.max() * h[rows].sum(1).max())   # a logit's error for the halves
+    z = float(z) + 2.0 ** -23 * 8 * float((h[rows] @ w[classes].t()).max())                  # ... and float's
+    for k in ("loss", "lse"):
+        assert float((got[k].double() - want[k])[rows].abs().max()) <= 2 * z + 2.0 ** -22 * float(want[k][rows].abs().max()), k
