@@ -284,7 +284,7 @@ int cac_grad_cosine(const cac_desc *d, const void *dW_a, const void *dW_b, void 
  * W [V, D] (a row for every class), b [V];
  *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,labels[t].
  * The logits are never kept: they pass through registers, and in the backward pass, which forms them once more, their gradients
- * through the workspace, a piece of the classes at a time (of up to 1 GiB: all of them where they take no more).
+ * through the workspace, a piece of the classes at a time (of up to 1 GiB, of float up to 2: all of them where they take no more).
  *   - A row whose label is ignore_index, or is no class (below 0, V or more), is left out: its loss and lse are 0, its
  *     gradient is 0, and its H is not read into any sum, whatever it holds.
  *   - A class can be masked by b = -infinity.  The loss of a row whose label is masked is +infinity (its gradient is

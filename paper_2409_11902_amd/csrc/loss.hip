@@ -1246,8 +1246,9 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->dp = (g.D + 7) / 8 * 8;
     const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
     p->row_bytes = e * p->dp;
-    // A piece's G and packed weights take 1 GiB at most, the weights alone half of that, or 4096 classes.  Smaller pieces cost more ends
-    // of launches and more sums of dH to add to: 4096 x 1024 x 32000 float 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one;
+    // A piece's G and packed weights take 1 GiB at most, the weights alone half of that, or 4096 classes; where one launch forms dW and dH of
+    // float, G as it is formed again lies beside it (apart, which would spare that, 4000 x 64 x 20000 takes 535 us and not 468: db's sums
+    // have nothing to run beside).  Smaller pieces cost more ends of launches and more sums of dH to add to: 4096 x 1024 x 32000 float 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one;
     // 2048 x 1024 x 200000 float forward 2.88 ms of 256 MiB, 2.75 of 512, 2.66 in one.
     const long per_class = (backward ? g.T * e : 0) + (p->pack_w ? p->row_bytes : 0);
     long piece = per_class ? ((backward ? 1024L : 512L) << 20) / per_class / 256 * 256 : g.V;
