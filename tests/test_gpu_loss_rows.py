@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2409_11902_amd import binding as B
-from test_gpu_loss import DEV, make, reference, run
+from test_gpu_loss import DEV, make, reference, rel, run
 
 pytestmark = pytest.mark.gpu
 
@@ -118,3 +118,72 @@ def test_rows_and_classes_in_pieces():
             assert float(((a - b).reshape(len(some), -1).norm(dim=1) / b.reshape(len(some), -1).norm(dim=1)).max()) <= 16 * part, k
     for row in (5, 77, 1000):
         assert float((got["dH"][row].double() - want["dH"][row]).norm() / want["dH"][row].norm()) <= 2e-5, row
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("T", [6, 80, 300])
+def test_classes_masked_by_the_lowest_number(T, dtype):
+    """The lowest number plus a logit is the lowest number again: every class is as probable, and all is finite."""
+    t = make(T, 64, 200, dtype, seed=9)
+    t["b"][:] = torch.finfo(t["b"].dtype).min
+    got = run(t)
+    for k in ("loss", "lse", "dH", "dW", "db"):
+        assert bool(torch.isfinite(got[k]).all()), k
+    t["b"][:] = 0
+    t["b"][100:] = torch.finfo(t["b"].dtype).min
+    t["labels"] %= 100
+    got = run(t)
+    if dtype == B.F32:
+        check_rows(t, got)
+    assert bool((got["dW"][100:] == 0).all()) and bool((got["db"][100:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("T", [24, 120, 300])
+def test_gradient_against_differences_along_itself(T, dtype):
+    """The loss rises by the sum of |gradient| a unit along the gradient's signs: a gradient of another direction does not tell that slope.
+
+    Steps are exact: operands lie on a grid of 2^-5 below 1, and all of them move by 2^-9 (float) or a twentieth of H and W by 2^-5 (bfloat16).
+    That moves logits by less than a fifth: a third derivative's part is below 0.04 / 6 of the slope, a bfloat16 gradient's roundings
+    another 2^-8, and the losses (of up to 10, times up to 1.1) are rounded twice each."""
+    t = make(T, 64, 150, dtype, seed=12)
+    t["gloss"] = t["gloss"].abs() + 0.1
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    for name in ("H", "W", "b"):
+        t[name] = ((t[name].float() * 32).round() / 32).clamp(-0.9375, 0.9375).to(t[name].dtype)
+    got = run(t)
+    for name, grad in (("H", "dH"), ("W", "dW"), ("b", "db")):
+        base, slope = t[name].float(), got[grad].float()
+        if dtype == B.F32:
+            step = slope.sign() * 2.0 ** -9
+        else:
+            some = torch.rand(base.shape, generator=g, device=DEV) < (0.05 if base.dim() == 2 else 1.0)
+            step = torch.where(some, slope.sign() * 2.0 ** -5, 0.0)
+        sums = []
+        for sign in (1, -1):
+            moved = dict(t)
+            moved[name] = (base + sign * step).to(t[name].dtype)
+            assert torch.equal(moved[name].float(), base + sign * step)
+            sums.append(float((run(moved)["loss"].double() * t["gloss"].double()).sum()))
+        want = float((slope.double() * 2 * step.double()).sum())
+        assert want > 0
+        assert abs(sums[0] - sums[1] - want) <= (0.04 / 6 + 2.0 ** -8) * want + T * 11 * 2.0 ** -22, (name, sums[0] - sums[1], want)
+
+
+@pytest.mark.parametrize("sharp", [1, 3])
+@pytest.mark.parametrize("shape", [(20, 256, 900), (64, 256, 4000), (256, 512, 21841), (700, 128, 333)])
+def test_labels_of_the_models_own_distribution(shape, sharp):
+    """A label that the model thinks probable has a gradient of any size, where one at random has one near -1, which bfloat16 holds exactly.
+
+    G and the result are rounded to bfloat16, by up to 2^-8 of themselves each, and terms are as independent as their errors are."""
+    t = make(*shape, B.BF16, seed=4)
+    t["W"] *= sharp
+    z = t["H"].float() @ t["W"].float().t() + (t["b"].float() if t["b"] is not None else 0)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    t["labels"] = torch.multinomial(z.softmax(1), 1, generator=g).squeeze(1)
+    t["gloss"][:] = 1.0 / shape[0]
+    got, want = run(t), reference(t)
+    for k in ("dH", "dW", "db"):
+        assert rel(got[k], want[k]) <= 2.0 ** -7, k
