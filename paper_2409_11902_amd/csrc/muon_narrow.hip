@@ -74,9 +74,10 @@ __device__ __forceinline__ s16x8 down(const unsigned char *m, int rs, int col0, 
     r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)(base + place(row + 4, chunk, rs) + at));
     return r.v;
 }
-__device__ __forceinline__ void three(s16x8 ah, s16x8 al, s16x8 bh, s16x8 bl, f32x16 *acc)
+// A product is the sum of those with lo and then of the others: the first are 2^-11 of it and round by as much less (64 x 64: 1.4e-6 off, as
+// float arithmetic is, and 1.7e-6 term by term).
+__device__ __forceinline__ void two(s16x8 ah, s16x8 al, s16x8 bh, s16x8 bl, f32x16 *acc)
 {
-    *acc = product<Split>(bh, ah, *acc);
     *acc = product<Split>(bl, ah, *acc);
     *acc = product<Split>(bh, al, *acc);
 }
@@ -128,10 +129,16 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
     auto gram = [&]() { // into the first group's s; A is free
         s = zeros();
         if (W > 64) asm volatile("" : "+v"(lane));
-#pragma unroll 2
-        for (int kk = 0; kk < W / 16 / KG; ++kk) {
+        constexpr int kSteps = W / 16 / KG;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
             const int k = kk * KG + group;
-            three(along(X, RS, wm * 32, k, 0, lane), along(X, RS, wm * 32, k, 1, lane), along(X, RS, wn * 32, k, 0, lane), along(X, RS, wn * 32, k, 1, lane), &s);
+            two(along(X, RS, wm * 32, k, 0, lane), along(X, RS, wm * 32, k, 1, lane), along(X, RS, wn * 32, k, 0, lane), along(X, RS, wn * 32, k, 1, lane), &s);
+        }
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+            const int k = kk * KG + group;
+            s = product<Split>(along(X, RS, wn * 32, k, 0, lane), along(X, RS, wm * 32, k, 0, lane), s);
         }
         if (KG == 1) return;
         f32x4 *sums = (f32x4 *)A + (wave & 3) * 256 + lane;
@@ -340,7 +347,9 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
             f32x16 acc = zeros();
 #pragma unroll
             for (int k = 0; k < kSide / 16; ++k)
-                three(along(A, 256, wm * 32, k, 0, lane), along(A, 256, wm * 32, k, 1, lane), along(A, 256, wn * 32, k, 0, lane), along(A, 256, wn * 32, k, 1, lane), &acc);
+                two(along(A, 256, wm * 32, k, 0, lane), along(A, 256, wm * 32, k, 1, lane), along(A, 256, wn * 32, k, 0, lane), along(A, 256, wn * 32, k, 1, lane), &acc);
+#pragma unroll
+            for (int k = 0; k < kSide / 16; ++k) acc = product<Split>(along(A, 256, wn * 32, k, 0, lane), along(A, 256, wm * 32, k, 0, lane), acc);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int i = wm * 32 + (lane & 31), j = wn * 32 + q * 8 + (lane >> 5) * 4;
@@ -362,7 +371,13 @@ template <typename TG, typename TO, bool UPDATE, int W, int KG> __global__ void 
             const s16x8 ph = along(B, 256, rb, k, 0, lane), pl = along(B, 256, rb, k, 1, lane);
 #pragma unroll
             for (int b = 0; b < kJobs; ++b)
-                three(ph, pl, down(X, RS, (cb + b * kApart) * 32, k, 0, lane), down(X, RS, (cb + b * kApart) * 32, k, 1, lane), &y[b]);
+                two(ph, pl, down(X, RS, (cb + b * kApart) * 32, k, 0, lane), down(X, RS, (cb + b * kApart) * 32, k, 1, lane), &y[b]);
+        }
+#pragma unroll
+        for (int k = 0; k < kSide / 16; ++k) {
+            const s16x8 ph = along(B, 256, rb, k, 0, lane);
+#pragma unroll
+            for (int b = 0; b < kJobs; ++b) y[b] = product<Split>(down(X, RS, (cb + b * kApart) * 32, k, 0, lane), ph, y[b]);
         }
         if (step + 1 == p.steps) {
             const float scale = ldexpf((UPDATE ? -p.lr : 1.f) * kTake * kTake * ratio, -lift);
