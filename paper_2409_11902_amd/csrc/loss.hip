@@ -8,8 +8,8 @@
 // Rows that are left out (label equal to ignore_index, or no class) are taken out of H when it is copied into the workspace: no
 // product reads them, whatever stands there, and the products get shorter by them.  Few rows, and short forward passes, stay where
 // they are: rows that are left out are loaded as zeros.
-// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float,
-// or as floats where there are few rows.  Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the
+// Sums are of 32 bits; G is rounded to bfloat16 for bfloat16 operands (its products' operands are), and held as two halves for float
+// (each row's beside the row's largest for dH, each class's beside the class's for dW and db), or as floats where there are few rows.  Of up to 32 bfloat16 rows, whose gradients may hang on a single number of G, what the
 // rounding took away is kept as 32 further rows of G: a tile has room for 64 rows, so that products of them cost nothing.
 #include "mm_core.h"
 #include "train_ends.h"
@@ -1227,7 +1227,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // passes that compact rows, find the largest numbers and split everything beforehand.  Packed beforehand and as they lie, both passes:
     //   bfloat16  16 x 256 x 300  28 and 23 us    64 x 700 x 5000  53 and 40 us    64 x 2048 x 30000  152 and 106 us
     //   float     40 x 256 x 300  39 and 34 us    64 x 2048 x 600  52 and 38 us    64 x 2048 x 30000  564 and 365 us
-    //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  77 and 81 us   128 x 1001 x 20000  240 and 281 us
+    //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  72 and 76 us   128 x 1001 x 20000  222 and 256 us
     // Forward passes of float read a large operand once so, where the other has few rows, and small ones save two launches: 128 x 2048 x
     // 30000  234 and 151 us, 12000 x 4000 x 64  193 and 88, 300 x 256 x 300  18 and 13, 1000 x 512 x 1000  25 and 19, 2000 x 1000 x 1000  44 and 47.
     // Short ones of bfloat16 save the launch that packs, though rows that are left out are multiplied then (512 x 1024 x 8000
@@ -1248,8 +1248,8 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->row_bytes = e * p->dp;
     // A piece's G and packed weights take 1 GiB at most, the weights alone half of that, or 4096 classes; where one launch forms dW and dH of
     // float, G as it is formed again lies beside it (apart, which would spare that, 4000 x 64 x 20000 takes 535 us and not 468: db's sums
-    // have nothing to run beside).  Smaller pieces cost more ends of launches and more sums of dH to add to: 4096 x 1024 x 32000 float 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one;
-    // 2048 x 1024 x 200000 float forward 2.88 ms of 256 MiB, 2.75 of 512, 2.66 in one.
+    // have nothing to run beside).  Smaller pieces cost more ends of launches and more sums of dH to add to: 4096 x 1024 x 32000 float
+    // 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one; 2048 x 1024 x 200000 float forward 2.88 ms of 256 MiB, 2.75 of 512, 2.66 in one.
     const long per_class = (backward ? g.T * e : 0) + (p->pack_w ? p->row_bytes : 0);
     long piece = per_class ? ((backward ? 1024L : 512L) << 20) / per_class / 256 * 256 : g.V;
     if (piece < 4096) piece = 4096;
@@ -1267,7 +1267,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->w = choose(f, piece, g.D, 1, g.T, false, 1);
     p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
-    // end where compute units run out of work (512 x 512 x 1500 float 75 us apart, 61 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
+    // end where compute units run out of work (512 x 512 x 1500 float 72 us apart, 57 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
     // 1024 x 2048 x 16000 341 and 379).
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
     p->pair = backward && (p->few || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));

@@ -11,7 +11,8 @@
 //           2e-8 of it in the mean, so sums come out as float arithmetic has them, from three products at 16 times the
 //           float instruction's rate.  A row of memory holds 8 hi, 8 lo, 8 hi, ...: a chunk of 16 bytes of one kind after one of
 //           the other, so that both formats are staged alike, 128 bytes of K to a row and pass.  Numbers are stored times a
-//           power of two that the caller takes out again, which keeps lo out of the subnormal range.
+//           power of two that the caller takes out again: lo is subnormal of numbers below 2^-15 of those that are stored as 2^13 and more, and
+//           they are off by up to 2^-25 as stored.
 //
 //   Raw   : floats as they lie, by the float instruction.  It needs no powers of two and no pass beforehand, and is what products of few
 //           rows take, whose time is that of reading the other operand once.  A chunk holds 4 numbers, two of them the 8 that a
@@ -336,11 +337,12 @@ template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU> struc
     static constexpr int kPerSimd = PER_CU * kWaves / 4; // waves that registers are shared by
 };
 // Measured, with what bounds them (a library's product of 8192 cubed reaches 1.23 PFLOP/s in bfloat16 and 1.33 in half precision on the same
-// card, 1.33 / 3 = 0.44 for three of them; bare matrix instructions 1.7):
-typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256: power.  7373 x 131072 x 4096 bfloat16 1.07 PFLOP/s; 4096 cubed Split 0.36
+// card, 1.33 / 3 = 0.44 for three of them; bare matrix instructions 1.7).  Under the two largest tiles the clock falls to 1.8 to 2.0 GHz of 2.4, and
+// matrix instructions are on 54 to 60 % of its cycles where sums are long (38 % of 1024 terms); LDS bank conflicts take 2 % at most under any:
+typedef Shape<2, 4, 4, 2, 128, 2, 1> Big;    // 256 x 256: the clock.  7373 x 131072 x 4096 bfloat16 1.07 PFLOP/s; 4096 cubed Split 0.36
 typedef Shape<2, 6, 3, 1, 128, 3, 1> Wide;   // 192 x 192: as Big, where its tiles fill the compute units better.  4096 cubed, symmetric, Split 0.31
 typedef Shape<2, 4, 2, 1, 128, 2, 2> Middle; // 128 x 128: what a compute unit takes in, 35 to 50 KB a us.  512 x 4608 x 512, three of them, Split 0.25
-typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64: latency.  A pass takes 0.27 us alone and 0.2 to 0.3 with two others beside it
+typedef Shape<2, 2, 1, 1, 128, 3, 3> Small;  // 64 x 64: latency (matrix instructions on 3 to 20 % of cycles).  A pass takes 0.27 us alone and 0.2 to 0.3 with two others beside it
 typedef Shape<1, 4, 1, 1, 128, 3, 2> Low;    // 32 x 128, for few rows of floats: reading b.  16 x 100000 x 1024 3.0 to 3.7 TB/s
 
 // All but the N youngest loads have arrived, the fragments asked for are in registers, and every wave of the workgroup says so.

@@ -187,3 +187,37 @@ def test_labels_of_the_models_own_distribution(shape, sharp):
     got, want = run(t), reference(t)
     for k in ("dH", "dW", "db"):
         assert rel(got[k], want[k]) <= 2.0 ** -7, k
+
+
+def test_float_gradients_captured_in_a_graph():
+    """G formed again for some classes, for a row, and not at all: every replay is the eager result, whatever the workspace held."""
+    for shape, low, small_row in (((300, 64, 700), True, False), ((300, 64, 700), False, True), ((300, 64, 700), False, False), ((900, 512, 9000), True, True)):
+        t = make(*shape, B.F32, out=0.1, seed=3)
+        d = t["desc"]
+        t["gloss"] = t["gloss"].abs() + 0.1
+        if low:
+            t["b"] = torch.zeros(shape[2], device=DEV)
+            d.has_bias = 1
+            t["b"][100:130] = -30
+        if small_row:
+            t["gloss"][5] = 1e-7
+        want = {k: v.clone() for k, v in run(t).items()}
+        out = {k: torch.empty_like(v) for k, v in want.items()}
+        ws = torch.empty(max(B.cac_loss_workspace_size(d, op) for op in (B.LOSS_FWD, B.LOSS_BWD)), dtype=torch.uint8, device=DEV)
+
+        def step():
+            B.cac_loss_fwd(d, t["H"], t["W"], t["b"], t["labels"], out["loss"], out["lse"], ws)
+            B.cac_loss_bwd(d, t["H"], t["W"], t["b"], t["labels"], out["lse"], t["gloss"], out["dH"], out["dW"], out["db"], ws)
+
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        for fill in (255, 0, 64):
+            for v in out.values():
+                v.fill_(7)
+            ws.fill_(fill)
+            graph.replay()
+            torch.cuda.synchronize()
+            for k in want:
+                assert torch.equal(out[k], want[k]), (shape, k)
