@@ -547,7 +547,7 @@ __device__ __forceinline__ float rest_of(float g)
 // be all of a class whose G lies down there.  The pass that forms G as two halves leaves every class's largest |G|; where that is below 2^-16, the
 // class's G is formed once more, times a power of two of its own, for dW and db (dH has G as it was first: there a row's G are added
 // up, improbable beside probable ones).  So is all of G where rows' gradients differ much (row_exp).  Tiles without such a class end at once.  Both passes of 512 x 512 x 1500 and 1000 x 1001 x 50257:
-// 51 and 1610 us without all this, 58 and 1640 where no class is improbable, 65 and 1950 where all tiles are formed again.
+// 52 and 1600 us without all this, 55 and 1620 where no class is improbable, 62 and 1920 where all tiles are formed again.
 constexpr float kSmallPeak = 0x1p-16f;
 __device__ __forceinline__ bool small_peak(uint32_t peak)
 {
@@ -569,22 +569,23 @@ __device__ __forceinline__ bool any_small_peak(const uint32_t *peak, int first, 
     return __any(any);
 }
 // (numbers are not negative, so that they are ordered as their bits are; the largest does not depend on the order of arrival)
-__device__ __forceinline__ void raise_peak(uint32_t *peak, float v)
+__device__ __forceinline__ void raise_peak(uint32_t *peak, float v) { atomicMax(peak, __float_as_uint(v)); }
+// of 2 N numbers N to a lane, the larger of its own and of the lane's 2 N apart
+template <int N> __device__ __forceinline__ void share_out(float (&v)[16], int lane)
 {
-    const uint32_t bits = __float_as_uint(v);
-    if (bits > __hip_atomic_load(peak, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(peak, bits);
+    const bool up = lane & 2 * N;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = fmaxf(up ? v[k + N] : v[k], __shfl_xor(up ? v[k] : v[k + N], 2 * N, 64));
 }
 // of a wave's 32 NI columns: v[j][4 q + k] as C lies, largest of the wave's blocks of rows.  Lanes that hold rows of the same columns share the numbers out.
 template <int NI> __device__ __forceinline__ void raise_peaks(uint32_t *peak, float (&v)[NI][16], const Place &p)
 {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-#pragma unroll
-        for (int n = 8; n > 0; n >>= 1) {
-            const bool up = p.lane & 2 * n;
-#pragma unroll
-            for (int k = 0; k < n; ++k) v[j][k] = fmaxf(up ? v[j][k + n] : v[j][k], __shfl_xor(up ? v[j][k] : v[j][k + n], 2 * n, 64));
-        }
+        share_out<8>(v[j], p.lane);
+        share_out<4>(v[j], p.lane);
+        share_out<2>(v[j], p.lane);
+        share_out<1>(v[j], p.lane);
         const float top = fmaxf(v[j][0], __shfl_xor(v[j][0], 1, 64));
         const int at = p.lane >> 1 & 15, n = p.n0 + j * 32 + (at >> 2) * 8 + (p.lane >> 5) * 4 + (at & 3);
         if (!(p.lane & 1) && n < p.N) raise_peak(peak + n, top);
@@ -1227,7 +1228,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     // passes that compact rows, find the largest numbers and split everything beforehand.  Packed beforehand and as they lie, both passes:
     //   bfloat16  16 x 256 x 300  28 and 23 us    64 x 700 x 5000  53 and 40 us    64 x 2048 x 30000  152 and 106 us
     //   float     40 x 256 x 300  39 and 34 us    64 x 2048 x 600  52 and 38 us    64 x 2048 x 30000  564 and 365 us
-    //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  72 and 76 us   128 x 1001 x 20000  222 and 256 us
+    //            128 x 1024 x 1000  52 and 40 us  128 x 700 x 5000  69 and 77 us   128 x 1001 x 20000  223 and 262 us
     // Forward passes of float read a large operand once so, where the other has few rows, and small ones save two launches: 128 x 2048 x
     // 30000  234 and 151 us, 12000 x 4000 x 64  193 and 88, 300 x 256 x 300  18 and 13, 1000 x 512 x 1000  25 and 19, 2000 x 1000 x 1000  44 and 47.
     // Short ones of bfloat16 save the launch that packs, though rows that are left out are multiplied then (512 x 1024 x 8000
@@ -1247,7 +1248,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     const int e = g.dtype == CAC_F32 ? 4 : 2; // bytes of a number, as it lies, in two halves, and of G
     p->row_bytes = e * p->dp;
     // A piece's G and packed weights take 1 GiB at most, the weights alone half of that, or 4096 classes; where one launch forms dW and dH of
-    // float, G as it is formed again lies beside it (apart, which would spare that, 4000 x 64 x 20000 takes 535 us and not 468: db's sums
+    // float, G as it is formed again lies beside it (apart, which would spare that, 4000 x 64 x 20000 takes 523 us and not 463: db's sums
     // have nothing to run beside).  Smaller pieces cost more ends of launches and more sums of dH to add to: 4096 x 1024 x 32000 float
     // 3.49 ms in pieces of 256 MiB, 3.08 of 1 GiB, 3.06 in one; 2048 x 1024 x 200000 float forward 2.88 ms of 256 MiB, 2.75 of 512, 2.66 in one.
     const long per_class = (backward ? g.T * e : 0) + (p->pack_w ? p->row_bytes : 0);
@@ -1267,7 +1268,7 @@ void plan_loss(const LossGeom &g, bool backward, LossPlan *p)
     p->w = choose(f, piece, g.D, 1, g.T, false, 1);
     p->h = choose(f, g.T, g.D, 1, piece, false, 128);
     // dW and dH together, in the smallest tiles, where both would take them anyway or there is little to multiply: one launch, and one
-    // end where compute units run out of work (512 x 512 x 1500 float 72 us apart, 57 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
+    // end where compute units run out of work (512 x 512 x 1500 float 68 us apart, 55 so; 1024 x 1024 x 8000 bfloat16 145 and 134,
     // 1024 x 2048 x 16000 341 and 379).
     const double work = 4.0 * g.T * g.D * piece * (p->split ? 3 : 1);
     p->pair = backward && (p->few || work < 7e10 || (p->w.shape == kSmall && p->h.shape == kSmall));
