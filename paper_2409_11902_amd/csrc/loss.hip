@@ -561,12 +561,20 @@ __device__ __forceinline__ int peak_exp(uint32_t peak)
     if (small_peak(peak)) frexpf(__uint_as_float(peak), &e);
     return e;
 }
-// of `count` classes, asked by a whole wave
-__device__ __forceinline__ bool any_small_peak(const uint32_t *peak, int first, int count, int lane)
+// Whether G of `count` classes is formed again: 1 or 0, asked by a whole wave.  (A number, which the compiler has to have: where this was a
+// condition of branches it left out the one that chooses between two places of G.)
+__device__ __forceinline__ int formed_again(const Meta &meta, const uint32_t *peak, int first, int count, int lane)
 {
-    bool any = false;
-    for (int k = lane; k < count; k += 64) any = any || small_peak(peak[first + k]);
-    return __any(any);
+    int any = *meta.uneven;
+    for (int k = lane; k < count; k += 64) any |= small_peak(peak[first + k]);
+    return __builtin_amdgcn_readfirstlane(__ballot(any != 0) != 0);
+}
+// `again` where r is 1, else `a`
+__device__ __forceinline__ const char *either(const void *a, const char *again, int r)
+{
+    const uint64_t x = (uint64_t)(uintptr_t)a, at = x ^ ((x ^ (uint64_t)(uintptr_t)again) & -(uint64_t)r);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return (const char *)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 // (numbers are not negative, so that they are ordered as their bits are; the largest does not depend on the order of arrival)
 __device__ __forceinline__ void raise_peak(uint32_t *peak, float v) { atomicMax(peak, __float_as_uint(v)); }
@@ -607,7 +615,7 @@ template <class K, bool AGAIN = false> struct Grad : Ending {
     };
     static __device__ __forceinline__ bool wanted(const Params &e, int first, int count, int lane)
     {
-        return *e.meta.uneven || any_small_peak(e.peak, first, count, lane);
+        return formed_again(e.meta, e.peak, first, count, lane) != 0;
     }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -721,7 +729,7 @@ template <class K> struct OutW : Ending {
     };
     static __device__ __forceinline__ const void *operand_a(const Params &e, const void *a, int first, int count, int lane)
     {
-        return e.again && (*e.meta.uneven || any_small_peak(e.peak, first, count, lane)) ? e.again : a;
+        return e.again ? either(a, e.again, formed_again(e.meta, e.peak, first, count, lane)) : a;
     }
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
@@ -860,7 +868,8 @@ template <class K> __device__ __forceinline__ void bias_sums(const Bias<K> &p, i
     const float largest = p.meta.largest(lane);
     // 8 chunks of columns by 8 rows to a wave
     const int chunk = block * 8 + (lane & 7), n = chunk * 8;
-    const char *G = K::kSplit && p.again && (*p.meta.uneven || any_small_peak(p.peak, block * 64, min(p.V - block * 64, 64), lane)) ? p.again : p.G;
+    const char *G = p.G;
+    if (K::kSplit && p.again) G = either(G, p.again, formed_again(p.meta, p.peak, block * 64, min(p.V - block * 64, 64), lane));
     float s[8] = {};
     if (n < p.V)
         for (int m = wave * 8 + (lane >> 3); m < count; m += 32) {
@@ -1176,7 +1185,7 @@ row_grad_kernel(const Meta meta, const float *__restrict__ part, long slice_stri
     constexpr int kThreads = 256 / kGradRows<K>; // of a row
     const int lane = threadIdx.x & 63, m = blockIdx.x * kGradRows<K> + threadIdx.x / kThreads, n = (blockIdx.y * kThreads + threadIdx.x % kThreads) * 4;
     const float largest = meta.largest(lane);
-    if (AGAIN && !*meta.uneven && !any_small_peak(peak, blockIdx.y * 64, min(V - (int)blockIdx.y * 64, 64), lane)) return;
+    if (AGAIN && !formed_again(meta, peak, blockIdx.y * 64, min(V - (int)blockIdx.y * 64, 64), lane)) return;
     float g[4] = {0.f, 0.f, 0.f, 0.f};
     if (m < meta.rows() && n < ((V + 7) & ~7)) {
         const int label = meta.label_of(m);

@@ -221,3 +221,22 @@ def test_float_gradients_captured_in_a_graph():
             torch.cuda.synchronize()
             for k in want:
                 assert torch.equal(out[k], want[k]), (shape, k)
+
+
+@pytest.mark.parametrize("shape", [(65, 40, 20000), (100, 256, 9000), (147, 101, 218), (200, 2047, 1000), (300, 256, 4000), (300, 1024, 700), (526, 64, 1576), (700, 72, 333),
+                                   (1500, 512, 12000), (3000, 300, 3000)])
+def test_improbable_classes_where_rows_weigh_the_same(shape):
+    """The mean's gradient: nothing but the classes themselves has G formed again, some tiles of it or all."""
+    T, D, V = shape
+    t = make(T, D, V, B.F32, bias=1, seed=5)
+    t["gloss"][:] = 1.0 / T
+    g = torch.Generator(device=DEV)
+    g.manual_seed(0)
+    low = torch.rand(V, generator=g, device=DEV) < 4 / V ** 0.5
+    low[:5] = False
+    t["b"] = torch.where(low, torch.rand(V, generator=g, device=DEV) * -50 - 15, 0.0)
+    t["labels"] %= 5
+    check_rows(t, run(t))
+    for want in (("dW",), ("db",)):
+        check_rows(t, gradients(t, want), want)
+
