@@ -351,6 +351,102 @@ int cac_orthogonalise(const cac_muon_desc *d, const void *G, void *O, void *ws, 
 int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, float momentum, float keep, float lr, void *ws,
                   size_t ws_bytes, void *stream);
 
+/* ---- Residual blocks between the convolutions' features and the loss --------------------------------
+ *
+ * Dropout, the dense layer with its ending, and the norms between blocks.  What their backward passes need is formed again and
+ * not kept: no mask, no pre-activation, no normalised row, no statistics.  What is written shares no memory with anything else that
+ * a call is given, but for what is said at each call.
+ *
+ * The mask of dropout is a function of {key, step} = rng[0], rng[1], two numbers of 64 bits ON THE DEVICE (a captured graph has another
+ * mask once the caller has written another step), of `site` (below 2^24: a number for every place in the network that drops) and of an
+ * element's row and column.  Philox 4x32 of ten rounds (Salmon, Moraes, Dror, Shaw, 2011) with key rng[0] makes 128 bits from the counter
+ * (g low, g high | site << 8, step low, step high), words of 32 bits, g = row * ceil(columns / 8) + column / 8.  They are the 16 bits of
+ * each of eight neighbours, column % 8 = 0 in the low half of the first word; an element whose bits are below round(65536 drop_p) is dropped, and
+ * the others are multiplied by 65536 / (65536 - round(65536 drop_p)).  drop(x) is zero where x is dropped, whatever it is.  A forward
+ * and a backward call have the same mask where rng's numbers, site, drop_p and the columns are the same.  rng is not read, and may be NULL, where
+ * round(65536 drop_p) is 0. */
+
+typedef enum cac_act { CAC_ACT_NONE = 0, CAC_ACT_RELU = 1, CAC_ACT_GELU = 2, CAC_ACT_SILU = 3 } cac_act; /* GELU: u Phi(u); SILU: u / (1 + exp(-u)) */
+
+/* Dropout: Y = R + alpha * drop(X), [rows, cols], Y dense.  R may be NULL (zeros).  Its gradient is the same call on dY without R.
+ * Y may take the place of a dense X or R. */
+typedef struct cac_dropout_desc {
+    uint32_t size;               /* sizeof(cac_dropout_desc) */
+    int32_t rows, cols;          /* cols at most 2^30; below 2^40 groups of eight in all */
+    int32_t ld_x, ld_r;          /* elements from a row of X (R) to the next; 0: cols */
+    int32_t dtype;               /* cac_dtype of X, R, Y */
+    float alpha, drop_p;         /* drop_p in [0, 1] */
+    uint32_t site;
+} cac_dropout_desc;
+
+int cac_dropout(const cac_dropout_desc *d, const void *X, const void *R, const uint64_t *rng, void *Y, void *stream);
+
+/* A dense layer: u = X W^T + b,  Y = R + alpha * drop(act(u)), X [T, D], W [N, D], b [N], R and Y [T, N] (Y dense).
+ * dtype CAC_F32 multiplies floats by float instructions.  dtype CAC_BF16 rounds the result once; in the backward pass drop(dY) act'(u) is
+ * rounded before it is multiplied with W and X (without act it is dY's own bits), not before it is summed for db.  Sums are float. */
+typedef enum cac_linear_op { CAC_LINEAR_FWD = 0, CAC_LINEAR_BWD = 1 } cac_linear_op;
+
+typedef struct cac_linear_desc {
+    uint32_t size;               /* sizeof(cac_linear_desc) */
+    int32_t T, D, N;             /* rows, features in, features out: at most 2^22, 2^18, 2^18 */
+    int32_t ld_x, ld_w, ld_r;    /* elements from a row of X (W, R) to the next, at most 2^20; 0: dense */
+    int32_t dtype;               /* cac_dtype of everything */
+    int32_t has_bias;
+    int32_t act;                 /* cac_act */
+    float alpha, drop_p;
+    uint32_t site;
+} cac_linear_desc;
+
+/* Host only. */
+int cac_linear_workspace_size(const cac_linear_desc *d, int op, size_t *bytes);
+int cac_linear_describe_plan(const cac_linear_desc *d, int op, char *buf, size_t buf_len);
+
+/* R may be NULL (zeros).  Y may take the place of a dense R. */
+int cac_linear_fwd(const cac_linear_desc *d, const void *X, const void *W, const void *b, const void *R, const uint64_t *rng, void *Y, void *ws,
+                   size_t ws_bytes, void *stream);
+
+/* From dY [T, N], dense, with dU = alpha * drop(dY) * act'(u), u formed again where there is an act:
+ *   dX = dU W [T, D],  dW = dU^T X [N, D],  db = column sums of dU [N],  all dense; any of them may be NULL and is not computed then.
+ * R's gradient is dY.  b is read where there is an act, X for that and for dW, W for that and for dX. */
+int cac_linear_bwd(const cac_linear_desc *d, const void *X, const void *W, const void *b, const void *dY, const uint64_t *rng, void *dX, void *dW, void *db,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* What stands between two blocks: a norm behind the one, the gate and the factor of its branch, the residual, and the norm before the other:
+ *   S = R + alpha * drop(gate * post(F)),   H = pre(S),   F, R, S, H [T, D] (S and H dense).
+ * post and pre are no norm (x itself; for pre, no H), rms: x / sqrt(mean(x^2) + eps) * w + b, or layer: (x - mean) / sqrt(mean((x - mean)^2) + eps)
+ * * w + b.  H is formed from S before S is rounded.  Weights, biases, the gate and their gradients are float; sums are float, in a fixed order. */
+typedef enum cac_norm { CAC_NORM_NONE = 0, CAC_NORM_RMS = 1, CAC_NORM_LAYER = 2 } cac_norm;
+typedef enum cac_block_norm_op { CAC_BLOCK_NORM_FWD = 0, CAC_BLOCK_NORM_BWD = 1 } cac_block_norm_op;
+
+typedef struct cac_block_norm_desc {
+    uint32_t size;               /* sizeof(cac_block_norm_desc) */
+    int32_t T, D;                /* at most 2^28 and 2^14 */
+    int32_t ld_f, ld_r;          /* elements from a row of F (R) to the next, at most 2^20; 0: D */
+    int32_t dtype;               /* cac_dtype of F, R, S, H and their gradients */
+    int32_t post, pre;           /* cac_norm */
+    int32_t gate_rows;           /* rows that share a row of the gate [ceil(T / gate_rows), D], such as an image's; T or more: one for all; 0: no gate */
+    float eps_post, eps_pre;
+    float alpha, drop_p;
+    uint32_t site;
+} cac_block_norm_desc;
+
+/* Host only.  (The forward pass needs no workspace.) */
+int cac_block_norm_workspace_size(const cac_block_norm_desc *d, int op, size_t *bytes);
+int cac_block_norm_describe_plan(const cac_block_norm_desc *d, int op, char *buf, size_t buf_len);
+
+/* R may be NULL (zeros), w_* NULL (ones), b_* NULL (zeros), S NULL (not kept).  S may take the place of a dense R. */
+int cac_block_norm_fwd(const cac_block_norm_desc *d, const void *F, const void *R, const float *gate, const float *w_post, const float *b_post,
+                       const float *w_pre, const float *b_pre, const uint64_t *rng, void *S, void *H, void *stream);
+
+/* From dH and dS (what reaches S by other ways; NULL: zeros):
+ *   dR = dS + the gradient of S through H,  a = alpha * drop(dR),  dgate = sums of a * post(F),  dF = the gradient of F from gate * a,
+ *   dw_*, db_*: sums over rows of a norm's gradient times its row before weights, and of the gradient.
+ * F is read where there is a post or a gate, S (as the forward pass wrote it) where there is a pre.  Any gradient may be NULL and is not computed then.
+ * dR may take the place of dS, dF of a dense F.  Each row's norm is a function of itself: with infinities or NaN it comes out as NaN, and in the sums. */
+int cac_block_norm_bwd(const cac_block_norm_desc *d, const void *F, const void *S, const float *gate, const float *w_post, const float *b_post,
+                       const float *w_pre, const void *dH, const void *dS, const uint64_t *rng, void *dR, void *dF, float *dgate, float *dw_post,
+                       float *db_post, float *dw_pre, float *db_pre, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

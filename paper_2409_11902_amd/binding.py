@@ -32,9 +32,15 @@ EXPORTS = (
     "conv_bwd_weight_and_data", "conv_bwd_weight_compressed_noalloc", "cac_bn_relu_fwd_compress", "cac_bn_bwd_compressed", "cac_probe",
     "cac_loss_workspace_size", "cac_loss_describe_plan", "cac_loss_fwd", "cac_loss_bwd",
     "cac_muon_workspace_size", "cac_muon_describe_plan", "cac_orthogonalise", "cac_muon_step",
+    "cac_dropout", "cac_linear_workspace_size", "cac_linear_describe_plan", "cac_linear_fwd", "cac_linear_bwd",
+    "cac_block_norm_workspace_size", "cac_block_norm_describe_plan", "cac_block_norm_fwd", "cac_block_norm_bwd",
 )
 LOSS_FWD, LOSS_BWD = 0, 1
 MUON_ORTHOGONALISE, MUON_STEP = 0, 1
+LINEAR_FWD, LINEAR_BWD = 0, 1
+BLOCK_NORM_FWD, BLOCK_NORM_BWD = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = range(4)
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
 PROBE_MFMA, PROBE_COPY, PROBE_READ, PROBE_MFMA_16X16, PROBE_MFMA_1WAVE = 0, 1, 2, 3, 4
 NOALLOC_SCRATCH_BYTES = 40 << 20
 
@@ -57,6 +63,23 @@ class cac_muon_desc(ctypes.Structure):
     _fields_ = [("size", ctypes.c_uint32)] + [
         (n, ctypes.c_int32) for n in ("batch", "rows", "cols", "dtype", "grad_dtype", "steps", "nesterov")
     ]
+
+
+class cac_dropout_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("rows", "cols", "ld_x", "ld_r", "dtype")] + [
+        ("alpha", ctypes.c_float), ("drop_p", ctypes.c_float), ("site", ctypes.c_uint32)]
+
+
+class cac_linear_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("T", "D", "N", "ld_x", "ld_w", "ld_r", "dtype", "has_bias", "act")
+    ] + [("alpha", ctypes.c_float), ("drop_p", ctypes.c_float), ("site", ctypes.c_uint32)]
+
+
+class cac_block_norm_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("T", "D", "ld_f", "ld_r", "dtype", "post", "pre", "gate_rows")
+    ] + [(n, ctypes.c_float) for n in ("eps_post", "eps_pre", "alpha", "drop_p")] + [("site", ctypes.c_uint32)]
 
 
 class CacError(RuntimeError):
@@ -108,6 +131,16 @@ def lib() -> ctypes.CDLL:
         L.cac_muon_describe_plan.argtypes = [mp, ctypes.c_int, ctypes.c_char_p, sz]
         L.cac_orthogonalise.argtypes = [mp, vp, vp, vp, sz, vp]
         L.cac_muon_step.argtypes = [mp, vp, vp, vp, fl, fl, fl, vp, sz, vp]
+        odp, idp, ndp = ctypes.POINTER(cac_dropout_desc), ctypes.POINTER(cac_linear_desc), ctypes.POINTER(cac_block_norm_desc)
+        L.cac_dropout.argtypes = [odp] + [vp] * 5
+        L.cac_linear_workspace_size.argtypes = [idp, ctypes.c_int, szp]
+        L.cac_linear_describe_plan.argtypes = [idp, ctypes.c_int, ctypes.c_char_p, sz]
+        L.cac_linear_fwd.argtypes = [idp] + [vp] * 7 + [sz, vp]
+        L.cac_linear_bwd.argtypes = [idp] + [vp] * 9 + [sz, vp]
+        L.cac_block_norm_workspace_size.argtypes = [ndp, ctypes.c_int, szp]
+        L.cac_block_norm_describe_plan.argtypes = [ndp, ctypes.c_int, ctypes.c_char_p, sz]
+        L.cac_block_norm_fwd.argtypes = [ndp] + [vp] * 11
+        L.cac_block_norm_bwd.argtypes = [ndp] + [vp] * 17 + [sz, vp]
         for n in EXPORTS[2:]:
             getattr(L, n).restype = ctypes.c_int
         _lib = L
@@ -131,6 +164,19 @@ def make_loss_desc(T, D, V, dtype=BF16, has_bias=0, ignore_index=-100, ld_h=0, l
 
 def make_muon_desc(rows, cols, batch=1, dtype=F32, grad_dtype=F32, steps=5, nesterov=1) -> cac_muon_desc:
     return cac_muon_desc(ctypes.sizeof(cac_muon_desc), batch, rows, cols, dtype, grad_dtype, steps, nesterov)
+
+
+def make_dropout_desc(rows, cols, dtype=BF16, p=0.0, alpha=1.0, site=0, ld_x=0, ld_r=0) -> cac_dropout_desc:
+    return cac_dropout_desc(ctypes.sizeof(cac_dropout_desc), rows, cols, ld_x, ld_r, dtype, alpha, p, site)
+
+
+def make_linear_desc(T, D, N, dtype=BF16, has_bias=0, act=ACT_NONE, alpha=1.0, p=0.0, site=0, ld_x=0, ld_w=0, ld_r=0) -> cac_linear_desc:
+    return cac_linear_desc(ctypes.sizeof(cac_linear_desc), T, D, N, ld_x, ld_w, ld_r, dtype, has_bias, act, alpha, p, site)
+
+
+def make_block_norm_desc(T, D, dtype=BF16, post=NORM_NONE, pre=NORM_RMS, gate_rows=0, eps_post=1e-5, eps_pre=1e-5, alpha=1.0, p=0.0, site=0,
+                         ld_f=0, ld_r=0) -> cac_block_norm_desc:
+    return cac_block_norm_desc(ctypes.sizeof(cac_block_norm_desc), T, D, ld_f, ld_r, dtype, post, pre, gate_rows, eps_post, eps_pre, alpha, p, site)
 
 
 def desc_from_spec(spec: synth.LayerSpec, has_bias: int = 1, **over) -> cac_desc:
@@ -298,6 +344,46 @@ def cac_orthogonalise(d, G, O, ws=None, stream=None):
 
 def cac_muon_step(d, G, M, W, momentum, keep, lr, ws=None, stream=None):
     _check((_lib or lib()).cac_muon_step(d, _ptr(G), _ptr(M), _ptr(W), momentum, keep, lr, *_ws(ws), _stream(stream)))
+
+
+def cac_dropout(d, X, R, rng, Y, stream=None):
+    _check((_lib or lib()).cac_dropout(d, _ptr(X), _ptr(R), _ptr(rng), _ptr(Y), _stream(stream)))
+
+
+def cac_linear_workspace_size(d: cac_linear_desc, op: int) -> int:
+    return _size_of(lib().cac_linear_workspace_size, d, op)
+
+
+def cac_linear_describe_plan(d: cac_linear_desc, op: int) -> str:
+    return _plan_of(lib().cac_linear_describe_plan, d, op)
+
+
+def cac_linear_fwd(d, X, W, b, R, rng, Y, ws=None, stream=None):
+    _check((_lib or lib()).cac_linear_fwd(d, _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(rng), _ptr(Y), *_ws(ws), _stream(stream)))
+
+
+def cac_linear_bwd(d, X, W, b, dY, rng, dX, dW, db, ws=None, stream=None):
+    _check((_lib or lib()).cac_linear_bwd(d, _ptr(X), _ptr(W), _ptr(b), _ptr(dY), _ptr(rng), _ptr(dX), _ptr(dW), _ptr(db), *_ws(ws),
+                                          _stream(stream)))
+
+
+def cac_block_norm_workspace_size(d: cac_block_norm_desc, op: int) -> int:
+    return _size_of(lib().cac_block_norm_workspace_size, d, op)
+
+
+def cac_block_norm_describe_plan(d: cac_block_norm_desc, op: int) -> str:
+    return _plan_of(lib().cac_block_norm_describe_plan, d, op)
+
+
+def cac_block_norm_fwd(d, F, R, gate, w_post, b_post, w_pre, b_pre, rng, S, H, stream=None):
+    _check((_lib or lib()).cac_block_norm_fwd(d, _ptr(F), _ptr(R), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(b_pre), _ptr(rng),
+                                              _ptr(S), _ptr(H), _stream(stream)))
+
+
+def cac_block_norm_bwd(d, F, S, gate, w_post, b_post, w_pre, dH, dS, rng, dR, dF, dgate, dw_post, db_post, dw_pre, db_pre, ws=None, stream=None):
+    _check((_lib or lib()).cac_block_norm_bwd(d, _ptr(F), _ptr(S), _ptr(gate), _ptr(w_post), _ptr(b_post), _ptr(w_pre), _ptr(dH), _ptr(dS),
+                                              _ptr(rng), _ptr(dR), _ptr(dF), _ptr(dgate), _ptr(dw_post), _ptr(db_post), _ptr(dw_pre), _ptr(db_pre),
+                                              *_ws(ws), _stream(stream)))
 
 
 # ---- host <-> device marshalling (type conversion only, no arithmetic)

@@ -12,23 +12,6 @@ static const char *tile_name(const TileChoice &c)
     return names[c.shape];
 }
 
-// A call's buffers: the first `outputs` are written, the others are read or are workspace.  No output may share memory with another
-// buffer (null and empty ones are left out).
-struct Buffer {
-    const void *p;
-    size_t bytes;
-    const char *name;
-};
-static int check_apart(const Buffer *b, int outputs, int all)
-{
-    for (int i = 0; i < outputs; ++i)
-        for (int k = i + 1; k < all; ++k)
-            if (b[i].p && b[k].p && b[k].bytes && share_memory(b[i].p, b[i].bytes, b[k].p, b[k].bytes))
-                return fail(CAC_ERR_INVALID_ARG, "%s shares memory with %s", b[i].name, b[k].name);
-    return CAC_OK;
-}
-
-static size_t bytes_of(int dtype) { return dtype == CAC_F32 ? 4 : 2; }
 // from the first number of a matrix to behind its last
 static size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
 

@@ -1,0 +1,507 @@
+// A dense layer with its ending, Y = R + alpha * drop(act(u)), u = X W^T + b, and its gradients:
+//   dU = drop(dY) act'(u),  dX = f dU W,  dW = f dU^T X,  db = f sum dU,  f = alpha over the probability of being kept.
+// Products by matrix instructions (mm_core.h); a product's ending runs where its sums lie. What act' needs of u is not kept but formed
+// again, so that the backward pass is three products; without act it is two.
+//   - bfloat16: dU is rounded once, as an operand has to be; f, which is no power of two, is left out of it and multiplied into the sums, so that without
+//     act dU is dY's bits. db is summed from dU before it is rounded.
+//   - float: by the float instruction, operands as they lie (a matrix of any scale, infinities and NaN as float arithmetic has them).
+// Sums are of 32 bits.
+#include "block.h"
+#include "mm_core.h"
+
+namespace cac {
+namespace dense {
+using namespace mm;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Phi(u) = erfc(-u / sqrt 2) / 2 and exp(-u^2 / 2). For u < 0, Phi = exp(-u^2 / 2) t P(t) with t = 1 / (1 + 0.45 |u| / sqrt 2): P is a least-squares
+// polynomial of erfcx(z) / (2 t), reweighted until its relative error, 3.2e-8, was level; in float 1.4e-7 in the mean, of small Phi too.
+__device__ __forceinline__ float normal_cdf(float u, float *bell)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.31819805153394637f, fabsf(u), 1.f)); // 0.45 / sqrt 2
+    *bell = __builtin_amdgcn_exp2f(u * u * (-0.5f * kLog2e));
+    float p = -0.020695475861430168f;
+    p = fmaf(p, t, 0.09534360468387604f);
+    p = fmaf(p, t, -0.1502906233072281f);
+    p = fmaf(p, t, 0.07119989395141602f);
+    p = fmaf(p, t, -0.011178647167980671f);
+    p = fmaf(p, t, 0.05997511371970177f);
+    p = fmaf(p, t, 0.08762608468532562f);
+    p = fmaf(p, t, 0.11413581669330597f);
+    p = fmaf(p, t, 0.12694157660007477f);
+    p = fmaf(p, t, 0.12694266438484192f);
+    const float below = p * t * *bell;
+    return u < 0.f ? below : 1.f - below;
+}
+__device__ __forceinline__ float activation(int act, float u)
+{
+    float bell;
+    if (act == CAC_ACT_RELU) return u <= 0.f ? 0.f : u; // (NaN stays NaN)
+    if (act == CAC_ACT_GELU) return u * normal_cdf(u, &bell);
+    if (act == CAC_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
+    return u;
+}
+__device__ __forceinline__ float slope(int act, float u)
+{
+    if (act == CAC_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+    if (act == CAC_ACT_GELU) {
+        float bell;
+        const float cdf = normal_cdf(u, &bell);
+        return fmaf(u * bell, 0.3989422804014327f, cdf); // 1 / sqrt(2 pi)
+    }
+    if (act == CAC_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
+        return s * fmaf(u, 1.f - s, 1.f);
+    }
+    return 1.f;
+}
+
+// What becomes of a product's sums, or of the sums of its slices.
+enum Kind {
+    kForward, // R + scale drop(act(sum + b))
+    kSlope,   // drop(dY) act'(sum + b), and its sums over rows
+    kScaled,  // scale * sum
+};
+struct Tail {
+    Kind kind;
+    int act, N;         // columns
+    const void *b;      // [N], or null
+    const void *other;  // R (or null), dY
+    long ld_other;
+    void *out;
+    long ld_out;
+    int cols_out;       // N, or up to where a row is padded with zeros
+    float *columns;     // kSlope: [parts][N], or null
+    bool wide_other;    // fours of a row start on 4 elements
+    bool wide_out;
+    float scale;
+    Drop d;
+    int across;         // groups of eight of a row of the mask
+};
+
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
+template <typename T> __device__ __forceinline__ void load_four(const T *p, int n, int N, bool wide, float (&v)[4])
+{
+    if (wide) {
+        const Four<T> f = *(const Four<T> *)p;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = Elem<T>::load(&f.v[k]);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = n + k < N ? Elem<T>::load(p + k) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void store_four(T *p, int n, int N, bool wide, const float (&v)[4])
+{
+    if (wide) {
+        Four<T> f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) Elem<T>::store(&f.v[k], v[k]);
+        *(Four<T> *)p = f;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (n + k < N) Elem<T>::store(p + k, v[k]);
+}
+
+// Four neighbours of row m from column n on; `words` are their 64 random bits, `v` comes as sums and goes as what was written.
+template <typename T> __device__ __forceinline__ void finish_four(const Tail &t, long m, int n, const float (&b)[4], const uint32_t (&words)[2], float (&v)[4])
+{
+    if (t.kind == kScaled) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] *= t.scale;
+    } else {
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        if (t.other && n < t.N) load_four((const T *)t.other + m * t.ld_other + n, n, t.N, t.wide_other, o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool kept = !t.d.limit || drop_keeps(words[k >> 1], k & 1, t.d.limit);
+            const float u = v[k] + b[k];
+            if (t.kind == kForward) v[k] = o[k] + (kept ? t.scale * activation(t.act, u) : 0.f);
+            else v[k] = kept && n + k < t.N ? (t.act == CAC_ACT_NONE ? o[k] : o[k] * slope(t.act, u)) : 0.f;
+        }
+    }
+    if (t.out) store_four((T *)t.out + m * t.ld_out + n, n, t.cols_out, t.wide_out, v);
+}
+
+// The other lane of a pair's.
+__device__ __forceinline__ uint32_t from_neighbour(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true); }
+
+// A product with its tail, or its slices' sums.  They go through a wave's LDS, 32 rows at a time: a lane then has four neighbours in the same
+// columns of every row that it comes to, and two lanes a group of the mask, of which each forms one in two.
+template <class T> struct Ended : Ending {
+    struct Params {
+        Tail t;
+        float *sums; // [slice][M][N]: no tail yet
+        long slice_stride;
+    };
+    template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+    {
+        typedef RowBlock<Fmt::kF32, NI> Block;
+        constexpr int kLanes = 8 * NI, kRows = 64 / kLanes; // lanes to a row, rows at once
+        const Tail &t = e.t;
+        const int n = p.n0 + p.lane % kLanes * 4, row0 = p.lane / kLanes;
+        const bool sums = e.sums != nullptr;
+        float b[4] = {0.f, 0.f, 0.f, 0.f}, columns[4] = {0.f, 0.f, 0.f, 0.f};
+        if (t.b && !sums) load_four((const T *)t.b + n, n, t.N, false, b);
+        const DropKey key = drop_key(t.d);
+        const bool drops = t.d.limit && !sums;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int m0 = p.m0 + i * 32;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = acc[i][j][q * 4 + k];
+                    Block::put(p.lds, p.lane, j, q, v);
+                }
+            asm volatile("" ::: "memory"); // (a wave's LDS accesses are in order; other lanes' stores are read here)
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int c = 0; c < 32 / kRows; c += 2) {
+                uint32_t words[2][2] = {{0, 0}, {0, 0}};
+                if (drops) {
+                    const bool odd = p.lane & 1;
+                    const Bits128 w = drop_bits(key, t.d.site, (uint64_t)(m0 + (c + odd) * kRows + row0) * t.across + (n >> 3));
+                    const uint32_t r0 = from_neighbour(odd ? w.w[0] : w.w[2]), r1 = from_neighbour(odd ? w.w[1] : w.w[3]);
+                    words[0][0] = odd ? r0 : w.w[0], words[0][1] = odd ? r1 : w.w[1];
+                    words[1][0] = odd ? w.w[2] : r0, words[1][1] = odd ? w.w[3] : r1;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = (c + h) * kRows + row0, m = m0 + row;
+                    const f32x4 x = *(const f32x4 *)(p.lds + row * Block::kPitch + p.lane % kLanes * 16);
+                    float v[4] = {x[0], x[1], x[2], x[3]};
+                    if (m >= p.M || n >= t.cols_out) continue;
+                    if (sums) {
+                        store_four(e.sums + p.slice * e.slice_stride + (long)m * p.N + n, n, p.N, (p.N & 3) == 0, v);
+                        continue;
+                    }
+                    finish_four<T>(t, m, n, b, words[h], v);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) columns[k] += v[k];
+                }
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (sums || !t.columns) return;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int s = kLanes; s < 64; s *= 2) columns[k] += __shfl_xor(columns[k], s, 64);
+        if (p.lane < kLanes && p.m0 < p.M && n < t.N) store_four(t.columns + (long)(p.m0 / (32 * MI)) * t.N + n, n, t.N, (t.N & 3) == 0, columns);
+    }
+};
+
+// A tail without a product before it: the slices' sums joined (slices > 0), or dY alone.  A thread has eight neighbours of every eighth row of
+// its block's.
+struct Join {
+    Tail t;
+    const float *sums;
+    long slice_stride;
+    int slices, rows_per_block;
+    long M;
+};
+template <typename T> __global__ void __launch_bounds__(256) join_kernel(const Join p)
+{
+    __shared__ float red[8][256];
+    const Tail &t = p.t;
+    const int col = threadIdx.x & 31, turn = threadIdx.x >> 5, n = blockIdx.y * 256 + col * 8;
+    const long m1 = min(p.M, (long)(blockIdx.x + 1) * p.rows_per_block);
+    const DropKey key = drop_key(t.d);
+    float b[2][4], columns[2][4] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[h][k] = t.b && n + h * 4 + k < t.N ? Elem<T>::load((const T *)t.b + n + h * 4 + k) : 0.f;
+    if (n < t.cols_out)
+        for (long m = (long)blockIdx.x * p.rows_per_block + turn; m < m1; m += 8) {
+            f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            if (t.N % 4 == 0) {
+                const float *x = p.sums + m * t.N + n;
+                const bool both = n + 8 <= t.N;
+                if (n < t.N)
+                    for (int k0 = 0; k0 < p.slices; k0 += 4) { // four slices on their way at a time
+                        f32x4 y[4][2];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                y[k][h] = k0 + k < p.slices && (h == 0 || both) ? *(const f32x4 *)(x + (k0 + k) * p.slice_stride + h * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) s[h] += y[k][h];
+                    }
+            } else {
+                for (int k = 0; k < p.slices; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < t.N) s[e >> 2][e & 3] += p.sums[k * p.slice_stride + m * t.N + n + e];
+            }
+            Bits128 w = {{0, 0, 0, 0}};
+            if (t.d.limit) w = drop_bits(key, t.d.site, (uint64_t)m * t.across + (n >> 3));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (n + h * 4 >= t.cols_out) continue;
+                const uint32_t words[2] = {w.w[2 * h], w.w[2 * h + 1]};
+                float v[4] = {s[h][0], s[h][1], s[h][2], s[h][3]};
+                finish_four<T>(t, m, n + h * 4, b[h], words, v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) columns[h][k] += v[k];
+            }
+        }
+    if (!t.columns) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[turn][col * 8 + e] = columns[e >> 2][e & 3];
+    __syncthreads();
+    const int c = threadIdx.x;
+    float s = 0.f;
+    for (int k = 0; k < 8; ++k) s += red[k][c];
+    if ((int)(blockIdx.y * 256) + c < t.N) t.columns[(long)blockIdx.x * t.N + blockIdx.y * 256 + c] = s;
+}
+
+// db from the parts' sums: a block of sixteen waves takes 64 columns.
+template <typename T> __global__ void __launch_bounds__(1024) bias_join_kernel(const float *part, int parts, int N, float scale, T *db)
+{
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (n < N) {
+        const float *p = part + n;
+        int r = wave;
+        for (; r + 48 < parts; r += 64) {
+            const float x0 = p[(long)r * N], x1 = p[(long)(r + 16) * N], x2 = p[(long)(r + 32) * N], x3 = p[(long)(r + 48) * N];
+            s += (x0 + x1) + (x2 + x3);
+        }
+        for (; r < parts; r += 16) s += p[(long)r * N];
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave || n >= N) return;
+    for (int w = 1; w < 16; ++w) s += red[w][lane];
+    Elem<T>::store(db + n, s * scale);
+}
+
+// Rows of any length and stride to rows of whole units of 16 bytes, padded with zeros; both operands in one launch.
+struct Pack {
+    const void *from[2];
+    void *to[2];
+    long rows[2], ld[2];
+    long groups[2]; // of eight elements, of all rows; 0: not this one
+    int columns;    // (both have the same)
+};
+template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const Pack p)
+{
+    const int across = (p.columns + 7) / 8;
+    for (long g = (long)blockIdx.x * 256 + threadIdx.x; g < p.groups[0] + p.groups[1]; g += (long)gridDim.x * 256) {
+        const bool second = g >= p.groups[0];
+        const long at = second ? g - p.groups[0] : g, row = at / across;
+        const int n = (int)(at - row * across) * 8;
+        const T *x = (const T *)(second ? p.from[1] : p.from[0]) + row * (second ? p.ld[1] : p.ld[0]);
+        float v[8];
+        read_eight(x, n, p.columns, false).get(v);
+        write_eight((T *)(second ? p.to[1] : p.to[0]) + at * 8, 0, 8, true, v);
+    }
+}
+
+} // namespace dense
+
+using namespace dense;
+
+// ---- host
+static bool choose_fits(Format f, long M, long N, long K, TileChoice *c)
+{
+    *c = choose(f, M, N, 1, K, false, 64);
+    return fits_grid(c->shape, tiles_of(c->shape, M, N, false) * c->slices);
+}
+static int rows_of_a_part(int shape) // of a tile, that one wave sums over
+{
+    static const int kRowsOf[kShapes] = {32 * Small::MI, 32 * Middle::MI, 32 * Wide::MI, 32 * Big::MI, 32 * Low::MI};
+    return kRowsOf[shape];
+}
+static long join_rows(long M) { return M < 2048 ? 8 : 64; } // of a block of join_kernel
+
+bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p)
+{
+    const bool real = g.dtype == CAC_F32;
+    const Format f = real ? kRaw : kBf16;
+    const long e = g.dtype == CAC_F32 ? 4 : 2, whole = 16 / e;
+    auto padded = [&](long n) { return (n + 7) / 8 * 8; };
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t o = at;
+        at += (bytes + 255) / 256 * 256;
+        return o;
+    };
+    *p = LinearPlan{};
+    p->pack_x = g.D % whole || g.ld_x % whole;
+    p->pack_w = g.D % whole || g.ld_w % whole;
+    p->ld_x = p->pack_x ? padded(g.D) : g.ld_x;
+    p->ld_w = p->pack_w ? padded(g.D) : g.ld_w;
+    p->again = backward && g.act != CAC_ACT_NONE;
+    p->grad = backward && (p->again || g.drops || g.N % whole);
+    p->ld_u = p->grad ? padded(g.N) : g.N;
+    size_t sums = 0;
+    auto product = [&](long M, long N, long K, TileChoice *c) {
+        if (!choose_fits(f, M, N, K, c)) return false;
+        if (c->slices > 1 && sums < (size_t)c->slices * M * N * 4) sums = (size_t)c->slices * M * N * 4;
+        return true;
+    };
+    if (!backward || p->again)
+        if (!product(g.T, g.N, g.D, &p->y)) return false;
+    if (p->pack_x) p->o_x = take(g.T * p->ld_x * e);
+    if (p->pack_w) p->o_w = take(g.N * p->ld_w * e);
+    if (backward) {
+        // (a tile of 32 rows has none that run down memory: dW of few features takes one of 64)
+        if (!product(g.T, g.D, g.N, &p->dx) || !product(real && g.N <= 32 ? 33 : g.N, g.D, g.T, &p->dw)) return false;
+        p->parts = p->again && p->y.slices == 1 ? cdiv(g.T, rows_of_a_part(p->y.shape)) : cdiv(g.T, join_rows(g.T));
+        if (p->grad) p->o_u = take(g.T * p->ld_u * e);
+        p->o_db = take((size_t)p->parts * g.N * 4);
+    }
+    p->o_sum = take(sums);
+    p->bytes = at;
+    return true;
+}
+
+namespace {
+
+template <typename T> struct Layer {
+    static constexpr bool kFloat = sizeof(T) == 4;
+    typedef typename std::conditional<kFloat, Raw, Bf16>::type P;
+    const LinearGeom &g;
+    const LinearPlan &p;
+    const Drop &d;
+    char *ws;
+    hipStream_t st;
+    hipError_t err = hipSuccess;
+
+    const void *x, *w; // as they are multiplied
+
+    void pack(const void *X, const void *W, bool need_x, bool need_w)
+    {
+        const bool px = p.pack_x && need_x, pw = p.pack_w && need_w;
+        x = px ? ws + p.o_x : X;
+        w = pw ? ws + p.o_w : W;
+        if (!px && !pw) return;
+        Pack a;
+        a.from[0] = X, a.from[1] = W;
+        a.to[0] = ws + p.o_x, a.to[1] = ws + p.o_w;
+        a.rows[0] = g.T, a.rows[1] = g.N;
+        a.ld[0] = g.ld_x, a.ld[1] = g.ld_w;
+        const long across = (g.D + 7) / 8;
+        a.groups[0] = px ? g.T * across : 0;
+        a.groups[1] = pw ? g.N * across : 0;
+        a.columns = (int)g.D;
+        const long blocks = (a.groups[0] + a.groups[1] + 255) / 256;
+        hipLaunchKernelGGL((pack_kernel<T>), dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, a);
+        err = hipGetLastError();
+    }
+    Tail tail(Kind kind, long N, void *out, long ld_out) const
+    {
+        Tail t = {};
+        t.kind = kind;
+        t.act = g.act;
+        t.N = (int)N;
+        t.out = out;
+        t.ld_out = ld_out;
+        t.cols_out = (int)N;
+        t.wide_out = N % 4 == 0 && ld_out % 4 == 0;
+        t.scale = g.alpha * d.scale;
+        t.across = (int)((N + 7) / 8);
+        return t;
+    }
+    void join(const Tail &t, long M, int slices)
+    {
+        Join j;
+        j.t = t;
+        j.sums = (const float *)(ws + p.o_sum);
+        j.slice_stride = M * t.N;
+        j.slices = slices;
+        j.M = M;
+        j.rows_per_block = (int)join_rows(M);
+        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)cdiv(M, j.rows_per_block), (unsigned)cdiv(t.cols_out, 256)), dim3(256), 0, st, j);
+        err = hipGetLastError();
+    }
+    // C = A B^T with a tail
+    template <Lay LA, Lay LB> void product(const void *a, long lda, const void *b, long ldb, long M, long N, long K, TileChoice c, const Tail &t)
+    {
+        if (err != hipSuccess) return;
+        mm::Params m = {};
+        m.a = a;
+        m.b = b;
+        m.lda = lda * sizeof(T);
+        m.ldb = ldb * sizeof(T);
+        m.M = (int)M;
+        m.N = (int)N;
+        m.K = (int)K;
+        m.batch = 1;
+        typename Ended<T>::Params e;
+        e.t = t;
+        e.sums = c.slices > 1 ? (float *)(ws + p.o_sum) : nullptr;
+        e.slice_stride = M * N;
+        if (e.sums) e.t.cols_out = (int)N;
+        err = launch<P, LA, LB, Ended<T>>(m, e, c, st);
+        if (err == hipSuccess && c.slices > 1) join(t, M, c.slices);
+    }
+    hipError_t forward(const void *X, const void *W, const void *b, const void *R, void *Y)
+    {
+        pack(X, W, true, true);
+        Tail t = tail(kForward, g.N, Y, g.N);
+        t.b = b;
+        t.other = R;
+        t.ld_other = g.ld_r;
+        t.wide_other = g.N % 4 == 0 && g.ld_r % 4 == 0;
+        t.d = d;
+        product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
+        return err;
+    }
+    hipError_t backward(const void *X, const void *W, const void *b, const void *dY, void *dX, void *dW, void *db)
+    {
+        pack(X, W, dW || p.again, dX || p.again);
+        const void *u = p.grad ? ws + p.o_u : dY;
+        Tail t = tail(kSlope, g.N, p.grad ? ws + p.o_u : nullptr, p.ld_u);
+        t.cols_out = (int)p.ld_u;
+        t.wide_out = true;
+        t.b = b;
+        t.other = dY;
+        t.ld_other = g.N;
+        t.wide_other = g.N % 4 == 0;
+        t.columns = db ? (float *)(ws + p.o_db) : nullptr;
+        t.d = d;
+        if (p.again) product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
+        else if (err == hipSuccess && (p.grad || db)) join(t, g.T, 0);
+        if (dX) product<Lay::kAlong, Lay::kDown>(u, p.ld_u, w, p.ld_w, g.T, g.D, g.N, p.dx, tail(kScaled, g.D, dX, g.D));
+        if (dW) product<Lay::kDown, Lay::kDown>(u, p.ld_u, x, p.ld_x, g.N, g.D, g.T, p.dw, tail(kScaled, g.D, dW, g.D));
+        if (db && err == hipSuccess) {
+            hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)cdiv(g.N, 64)), dim3(1024), 0, st, (const float *)(ws + p.o_db), (int)p.parts, (int)g.N,
+                               g.alpha * d.scale, (T *)db);
+            err = hipGetLastError();
+        }
+        return err;
+    }
+};
+
+} // namespace
+
+hipError_t launch_linear_fwd(const LinearGeom &g, const LinearPlan &p, const Drop &d, const void *X, const void *W, const void *b, const void *R,
+                             void *Y, void *ws, hipStream_t st)
+{
+    if (g.dtype == CAC_F32) return Layer<float>{g, p, d, (char *)ws, st}.forward(X, W, b, R, Y);
+    return Layer<bf16_t>{g, p, d, (char *)ws, st}.forward(X, W, b, R, Y);
+}
+
+hipError_t launch_linear_bwd(const LinearGeom &g, const LinearPlan &p, const Drop &d, const void *X, const void *W, const void *b, const void *dY,
+                             void *dX, void *dW, void *db, void *ws, hipStream_t st)
+{
+    if (g.dtype == CAC_F32) return Layer<float>{g, p, d, (char *)ws, st}.backward(X, W, b, dY, dX, dW, db);
+    return Layer<bf16_t>{g, p, d, (char *)ws, st}.backward(X, W, b, dY, dX, dW, db);
+}
+
+} // namespace cac

@@ -1,0 +1,301 @@
+"""The norms between two blocks on the GPU, against their formulas in 64 bits.
+
+Tolerances.  A row's sums go through at most 16 terms in a lane, 6 steps of a wave and 16 waves: 38 roundings of 2^-24 of the sum of magnitudes, E = 2^-18
+with what follows them.  So xhat is off by E (|xhat| + |mean| / spread), its gradient's product by as much again; a row's bounds take the largest of the row.  Results are
+rounded to half a step.  Sums over T rows go through at most T / 64 + 64 roundings, of 2^-24 of the sum of magnitudes each, beside what their terms are off by."""
+import numpy as np
+import pytest
+import torch
+
+from block_util import DEV, HALF, TYPES, Scratch, close, keep_factor, make_rng, norm, norm_back, rel, rows
+from paper_2409_11902_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+E, SITE, EPS = 2.0 ** -18, 21, (1e-5, 1e-3)
+NAMES = ("gate", "w_post", "b_post", "w_pre", "b_pre")
+
+
+def make(T, D, dtype, post, pre, gate_rows=0, p=0.0, alpha=1.0, res=True, weights=True, ld_f=0, ld_r=0, ds=True, seed=0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed + T + 3 * D)
+
+    def vector(*shape, mean):
+        return torch.randn(*shape, generator=g, device=DEV) * 0.3 + mean
+
+    t = {"F": rows(g, T, D, ld_f, dtype, 1.0, 0.2), "R": rows(g, T, D, ld_r, dtype, 2.0, -0.3) if res else None,
+         "dH": rows(g, T, D, 0, dtype) if pre else None, "dS": rows(g, T, D, 0, dtype) if ds or not pre else None}
+    t["gate"] = vector(-(-T // gate_rows), D, mean=0.5) if gate_rows else None
+    for k, on in (("post", post), ("pre", pre)):
+        t["w_" + k] = vector(D, mean=1.0) if on and weights else None
+        t["b_" + k] = vector(D, mean=0.1) if on and weights and on == B.NORM_LAYER else None
+    t["rng"] = make_rng(4 + seed, 1)
+    t["desc"] = B.make_block_norm_desc(T, D, dtype=dtype, post=post, pre=pre, gate_rows=gate_rows, eps_post=EPS[0], eps_pre=EPS[1], alpha=alpha, p=p, site=SITE,
+                                       ld_f=ld_f, ld_r=ld_r)
+    return t
+
+
+def top(x):
+    return x.abs().amax(1, keepdim=True)
+
+
+def reference(t):
+    d = t["desc"]
+    T, D, half = d.T, d.D, HALF[d.dtype]
+    alpha = float(np.float32(d.alpha))
+    keep = keep_factor(T, D, d.drop_p, d.site, t["rng"].tolist()).to(DEV) * alpha
+    f = t["F"].double()
+    n, fhat, finv, fmean = norm(d.post, f, EPS[0], t["w_post"], t["b_post"])
+    gate = t["gate"].double()[torch.arange(T, device=DEV) // d.gate_rows] if d.gate_rows else 1.0
+    r, e = {}, {}
+    part = keep * gate * n
+    total = part + (t["R"].double() if t["R"] is not None else 0.0)
+    e_n = E * (top(n) + fmean.abs() * finv * (top(t["w_post"].double()[None]) if t["w_post"] is not None else 1.0)) if d.post else torch.zeros_like(n[:, :1])
+    e_total = (keep * gate).abs() * e_n + 2.0 ** -22 * (part.abs() + total.abs())
+    r["S"], e["S"] = total, e_total + half * total.abs()
+    if d.pre:
+        h, hhat, hinv, hmean = norm(d.pre, total, EPS[1], t["w_pre"], t["b_pre"])
+        w = t["w_pre"].double().abs() if t["w_pre"] is not None else 1.0
+        r["H"] = h
+        e["H"] = w * (E * (top(hhat) + hmean.abs() * hinv) + hinv * (e_total + top(hhat) * top(e_total) + top(e_total))) + 2.0 ** -22 * h.abs() + half * h.abs()
+    # backward: S as the caller has it
+    s = t["S"].double()
+    g = t["dS"].double() if t["dS"] is not None else torch.zeros_like(f)
+    e_g = 2.0 ** -22 * g.abs()
+    if d.pre:
+        _, shat, sinv, smean = norm(d.pre, s, EPS[1], None, None)
+        dh = t["dH"].double()
+        gw = dh * t["w_pre"].double() if t["w_pre"] is not None else dh
+        g = g + norm_back(d.pre, shat, sinv, gw)
+        e_s = E * (top(shat) + smean.abs() * sinv)          # of shat
+        e_g = e_g + 4 * sinv * (top(gw) * (E + e_s) * (1 + top(shat))) + 2.0 ** -22 * g.abs()
+        r["w_pre"], r["b_pre"] = (dh * shat).sum(0), dh.sum(0)
+        e["w_pre"], e["b_pre"] = (dh.abs() * e_s).sum(0), 0.0 * r["b_pre"]
+        sizes = {"w_pre": (dh * shat).abs().sum(0), "b_pre": dh.abs().sum(0)}
+    else:
+        sizes = {}
+    r["dR"], e["dR"] = g, e_g + half * g.abs()
+    a, e_a = keep * g, keep.abs() * e_g + 2.0 ** -22 * (keep * g).abs()
+    dn, e_dn = a * gate, (e_a * (gate.abs() if d.gate_rows else 1.0)) + 2.0 ** -22 * (a * gate).abs()
+    if d.gate_rows:
+        at = torch.arange(T, device=DEV) // d.gate_rows
+        zero = torch.zeros_like(t["gate"].double())
+        r["gate"] = zero.index_add(0, at, a * n)
+        e["gate"] = zero.index_add(0, at, e_a * n.abs() + a.abs() * e_n)
+        sizes["gate"] = zero.index_add(0, at, (a * n).abs())
+    r["dF"], e["dF"] = dn, e_dn
+    if d.post:
+        gw = dn * t["w_post"].double() if t["w_post"] is not None else dn
+        ww = top(t["w_post"].double()[None]) if t["w_post"] is not None else 1.0
+        e_f = E * (top(fhat) + fmean.abs() * finv)
+        r["dF"] = norm_back(d.post, fhat, finv, gw)
+        e["dF"] = finv * (ww * e_dn + (ww * top(e_dn) + 4 * top(gw) * (E + e_f)) * (1 + top(fhat)) ** 2) + 2.0 ** -22 * r["dF"].abs()
+        r["w_post"], r["b_post"] = (dn * fhat).sum(0), dn.sum(0)
+        e["w_post"], e["b_post"] = (e_dn * fhat.abs() + dn.abs() * e_f).sum(0), e_dn.sum(0)
+        sizes["w_post"], sizes["b_post"] = (dn * fhat).abs().sum(0), dn.abs().sum(0)
+    e["dF"] = e["dF"] + half * r["dF"].abs()
+    for k, v in sizes.items():
+        e[k] = e[k] + 2.0 ** -24 * (T / 64 + 64) * v
+    return r, e
+
+
+def forward(t, with_s=True):
+    from gpu_util import Guarded
+    d = t["desc"]
+    o = {k: Guarded((d.T, d.D), TYPES[d.dtype]) for k in ("S", "H")}
+    h = o["H"].t if d.pre else None
+    B.cac_block_norm_fwd(d, t["F"], t["R"], *(t[k] for k in NAMES), t["rng"], o["S"].t if with_s else None, h)
+    torch.cuda.synchronize()
+    for k, v in o.items():
+        v.check(k)
+    if not d.pre:
+        assert bool((o["H"].raw == 0xA5).all())
+    return {k: v.t for k, v in o.items() if (k == "H" and d.pre) or (k == "S" and with_s)}
+
+
+def backward(t, want=None):
+    from gpu_util import Guarded
+    d, td = t["desc"], TYPES[t["desc"].dtype]
+    o = {"dR": Guarded((d.T, d.D), td), "dF": Guarded((d.T, d.D), td)}
+    if t["gate"] is not None:
+        o["gate"] = Guarded(t["gate"].shape, torch.float32)
+    for k, on in (("post", d.post), ("pre", d.pre)):
+        if on:
+            o["w_" + k], o["b_" + k] = Guarded((d.D,), torch.float32), Guarded((d.D,), torch.float32)
+    ask = {k: v.t if want is None or k in want else None for k, v in o.items()}
+    s = Scratch(B.cac_block_norm_workspace_size(d, B.BLOCK_NORM_BWD))
+    B.cac_block_norm_bwd(d, t["F"], t["S"] if d.pre else None, t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["dH"], t["dS"], t["rng"],
+                         ask["dR"], ask["dF"], *(ask.get(k) for k in NAMES), s.ws)
+    torch.cuda.synchronize()
+    s.check()
+    for k, v in o.items():
+        v.check(k)
+        if ask[k] is None:
+            assert bool((v.raw == 0xA5).all())
+    return {k: v for k, v in ask.items() if v is not None}
+
+
+def check(t):
+    got = forward(t)
+    t["S"] = got["S"].clone()
+    r, e = reference(t)
+    got.update(backward(t))
+    limit = 1e-5 if t["desc"].dtype == B.F32 else 2.0 ** -8
+    for k, v in got.items():
+        close(k, v, r[k], e[k])
+        if t["desc"].D == 1:
+            continue  # a row of one number is normalised to 1 less eps / (2 x^2): its gradient, g (1 - xhat^2), is 1e-5 of what is subtracted, and 2^-23 of that 1.2 %
+        tight = 1e-5 if v.dtype == torch.float32 else limit
+        assert rel(v, r[k]) <= tight, (k, rel(v, r[k]))
+
+
+SHAPES = [(1, 1), (1, 8), (1, 512), (1, 2048), (2, 9), (3, 77), (5, 16384), (7, 513), (33, 1001), (64, 512), (130, 1024), (257, 2047), (300, 96), (1500, 520), (40, 4104), (33, 8192),
+          (20, 9000), (5000, 24)]
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("post,pre", [(0, 1), (0, 2), (1, 0), (2, 0), (1, 1), (2, 2), (1, 2)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_norms(shape, post, pre, dtype):
+    check(make(*shape, dtype, post, pre, alpha=0.7))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("gate_rows", [1, 2, 3, 7, 49, 64, 100, 1000, 100000])
+@pytest.mark.parametrize("shape", [(1, 64), (64, 512), (300, 1001), (1030, 96), (490, 2048), (20, 16384)])
+def test_gates_and_dropout(shape, gate_rows, dtype):
+    check(make(*shape, dtype, 2 if shape[1] % 2 else 1, (gate_rows % 3), gate_rows=gate_rows, p=0.3, alpha=-1.3))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("G", [1, 5])
+def test_many_gates(G, dtype):
+    check(make(20000, 40, dtype, 1, 1, gate_rows=G, p=0.1))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("D,ld_f,ld_r", [(96, 104, 0), (96, 0, 97), (97, 99, 101), (96, 98, 100), (2048, 2056, 4096)])
+def test_strides(D, ld_f, ld_r, dtype):
+    check(make(45, D, dtype, 1, 2, gate_rows=9, p=0.2, ld_f=ld_f, ld_r=ld_r))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("post,pre", [(0, 1), (1, 2), (2, 0), (0, 0)])
+def test_without_weights_or_residual(post, pre, dtype):
+    check(make(50, 200, dtype, post, pre, res=False, weights=False, ds=False, gate_rows=0 if post else 50))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_a_norm_alone(dtype):
+    """H alone, of F as it is; S is F then."""
+    t = make(60, 300, dtype, 0, 2, res=False)
+    got = forward(t, with_s=False)
+    t["S"] = t["F"].clone()
+    r, e = reference(t)
+    close("H", got["H"], r["H"], e["H"])
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_some_gradients(dtype):
+    t = make(700, 136, dtype, 2, 2, gate_rows=70, p=0.2)
+    t["S"] = forward(t)["S"].clone()
+    every = backward(t)
+    for want in (("dR",), ("dF",), ("gate",), ("w_post", "b_pre"), ("b_post",), ("w_pre", "dF")):
+        some = backward(t, want)
+        assert set(some) == set(want) and all(torch.equal(some[k], every[k]) for k in want)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("D", [512, 1001])
+def test_in_place(D, dtype):
+    t = make(90, D, dtype, 1, 1, gate_rows=30, p=0.2)
+    want = {k: v.clone() for k, v in forward(t).items()}
+    t["S"] = want["S"].clone()
+    grads = {k: v.clone() for k, v in backward(t).items()}
+    H = torch.empty_like(want["H"])
+    B.cac_block_norm_fwd(t["desc"], t["F"], t["R"], *(t[k] for k in NAMES), t["rng"], t["R"], H)
+    assert torch.equal(t["R"], want["S"]) and torch.equal(H, want["H"])
+    ws = torch.empty(B.cac_block_norm_workspace_size(t["desc"], B.BLOCK_NORM_BWD), dtype=torch.uint8, device=DEV)
+    B.cac_block_norm_bwd(t["desc"], t["F"], t["S"], t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["dH"], t["dS"], t["rng"], t["dS"], t["F"],
+                         None, None, None, None, None, ws)
+    assert torch.equal(t["dS"], grads["dR"]) and torch.equal(t["F"], grads["dF"])
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_rows_of_one_number_zeros_infinities_and_nan(dtype):
+    t = make(40, 200, dtype, 2, 2, res=True)
+    clean = {k: v.clone() for k, v in forward(t).items()}
+    t["F"][3], t["R"][3] = 0, 0                   # a row of zeros is b_post, then normalised
+    t["F"][4] = 2.5                               # no spread: eps alone
+    t["F"][5, 7], t["F"][6, 9], t["R"][7, 0] = float("nan"), float("inf"), float("inf")
+    got = forward(t)
+    t["S"] = got["S"].clone()
+    r, e = reference(t)
+    good = torch.ones(40, dtype=torch.bool, device=DEV)
+    good[5:8] = False
+    for k in ("S", "H"):
+        close(k, got[k][good], r[k][good], e[k][good])
+        assert torch.equal(got[k][8:], clean[k][8:])
+        assert bool(torch.isnan(got[k][5]).all())
+    assert bool(torch.isnan(got["H"][6]).all()) and bool(torch.isnan(got["H"][7]).all())
+    back = backward(t)
+    for k in ("dR", "dF"):
+        close(k, back[k][good], r[k][good], e[k][good])
+    assert bool(torch.isnan(back["dR"][5]).all()) and bool(torch.isnan(back["w_pre"]).all())
+
+
+def test_gradients_against_differences():
+    """Central differences of the formula in 64 bits along random directions."""
+    t = make(24, 50, B.F32, 2, 2, gate_rows=6, p=0.25, alpha=0.7)
+    keep = keep_factor(24, 50, 0.25, SITE, t["rng"].tolist()).to(DEV) * float(np.float32(0.7))
+    at = {k: t[k].double() for k in ("F", "R", *NAMES)}
+
+    def both(v):
+        n = norm(2, v["F"], EPS[0], v["w_post"], v["b_post"])[0]
+        s = v["R"] + keep * v["gate"].repeat_interleave(6, 0) * n
+        return s, norm(2, s, EPS[1], v["w_pre"], v["b_pre"])[0]
+
+    def value(v):
+        s, h = both(v)
+        return float((s * t["dS"].double()).sum() + (h * t["dH"].double()).sum())
+
+    t["S"] = both(at)[0].float()
+    got = backward(t)
+    got = {"F": got["dF"], "R": got["dR"], **{k: got[k] for k in NAMES}}
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    for k, grad in got.items():
+        v = torch.randn(at[k].shape, generator=g, device=DEV, dtype=torch.float64)
+        h = 1e-5
+        slope = (value({**at, k: at[k] + h * v}) - value({**at, k: at[k] - h * v})) / (2 * h)
+        assert abs(float((grad.double() * v).sum()) - slope) <= 2e-5 * float(grad.double().norm() * v.norm()), k
+
+
+@pytest.mark.parametrize("shape,gate_rows", [((1, 2048), 0), ((3000, 512), 3000), ((600, 2049), 50)])
+def test_replays(shape, gate_rows):
+    t = make(*shape, B.BF16, 1, 2, gate_rows=gate_rows, p=0.2)
+    d = t["desc"]
+    ws = torch.empty(max(16, B.cac_block_norm_workspace_size(d, B.BLOCK_NORM_BWD)), dtype=torch.uint8, device=DEV)
+
+    def new():
+        o = [torch.empty(d.T, d.D, dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+        return o + [torch.empty_like(t["gate"]) if gate_rows else None] + [torch.empty(d.D, device=DEV) for _ in range(4)]
+
+    def both(o):
+        B.cac_block_norm_fwd(d, t["F"], t["R"], *(t[k] for k in NAMES), t["rng"], o[0], o[1])
+        B.cac_block_norm_bwd(d, t["F"], o[0], t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["dH"], t["dS"], t["rng"], o[2], o[3], *o[4:], ws)
+
+    o = new()
+    both(o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(o)
+    for step in range(3):
+        t["rng"][1] = step
+        graph.replay()
+        got = [x.clone() for x in o if x is not None]
+        want = new()
+        ws.fill_(0xFF)
+        both(want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, [x for x in want if x is not None]))
