@@ -246,8 +246,8 @@ int cac_block_norm_describe_plan(const cac_block_norm_desc *d, int op, char *buf
     int rc = make_norm(d, op == CAC_BLOCK_NORM_BWD, &g, &p, &drop);
     if (rc) return rc;
     if (!buf || buf_len == 0) return fail(CAC_ERR_INVALID_ARG, "buf is NULL or empty");
-    snprintf(buf, buf_len, "%ld workgroups, %d rows at once of %d waves, %d groups of eight to a lane%s", p.blocks, p.slots, p.waves, p.chunks,
-             p.own_groups ? ", gates by rows" : "");
+    snprintf(buf, buf_len, "%ld workgroups, %d rows at once of %d lanes, %d groups of eight to a lane%s", p.split.blocks, p.slots, p.lanes * p.waves, p.chunks,
+             p.two ? ", sums by themselves" : "");
     return CAC_OK;
 }
 

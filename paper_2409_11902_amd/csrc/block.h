@@ -20,14 +20,18 @@ struct NormGeom {
     long gate_rows;       // rows that share one of the gate's; 0: no gate
     float eps_post, eps_pre, alpha;
 };
-struct NormPlan {
-    int waves, chunks;      // to a row; groups of eight to a lane
-    int slots;              // rows that a workgroup has in hand at once
-    bool own_groups;        // backward: a slot has groups of the gate to itself
-    long groups;            // of rows with one gate (1 where there is none)
-    long per_group;         // backward: workgroups that share a group
+struct NormSplit { // which rows a workgroup has
+    bool own_groups;                      // backward: a slot has groups of the gate to itself
+    long per_group;                       // backward: workgroups that share a group
     long blocks, rows_per_block;
-    size_t bytes;
+};
+struct NormPlan {
+    int lanes, waves, chunks;             // to a row; groups of eight to a lane
+    int slots;                            // rows that a workgroup has in hand at once
+    long groups;                          // of rows with one gate (1 where there is none)
+    NormSplit split, sums;                // sums: of the backward pass' sums over rows
+    bool two;                             // ... which have a launch of their own
+    size_t o_known, bytes;
 };
 struct NormParams { const float *gate, *w_post, *b_post, *w_pre, *b_pre; };
 struct NormGrads { float *gate, *w_post, *b_post, *w_pre, *b_pre; };

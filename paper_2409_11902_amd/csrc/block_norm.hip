@@ -5,7 +5,7 @@
 // A norm's statistics of a row are formed from the row in registers, in the forward pass and again in the backward pass, so that neither they
 // nor the normalised row nor the mask is kept: what the backward pass reads is F and S.  With xhat = (x - mean) / sqrt(var + eps), g the gradient of
 // xhat:  dx = (g - mean(g) - xhat mean(g xhat)) / sqrt(var + eps), without the first two means for rms.
-// Bound by memory: every row is read and written once.  A row is spread over the lanes of one to sixteen waves, eight
+// Bound by memory: every row is read and written once.  A row is spread over the lanes of a quarter of a wave to sixteen waves, eight
 // neighbours to a lane (two groups of eight above 8192 columns); weights stay in registers while a workgroup goes from row to
 // row, and so do the sums over rows, whose order is fixed: a workgroup's, then the workgroups'.
 #include "block.h"
@@ -13,174 +13,242 @@
 namespace cac {
 
 struct NormArgs {
-    NormGeom g;
-    NormPlan p;
-    Drop d;
-    NormParams w;
+    int T, D, across;            // across: groups of eight to a row
+    int post, pre;               // cac_norm
+    int gate_rows, groups;       // rows that share a row of the gate (0: no gate), and how many such groups
+    int rows_per_block, blocks, per_group;
+    bool own;                    // backward: a slot has groups of the gate to itself
+    long ld_f, ld_r;
+    float eps_post, eps_pre;
     float scale;                 // alpha over the probability of being kept
     float inv_d;
-    bool wide, wide_f, wide_r;   // rows of whole groups on 16 bytes: the dense ones, F's, R's
+    Drop d;
+    NormParams w;
     const void *F, *R, *S_in, *dH, *dS;
     void *S, *H, *dR, *dF;
     NormGrads o;
     float *part;                 // [5][blocks][D], of the sums in NormGrads' order
+    float *known;                // [T][8] of long rows: mean and inverse spread of F and of S, mean and projection of pre's gradient
 };
 
-// The sum over a wave in every lane, in one order for all of them.
-__device__ __forceinline__ float wave_total(float x)
+// The sum over LANES neighbouring lanes in every one of them, in one order for all.
+template <int LANES> __device__ __forceinline__ float lanes_total(float x)
 {
     auto moved = [](float v, auto ctrl) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
-    x += moved(x, std::integral_constant<int, 0xB1>());  // neighbours
-    x += moved(x, std::integral_constant<int, 0x4E>());  // pairs
-    x += moved(x, std::integral_constant<int, 0x141>()); // fours, mirrored
-    x += moved(x, std::integral_constant<int, 0x140>()); // eights, mirrored
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    if (LANES >= 2) x += moved(x, std::integral_constant<int, 0xB1>());   // neighbours
+    if (LANES >= 4) x += moved(x, std::integral_constant<int, 0x4E>());   // pairs
+    if (LANES >= 8) x += moved(x, std::integral_constant<int, 0x141>());  // fours, mirrored
+    if (LANES >= 16) x += moved(x, std::integral_constant<int, 0x140>()); // eights, mirrored
+    if (LANES >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (LANES >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return x;
 }
 
-// The sums of two numbers over the WPR waves of a row.  `red` holds two turns, so that one meeting is enough: a wave that writes a turn's
-// numbers has met since the others read those of the turn before.
-template <int WPR> struct RowSum {
-    float2 *red; // [2][waves of the workgroup]
-    int wave, waves, turn;
-    __device__ __forceinline__ void operator()(float &a, float &b)
+// How a row lies in a workgroup: over LANES lanes of each of WPR waves, CH groups of eight to a lane.  WHOLE: rows are whole eights.
+template <int LANES_, int WPR_, int CH_, bool WHOLE_> struct Rows {
+    static constexpr int LANES = LANES_, WPR = WPR_, CH = CH_;
+    static constexpr bool WHOLE = WHOLE_;
+    static constexpr int kColumns = 8 * LANES * WPR * CH;
+    static_assert(LANES == 64 || WPR == 1, "part of a wave, or waves");
+    int n[CH], count[CH]; // the lane's first columns, and how many of its eights there are
+    int slot;             // which of the workgroup's rows
+    __device__ __forceinline__ Rows(int D, int first = 0)
     {
-        a = wave_total(a);
-        b = wave_total(b);
-        if (WPR == 1) return;
-        float2 *r = red + turn * waves;
-        if ((threadIdx.x & 63) == 0) r[wave] = make_float2(a, b);
-        __syncthreads();
-        const int first = wave / WPR * WPR;
-        a = b = 0.f;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        slot = LANES == 64 ? wave / WPR : (int)threadIdx.x / LANES;
 #pragma unroll
-        for (int k = 0; k < WPR; ++k) {
-            const float2 v = r[first + k];
-            a += v.x;
-            b += v.y;
+        for (int c = 0; c < CH; ++c) {
+            n[c] = first + ((c * WPR + wave % WPR) * LANES + threadIdx.x % LANES) * 8;
+            count[c] = min(max(D - n[c], 0), 8);
         }
-        turn ^= 1;
     }
 };
 
-// eight of a vector of weights, `otherwise` where there is none
-__device__ __forceinline__ void eight_weights(const float *w, int n, int D, float otherwise, float (&v)[8])
-{
-    if (!w) {
+// Where the WPR waves of a row meet: lane i goes away with the numbers of wave i % WPR.  `red` holds two turns, so that one meeting is enough: a
+// wave that writes a turn's numbers has met since the others read those of the turn before.
+template <class L> struct Meeting {
+    float *red; // [2][waves of the workgroup][8]
+    int waves, turn;
+    float columns; // of a row in wave lane % WPR
+    __device__ __forceinline__ Meeting(float *lds, int all, int D) : red(lds), waves(all), turn(0)
+    {
+        const int w = (threadIdx.x & 63) % L::WPR;
+        int n = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = otherwise;
-    } else if (D % 4 == 0 && n + 8 <= D) { // (rows of the gate start on 16 bytes then)
+        for (int c = 0; c < L::CH; ++c) n += min(max(D - (c * L::WPR + w) * L::LANES * 8, 0), L::LANES * 8);
+        columns = (float)n;
+    }
+    // of which a wave's lanes all have the same
+    template <int N> __device__ __forceinline__ void operator()(float (&x)[N])
+    {
+        static_assert(N <= 8, "eight to a wave");
+        if (L::WPR == 1) return;
+        float *r = red + turn * waves * 8;
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) r[wave * 8 + i] = x[i];
+        }
+        __syncthreads();
+        r += (wave / L::WPR * L::WPR + lane % L::WPR) * 8;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = r[i];
+        turn ^= 1;
+    }
+    // over a row's waves, of a number that lane i has of wave i % WPR
+    __device__ __forceinline__ float total(float x) const { return lanes_total<L::WPR>(x); }
+};
+
+// 1 / sqrt(x): the instruction's 22 bits, and a step of Newton's
+__device__ __forceinline__ float inverse_root(float x)
+{
+    const float y = __builtin_amdgcn_rsqf(x), r = fmaf(-x * y, y, 1.f);
+    return x > 0.f && x < INFINITY ? fmaf(0.5f * y, r, y) : y;
+}
+
+// eight of a vector of weights, `otherwise` where there is none, zeros past its end
+__device__ __forceinline__ void eight_weights(const float *w, int n, int count, float otherwise, float (&v)[8])
+{
+    if (w && count == 8) {
         Eight<float> x;
         x.read(w + n);
         x.get(v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = n + e < D ? w[n + e] : 0.f;
+        return;
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < count ? (w ? w[n + e] : otherwise) : 0.f;
 }
 
-// Mean (zero for rms) and one over the spread of a row,
-template <int WPR, int CH>
-__device__ __forceinline__ float2 statistics(int kind, float eps, const float (&a)[CH][8], const int (&count)[CH], float inv_d, RowSum<WPR> &sum)
+// Sum of a row's (x - mean)^2 in a lane.  What is read past a row's end is zero, and the mean away from it.
+template <class L> __device__ __forceinline__ float squares(int kind, const float (&x)[L::CH][8], float mean, const L &l)
 {
-    float m = 0.f, v = 0.f, none = 0.f;
-    if (kind == CAC_NORM_LAYER) {
+    float v = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < L::CH; ++c) {
+        float u = 0.f;
+        if (kind == CAC_NORM_RMS) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m += a[c][e];
-        sum(m, none);
-        m *= inv_d;
-    }
+            for (int e = 0; e < 8; ++e) u += x[c][e] * x[c][e];
+        } else if (L::WHOLE) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = e < count[c] ? a[c][e] - m : 0.f; // (what is read past a row's end is zero, and the mean away from it)
-            v += x * x;
-        }
-    none = 0.f;
-    sum(v, none);
-    return make_float2(m, 1.f / sqrtf(v * inv_d + eps));
-}
-// ... and of two rows with the meetings of one.
-template <int WPR, int CH>
-__device__ __forceinline__ void statistics2(int kind_a, float eps_a, const float (&a)[CH][8], float2 *of_a, int kind_b, float eps_b, const float (&b)[CH][8], float2 *of_b,
-                                            const int (&count)[CH], float inv_d, RowSum<WPR> &sum)
-{
-    float ma = 0.f, mb = 0.f, va = 0.f, vb = 0.f;
-    if (kind_a == CAC_NORM_LAYER || kind_b == CAC_NORM_LAYER) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
+            for (int e = 0; e < 8; ++e) u += (x[c][e] - mean) * (x[c][e] - mean);
+            u = l.count[c] ? u : 0.f;
+        } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                ma += a[c][e];
-                mb += b[c][e];
+                const float y = e < l.count[c] ? x[c][e] - mean : 0.f;
+                u += y * y;
             }
-        sum(ma, mb);
-        ma = kind_a == CAC_NORM_LAYER ? ma * inv_d : 0.f;
-        mb = kind_b == CAC_NORM_LAYER ? mb * inv_d : 0.f;
+        }
+        v += u;
+    }
+    return v;
+}
+template <class L> __device__ __forceinline__ float lane_sum(const float (&x)[L::CH][8])
+{
+    float v = 0.f;
+#pragma unroll
+    for (int c = 0; c < L::CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v += x[c][e];
+    return v;
+}
+
+// A row's mean and the sum of squares about it come from one meeting: each wave has its own mean and the squares about that, and
+//   sum (x - mean)^2 = sum over waves of (squares about the wave's mean + columns (wave's mean - mean)^2).
+struct Stats { float mean, inv; }; // mean is 0 for rms
+template <class L> __device__ __forceinline__ float wave_mean(int kind, const float (&x)[L::CH][8], const Meeting<L> &meet)
+{
+    if (kind != CAC_NORM_LAYER) return 0.f;
+    const float n = L::WPR == 1 ? meet.columns : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(meet.columns), __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % L::WPR));
+    return lanes_total<L::LANES>(lane_sum<L>(x)) * __builtin_amdgcn_rcpf(fmaxf(n, 1.f)); // (any number near the mean will do, the same for all)
+}
+// from the waves' means m and squares q
+template <class L> __device__ __forceinline__ Stats joined_stats(int kind, float eps, float m, float q, float inv_d, const Meeting<L> &meet)
+{
+    float mean = 0.f;
+    if (kind == CAC_NORM_LAYER && L::WPR == 1) mean = m;
+    if (kind == CAC_NORM_LAYER && L::WPR > 1) {
+        mean = meet.total(meet.columns * m) * inv_d;
+        q += meet.columns * ((m - mean) * (m - mean));
+    }
+    return Stats{mean, inverse_root(meet.total(q) * inv_d + eps)};
+}
+template <class L> __device__ __forceinline__ Stats statistics(int kind, float eps, const float (&x)[L::CH][8], const L &l, const NormArgs &a, Meeting<L> &meet)
+{
+    float of[2];
+    of[0] = wave_mean<L>(kind, x, meet);
+    of[1] = lanes_total<L::LANES>(squares(kind, x, of[0], l));
+    meet(of);
+    return joined_stats<L>(kind, eps, of[0], of[1], a.inv_d, meet);
+}
+// the row before weights
+template <class L> __device__ __forceinline__ void normalise(int kind, Stats s, float (&x)[L::CH][8])
+{
+    if (kind == CAC_NORM_NONE) return;
+    if (kind == CAC_NORM_LAYER) {
+#pragma unroll
+        for (int c = 0; c < L::CH; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[c][e] -= s.mean;
     }
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < L::CH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = e < count[c] ? a[c][e] - ma : 0.f, y = e < count[c] ? b[c][e] - mb : 0.f;
-            va += x * x;
-            vb += y * y;
-        }
-    sum(va, vb);
-    *of_a = make_float2(ma, 1.f / sqrtf(va * inv_d + eps_a));
-    *of_b = make_float2(mb, 1.f / sqrtf(vb * inv_d + eps_b));
+        for (int e = 0; e < 8; ++e) x[c][e] *= s.inv;
+}
+// g, the gradient of the normalised row x, to that of the row, which is added to `to`; mean: of g (0 for rms), along: of g x
+template <class L> __device__ __forceinline__ void add_gradient(float inv, float mean, float along, const float (&x)[L::CH][8], const float (&g)[L::CH][8], float (&to)[L::CH][8])
+{
+#pragma unroll
+    for (int c = 0; c < L::CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[c][e] += inv * (g[c][e] - mean - x[c][e] * along);
 }
 
 template <int WPR> constexpr int kFwdWaves = WPR > 4 ? WPR : 4;
 template <int WPR> constexpr int kBwdWaves = WPR > 8 ? WPR : 8;
 
-template <typename T, int WPR, int CH> __global__ void __launch_bounds__(64 * kFwdWaves<WPR>) norm_fwd_kernel(const NormArgs a)
+template <typename T, class L> __global__ void __launch_bounds__(64 * kFwdWaves<L::WPR>) norm_fwd_kernel(const NormArgs a)
 {
-    constexpr int kWaves = kFwdWaves<WPR>, kSlots = kWaves / WPR;
-    __shared__ float2 red[2 * kWaves];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slot = wave / WPR, D = (int)a.g.D;
-    RowSum<WPR> sum{red, wave, kWaves, 0};
-    const long r0 = blockIdx.x * a.p.rows_per_block, r1 = min(a.g.T, r0 + a.p.rows_per_block);
-    int n[CH], count[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        n[c] = ((c * WPR + wave % WPR) * 64 + lane) * 8;
-        count[c] = min(max(D - n[c], 0), 8);
-    }
-    const int across = (D + 7) / 8;
+    constexpr int kWaves = kFwdWaves<L::WPR>, kSlots = kWaves * 64 / L::LANES / L::WPR, CH = L::CH;
+    __shared__ float red[16 * kWaves];
+    const int D = a.D;
+    const L l(D);
+    Meeting<L> meet(red, kWaves, D);
+    const int r0 = blockIdx.x * a.rows_per_block, r1 = min(a.T, r0 + a.rows_per_block);
     const DropKey key = drop_key(a.d);
     Eight<T> f[CH], r[CH];
     auto ask = [&](long row) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
-            if (count[c]) {
-                f[c] = read_eight((const T *)a.F + row * a.g.ld_f, n[c], D, a.wide_f);
-                if (a.R) r[c] = read_eight((const T *)a.R + row * a.g.ld_r, n[c], D, a.wide_r);
+            if (l.count[c]) {
+                f[c] = read_eight<L::WHOLE>((const T *)a.F + row * a.ld_f, l.n[c], D);
+                if (a.R) r[c] = read_eight<L::WHOLE>((const T *)a.R + row * a.ld_r, l.n[c], D);
             }
     };
-    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        f[c].set(zero);
-        r[c].set(zero);
+        f[c].clear();
+        r[c].clear();
     }
-    if (r0 + slot < r1) ask(r0 + slot);
-    float w_post[CH][8], b_post[CH][8], w_pre[CH][8], b_pre[CH][8], gate[CH][8];
+    if (r0 + l.slot < r1) ask(r0 + l.slot);
+    // post's weights, the gate and the branch's factor as one factor and one summand, zeros past a row's end
+    float w_pre[CH][8], b_pre[CH][8], factor[CH][8], summand[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        eight_weights(a.w.w_post, n[c], D, 1.f, w_post[c]);
-        eight_weights(a.w.b_post, n[c], D, 0.f, b_post[c]);
-        eight_weights(a.w.w_pre, n[c], D, 1.f, w_pre[c]);
-        eight_weights(a.w.b_pre, n[c], D, 0.f, b_pre[c]);
+        eight_weights(a.w.w_pre, l.n[c], l.count[c], 1.f, w_pre[c]);
+        eight_weights(a.w.b_pre, l.n[c], l.count[c], 0.f, b_pre[c]);
     }
-    long group = -1;
-    for (long base = r0; base < r1; base += kSlots) {
-        const long row = base + slot;
+    int group = -1, last = -1; // the gate's row at hand, and the last of T that it is of
+    for (int base = r0; base < r1; base += kSlots) {
+        const int row = base + l.slot;
         const bool there = row < r1;
         float v[CH][8], s[CH][8];
 #pragma unroll
@@ -189,209 +257,312 @@ template <typename T, int WPR, int CH> __global__ void __launch_bounds__(64 * kF
             r[c].get(s[c]);
         }
         if (row + kSlots < r1) ask(row + kSlots);
-        const long here = a.g.gate_rows ? row / a.g.gate_rows : 0;
-        if (here != group) {
-            group = here;
+        if (row > last) {
+            group = a.gate_rows && there ? row / a.gate_rows : 0;
+            last = a.gate_rows && there ? group * a.gate_rows + a.gate_rows - 1 : a.T;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) eight_weights(a.w.gate && there ? a.w.gate + here * D : nullptr, n[c], D, 1.f, gate[c]);
+            for (int c = 0; c < CH; ++c) {
+                float gate[8];
+                eight_weights(a.w.w_post, l.n[c], l.count[c], 1.f, factor[c]);
+                eight_weights(a.w.b_post, l.n[c], l.count[c], 0.f, summand[c]);
+                eight_weights(a.w.gate ? a.w.gate + (long)group * D : nullptr, l.n[c], l.count[c], 1.f, gate);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    factor[c][e] *= gate[e] * a.scale;
+                    summand[c][e] *= gate[e] * a.scale;
+                }
+            }
         }
-        if (a.g.post != CAC_NORM_NONE) {
-            const float2 st = statistics<WPR, CH>(a.g.post, a.g.eps_post, v, count, a.inv_d, sum);
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[c][e] = (v[c][e] - st.x) * st.y * w_post[c][e] + b_post[c][e];
-        }
+        if (a.post != CAC_NORM_NONE) normalise<L>(a.post, statistics(a.post, a.eps_post, v, l, a, meet), v);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[c][e] *= gate[c][e];
-            drop_eight(key, a.d, (uint64_t)(row * across + (n[c] >> 3)), a.scale, v[c]);
+            for (int e = 0; e < 8; ++e) v[c][e] = v[c][e] * factor[c][e] + summand[c][e];
+            drop_eight(key, a.d, (uint64_t)row * a.across + (l.n[c] >> 3), v[c]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[c][e] = e < count[c] ? s[c][e] + v[c][e] : 0.f;
-            if (there && count[c] && a.S) write_eight((T *)a.S + row * D, n[c], D, a.wide, s[c]);
+            for (int e = 0; e < 8; ++e) s[c][e] += v[c][e];
+            if (there && l.count[c] && a.S) write_eight<L::WHOLE>((T *)a.S + (long)row * D, l.n[c], D, s[c]);
         }
         if (!a.H) continue;
-        const float2 st = statistics<WPR, CH>(a.g.pre, a.g.eps_pre, s, count, a.inv_d, sum);
+        normalise<L>(a.pre, statistics(a.pre, a.eps_pre, s, l, a, meet), s);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[c][e] = (s[c][e] - st.x) * st.y * w_pre[c][e] + b_pre[c][e];
-            if (there && count[c]) write_eight((T *)a.H + row * D, n[c], D, a.wide, s[c]);
+            for (int e = 0; e < 8; ++e) s[c][e] = s[c][e] * w_pre[c][e] + b_pre[c][e];
+            if (there && l.count[c]) write_eight<L::WHOLE>((T *)a.H + (long)row * D, l.n[c], D, s[c]);
         }
     }
 }
 
 enum { kGate, kWPost, kBPost, kWPre, kBPre, kSums };
 
-template <typename T, int WPR, int CH> __global__ void __launch_bounds__(64 * kBwdWaves<WPR>, 4) norm_bwd_kernel(const NormArgs a)
+// The sums over rows that the gate and post's weights need are two, of a and of a xhat, as long as the gate is the same:
+//   dgate = w sum(a xhat) + b sum(a),  dw = gate sum(a xhat),  db = gate sum(a).
+// A workgroup has rows of one group (a run of them, its slots taking turns); or (own_groups) every slot has groups to itself, and adds
+// a group's sums up in LDS when it ends.
+// Both parts in one pass where a workgroup's registers hold a row and its sums; of longer rows the row part leaves what it knows of a row, eight numbers,
+// and the sum part has 512 columns to a workgroup and reads the rows again.
+enum Part { kBoth, kRowPart, kSumPart };
+template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 * kBwdWaves<L::WPR>, 2) norm_bwd_kernel(const NormArgs a)
 {
-    constexpr int kWaves = kBwdWaves<WPR>, kSlots = kWaves / WPR, kColumns = 512 * WPR * CH;
-    __shared__ float2 red[2 * kWaves];
-    __shared__ float joined[kSlots > 1 ? (kSlots - 1) * kColumns : 1];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slot = wave / WPR, D = (int)a.g.D;
-    RowSum<WPR> sum{red, wave, kWaves, 0};
-    int n[CH], count[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        n[c] = ((c * WPR + wave % WPR) * 64 + lane) * 8;
-        count[c] = min(max(D - n[c], 0), 8);
-    }
-    const int across = (D + 7) / 8;
+    constexpr int kWaves = kBwdWaves<L::WPR>, kThreads = 64 * kWaves, kSlots = kThreads / L::LANES / L::WPR, CH = L::CH;
+    constexpr bool kTakesSums = PART != kRowPart, kAhead = PART != kRowPart && (CH == 1 || sizeof(T) == 2); // (else there are no registers for a row ahead)
+    __shared__ float red[16 * kWaves];
+    __shared__ float kept[kTakesSums ? 2 : 1][CH][8][kTakesSums ? kThreads : 1]; // own_groups: sums for w_post and b_post
+    __shared__ float joined[kSlots > 1 ? kThreads * 8 : 1];
+    const int D = a.D;
+    const L l(D, PART == kSumPart ? blockIdx.y * L::kColumns : 0);
+    Meeting<L> meet(red, kWaves, D);
     const DropKey key = drop_key(a.d);
-    const bool post = a.g.post != CAC_NORM_NONE, pre = a.g.pre != CAC_NORM_NONE, gated = a.w.gate != nullptr;
+    const bool post = a.post != CAC_NORM_NONE, pre = a.pre != CAC_NORM_NONE, own = a.own, wants_a = a.o.b_post || (a.o.gate && a.w.b_post);
 
-    // Rows: a run of one group's, the slots taking turns; or (own_groups) every slot has whole groups to itself, this many apart.
-    const long G = a.g.gate_rows ? a.g.gate_rows : a.g.T;
-    const long slots_all = a.p.blocks * kSlots, first_group = a.p.own_groups ? blockIdx.x * kSlots + slot : blockIdx.x / a.p.per_group;
-    const long r0 = first_group * G + (blockIdx.x % a.p.per_group) * a.p.rows_per_block;
-    const long r1 = min(min(a.g.T, first_group * G + G), r0 + a.p.rows_per_block);
-    const long turns = a.p.own_groups ? (a.p.groups + slots_all - 1) / slots_all * G : (a.p.rows_per_block + kSlots - 1) / kSlots;
+    const int rows = a.T, G = a.gate_rows ? a.gate_rows : rows, slots_all = a.blocks * kSlots, groups = a.groups;
+    int group = own ? blockIdx.x * kSlots + l.slot : blockIdx.x / (unsigned)a.per_group;
+    const int per_block = a.rows_per_block, r0 = group * (own ? 0 : G) + blockIdx.x % (unsigned)a.per_group * per_block;
+    const int r1 = min(rows, min(own ? 0 : group * G + G, r0 + per_block));
+    const int turns = own ? (groups + slots_all - 1) / slots_all * G : (per_block + kSlots - 1) / kSlots;
+    // the row of a turn, or one past the last
+    int asked = r0 + l.slot, asked_group = group;
+    if (own) asked = 0;
+    auto next_row = [&]() {
+        int row = asked;
+        if (!own) {
+            asked += kSlots;
+            return row < r1 ? row : rows;
+        }
+        row = asked_group < groups ? min(asked_group * G + row, rows) : rows;
+        if (++asked == G) {
+            asked = 0;
+            asked_group += slots_all;
+        }
+        return row;
+    };
+    Eight<T> x[4][CH];
+    auto ask = [&](long row) {
+        if (row >= rows) return;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (l.count[c]) {
+                if (a.F) x[0][c] = read_eight<L::WHOLE>((const T *)a.F + row * a.ld_f, l.n[c], D);
+                if (pre) x[1][c] = read_eight<L::WHOLE>((const T *)a.S_in + row * D, l.n[c], D);
+                if (pre) x[2][c] = read_eight<L::WHOLE>((const T *)a.dH + row * D, l.n[c], D);
+                if (a.dS) x[3][c] = read_eight<L::WHOLE>((const T *)a.dS + row * D, l.n[c], D);
+            }
+    };
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) x[k][c].clear();
 
-    float w_post[CH][8], b_post[CH][8], w_pre[CH][8], gate[CH][8], total[kSums][CH][8];
+    float w_pre[CH][8], factor[CH][8], sum_a[CH][8], sum_ax[CH][8], sum_h[CH][8], sum_hx[CH][8];
+    auto gate_factor = [&](int g) { // gate times w_post times the branch's factor, zeros past a row's end
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            float gate[8];
+            eight_weights(a.w.w_post, l.n[c], l.count[c], 1.f, factor[c]);
+            eight_weights(a.w.gate && g < groups ? a.w.gate + (long)g * D : nullptr, l.n[c], l.count[c], 1.f, gate);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) factor[c][e] *= gate[e] * a.scale;
+        }
+    };
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        eight_weights(a.w.w_post, n[c], D, 1.f, w_post[c]);
-        eight_weights(a.w.b_post, n[c], D, 0.f, b_post[c]);
-        eight_weights(a.w.w_pre, n[c], D, 1.f, w_pre[c]);
+        eight_weights(a.w.w_pre, l.n[c], l.count[c], 1.f, w_pre[c]);
 #pragma unroll
-        for (int k = 0; k < kSums; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) total[k][c][e] = 0.f;
+        for (int e = 0; e < 8; ++e) {
+            sum_a[c][e] = sum_ax[c][e] = sum_h[c][e] = sum_hx[c][e] = 0.f;
+            if constexpr (kTakesSums)
+                if (own) kept[0][c][e][threadIdx.x] = kept[1][c][e][threadIdx.x] = 0.f;
+        }
     }
-    long group = -1, in_group = 0, own = first_group;
-    for (long t = 0; t < turns; ++t) {
-        long row = r0 + t * kSlots + slot;
-        bool there = row < r1;
-        long here = first_group;
-        if (a.p.own_groups) {
-            row = own * G + in_group;
-            there = own < a.p.groups && row < a.g.T;
-            here = own;
-        }
-        if (here != group && there) {
-            group = here;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) eight_weights(gated ? a.w.gate + here * D : nullptr, n[c], D, 1.f, gate[c]);
-        }
+    gate_factor(group);
+    int now = kAhead ? next_row() : 0, in_group = 0;
+    if (kAhead) ask(now);
+    for (int t = 0; t < turns; ++t) {
+        if (!kAhead) ask(now = next_row());
+        const long row = now;
+        const bool there = now < rows;
+        if (kAhead) now = t + 1 < turns ? next_row() : rows;
         float f[CH][8], s[CH][8], g[CH][8], h[CH][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            Eight<T> x[4];
-            const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[k].set(zero);
-            if (there && count[c]) {
-                if (a.F) x[0] = read_eight((const T *)a.F + row * a.g.ld_f, n[c], D, a.wide_f);
-                if (pre) x[1] = read_eight((const T *)a.S_in + row * D, n[c], D, a.wide);
-                if (pre) x[2] = read_eight((const T *)a.dH + row * D, n[c], D, a.wide);
-                if (a.dS) x[3] = read_eight((const T *)a.dS + row * D, n[c], D, a.wide);
-            }
-            x[0].get(f[c]);
-            x[1].get(s[c]);
-            x[2].get(h[c]);
-            x[3].get(g[c]);
+            x[0][c].get(f[c]);
+            x[1][c].get(s[c]);
+            x[2][c].get(h[c]);
+            x[3][c].get(g[c]);
         }
-        float2 of_s = make_float2(0.f, 1.f), of_f = make_float2(0.f, 1.f);
-        if (post && pre) statistics2<WPR, CH>(a.g.pre, a.g.eps_pre, s, &of_s, a.g.post, a.g.eps_post, f, &of_f, count, a.inv_d, sum);
-        else if (pre) of_s = statistics<WPR, CH>(a.g.pre, a.g.eps_pre, s, count, a.inv_d, sum);
-        else if (post) of_f = statistics<WPR, CH>(a.g.post, a.g.eps_post, f, count, a.inv_d, sum);
-        if (pre) {
-            float mean = 0.f, along = 0.f;
+        if (kAhead) ask(now);
+        Stats of_s = {0.f, 1.f}, of_f = {0.f, 1.f};
+        float mean = 0.f, along = 0.f; // of pre's gradient
+        if constexpr (PART == kSumPart) {
+            const float *k = a.known + (there ? row : 0) * 8;
+            of_f = Stats{k[0], k[1]};
+            of_s = Stats{k[2], k[3]};
+            mean = k[4];
+            along = k[5];
+        } else {
+            float first[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; // means and squares of F and S; sums of w dH and w dH (S - S's mean)
+            if (post) {
+                first[0] = wave_mean<L>(a.post, f, meet);
+                first[1] = lanes_total<L::LANES>(squares(a.post, f, first[0], l));
+            }
+            if (pre) {
+                first[2] = wave_mean<L>(a.pre, s, meet);
+                first[3] = lanes_total<L::LANES>(squares(a.pre, s, first[2], l));
+                float with = 0.f;
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[c][e] = (s[c][e] - of_s.x) * of_s.y;
-                    if (there) total[kWPre][c][e] += h[c][e] * s[c][e];
-                    total[kBPre][c][e] += h[c][e];
-                    h[c][e] *= w_pre[c][e];
-                    mean += h[c][e];
-                    along += h[c][e] * s[c][e];
+                    for (int e = 0; e < 8; ++e) {
+                        const float hw = h[c][e] * w_pre[c][e];
+                        first[4] += hw;
+                        with += hw * (s[c][e] - first[2]);
+                    }
+                if (a.pre == CAC_NORM_LAYER) first[4] = lanes_total<L::LANES>(first[4]);
+                first[5] = lanes_total<L::LANES>(with);
+            }
+            if (post || pre) meet(first);
+            if (post) of_f = joined_stats<L>(a.post, a.eps_post, first[0], first[1], a.inv_d, meet);
+            if (pre) {
+                of_s = joined_stats<L>(a.pre, a.eps_pre, first[2], first[3], a.inv_d, meet);
+                along = first[5];
+                if (a.pre == CAC_NORM_LAYER) {
+                    mean = meet.total(first[4]) * a.inv_d;
+                    if (L::WPR > 1) along += (first[2] - of_s.mean) * first[4];
                 }
-            sum(mean, along);
-            mean = a.g.pre == CAC_NORM_LAYER ? mean * a.inv_d : 0.f;
-            along *= a.inv_d;
+                along = meet.total(along) * (of_s.inv * a.inv_d);
+            }
+            if (PART == kRowPart && there && threadIdx.x == 0) {
+                float *k = a.known + row * 8;
+                k[0] = of_f.mean, k[1] = of_f.inv, k[2] = of_s.mean, k[3] = of_s.inv, k[4] = mean, k[5] = along;
+            }
+        }
+        if (pre) {
+            normalise<L>(a.pre, of_s, s);
+            if (kTakesSums && there) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        sum_hx[c][e] += h[c][e] * s[c][e];
+                        sum_h[c][e] += h[c][e];
+                    }
+            }
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[c][e] += of_s.y * (h[c][e] - mean - s[c][e] * along);
+                for (int e = 0; e < 8; ++e) h[c][e] *= w_pre[c][e];
+            add_gradient<L>(of_s.inv, mean, along, s, h, g);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            if (there && count[c] && a.dR) write_eight((T *)a.dR + row * D, n[c], D, a.wide, g[c]);
-            drop_eight(key, a.d, (uint64_t)(row * across + (n[c] >> 3)), a.scale, g[c]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g[c][e] = e < count[c] && there ? g[c][e] : 0.f;
+            if (PART != kSumPart && there && l.count[c] && a.dR) write_eight<L::WHOLE>((T *)a.dR + row * D, l.n[c], D, g[c]);
+            drop_eight(key, a.d, (uint64_t)row * a.across + (l.n[c] >> 3), g[c]); // (the factor comes last, to these and to the sums of them)
         }
-        if (there) {
+        if (post) normalise<L>(a.post, of_f, f);
+        if (kTakesSums && there) {
 #pragma unroll
             for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    f[c][e] = (f[c][e] - of_f.x) * of_f.y;
-                    total[kGate][c][e] += g[c][e] * (f[c][e] * w_post[c][e] + b_post[c][e]);
-                    g[c][e] *= gate[c][e];
-                    total[kWPost][c][e] += g[c][e] * f[c][e];
-                    total[kBPost][c][e] += g[c][e];
-                }
-        }
-        if (post) {
-            float mean = 0.f, along = 0.f;
+                for (int e = 0; e < 8; ++e) sum_ax[c][e] += g[c][e] * f[c][e];
+            if (wants_a) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    g[c][e] *= w_post[c][e];
-                    mean += g[c][e];
-                    along += g[c][e] * f[c][e];
-                }
-            sum(mean, along);
-            mean = a.g.post == CAC_NORM_LAYER ? mean * a.inv_d : 0.f;
-            along *= a.inv_d;
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[c][e] = of_f.y * (g[c][e] - mean - f[c][e] * along);
-        }
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (there && count[c] && a.dF) write_eight((T *)a.dF + row * D, n[c], D, a.wide, g[c]);
-        if (a.p.own_groups && (++in_group == G || t + 1 == turns)) { // a whole group's gate
-            in_group = 0;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                if (own < a.p.groups && a.o.gate) write_eight(a.o.gate + own * D, n[c], D, D % 4 == 0 && n[c] + 8 <= D, total[kGate][c]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) total[kGate][c][e] = 0.f;
+                    for (int e = 0; e < 8; ++e) sum_a[c][e] += g[c][e];
             }
-            own += slots_all;
+        }
+        if constexpr (PART != kSumPart) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g[c][e] *= factor[c][e];
+                    h[c][e] = 0.f;
+                }
+            if (post) {
+                float second[2] = {0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) second[1] += g[c][e] * f[c][e];
+                if (a.post == CAC_NORM_LAYER) second[0] = lanes_total<L::LANES>(lane_sum<L>(g));
+                second[1] = lanes_total<L::LANES>(second[1]);
+                meet(second);
+                add_gradient<L>(of_f.inv, a.post == CAC_NORM_LAYER ? meet.total(second[0]) * a.inv_d : 0.f, meet.total(second[1]) * a.inv_d, f, g, h);
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (there && l.count[c] && a.dF) write_eight<L::WHOLE>((T *)a.dF + row * D, l.n[c], D, post ? h[c] : g[c]);
+        }
+        if (own && ++in_group == G) { // a whole group's
+            in_group = 0;
+            if constexpr (kTakesSums)
+                if (group < groups)
+#pragma unroll
+                    for (int c = 0; c < CH; ++c) {
+                        float w[8], b[8];
+                        eight_weights(a.w.gate + (long)group * D, l.n[c], l.count[c], 1.f, w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            kept[0][c][e][threadIdx.x] += w[e] * (a.scale * sum_ax[c][e]);
+                            kept[1][c][e][threadIdx.x] += w[e] * (a.scale * sum_a[c][e]);
+                        }
+                        eight_weights(a.w.w_post, l.n[c], l.count[c], 1.f, w);
+                        eight_weights(a.w.b_post, l.n[c], l.count[c], 0.f, b);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            w[e] = a.scale * (w[e] * sum_ax[c][e] + b[e] * sum_a[c][e]);
+                            sum_ax[c][e] = sum_a[c][e] = 0.f;
+                        }
+                        if (a.o.gate && l.count[c]) write_eight(a.o.gate + (long)group * D, l.n[c], D, w);
+                    }
+            group += slots_all;
+            gate_factor(group);
         }
     }
 
+    if constexpr (!kTakesSums) return;
     float *const out[kSums] = {a.o.gate, a.o.w_post, a.o.b_post, a.o.w_pre, a.o.b_pre};
 #pragma unroll
     for (int k = 0; k < kSums; ++k) {
-        if (!out[k] || (k == kGate && a.p.own_groups)) continue;
-        if (kSlots > 1) {
-            const int at = (wave % WPR * 64 + lane) * 8; // (CH is 1 where there are slots)
-            if (slot > 0) {
-                Eight<float> x;
-                x.set(total[k][0]);
-                x.write(joined + (slot - 1) * kColumns + at);
+        if (!out[k] || (k == kGate && own)) continue;
+        float *to = k == kGate ? (a.per_group == 1 ? out[k] + (long)group * D : nullptr) : a.blocks == 1 ? out[k] : nullptr;
+        if (!to) to = a.part + ((long)k * a.blocks + blockIdx.x) * D;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            float v[8];
+            if (k == kWPre || k == kBPre) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = k == kWPre ? sum_hx[c][e] : sum_h[c][e];
+            } else if (own) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = kept[kTakesSums && k != kWPost ? 1 : 0][c][e][kTakesSums ? threadIdx.x : 0];
+            } else {
+                float w[8], b[8];
+                eight_weights(k == kGate ? a.w.w_post : a.w.gate ? a.w.gate + (long)group * D : nullptr, l.n[c], l.count[c], 1.f, w);
+                eight_weights(a.w.b_post, l.n[c], l.count[c], 0.f, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = a.scale * (k == kGate ? w[e] * sum_ax[c][e] + b[e] * sum_a[c][e] : w[e] * (k == kWPost ? sum_ax[c][e] : sum_a[c][e]));
             }
-            __syncthreads();
-            if (slot == 0)
-                for (int i = 0; i < kSlots - 1; ++i)
+            if (kSlots > 1) { // (CH is 1 where there are slots)
+                Eight<float> y;
+                y.set(v);
+                y.write(joined + l.slot * L::kColumns + l.n[0] % L::kColumns);
+                __syncthreads();
+                if (l.slot == 0)
+                    for (int i = 1; i < kSlots; ++i) {
+                        float u[8];
+                        y.read(joined + i * L::kColumns + l.n[0] % L::kColumns);
+                        y.get(u);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) total[k][0][e] += joined[i * kColumns + at + e];
-            __syncthreads();
+                        for (int e = 0; e < 8; ++e) v[e] += u[e];
+                    }
+                __syncthreads();
+            }
+            if (l.slot == 0 && l.count[c]) write_eight(to, l.n[c], D, v);
         }
-        if (slot > 0) continue;
-        float *to = k == kGate ? (a.p.per_group == 1 ? out[k] + first_group * D : nullptr) : a.p.blocks == 1 ? out[k] : nullptr;
-        if (!to) to = a.part + (k * a.p.blocks + blockIdx.x) * D;
-#pragma unroll
-        for (int c = 0; c < CH; ++c) write_eight(to, n[c], D, D % 4 == 0 && n[c] + 8 <= D, total[k][c]);
     }
 }
 
@@ -399,12 +570,12 @@ template <typename T, int WPR, int CH> __global__ void __launch_bounds__(64 * kB
 __global__ void __launch_bounds__(1024) norm_join_kernel(const NormArgs a)
 {
     __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.g.D, col = blockIdx.x * 64 + lane;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D, col = blockIdx.x * 64 + lane;
     const int k = blockIdx.y < 4 ? kWPost + blockIdx.y : kGate;
-    const long group = blockIdx.y < 4 ? 0 : blockIdx.y - 4, rows = k == kGate ? a.p.per_group : a.p.blocks;
+    const long group = blockIdx.y < 4 ? 0 : blockIdx.y - 4, rows = k == kGate ? a.per_group : a.blocks;
     float *to = k == kGate ? a.o.gate : k == kWPost ? a.o.w_post : k == kBPost ? a.o.b_post : k == kWPre ? a.o.w_pre : a.o.b_pre;
     if (!to) return;
-    const float *p = a.part + (k * a.p.blocks + group * rows) * D + col;
+    const float *p = a.part + ((long)k * a.blocks + group * rows) * D + col;
     float s = 0.f;
     if (col < D) {
         long r = wave;
@@ -424,73 +595,121 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const NormArgs a)
 // ---- host
 static long cdiv(long a, long b) { return (a + b - 1) / b; }
 
+// Which rows a workgroup of the backward pass has, of `slots` at once and `most` workgroups.
+static NormSplit split_rows(const NormGeom &g, long groups, int slots, long most)
+{
+    NormSplit s;
+    const long G = g.gate_rows ? g.gate_rows : g.T;
+    s.own_groups = groups > 1 && (groups * 2 >= most * slots || G <= 4);
+    s.per_group = 1;
+    s.rows_per_block = 0;
+    if (s.own_groups) {
+        s.blocks = cdiv(groups, slots);
+        if (s.blocks > most) s.blocks = most;
+        return s;
+    }
+    const long per = most / groups > 0 ? most / groups : 1;
+    s.rows_per_block = cdiv(G, per);
+    if (s.rows_per_block < slots) s.rows_per_block = slots;
+    s.per_group = cdiv(G, s.rows_per_block);
+    s.blocks = groups * s.per_group;
+    return s;
+}
+
 void plan_norm(const NormGeom &g, bool backward, NormPlan *p)
 {
-    p->chunks = g.D > 8192 ? 2 : 1;
+    *p = NormPlan{};
+    p->lanes = g.D <= 128 ? 16 : g.D <= 256 ? 32 : 64;
+    p->chunks = g.D > (backward ? 4096 : 8192) ? 2 : 1;
     p->waves = 1;
     while (p->waves * 512 * p->chunks < g.D) p->waves *= 2;
     const int least = backward ? 8 : 4, waves = p->waves > least ? p->waves : least;
-    p->slots = waves / p->waves;
-    p->own_groups = false;
+    p->slots = waves * 64 / p->lanes / p->waves;
     p->groups = g.gate_rows ? cdiv(g.T, g.gate_rows) : 1;
-    p->per_group = 1;
     if (!backward) {
-        p->blocks = cdiv(g.T, p->slots);
-        const long most = 256 * 16 / waves;
-        if (p->blocks > most) p->blocks = most;
-        p->rows_per_block = cdiv(g.T, p->blocks);
-        p->blocks = cdiv(g.T, p->rows_per_block);
-        p->bytes = 0;
+        const long most = 256 * 16 / waves; // (all at once)
+        p->split.blocks = cdiv(g.T, p->slots);
+        if (p->split.blocks > most) p->split.blocks = most;
+        p->split.rows_per_block = cdiv(g.T, p->split.blocks);
+        p->split.blocks = cdiv(g.T, p->split.rows_per_block);
         return;
     }
-    const long most = 256 * 16 / waves, G = g.gate_rows ? g.gate_rows : g.T;
-    if (p->groups > 1 && (p->groups * 2 >= most * p->slots || G <= 4)) {
-        p->own_groups = true;
-        p->blocks = cdiv(p->groups, p->slots);
-        if (p->blocks > most) p->blocks = most;
-        p->rows_per_block = 0;
-    } else {
-        const long per = most / p->groups > 0 ? most / p->groups : 1;
-        p->rows_per_block = cdiv(G, per);
-        if (p->rows_per_block < p->slots) p->rows_per_block = p->slots;
-        p->per_group = cdiv(G, p->rows_per_block);
-        p->blocks = p->groups * p->per_group;
-    }
-    p->bytes = p->blocks > 1 ? (size_t)kSums * p->blocks * g.D * sizeof(float) : 0;
+    p->split = split_rows(g, p->groups, p->slots, 256);
+    p->two = g.D > 8192;
+    p->sums = p->two ? split_rows(g, p->groups, 8, cdiv(1024, cdiv(g.D, 512))) : p->split;
+    p->bytes = p->sums.blocks > 1 ? (size_t)kSums * p->sums.blocks * g.D * sizeof(float) : 0;
+    p->bytes = (p->bytes + 255) / 256 * 256;
+    p->o_known = p->bytes;
+    if (p->two) p->bytes += (size_t)g.T * 8 * sizeof(float);
+}
+
+static void use(NormArgs &a, const NormSplit &s)
+{
+    a.rows_per_block = (int)s.rows_per_block;
+    a.blocks = (int)s.blocks;
+    a.per_group = (int)s.per_group;
+    a.own = s.own_groups;
 }
 
 static NormArgs arguments(const NormGeom &g, const NormPlan &p, const Drop &d, const NormParams &w)
 {
     NormArgs a = {};
-    a.g = g;
-    a.p = p;
-    a.d = d;
-    a.w = w;
+    a.T = (int)g.T;
+    a.D = (int)g.D;
+    a.across = (int)cdiv(g.D, 8);
+    a.post = g.post;
+    a.pre = g.pre;
+    a.gate_rows = (int)g.gate_rows;
+    a.groups = (int)p.groups;
+    use(a, p.split);
+    a.ld_f = g.ld_f;
+    a.ld_r = g.ld_r;
+    a.eps_post = g.eps_post;
+    a.eps_pre = g.eps_pre;
     a.scale = g.alpha * d.scale;
     a.inv_d = 1.f / (float)g.D;
-    const long whole = g.dtype == CAC_F32 ? 4 : 8;
-    a.wide = g.D % 8 == 0;
-    a.wide_f = a.wide && g.ld_f % whole == 0;
-    a.wide_r = a.wide && g.ld_r % whole == 0;
+    a.d = d;
+    a.w = w;
     return a;
 }
 
-template <typename T, int WPR, int CH> static hipError_t launch_of(const NormArgs &a, bool backward, hipStream_t st)
+template <typename T, class L> static hipError_t launch_fwd(const NormArgs &a, hipStream_t st)
 {
-    if (backward) hipLaunchKernelGGL((norm_bwd_kernel<T, WPR, CH>), dim3((unsigned)a.p.blocks), dim3(64 * kBwdWaves<WPR>), 0, st, a);
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, WPR, CH>), dim3((unsigned)a.p.blocks), dim3(64 * kFwdWaves<WPR>), 0, st, a);
+    hipLaunchKernelGGL((norm_fwd_kernel<T, L>), dim3((unsigned)a.blocks), dim3(64 * kFwdWaves<L::WPR>), 0, st, a);
     return hipGetLastError();
 }
-template <typename T> static hipError_t launch_rows(const NormArgs &a, bool backward, hipStream_t st)
+template <typename T, class L, Part PART = kBoth> static hipError_t launch_bwd(const NormArgs &a, hipStream_t st)
 {
-    if (a.p.chunks == 2) return launch_of<T, 16, 2>(a, backward, st);
-    switch (a.p.waves) {
-    case 1: return launch_of<T, 1, 1>(a, backward, st);
-    case 2: return launch_of<T, 2, 1>(a, backward, st);
-    case 4: return launch_of<T, 4, 1>(a, backward, st);
-    case 8: return launch_of<T, 8, 1>(a, backward, st);
-    default: return launch_of<T, 16, 1>(a, backward, st);
+    const unsigned across = PART == kSumPart ? (unsigned)cdiv(a.D, L::kColumns) : 1;
+    hipLaunchKernelGGL((norm_bwd_kernel<T, L, PART>), dim3((unsigned)a.blocks, across), dim3(64 * kBwdWaves<L::WPR>), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, bool WHOLE> static hipError_t launch_rows(NormArgs a, const NormPlan &p, bool backward, hipStream_t st)
+{
+#define CAC_ROWS(LANES, WPR) \
+    return backward ? launch_bwd<T, Rows<LANES, WPR, 1, WHOLE>>(a, st) : launch_fwd<T, Rows<LANES, WPR, 1, WHOLE>>(a, st)
+    if (p.two) {
+        hipError_t e = launch_bwd<T, Rows<64, 16, 2, WHOLE>, kRowPart>(a, st);
+        if (e != hipSuccess || !(a.o.gate || a.o.w_post || a.o.b_post || a.o.w_pre || a.o.b_pre)) return e;
+        use(a, p.sums);
+        return launch_bwd<T, Rows<64, 1, 1, WHOLE>, kSumPart>(a, st);
     }
+    if (p.chunks == 2) return backward ? launch_bwd<T, Rows<64, 8, 2, WHOLE>>(a, st) : launch_fwd<T, Rows<64, 16, 2, WHOLE>>(a, st);
+    if (p.lanes == 16) CAC_ROWS(16, 1);
+    if (p.lanes == 32) CAC_ROWS(32, 1);
+    switch (p.waves) {
+    case 1: CAC_ROWS(64, 1);
+    case 2: CAC_ROWS(64, 2);
+    case 4: CAC_ROWS(64, 4);
+    case 8: CAC_ROWS(64, 8);
+    default: return launch_fwd<T, Rows<64, 16, 1, WHOLE>>(a, st);
+    }
+#undef CAC_ROWS
+}
+static hipError_t launch_norm(const NormArgs &a, const NormPlan &p, int dtype, bool backward, hipStream_t st)
+{
+    if (dtype == CAC_F32) return a.D % 8 ? launch_rows<float, false>(a, p, backward, st) : launch_rows<float, true>(a, p, backward, st);
+    return a.D % 8 ? launch_rows<bf16_t, false>(a, p, backward, st) : launch_rows<bf16_t, true>(a, p, backward, st);
 }
 
 hipError_t launch_norm_fwd(const NormGeom &g, const NormPlan &p, const Drop &d, const void *F, const void *R, const NormParams &w, void *S, void *H,
@@ -501,7 +720,7 @@ hipError_t launch_norm_fwd(const NormGeom &g, const NormPlan &p, const Drop &d, 
     a.R = R;
     a.S = S;
     a.H = H;
-    return g.dtype == CAC_F32 ? launch_rows<float>(a, false, st) : launch_rows<bf16_t>(a, false, st);
+    return launch_norm(a, p, g.dtype, false, st);
 }
 
 hipError_t launch_norm_bwd(const NormGeom &g, const NormPlan &p, const Drop &d, const void *F, const void *S, const NormParams &w, const void *dH,
@@ -516,10 +735,12 @@ hipError_t launch_norm_bwd(const NormGeom &g, const NormPlan &p, const Drop &d, 
     a.dF = dF;
     a.o = o;
     a.part = (float *)ws;
-    hipError_t e = g.dtype == CAC_F32 ? launch_rows<float>(a, true, st) : launch_rows<bf16_t>(a, true, st);
-    if (e != hipSuccess || p.blocks == 1) return e;
-    const bool gates = o.gate && !p.own_groups && p.per_group > 1;
+    a.known = (float *)((char *)ws + p.o_known);
+    hipError_t e = launch_norm(a, p, g.dtype, true, st);
+    if (e != hipSuccess || p.sums.blocks == 1) return e;
+    const bool gates = o.gate && !p.sums.own_groups && p.sums.per_group > 1;
     if (!gates && !o.w_post && !o.b_post && !o.w_pre && !o.b_pre) return hipSuccess;
+    use(a, p.sums);
     hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)cdiv(g.D, 64), (unsigned)(4 + (gates ? p.groups : 0))), dim3(1024), 0, st, a);
     return hipGetLastError();
 }

@@ -6,7 +6,7 @@
 // them, 16 bits each: the counter is (group low, group high | site << 8, step low, step high), the group row * ceil(columns / 8) + column / 8.
 // An element whose 16 bits are below limit = round(65536 p) is dropped and the others are multiplied by 65536 / (65536 - limit), the inverse
 // of the probability that 16 bits really give, so that the mean is kept exactly.
-// Twenty products at a quarter of the full rate and 40 exclusive ors make 0.3 us of a compute unit's time for 4096 elements: about 3.5e12 elements a
+// Twenty products at a quarter of the full rate and 20 exclusive ors of three words make 0.3 us of a compute unit's time for 4096 elements: about 3.5e12 elements a
 // second on the whole card, above what it can read and write in 16 bits (5e12 bytes a second).  Sixteen bits an element and not 32 halve
 // that; the probability is a multiple of 2^-16 then.
 #pragma once
@@ -41,7 +41,7 @@ __device__ __forceinline__ Bits128 drop_bits(const DropKey &key, uint32_t site, 
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-        const uint32_t n0 = (uint32_t)(b >> 32) ^ c1 ^ k0, n2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        const uint32_t n0 = __builtin_amdgcn_bitop3_b32((uint32_t)(b >> 32), c1, k0, 0x96), n2 = __builtin_amdgcn_bitop3_b32((uint32_t)(a >> 32), c3, k1, 0x96); // a ^ b ^ c
         c1 = (uint32_t)b;
         c3 = (uint32_t)a;
         c0 = n0;
@@ -52,74 +52,111 @@ __device__ __forceinline__ Bits128 drop_bits(const DropKey &key, uint32_t site, 
     return Bits128{{c0, c1, c2, c3}};
 }
 
-// element e of a word's two, e = 0 or 1
-__device__ __forceinline__ bool drop_keeps(uint32_t word, int e, uint32_t limit) { return (e ? word >> 16 : word & 0xffffu) >= limit; }
+// element e of a word's two, e = 0 or 1: its 16 bits, on top of a word, against limit 2^16 - 1 (limit is at least 1)
+__device__ __forceinline__ bool drop_keeps(uint32_t word, int e, uint32_t limit) { return (e ? word | 0xffffu : word << 16 | 0xffffu) > (limit << 16) - 1; }
 
-// eight neighbours of one group: what is kept times `scale`, zeros for the others (whatever stands there)
-__device__ __forceinline__ void drop_eight(const DropKey &key, const Drop &d, uint64_t group, float scale, float (&v)[8])
+// eight neighbours of one group: zeros for what is dropped (whatever stands there)
+__device__ __forceinline__ void drop_eight(const DropKey &key, const Drop &d, uint64_t group, float (&v)[8])
 {
-    if (!d.limit) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= scale;
-        return;
-    }
+    if (!d.limit) return;
     const Bits128 b = drop_bits(key, d.site, group);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = drop_keeps(b.w[e >> 1], e & 1, d.limit) ? v[e] * scale : 0.f;
+    for (int e = 0; e < 8; ++e) v[e] = drop_keeps(b.w[e >> 1], e & 1, d.limit) ? v[e] : 0.f;
 }
 
-// ---- eight neighbours of a row as floats
+// ---- eight neighbours of a row as floats.  Rows may start anywhere: loads and stores of 16 bytes take any address of an element.
+typedef uint32_t whole16 __attribute__((ext_vector_type(4)));
+typedef whole16 any16 __attribute__((aligned(2)));
+
 template <typename T> struct Eight;
 template <> struct Eight<float> {
-    float4 a, b;
-    __device__ __forceinline__ void read(const float *p) { a = ((const float4 *)p)[0], b = ((const float4 *)p)[1]; }
-    __device__ __forceinline__ void write(float *p) const { ((float4 *)p)[0] = a, ((float4 *)p)[1] = b; }
-    __device__ __forceinline__ void get(float (&v)[8]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w; }
-    __device__ __forceinline__ void set(const float (&v)[8]) { a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]); }
-};
-template <> struct Eight<bf16_t> {
-    uint4 a;
-    __device__ __forceinline__ void read(const bf16_t *p) { a = *(const uint4 *)p; }
-    __device__ __forceinline__ void write(bf16_t *p) const { *(uint4 *)p = a; }
+    whole16 a, b;
+    __device__ __forceinline__ void read(const float *p) { a = ((const any16 *)p)[0], b = ((const any16 *)p)[1]; }
+    __device__ __forceinline__ void write(float *p) const { ((any16 *)p)[0] = a, ((any16 *)p)[1] = b; }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
-        const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(a[e]), v[4 + e] = __uint_as_float(b[e]);
+    }
+    __device__ __forceinline__ void set(const float (&v)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = __float_as_uint(v[e]), b[e] = __float_as_uint(v[4 + e]);
+    }
+    __device__ __forceinline__ void clear() { a = b = whole16{0, 0, 0, 0}; }
+    // s elements towards the first, zeros after them
+    __device__ __forceinline__ void shift(int s)
+    {
+        if (s & 4) a = b, b = whole16{0, 0, 0, 0};
+        if (s & 2) a = whole16{a[2], a[3], b[0], b[1]}, b = whole16{b[2], b[3], 0, 0};
+        if (s & 1) a = whole16{a[1], a[2], a[3], b[0]}, b = whole16{b[1], b[2], b[3], 0};
+    }
+};
+template <> struct Eight<bf16_t> {
+    whole16 a;
+    __device__ __forceinline__ void read(const bf16_t *p) { a = *(const any16 *)p; }
+    __device__ __forceinline__ void write(bf16_t *p) const { *(any16 *)p = a; }
+    __device__ __forceinline__ void get(float (&v)[8]) const
+    {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            v[2 * k] = __uint_as_float(u[k] << 16);
-            v[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+            v[2 * k] = __uint_as_float(a[k] << 16);
+            v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u);
         }
     }
     __device__ __forceinline__ void set(const float (&v)[8])
     {
-        a = make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7]));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = f32x2_to_bf16x2(v[2 * k], v[2 * k + 1]);
+    }
+    __device__ __forceinline__ void clear() { a = whole16{0, 0, 0, 0}; }
+    __device__ __forceinline__ void shift(int s)
+    {
+        if (s & 4) a = whole16{a[2], a[3], 0, 0};
+        if (s & 2) a = whole16{a[1], a[2], a[3], 0};
+        if (s & 1) a = whole16{a[0] >> 16 | a[1] << 16, a[1] >> 16 | a[2] << 16, a[2] >> 16 | a[3] << 16, a[3] >> 16};
     }
 };
-// of a row of `columns` from column n on; `wide`: every group is whole and starts on 16 bytes
-template <typename T> __device__ __forceinline__ Eight<T> read_eight(const T *row, int n, int columns, bool wide)
+// of a row of `columns` from column n on, n below columns; zeros past its end.  WHOLE: rows are whole eights.
+template <bool WHOLE = false, typename T> __device__ __forceinline__ Eight<T> read_eight(const T *row, int n, int columns)
 {
     Eight<T> r;
-    if (wide) {
+    if (WHOLE || n + 8 <= columns) {
         r.read(row + n);
-        return r;
-    }
-    float v[8];
+    } else if (columns >= 8) { // the row's last eight, those before n taken out
+        r.read(row + columns - 8);
+        r.shift(n + 8 - columns);
+    } else {
+        float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = n + e < columns ? Elem<T>::load(row + n + e) : 0.f;
-    r.set(v);
+        for (int e = 0; e < 8; ++e) v[e] = n + e < columns ? Elem<T>::load(row + n + e) : 0.f;
+        r.set(v);
+    }
     return r;
 }
-template <typename T> __device__ __forceinline__ void write_eight(T *row, int n, int columns, bool wide, const float (&v)[8])
+template <bool WHOLE = false, typename T> __device__ __forceinline__ void write_eight(T *row, int n, int columns, const float (&v)[8])
 {
-    if (wide) {
-        Eight<T> r;
-        r.set(v);
+    Eight<T> r;
+    r.set(v);
+    if (WHOLE || n + 8 <= columns) {
         r.write(row + n);
         return;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (n + e < columns) Elem<T>::store(row + n + e, v[e]);
+    struct alignas(sizeof(T)) Four { T x[4]; };
+    struct alignas(sizeof(T)) Two { T x[2]; };
+    const int count = columns - n;
+    T *p = row + n;
+    if (count & 4) {
+        *(Four *)p = *(const Four *)&r;
+        p += 4;
+        r.shift(4);
+    }
+    if (count & 2) {
+        *(Two *)p = *(const Two *)&r;
+        p += 2;
+        r.shift(2);
+    }
+    if (count & 1) *p = *(const T *)&r;
 }
 
 } // namespace cac

@@ -13,12 +13,11 @@ struct DropArgs {
     int step_cols;
     int cols;
     long ld_x, ld_r;
-    bool vector;
     float scale;
     Drop d;
 };
 
-template <typename T, bool RES> __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a, const T *X, const T *R, T *Y)
+template <typename T, bool RES, bool WHOLE> __global__ void __launch_bounds__(kThreads) dropout_kernel(const DropArgs a, const T *X, const T *R, T *Y)
 {
     const DropKey key = drop_key(a.d);
     const long stride = (long)gridDim.x * kThreads;
@@ -27,18 +26,20 @@ template <typename T, bool RES> __global__ void __launch_bounds__(kThreads) drop
     int col = (int)(g - row * a.wide);
     for (; g < a.groups; g += stride) {
         const int n = col * 8;
-        Eight<T> x = read_eight(X + row * a.ld_x, n, a.cols, a.vector), r;
-        if (RES) r = read_eight(R + row * a.ld_r, n, a.cols, a.vector);
+        Eight<T> x = read_eight<WHOLE>(X + row * a.ld_x, n, a.cols), r;
+        if (RES) r = read_eight<WHOLE>(R + row * a.ld_r, n, a.cols);
         float v[8];
         x.get(v);
-        drop_eight(key, a.d, (uint64_t)g, a.scale, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+        drop_eight(key, a.d, (uint64_t)g, v);
         if (RES) {
             float w[8];
             r.get(w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += w[e];
         }
-        write_eight(Y + row * a.cols, n, a.cols, a.vector, v);
+        write_eight<WHOLE>(Y + row * a.cols, n, a.cols, v);
         row += a.step_rows;
         col += a.step_cols;
         if (col >= a.wide) {
@@ -50,21 +51,20 @@ template <typename T, bool RES> __global__ void __launch_bounds__(kThreads) drop
 
 template <typename T> static hipError_t launch(const DropGeom &g, const Drop &d, const void *X, const void *R, void *Y, hipStream_t st)
 {
-    constexpr long kWhole = 16 / sizeof(T); // elements that start on 16 bytes
     DropArgs a;
     a.wide = (int)((g.cols + 7) / 8);
     a.groups = g.rows * a.wide;
     a.cols = (int)g.cols;
     a.ld_x = g.ld_x;
     a.ld_r = g.ld_r;
-    a.vector = g.cols % 8 == 0 && g.ld_x % kWhole == 0 && (!R || g.ld_r % kWhole == 0);
     a.scale = g.alpha * d.scale;
     a.d = d;
     const long blocks = (a.groups + kThreads - 1) / kThreads, grid = blocks < 4096 ? blocks : 4096;
     a.step_rows = grid * kThreads / a.wide;
     a.step_cols = (int)(grid * kThreads % a.wide);
-    if (R) hipLaunchKernelGGL((dropout_kernel<T, true>), dim3((unsigned)grid), dim3(kThreads), 0, st, a, (const T *)X, (const T *)R, (T *)Y);
-    else hipLaunchKernelGGL((dropout_kernel<T, false>), dim3((unsigned)grid), dim3(kThreads), 0, st, a, (const T *)X, (const T *)nullptr, (T *)Y);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a, (const T *)X, (const T *)R, (T *)Y); };
+    if (g.cols % 8) go(R ? dropout_kernel<T, true, false> : dropout_kernel<T, false, false>);
+    else go(R ? dropout_kernel<T, true, true> : dropout_kernel<T, false, true>);
     return hipGetLastError();
 }
 

@@ -306,8 +306,8 @@ template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const P
         const int n = (int)(at - row * across) * 8;
         const T *x = (const T *)(second ? p.from[1] : p.from[0]) + row * (second ? p.ld[1] : p.ld[0]);
         float v[8];
-        read_eight(x, n, p.columns, false).get(v);
-        write_eight((T *)(second ? p.to[1] : p.to[0]) + at * 8, 0, 8, true, v);
+        read_eight(x, n, p.columns).get(v);
+        write_eight((T *)(second ? p.to[1] : p.to[0]) + at * 8, 0, 8, v);
     }
 }
 
