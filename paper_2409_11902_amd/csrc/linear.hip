@@ -34,27 +34,46 @@ __device__ __forceinline__ float normal_cdf(float u, float *bell)
     const float below = p * t * *bell;
     return u < 0.f ? below : 1.f - below;
 }
-__device__ __forceinline__ float activation(int act, float u)
+template <int ACT> __device__ __forceinline__ float activation(float u)
 {
     float bell;
-    if (act == CAC_ACT_RELU) return u <= 0.f ? 0.f : u; // (NaN stays NaN)
-    if (act == CAC_ACT_GELU) return u * normal_cdf(u, &bell);
-    if (act == CAC_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
+    if (ACT == CAC_ACT_RELU) return u <= 0.f ? 0.f : u; // (NaN stays NaN)
+    if (ACT == CAC_ACT_GELU) return u * normal_cdf(u, &bell);
+    if (ACT == CAC_ACT_SILU) return u * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
     return u;
 }
-__device__ __forceinline__ float slope(int act, float u)
+template <int ACT> __device__ __forceinline__ float slope(float u)
 {
-    if (act == CAC_ACT_RELU) return u > 0.f ? 1.f : 0.f;
-    if (act == CAC_ACT_GELU) {
+    if (ACT == CAC_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+    if (ACT == CAC_ACT_GELU) {
         float bell;
         const float cdf = normal_cdf(u, &bell);
         return fmaf(u * bell, 0.3989422804014327f, cdf); // 1 / sqrt(2 pi)
     }
-    if (act == CAC_ACT_SILU) {
+    if (ACT == CAC_ACT_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
         return s * fmaf(u, 1.f - s, 1.f);
     }
     return 1.f;
+}
+
+// 256 x 256 with the loads between the products: a pass of 64 terms takes 1.56 us then (1.37 PFLOP/s; 1.62 with the loads together), and what comes before
+// and after a tile's passes 14 us, of which 7 are 33 MB on their way to memory from all tiles at once.  Four waves of 128 x 128 (half the LDS
+// reads) take 1.64 us a pass and twice as long at a tile's end; passes of 32 terms four or five deep, 256 x 128 and 128 x 128 two to a compute unit are slower too
+// (8192 x 2048 x 8192: 257 us; 396, 276, 311 and 324).
+typedef Shape<2, 4, 4, 2, 128, 2, 1, true> Large;
+
+template <class P, Lay LA, Lay LB, class Epi>
+hipError_t launch_tiles(const Params &p, const typename Epi::Params &e, TileChoice c, hipStream_t st)
+{
+    if constexpr (P::kRaw) {
+        if constexpr (LA == Lay::kAlong)
+            if (c.shape == kLow) return launch_shape<P, LA, LB, Low, Epi>(p, e, c.slices, st);
+    } else {
+        if (c.shape == kBig) return launch_shape<P, LA, LB, Large, Epi>(p, e, c.slices, st);
+        if (c.shape == kMiddle) return launch_shape<P, LA, LB, Middle, Epi>(p, e, c.slices, st);
+    }
+    return launch_shape<P, LA, LB, Small, Epi>(p, e, c.slices, st);
 }
 
 // What becomes of a product's sums, or of the sums of its slices.
@@ -62,6 +81,7 @@ enum Kind {
     kForward, // R + scale drop(act(sum + b))
     kSlope,   // drop(dY) act'(sum + b), and its sums over rows
     kScaled,  // scale * sum
+    kSums,    // a slice's sums as they are
 };
 struct Tail {
     Kind kind;
@@ -73,32 +93,70 @@ struct Tail {
     long ld_out;
     int cols_out;       // N, or up to where a row is padded with zeros
     float *columns;     // kSlope: [parts][N], or null
-    bool wide_other;    // fours of a row start on 4 elements
-    bool wide_out;
     float scale;
     Drop d;
     int across;         // groups of eight of a row of the mask
 };
 
-template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
-template <typename T> __device__ __forceinline__ void load_four(const T *p, int n, int N, bool wide, float (&v)[4])
-{
-    if (wide) {
-        const Four<T> f = *(const Four<T> *)p;
+// ---- four neighbours of a row, which may start anywhere
+template <typename T> struct Quad;
+template <> struct Quad<float> {
+    typedef uint32_t V __attribute__((ext_vector_type(4)));
+    typedef V Any __attribute__((aligned(4)));
+    V a;
+    __device__ __forceinline__ void read(const float *p) { a = *(const Any *)p; }
+    __device__ __forceinline__ void write(float *p) const { *(Any *)p = a; }
+    __device__ __forceinline__ void get(float (&v)[4]) const
+    {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = Elem<T>::load(&f.v[k]);
-        return;
+        for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(a[k]);
     }
+    __device__ __forceinline__ void set(const float (&v)[4])
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = __float_as_uint(v[k]);
+    }
+};
+template <> struct Quad<bf16_t> {
+    typedef uint32_t V __attribute__((ext_vector_type(2)));
+    typedef V Any __attribute__((aligned(2)));
+    V a;
+    __device__ __forceinline__ void read(const bf16_t *p) { a = *(const Any *)p; }
+    __device__ __forceinline__ void write(bf16_t *p) const { *(Any *)p = a; }
+    __device__ __forceinline__ void get(float (&v)[4]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            v[2 * k] = __uint_as_float(a[k] << 16);
+            v[2 * k + 1] = __uint_as_float(a[k] & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[4])
+    {
+        a[0] = f32x2_to_bf16x2(v[0], v[1]);
+        a[1] = f32x2_to_bf16x2(v[2], v[3]);
+    }
+};
+// from column n on; zeros past N
+template <typename T> __device__ __forceinline__ Quad<T> read_quad(const T *p, int n, int N)
+{
+    Quad<T> q;
+    if (n + 4 <= N) {
+        q.read(p);
+        return q;
+    }
+    float v[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = n + k < N ? Elem<T>::load(p + k) : 0.f;
+    q.set(v);
+    return q;
 }
-template <typename T> __device__ __forceinline__ void store_four(T *p, int n, int N, bool wide, const float (&v)[4])
+template <typename T> __device__ __forceinline__ void write_quad(T *p, int n, int N, const float (&v)[4])
 {
-    if (wide) {
-        Four<T> f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) Elem<T>::store(&f.v[k], v[k]);
-        *(Four<T> *)p = f;
+    if (n + 4 <= N) {
+        Quad<T> q;
+        q.set(v);
+        q.write(p);
         return;
     }
 #pragma unroll
@@ -106,32 +164,46 @@ template <typename T> __device__ __forceinline__ void store_four(T *p, int n, in
         if (n + k < N) Elem<T>::store(p + k, v[k]);
 }
 
-// Four neighbours of row m from column n on; `words` are their 64 random bits, `v` comes as sums and goes as what was written.
-template <typename T> __device__ __forceinline__ void finish_four(const Tail &t, long m, int n, const float (&b)[4], const uint32_t (&words)[2], float (&v)[4])
+// Four neighbours from column n on; `words` are their 64 random bits, `o` R's or dY's; `v` comes as sums and goes as what is written.
+template <Kind KIND, int ACT> __device__ __forceinline__ void finish_four(const Tail &t, int n, const float (&b)[4], const float (&o)[4], const uint32_t (&words)[2], float (&v)[4])
 {
-    if (t.kind == kScaled) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] *= t.scale;
-    } else {
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
-        if (t.other && n < t.N) load_four((const T *)t.other + m * t.ld_other + n, n, t.N, t.wide_other, o);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const bool kept = !t.d.limit || drop_keeps(words[k >> 1], k & 1, t.d.limit);
-            const float u = v[k] + b[k];
-            if (t.kind == kForward) v[k] = o[k] + (kept ? t.scale * activation(t.act, u) : 0.f);
-            else v[k] = kept && n + k < t.N ? (t.act == CAC_ACT_NONE ? o[k] : o[k] * slope(t.act, u)) : 0.f;
+    for (int k = 0; k < 4; ++k) {
+        if (KIND == kScaled) {
+            v[k] *= t.scale;
+        } else if (KIND == kForward) {
+            const float y = t.scale * activation<ACT>(v[k] + b[k]);
+            v[k] = o[k] + (!t.d.limit || drop_keeps(words[k >> 1], k & 1, t.d.limit) ? y : 0.f);
+        } else if (KIND == kSlope) {
+            const float g = ACT == CAC_ACT_NONE ? o[k] : o[k] * slope<ACT>(v[k] + b[k]);
+            v[k] = (!t.d.limit || drop_keeps(words[k >> 1], k & 1, t.d.limit)) && n + k < t.N ? g : 0.f;
         }
     }
-    if (t.out) store_four((T *)t.out + m * t.ld_out + n, n, t.cols_out, t.wide_out, v);
+}
+
+// fn(kind, act) of a tail's, as constants: asked for at every four they were branches that took 25 us of a tile
+template <bool PLAIN, class Fn> __device__ __forceinline__ void with_kind(const Tail &t, Fn fn)
+{
+    auto acts = [&](auto kind) {
+        if (t.act == CAC_ACT_GELU) fn(kind, std::integral_constant<int, CAC_ACT_GELU>());
+        else if (t.act == CAC_ACT_SILU) fn(kind, std::integral_constant<int, CAC_ACT_SILU>());
+        else if (t.act == CAC_ACT_RELU) fn(kind, std::integral_constant<int, CAC_ACT_RELU>());
+        else fn(kind, std::integral_constant<int, CAC_ACT_NONE>());
+    };
+    typedef std::integral_constant<int, CAC_ACT_NONE> None;
+    if (t.kind == kSums) fn(std::integral_constant<Kind, kSums>(), None());
+    else if constexpr (PLAIN) fn(std::integral_constant<Kind, kScaled>(), None());
+    else if (t.kind == kForward) acts(std::integral_constant<Kind, kForward>());
+    else acts(std::integral_constant<Kind, kSlope>());
 }
 
 // The other lane of a pair's.
 __device__ __forceinline__ uint32_t from_neighbour(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true); }
 
 // A product with its tail, or its slices' sums.  They go through a wave's LDS, 32 rows at a time: a lane then has four neighbours in the same
-// columns of every row that it comes to, and two lanes a group of the mask, of which each forms one in two.
-template <class T> struct Ended : Ending {
+// columns of every row that it comes to, and two lanes a group of the mask, of which each forms one in two.  R (dY) of 32 rows is on its way while the
+// 32 before are dealt with.  PLAIN: no more than a factor.
+template <class T, bool PLAIN> struct Ended : Ending {
     struct Params {
         Tail t;
         float *sums; // [slice][M][N]: no tail yet
@@ -139,15 +211,31 @@ template <class T> struct Ended : Ending {
     };
     template <int MI, int NI> static __device__ __forceinline__ void run(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
     {
+        with_kind<PLAIN>(e.t, [&](auto kind, auto act) { rows<decltype(kind)::value, decltype(act)::value, MI, NI>(e, acc, p); });
+    }
+    template <Kind KIND, int ACT, int MI, int NI> static __device__ __forceinline__ void rows(const Params &e, const f32x16 (&acc)[MI][NI], const Place &p)
+    {
         typedef RowBlock<Fmt::kF32, NI> Block;
-        constexpr int kLanes = 8 * NI, kRows = 64 / kLanes; // lanes to a row, rows at once
+        constexpr int kLanes = 8 * NI, kRows = 64 / kLanes, kTurns = 32 / kRows; // lanes to a row, rows at once, turns to 32
+        constexpr bool kOther = KIND == kForward || KIND == kSlope;
         const Tail &t = e.t;
         const int n = p.n0 + p.lane % kLanes * 4, row0 = p.lane / kLanes;
-        const bool sums = e.sums != nullptr;
         float b[4] = {0.f, 0.f, 0.f, 0.f}, columns[4] = {0.f, 0.f, 0.f, 0.f};
-        if (t.b && !sums) load_four((const T *)t.b + n, n, t.N, false, b);
+        const bool other = kOther && t.other && n < t.N;
+        if (kOther && t.b && n < t.N) read_quad((const T *)t.b + n, n, t.N).get(b);
         const DropKey key = drop_key(t.d);
-        const bool drops = t.d.limit && !sums;
+        Quad<T> o[kTurns];
+        auto ask = [&](int m0) {
+#pragma unroll
+            for (int c = 0; c < kTurns; ++c) {
+                const int m = m0 + c * kRows + row0;
+                if (other && m < p.M) o[c] = read_quad((const T *)t.other + (long)m * t.ld_other + n, n, t.N);
+            }
+        };
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kTurns; ++c) o[c].set(zero);
+        if (kOther) ask(p.m0);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int m0 = p.m0 + i * 32;
@@ -162,10 +250,20 @@ template <class T> struct Ended : Ending {
                 }
             asm volatile("" ::: "memory"); // (a wave's LDS accesses are in order; other lanes' stores are read here)
             __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-            for (int c = 0; c < 32 / kRows; c += 2) {
+            f32x4 x[kTurns];
+            Quad<T> was[kTurns];
+#pragma unroll
+            for (int c = 0; c < kTurns; ++c) {
+                x[c] = *(const f32x4 *)(p.lds + (c * kRows + row0) * Block::kPitch + p.lane % kLanes * 16);
+                was[c] = o[c];
+            }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
+            if (kOther && i + 1 < MI) ask(m0 + 32);
+#pragma unroll
+            for (int c = 0; c < kTurns; c += 2) {
                 uint32_t words[2][2] = {{0, 0}, {0, 0}};
-                if (drops) {
+                if (kOther && t.d.limit) {
                     const bool odd = p.lane & 1;
                     const Bits128 w = drop_bits(key, t.d.site, (uint64_t)(m0 + (c + odd) * kRows + row0) * t.across + (n >> 3));
                     const uint32_t r0 = from_neighbour(odd ? w.w[0] : w.w[2]), r1 = from_neighbour(odd ? w.w[1] : w.w[3]);
@@ -174,28 +272,29 @@ template <class T> struct Ended : Ending {
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int row = (c + h) * kRows + row0, m = m0 + row;
-                    const f32x4 x = *(const f32x4 *)(p.lds + row * Block::kPitch + p.lane % kLanes * 16);
-                    float v[4] = {x[0], x[1], x[2], x[3]};
+                    const int m = m0 + (c + h) * kRows + row0;
+                    float v[4] = {x[c + h][0], x[c + h][1], x[c + h][2], x[c + h][3]}, from[4];
+                    was[c + h].get(from);
+                    finish_four<KIND, ACT>(t, n, b, from, words[h], v);
                     if (m >= p.M || n >= t.cols_out) continue;
-                    if (sums) {
-                        store_four(e.sums + p.slice * e.slice_stride + (long)m * p.N + n, n, p.N, (p.N & 3) == 0, v);
+                    if (KIND == kSums) {
+                        write_quad(e.sums + p.slice * e.slice_stride + (long)m * p.N + n, n, p.N, v);
                         continue;
                     }
-                    finish_four<T>(t, m, n, b, words[h], v);
+                    if (t.out) write_quad((T *)t.out + (long)m * t.ld_out + n, n, t.cols_out, v);
+                    if (KIND == kSlope) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) columns[k] += v[k];
+                        for (int k = 0; k < 4; ++k) columns[k] += v[k];
+                    }
                 }
             }
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
         }
-        if (sums || !t.columns) return;
+        if (KIND != kSlope || !t.columns) return;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int s = kLanes; s < 64; s *= 2) columns[k] += __shfl_xor(columns[k], s, 64);
-        if (p.lane < kLanes && p.m0 < p.M && n < t.N) store_four(t.columns + (long)(p.m0 / (32 * MI)) * t.N + n, n, t.N, (t.N & 3) == 0, columns);
+        if (p.lane < kLanes && p.m0 < p.M && n < t.N) write_quad(t.columns + (long)(p.m0 / (32 * MI)) * t.N + n, n, t.N, columns);
     }
 };
 
@@ -208,9 +307,8 @@ struct Join {
     int slices, rows_per_block;
     long M;
 };
-template <typename T> __global__ void __launch_bounds__(256) join_kernel(const Join p)
+template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_rows_of(const Join &p, float (*red)[256])
 {
-    __shared__ float red[8][256];
     const Tail &t = p.t;
     const int col = threadIdx.x & 31, turn = threadIdx.x >> 5, n = blockIdx.y * 256 + col * 8;
     const long m1 = min(p.M, (long)(blockIdx.x + 1) * p.rows_per_block);
@@ -222,42 +320,48 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const J
         for (int k = 0; k < 4; ++k) b[h][k] = t.b && n + h * 4 + k < t.N ? Elem<T>::load((const T *)t.b + n + h * 4 + k) : 0.f;
     if (n < t.cols_out)
         for (long m = (long)blockIdx.x * p.rows_per_block + turn; m < m1; m += 8) {
-            f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-            if (t.N % 4 == 0) {
-                const float *x = p.sums + m * t.N + n;
-                const bool both = n + 8 <= t.N;
-                if (n < t.N)
-                    for (int k0 = 0; k0 < p.slices; k0 += 4) { // four slices on their way at a time
-                        f32x4 y[4][2];
+            Quad<T> o[2];
+            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
+            for (int h = 0; h < 2; ++h) {
+                o[h].set(zero);
+                if (KIND != kScaled && t.other && n + h * 4 < t.N) o[h] = read_quad((const T *)t.other + m * t.ld_other + n + h * 4, n + h * 4, t.N);
+            }
+            float s[2][4] = {};
+            for (int k0 = 0; k0 < p.slices; k0 += 4) { // four slices on their way at a time
+                Quad<float> y[4][2];
 #pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                y[k][h] = k0 + k < p.slices && (h == 0 || both) ? *(const f32x4 *)(x + (k0 + k) * p.slice_stride + h * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) s[h] += y[k][h];
+                    for (int h = 0; h < 2; ++h) {
+                        y[k][h].set(zero);
+                        if (k0 + k < p.slices && n + h * 4 < t.N) y[k][h] = read_quad(p.sums + (k0 + k) * p.slice_stride + m * t.N + n + h * 4, n + h * 4, t.N);
                     }
-            } else {
-                for (int k = 0; k < p.slices; ++k)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (n + e < t.N) s[e >> 2][e & 3] += p.sums[k * p.slice_stride + m * t.N + n + e];
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float z[4];
+                        y[k][h].get(z);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) s[h][q] += z[q];
+                    }
             }
             Bits128 w = {{0, 0, 0, 0}};
-            if (t.d.limit) w = drop_bits(key, t.d.site, (uint64_t)m * t.across + (n >> 3));
+            if (KIND != kScaled && t.d.limit) w = drop_bits(key, t.d.site, (uint64_t)m * t.across + (n >> 3));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 if (n + h * 4 >= t.cols_out) continue;
                 const uint32_t words[2] = {w.w[2 * h], w.w[2 * h + 1]};
-                float v[4] = {s[h][0], s[h][1], s[h][2], s[h][3]};
-                finish_four<T>(t, m, n + h * 4, b[h], words, v);
+                float from[4];
+                o[h].get(from);
+                finish_four<KIND, ACT>(t, n + h * 4, b[h], from, words, s[h]);
+                if (t.out) write_quad((T *)t.out + m * t.ld_out + n + h * 4, n + h * 4, t.cols_out, s[h]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) columns[h][k] += v[k];
+                for (int k = 0; k < 4; ++k) columns[h][k] += s[h][k];
             }
         }
-    if (!t.columns) return;
+    if (KIND != kSlope || !t.columns) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[turn][col * 8 + e] = columns[e >> 2][e & 3];
     __syncthreads();
@@ -265,6 +369,12 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const J
     float s = 0.f;
     for (int k = 0; k < 8; ++k) s += red[k][c];
     if ((int)(blockIdx.y * 256) + c < t.N) t.columns[(long)blockIdx.x * t.N + blockIdx.y * 256 + c] = s;
+}
+template <typename T> __global__ void __launch_bounds__(256) join_kernel(const Join p)
+{
+    __shared__ float red[8][256];
+    if (p.t.kind == kScaled) join_rows_of<T, kScaled, CAC_ACT_NONE>(p, red);
+    else with_kind<false>(p.t, [&](auto kind, auto act) { join_rows_of<T, decltype(kind)::value, decltype(act)::value>(p, red); });
 }
 
 // db from the parts' sums: a block of sixteen waves takes 64 columns.
@@ -323,7 +433,7 @@ static bool choose_fits(Format f, long M, long N, long K, TileChoice *c)
 }
 static int rows_of_a_part(int shape) // of a tile, that one wave sums over
 {
-    static const int kRowsOf[kShapes] = {32 * Small::MI, 32 * Middle::MI, 32 * Wide::MI, 32 * Big::MI, 32 * Low::MI};
+    static const int kRowsOf[kShapes] = {32 * Small::MI, 32 * Middle::MI, 32 * Wide::MI, 32 * Large::MI, 32 * Low::MI};
     return kRowsOf[shape];
 }
 static long join_rows(long M) { return M < 2048 ? 8 : 64; } // of a block of join_kernel
@@ -412,7 +522,6 @@ template <typename T> struct Layer {
         t.out = out;
         t.ld_out = ld_out;
         t.cols_out = (int)N;
-        t.wide_out = N % 4 == 0 && ld_out % 4 == 0;
         t.scale = g.alpha * d.scale;
         t.across = (int)((N + 7) / 8);
         return t;
@@ -442,12 +551,16 @@ template <typename T> struct Layer {
         m.N = (int)N;
         m.K = (int)K;
         m.batch = 1;
-        typename Ended<T>::Params e;
+        typedef Ended<T, LB == Lay::kDown> Epi;
+        typename Epi::Params e;
         e.t = t;
         e.sums = c.slices > 1 ? (float *)(ws + p.o_sum) : nullptr;
         e.slice_stride = M * N;
-        if (e.sums) e.t.cols_out = (int)N;
-        err = launch<P, LA, LB, Ended<T>>(m, e, c, st);
+        if (e.sums) {
+            e.t.kind = kSums;
+            e.t.cols_out = (int)N;
+        }
+        err = launch_tiles<P, LA, LB, Epi>(m, e, c, st);
         if (err == hipSuccess && c.slices > 1) join(t, M, c.slices);
     }
     hipError_t forward(const void *X, const void *W, const void *b, const void *R, void *Y)
@@ -457,7 +570,6 @@ template <typename T> struct Layer {
         t.b = b;
         t.other = R;
         t.ld_other = g.ld_r;
-        t.wide_other = g.N % 4 == 0 && g.ld_r % 4 == 0;
         t.d = d;
         product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
         return err;
@@ -468,11 +580,9 @@ template <typename T> struct Layer {
         const void *u = p.grad ? ws + p.o_u : dY;
         Tail t = tail(kSlope, g.N, p.grad ? ws + p.o_u : nullptr, p.ld_u);
         t.cols_out = (int)p.ld_u;
-        t.wide_out = true;
         t.b = b;
         t.other = dY;
         t.ld_other = g.N;
-        t.wide_other = g.N % 4 == 0;
         t.columns = db ? (float *)(ws + p.o_db) : nullptr;
         t.d = d;
         if (p.again) product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);

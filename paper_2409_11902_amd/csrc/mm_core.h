@@ -138,20 +138,26 @@ template <class P, Lay L, int T, int R, int NW, bool COUNTS> struct Stage {
             off[i] = there ? (uint32_t)(row * (int)ld + c * kUnit) : kNowhere;
         }
     }
-    // the next pass into LDS at byte address `lds`; behind the last that is zeros
-    __device__ __forceinline__ void load(uint32_t lds, int wave)
+    // load i of the next pass into LDS at byte address `lds`; behind the last pass that is zeros
+    __device__ __forceinline__ void load_one(int i, uint32_t lds, int wave)
     {
         const uint64_t from = (uint64_t)(uintptr_t)base;
         const u32x4 rs = {(uint32_t)from, (uint32_t)(from >> 32) & 0xffffu, 0x7fffffffu, 0x00020000u};
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int here = L == Lay::kDown ? at + i * kStep : kStep == 8 && i % 2 ? at ^ 4 * kOf16 : at; // (8 rows on: four chunks apart)
-            const uint32_t o = here < left ? off[i] : kNowhere;
-            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 64 * kUnit);
-            load_to_lds<kUnit>(rs, o, to);
-        }
+        const int here = L == Lay::kDown ? at + i * kStep : kStep == 8 && i % 2 ? at ^ 4 * kOf16 : at; // (8 rows on: four chunks apart)
+        const uint32_t o = here < left ? off[i] : kNowhere;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NW + wave) * 64 * kUnit);
+        load_to_lds<kUnit>(rs, o, to);
+    }
+    __device__ __forceinline__ void advance()
+    {
         base += step;
         left -= L == Lay::kAlong ? kUnits : kPass<P, R>;
+    }
+    __device__ __forceinline__ void load(uint32_t lds, int wave)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load_one(i, lds, wave);
+        advance();
     }
 };
 
@@ -331,7 +337,10 @@ struct Place {
 };
 
 // How a workgroup's tile is made of waves' parts, and how it is staged: R bytes of K to a row and pass, ST passes in LDS.
-template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU> struct Shape {
+// MIXED: a pass' loads are issued one between two products (a wave waits to issue a load while others' are taken in, 16 cycles each, and
+// issues nothing else meanwhile), else all together.
+template <int WM_, int WN_, int MI_, int NI_, int R_, int ST_, int PER_CU, bool MIXED = false> struct Shape {
+    static constexpr bool kMixed = MIXED;
     static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, R = R_, ST = ST_, kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int TM = 32 * MI * WM, TN = 32 * NI * WN, kBuffer = (TM + TN) * R, kLds = ST * kBuffer;
     static constexpr int kPerSimd = PER_CU * kWaves / 4; // waves that registers are shared by
@@ -439,10 +448,29 @@ __device__ __forceinline__ void mm_tile(const Params &p, const typename Epi::Par
                 } else {
                     const uint32_t next = cur + S::kBuffer == lds_end ? lds : cur + S::kBuffer;
                     meet<kAhead>(); // the next pass has arrived; this one's last fragments are in registers
-                    load(cur);
+                    if (!S::kMixed) load(cur);
                     read((s + 1) & 1, next, 0);
+                    if constexpr (S::kMixed) {
+                        static_assert(!S::kMixed || (!P::kRaw && P::kParts == 1), "bfloat16");
+                        constexpr int kA = decltype(sa)::kLoads, kB = decltype(sb)::kLoads;
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int k = 0; k < MI * NI; ++k) {
+                            acc[k / NI][k % NI] = product<P>(b[s & 1][0][k % NI], a[s & 1][0][k / NI], acc[k / NI][k % NI]);
+                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int i = k * (kA + kB) / (MI * NI); i < (k + 1) * (kA + kB) / (MI * NI); ++i) {
+                                if (i < kA) sa.load_one(i, cur, wave);
+                                else sb.load_one(i - kA, cur + TM * S::R, wave);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                        sa.advance();
+                        sb.advance();
+                    }
                     cur = next;
                 }
+                if (S::kMixed && s + 1 == kSteps) continue;
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (P::kRaw) { // (term e of a lane's eight: one of the first 8 with one of the second)
 #pragma unroll
