@@ -139,7 +139,8 @@ int cac_linear_describe_plan(const cac_linear_desc *d, int op, char *buf, size_t
     auto more = [&](const char *fmt, const char *tile, int slices) {
         if (n > 0 && (size_t)n < buf_len) n += snprintf(buf + n, buf_len - n, fmt, tile, slices);
     };
-    if (op == CAC_LINEAR_FWD || p.again) more("; pre-activation: tile %s in %d slices", kTiles[p.y.shape], p.y.slices);
+    if ((op == CAC_LINEAR_FWD || p.again) && p.few) more("; pre-activation: %s%.0d", "few rows", 0);
+    else if (op == CAC_LINEAR_FWD || p.again) more("; pre-activation: tile %s in %d slices", kTiles[p.y.shape], p.y.slices);
     if (op == CAC_LINEAR_BWD) {
         more("; dX: tile %s in %d slices", kTiles[p.dx.shape], p.dx.slices);
         more("; dW: tile %s in %d slices", kTiles[p.dw.shape], p.dw.slices);

@@ -50,12 +50,13 @@ struct LinearGeom {
     bool drops;
 };
 struct LinearPlan {
+    bool few;                // few rows: W is read as it lies, by workgroups that have all rows of some features
     bool pack_x, pack_w;     // rows that are not whole numbers of 16 bytes go through the workspace
     bool again;              // backward: the pre-activation is formed again
     bool grad;               // backward: the pre-activation's gradient is a matrix of its own (else it is dY)
     long ld_x, ld_w, ld_u;   // elements from a row of the operands, as they are multiplied, to the next
     TileChoice y, dx, dw;
-    long parts;              // of the rows, that db is summed in
+    long parts;              // of the rows, that db is summed in (0: in one)
     size_t o_x, o_w, o_u, o_db, o_sum, bytes;
 };
 bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p); // false: a product too large for one grid

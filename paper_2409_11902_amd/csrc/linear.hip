@@ -377,6 +377,143 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const J
     else with_kind<false>(p.t, [&](auto kind, auto act) { join_rows_of<T, decltype(kind)::value, decltype(act)::value>(p, red); });
 }
 
+// ---- Few rows (up to 32): a workgroup has 16 features of all of them, and reads its rows of W once, as they lie, whatever they start on.  Its waves share the
+// terms out, 64 (float: 32) at a time and wave; fragments come straight from memory, since a wave has no use for another's, and the waves' sums are
+// joined in LDS, so that there is one launch.  Bound by reading W.
+struct Few {
+    Tail t;
+    const void *X, *W;
+    long ld_x, ld_w;
+    int T, K;
+    void *db;       // kSlope: of T's type, times `factor`, or null
+    float factor;
+};
+// a step's terms of one row: 8 (float: 4) to a lane
+template <typename T> struct Terms;
+template <> struct Terms<bf16_t> {
+    static constexpr int kLane = 8, kStep = 32;
+    Eight<bf16_t> v;
+    __device__ __forceinline__ void clear() { v.clear(); }
+    template <bool WHOLE> __device__ __forceinline__ void read(const bf16_t *row, int k, int K) { v = read_eight<WHOLE>(row, k, K); }
+    static __device__ __forceinline__ f32x4 product(const Terms &a, const Terms &b, f32x4 c)
+    {
+        union { whole16 u; bf16x8 h; } x, y;
+        x.u = a.v.a;
+        y.u = b.v.a;
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.h, y.h, c, 0, 0, 0);
+    }
+};
+template <> struct Terms<float> {
+    static constexpr int kLane = 4, kStep = 16;
+    Quad<float> v;
+    __device__ __forceinline__ void clear() { v.a = Quad<float>::V{0, 0, 0, 0}; }
+    template <bool WHOLE> __device__ __forceinline__ void read(const float *row, int k, int K)
+    {
+        if (WHOLE) v.read(row + k);
+        else v = read_quad(row + k, k, K);
+    }
+    static __device__ __forceinline__ f32x4 product(const Terms &a, const Terms &b, f32x4 c)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.v.a[e]), __uint_as_float(b.v.a[e]), c, 0, 0, 0);
+        return c;
+    }
+};
+// TB: sixteens of rows.  WHOLE: rows of whole lane's terms
+template <typename T, int TB, int WAVES, bool WHOLE> __global__ void __launch_bounds__(64 * WAVES) few_kernel(const Few p)
+{
+    typedef Terms<T> Part;
+    constexpr int kAhead = 4; // steps on their way at a time
+    __shared__ f32x4 red[WAVES][TB][64];
+    __shared__ float db[TB][16];
+    const Tail &t = p.t;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * 16, steps = (p.K + Part::kStep - 1) / Part::kStep;
+    const T *w = (const T *)p.W + (long)min(n0 + (lane & 15), t.N - 1) * p.ld_w; // (what is past the last feature is not stored)
+    const T *x[TB];
+    bool row[TB];
+#pragma unroll
+    for (int i = 0; i < TB; ++i) {
+        row[i] = i * 16 + (lane & 15) < p.T;
+        x[i] = (const T *)p.X + (long)(row[i] ? i * 16 + (lane & 15) : 0) * p.ld_x;
+    }
+    const int k0 = (lane >> 4) * Part::kLane;
+    struct Steps { Part a[kAhead], b[TB][kAhead]; } one, two;
+    auto ask = [&](Steps &q, int s) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = (s + u) * Part::kStep + k0;
+            q.a[u].clear();
+            if (k < p.K) q.a[u].template read<WHOLE>(w, k, p.K);
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+                q.b[i][u].clear();
+                if (k < p.K && row[i]) q.b[i][u].template read<WHOLE>(x[i], k, p.K);
+            }
+        }
+    };
+    f32x4 acc[TB];
+#pragma unroll
+    for (int i = 0; i < TB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const Steps &q) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < TB; ++i) acc[i] = Part::product(q.a[u], q.b[i][u], acc[i]);
+    };
+    constexpr int kStride = WAVES * kAhead;
+    ask(one, wave * kAhead);
+    for (int s = wave * kAhead; s < steps; s += 2 * kStride) {
+        ask(two, s + kStride); // (zeros behind the last)
+        multiply(one);
+        if (s + 2 * kStride < steps) ask(one, s + 2 * kStride);
+        multiply(two);
+    }
+#pragma unroll
+    for (int i = 0; i < TB; ++i) red[wave][i][lane] = acc[i];
+    __syncthreads();
+    // a wave's 16 rows by 16 features: a lane has four neighbours of a row
+    const int i = wave, m = i * 16 + (lane & 15), n = n0 + (lane >> 4) * 4;
+    float columns[4] = {0.f, 0.f, 0.f, 0.f};
+    if (i < TB) {
+        f32x4 sum = red[0][i][lane];
+        for (int k = 1; k < WAVES; ++k) sum += red[k][i][lane];
+        float v[4] = {sum[0], sum[1], sum[2], sum[3]}, bias[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};
+        const bool there = m < p.T && n < t.cols_out;
+        if (t.b && n < t.N) read_quad((const T *)t.b + n, n, t.N).get(bias);
+        if (t.other && there && n < t.N) read_quad((const T *)t.other + (long)m * t.ld_other + n, n, t.N).get(o);
+        uint32_t words[2] = {0, 0};
+        if (t.d.limit) {
+            const Bits128 r = drop_bits(drop_key(t.d), t.d.site, (uint64_t)m * t.across + (n >> 3));
+            words[0] = n & 4 ? r.w[2] : r.w[0];
+            words[1] = n & 4 ? r.w[3] : r.w[1];
+        }
+        with_kind<false>(t, [&](auto kind, auto act) { finish_four<decltype(kind)::value, decltype(act)::value>(t, n, bias, o, words, v); });
+        if (there) {
+            if (t.out) write_quad((T *)t.out + (long)m * t.ld_out + n, n, t.cols_out, v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) columns[k] = v[k];
+        }
+        if (p.db) { // over 16 rows: lanes of the same features
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                for (int s = 1; s < 16; s *= 2) columns[k] += __shfl_xor(columns[k], s, 64);
+            }
+            if ((lane & 15) == 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) db[i][(lane >> 4) * 4 + k] = columns[k];
+        }
+    }
+    if (!p.db) return;
+    __syncthreads();
+    if (threadIdx.x < 16 && n0 + (int)threadIdx.x < t.N) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < TB; ++k) s += db[k][threadIdx.x];
+        Elem<T>::store((T *)p.db + n0 + threadIdx.x, s * p.factor);
+    }
+}
+
 // db from the parts' sums: a block of sixteen waves takes 64 columns.
 template <typename T> __global__ void __launch_bounds__(1024) bias_join_kernel(const float *part, int parts, int N, float scale, T *db)
 {
@@ -426,11 +563,52 @@ template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const P
 using namespace dense;
 
 // ---- host
-static bool choose_fits(Format f, long M, long N, long K, TileChoice *c)
+constexpr int kFewRows = 32;
+
+// Microseconds of M x N sums of K terms in a tile and a number of slices.  What a pass takes on a compute unit with one workgroup and with as many
+// as it holds, and what comes before and after a workgroup's passes: from 8192 x 64 x 8192 to 8192 x 8192 x 2048 bfloat16 within 8 %. The slices' sums
+// are written, read and joined in a launch of their own, 4 us.
+static double tiles_us(Format f, int shape, long M, long N, long K, int slices)
 {
-    *c = choose(f, M, N, 1, K, false, 64);
-    return fits_grid(c->shape, tiles_of(c->shape, M, N, false) * c->slices);
+    struct Price { int holds; double alone, full, once, once_full; };
+    static const Price kBf[] = {{3, 0.27, 0.62, 2.5, 4.0}, {2, 0.77, 1.06, 3.5, 7.0}, {}, {1, 1.56, 1.56, 9.0, 14.0}, {}},
+                       kRawOf[] = {{3, 0.5, 1.4, 2.5, 4.0}, {}, {}, {}, {2, 0.5, 1.0, 2.5, 4.0}};
+    const Price &p = (f == kRaw ? kRawOf : kBf)[shape];
+    const double n = cdiv(cdiv(K, kTerms[f]), slices);
+    const long wgs = tiles_of(shape, M, N, false) * slices, round = 256L * p.holds, rest = wgs % round;
+    double us = (wgs / round) * (p.full * n + p.once_full);
+    if (rest) {
+        const double share = rest <= 256 ? rest / 256.0 * (p.holds == 1) : (rest - 256.0) / (round - 256);
+        const double pass = rest <= 256 ? p.alone : p.alone + share * (p.full - p.alone);
+        us += pass * n + p.once + share * (p.once_full - p.once);
+    }
+    if (slices > 1) us += 4.0 + 3.2e-6 * slices * M * N;
+    return us;
 }
+// The cheapest; false: too many tiles for one grid.  DOWN: a's terms run down memory, which tiles of 32 rows have no layout for.
+static bool choose_tiles(Format f, long M, long N, long K, bool down, TileChoice *c, double *least)
+{
+    *least = 1e30;
+    for (int shape = 0; shape < kShapes; ++shape) {
+        if (f == kRaw ? shape != kSmall && shape != kLow : shape == kLow || shape == kWide) continue;
+        if (f == kRaw && (shape == kLow) != (M <= 32 && !down)) continue;
+        const long tiles = tiles_of(shape, M, N, false);
+        for (int slices = 1; slices <= 64; slices += slices < 4 ? 1 : slices / 4 * 2) {
+            if (slices > 1 && (cdiv(K, kTerms[f]) / slices < 4 || tiles * slices > 2048)) break;
+            if (!fits_grid(shape, tiles * slices)) break;
+            const double us = tiles_us(f, shape, M, N, K, slices);
+            if (us < *least) {
+                *least = us;
+                *c = TileChoice{shape, slices};
+            }
+        }
+    }
+    return *least < 1e30;
+}
+// ... and of few rows by few_kernel: a compute unit takes in 35 KB a us, its features' rows of W and for each sixteen of them X (16 x 4096 x 4096
+// bfloat16 10.9 us, 16 x 8192 x 2048 17.9, 1 x 8192 x 512 float 22)
+static double few_us(long T, long N, long K, long e) { return 2.6 + cdiv(cdiv(N, 16), 256) * (16.0 + T) * K * e / 35e3; }
+
 static int rows_of_a_part(int shape) // of a tile, that one wave sums over
 {
     static const int kRowsOf[kShapes] = {32 * Small::MI, 32 * Middle::MI, 32 * Wide::MI, 32 * Large::MI, 32 * Low::MI};
@@ -440,8 +618,7 @@ static long join_rows(long M) { return M < 2048 ? 8 : 64; } // of a block of joi
 
 bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p)
 {
-    const bool real = g.dtype == CAC_F32;
-    const Format f = real ? kRaw : kBf16;
+    const Format f = g.dtype == CAC_F32 ? kRaw : kBf16;
     const long e = g.dtype == CAC_F32 ? 4 : 2, whole = 16 / e;
     auto padded = [&](long n) { return (n + 7) / 8 * 8; };
     size_t at = 0;
@@ -459,19 +636,24 @@ bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p)
     p->grad = backward && (p->again || g.drops || g.N % whole);
     p->ld_u = p->grad ? padded(g.N) : g.N;
     size_t sums = 0;
-    auto product = [&](long M, long N, long K, TileChoice *c) {
-        if (!choose_fits(f, M, N, K, c)) return false;
+    double us;
+    auto product = [&](long M, long N, long K, bool down, TileChoice *c) {
+        if (!choose_tiles(f, M, N, K, down, c, &us)) return false;
         if (c->slices > 1 && sums < (size_t)c->slices * M * N * 4) sums = (size_t)c->slices * M * N * 4;
         return true;
     };
-    if (!backward || p->again)
-        if (!product(g.T, g.N, g.D, &p->y)) return false;
+    if (!backward || p->again) {
+        if (!product(g.T, g.N, g.D, false, &p->y)) return false;
+        if ((p->pack_x || p->pack_w) && !backward) us += 4.0 + (g.T + g.N) * g.D * e * 1e-6 / 1.5;
+        p->few = g.T <= kFewRows && few_us(g.T, g.N, g.D, e) < us;
+        if (p->few) sums = 0;
+        if (p->few && !backward) p->pack_x = p->pack_w = false;
+    }
     if (p->pack_x) p->o_x = take(g.T * p->ld_x * e);
     if (p->pack_w) p->o_w = take(g.N * p->ld_w * e);
     if (backward) {
-        // (a tile of 32 rows has none that run down memory: dW of few features takes one of 64)
-        if (!product(g.T, g.D, g.N, &p->dx) || !product(real && g.N <= 32 ? 33 : g.N, g.D, g.T, &p->dw)) return false;
-        p->parts = p->again && p->y.slices == 1 ? cdiv(g.T, rows_of_a_part(p->y.shape)) : cdiv(g.T, join_rows(g.T));
+        if (!product(g.T, g.D, g.N, false, &p->dx) || !product(g.N, g.D, g.T, true, &p->dw)) return false;
+        p->parts = p->again && p->few ? 0 : p->again && p->y.slices == 1 ? cdiv(g.T, rows_of_a_part(p->y.shape)) : cdiv(g.T, join_rows(g.T));
         if (p->grad) p->o_u = take(g.T * p->ld_u * e);
         p->o_db = take((size_t)p->parts * g.N * 4);
     }
@@ -538,6 +720,34 @@ template <typename T> struct Layer {
         hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)cdiv(M, j.rows_per_block), (unsigned)cdiv(t.cols_out, 256)), dim3(256), 0, st, j);
         err = hipGetLastError();
     }
+    void few(const void *X, const void *W, const Tail &t, void *db)
+    {
+        if (err != hipSuccess) return;
+        Few f;
+        f.t = t;
+        f.X = X;
+        f.W = W;
+        f.ld_x = g.ld_x;
+        f.ld_w = g.ld_w;
+        f.T = (int)g.T;
+        f.K = (int)g.D;
+        f.db = db;
+        f.factor = t.scale;
+        auto go = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(t.cols_out, 16)), dim3(64 * waves), 0, st, f); };
+        // a wave has 4 steps at a time; with more waves than that gives work to, the others only wait
+        const bool wide = g.D > 4 * 4 * Terms<T>::kStep;
+        auto waves = [&](auto sixteens, auto whole) {
+            if (wide) go(few_kernel<T, decltype(sixteens)::value, 16, decltype(whole)::value>, 16);
+            else go(few_kernel<T, decltype(sixteens)::value, 4, decltype(whole)::value>, 4);
+        };
+        auto rows = [&](auto sixteens) {
+            if (g.D % Terms<T>::kLane) waves(sixteens, std::false_type());
+            else waves(sixteens, std::true_type());
+        };
+        if (g.T <= 16) rows(std::integral_constant<int, 1>());
+        else rows(std::integral_constant<int, 2>());
+        err = hipGetLastError();
+    }
     // C = A B^T with a tail
     template <Lay LA, Lay LB> void product(const void *a, long lda, const void *b, long ldb, long M, long N, long K, TileChoice c, const Tail &t)
     {
@@ -571,12 +781,13 @@ template <typename T> struct Layer {
         t.other = R;
         t.ld_other = g.ld_r;
         t.d = d;
-        product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
+        if (p.few) few(X, W, t, nullptr);
+        else product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
         return err;
     }
     hipError_t backward(const void *X, const void *W, const void *b, const void *dY, void *dX, void *dW, void *db)
     {
-        pack(X, W, dW || p.again, dX || p.again);
+        pack(X, W, dW || (p.again && !p.few), dX || (p.again && !p.few));
         const void *u = p.grad ? ws + p.o_u : dY;
         Tail t = tail(kSlope, g.N, p.grad ? ws + p.o_u : nullptr, p.ld_u);
         t.cols_out = (int)p.ld_u;
@@ -585,11 +796,12 @@ template <typename T> struct Layer {
         t.ld_other = g.N;
         t.columns = db ? (float *)(ws + p.o_db) : nullptr;
         t.d = d;
-        if (p.again) product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
+        if (p.again && p.few) few(X, W, t, db);
+        else if (p.again) product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
         else if (err == hipSuccess && (p.grad || db)) join(t, g.T, 0);
         if (dX) product<Lay::kAlong, Lay::kDown>(u, p.ld_u, w, p.ld_w, g.T, g.D, g.N, p.dx, tail(kScaled, g.D, dX, g.D));
         if (dW) product<Lay::kDown, Lay::kDown>(u, p.ld_u, x, p.ld_x, g.N, g.D, g.T, p.dw, tail(kScaled, g.D, dW, g.D));
-        if (db && err == hipSuccess) {
+        if (db && p.parts && err == hipSuccess) {
             hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)cdiv(g.N, 64)), dim3(1024), 0, st, (const float *)(ws + p.o_db), (int)p.parts, (int)g.N,
                                g.alpha * d.scale, (T *)db);
             err = hipGetLastError();
