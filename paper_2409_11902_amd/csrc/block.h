@@ -56,8 +56,9 @@ struct LinearPlan {
     bool grad;               // backward: the pre-activation's gradient is a matrix of its own (else it is dY)
     long ld_x, ld_w, ld_u;   // elements from a row of the operands, as they are multiplied, to the next
     TileChoice y, dx, dw;
+    bool together;           // backward: dX, dW and db in one launch, where both are asked for
     long parts;              // of the rows, that db is summed in (0: in one)
-    size_t o_x, o_w, o_u, o_db, o_sum, bytes;
+    size_t o_x, o_w, o_u, o_db, o_sum, o_sum2, bytes;
 };
 bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p); // false: a product too large for one grid
 hipError_t launch_linear_fwd(const LinearGeom &g, const LinearPlan &p, const Drop &d, const void *X, const void *W, const void *b, const void *R,

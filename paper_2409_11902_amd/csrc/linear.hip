@@ -6,6 +6,8 @@
 //     act dU is dY's bits. db is summed from dU before it is rounded.
 //   - float: by the float instruction, operands as they lie (a matrix of any scale, infinities and NaN as float arithmetic has them).
 // Sums are of 32 bits.
+#include <algorithm>
+
 #include "block.h"
 #include "mm_core.h"
 
@@ -370,9 +372,12 @@ template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_r
     for (int k = 0; k < 8; ++k) s += red[k][c];
     if ((int)(blockIdx.y * 256) + c < t.N) t.columns[(long)blockIdx.x * t.N + blockIdx.y * 256 + c] = s;
 }
-template <typename T> __global__ void __launch_bounds__(256) join_kernel(const Join p)
+struct Joins { Join j[2]; };
+template <typename T> __global__ void __launch_bounds__(256) join_kernel(const Joins both)
 {
     __shared__ float red[8][256];
+    const Join &p = both.j[blockIdx.z];
+    if ((long)blockIdx.x * p.rows_per_block >= p.M || (int)blockIdx.y * 256 >= p.t.cols_out) return;
     if (p.t.kind == kScaled) join_rows_of<T, kScaled, CAC_ACT_NONE>(p, red);
     else with_kind<false>(p.t, [&](auto kind, auto act) { join_rows_of<T, decltype(kind)::value, decltype(act)::value>(p, red); });
 }
@@ -514,26 +519,77 @@ template <typename T, int TB, int WAVES, bool WHOLE> __global__ void __launch_bo
     }
 }
 
-// db from the parts' sums: a block of sixteen waves takes 64 columns.
-template <typename T> __global__ void __launch_bounds__(1024) bias_join_kernel(const float *part, int parts, int N, float scale, T *db)
+// ---- db from the parts' sums: a block takes 64 columns, and every sixteenth part at a time, however many waves it has, so that the order is one.
+struct Bias {
+    const float *part;
+    int parts, N;
+    float scale;
+    void *db;
+};
+template <typename T, int WAVES> __device__ __forceinline__ void bias_sums(const Bias &p, int block, float (*red)[64])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = block * 64 + lane;
+    for (int q = wave; q < 16; q += WAVES) {
+        float s = 0.f;
+        if (n < p.N) {
+            const float *x = p.part + n;
+            int r = q;
+            for (; r + 7 * 16 < p.parts; r += 8 * 16) { // eight on their way at a time
+                float y[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) y[k] = x[(long)(r + k * 16) * p.N];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += y[k];
+            }
+            for (; r < p.parts; r += 16) s += x[(long)r * p.N];
+        }
+        red[q][lane] = s;
+    }
+    __syncthreads();
+    if (wave || n >= p.N) return;
+    float s = red[0][lane];
+    for (int q = 1; q < 16; ++q) s += red[q][lane];
+    Elem<T>::store((T *)p.db + n, s * p.scale);
+}
+template <typename T> __global__ void __launch_bounds__(1024) bias_join_kernel(const Bias p)
 {
     __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = blockIdx.x * 64 + lane;
-    float s = 0.f;
-    if (n < N) {
-        const float *p = part + n;
-        int r = wave;
-        for (; r + 48 < parts; r += 64) {
-            const float x0 = p[(long)r * N], x1 = p[(long)(r + 16) * N], x2 = p[(long)(r + 32) * N], x3 = p[(long)(r + 48) * N];
-            s += (x0 + x1) + (x2 + x3);
-        }
-        for (; r < parts; r += 16) s += p[(long)r * N];
+    bias_sums<T, 16>(p, blockIdx.x, red);
+}
+
+// ---- dX, dW and db in one launch: the products' workgroups fill the compute units together, and the longer sums begin first.
+template <typename T> struct Pair {
+    Params x, w;
+    typename Ended<T, true>::Params ex, ew;
+    Bias b;
+    unsigned blocks_first, blocks_second;
+    bool x_first;
+};
+template <class P, class S, typename T> __global__ void __launch_bounds__(S::kThreads, S::kPerSimd) pair_kernel(const Pair<T> p)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    unsigned block = blockIdx.x;
+    const bool first = block < p.blocks_first;
+    if (!first) block -= p.blocks_first;
+    if (!first && block >= p.blocks_second) {
+        bias_sums<T, S::kWaves>(p.b, block - p.blocks_second, (float(*)[64])smem);
+    } else if (first == p.x_first) {
+        mm_tile<P, Lay::kAlong, Lay::kDown, S, Ended<T, true>>(p.x, p.ex, block, smem);
+    } else {
+        mm_tile<P, Lay::kDown, Lay::kDown, S, Ended<T, true>>(p.w, p.ew, block, smem);
     }
-    red[wave][lane] = s;
-    __syncthreads();
-    if (wave || n >= N) return;
-    for (int w = 1; w < 16; ++w) s += red[w][lane];
-    Elem<T>::store(db + n, s * scale);
+}
+template <class P, class S, typename T> hipError_t launch_pair(Pair<T> p, TileChoice cx, TileChoice cw, hipStream_t st)
+{
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(pair_kernel<P, S, T>), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+    if (attr != hipSuccess) return attr;
+    const unsigned bx = place_tiles<S>(&p.x, false, cx.slices, kPass<P, S::R>), bw = place_tiles<S>(&p.w, false, cw.slices, kPass<P, S::R>);
+    p.x_first = p.x.kt_slice >= p.w.kt_slice;
+    p.blocks_first = p.x_first ? bx : bw;
+    p.blocks_second = p.x_first ? bw : bx;
+    const unsigned bias = p.b.db ? (unsigned)cdiv(p.b.N, 64) : 0;
+    hipLaunchKernelGGL((pair_kernel<P, S, T>), dim3(bx + bw + bias), dim3(S::kThreads), S::kLds, st, p);
+    return hipGetLastError();
 }
 
 // Rows of any length and stride to rows of whole units of 16 bytes, padded with zeros; both operands in one launch.
@@ -605,7 +661,35 @@ static bool choose_tiles(Format f, long M, long N, long K, bool down, TileChoice
     }
     return *least < 1e30;
 }
-// ... and of few rows by few_kernel: a compute unit takes in 35 KB a us, its features' rows of W and for each sixteen of them X (16 x 4096 x 4096
+// dX and dW in one launch, tiles of one kind: what all workgroups take of the compute units, or the longest of them.
+struct PairChoice { TileChoice x, w; double us; };
+static PairChoice choose_pair(Format f, const LinearGeom &g)
+{
+    struct Price { int holds; double alone, full, once; };
+    static const Price kBf[] = {{3, 0.27, 0.62, 4.0}, {2, 0.77, 1.06, 7.0}, {}, {1, 1.56, 1.56, 14.0}}, kRawOf[] = {{3, 0.5, 1.4, 4.0}};
+    PairChoice best = {{}, {}, 1e30};
+    for (int shape : {kSmall, kMiddle, kBig}) {
+        if (f == kRaw && shape != kSmall) continue;
+        const Price &p = (f == kRaw ? kRawOf : kBf)[shape];
+        const long tx = tiles_of(shape, g.T, g.D, false), tw = tiles_of(shape, g.N, g.D, false);
+        const int nx = cdiv(g.N, kTerms[f]), nw = cdiv(g.T, kTerms[f]);
+        for (int sx = 1; sx <= 32; sx *= 2)
+            for (int sw = 1; sw <= 32; sw *= 2) {
+                if ((sx > 1 && (nx / sx < 4 || tx * sx > 2048)) || (sw > 1 && (nw / sw < 4 || tw * sw > 2048))) continue;
+                const long wgs = tx * sx + tw * sw;
+                if (!fits_grid(shape, wgs + cdiv(g.N, 64) + 16)) continue;
+                // with fewer workgroups than the card holds a pass takes less
+                const double fill = std::min(1.0, std::max(0.0, (wgs / 256.0 - 1) / std::max(1, p.holds - 1))), pass = p.alone + fill * (p.full - p.alone);
+                const double once = p.holds == 1 ? p.once : 2.5 + fill * (p.once - 2.5);
+                const double cx = cdiv(nx, sx) * pass + once, cw = cdiv(nw, sw) * pass + once;
+                double us = std::max(std::max(cx, cw), (tx * sx * cx + tw * sw * cw) / (256.0 * p.holds));
+                if (sx > 1 || sw > 1) us += 4.0 + 3.2e-6 * ((sx > 1 ? sx * g.T * g.D : 0) + (sw > 1 ? sw * g.N * g.D : 0));
+                if (us < best.us) best = PairChoice{{shape, sx}, {shape, sw}, us};
+            }
+    }
+    return best;
+}
+// Few rows by few_kernel: a compute unit takes in 35 KB a us, its features' rows of W and for each sixteen of them X (16 x 4096 x 4096
 // bfloat16 10.9 us, 16 x 8192 x 2048 17.9, 1 x 8192 x 512 float 22)
 static double few_us(long T, long N, long K, long e) { return 2.6 + cdiv(cdiv(N, 16), 256) * (16.0 + T) * K * e / 35e3; }
 
@@ -652,12 +736,29 @@ bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p)
     if (p->pack_x) p->o_x = take(g.T * p->ld_x * e);
     if (p->pack_w) p->o_w = take(g.N * p->ld_w * e);
     if (backward) {
-        if (!product(g.T, g.D, g.N, false, &p->dx) || !product(g.N, g.D, g.T, true, &p->dw)) return false;
+        double both = 4.0; // (a launch)
+        if (!product(g.T, g.D, g.N, false, &p->dx)) return false;
+        both += us;
+        if (!product(g.N, g.D, g.T, true, &p->dw)) return false;
+        both += us;
+        const PairChoice pair = choose_pair(f, g);
+        if (pair.us < both) {
+            p->together = true;
+            p->dx = pair.x;
+            p->dw = pair.w;
+        }
         p->parts = p->again && p->few ? 0 : p->again && p->y.slices == 1 ? cdiv(g.T, rows_of_a_part(p->y.shape)) : cdiv(g.T, join_rows(g.T));
         if (p->grad) p->o_u = take(g.T * p->ld_u * e);
         p->o_db = take((size_t)p->parts * g.N * 4);
     }
     p->o_sum = take(sums);
+    if (p->together) {
+        const size_t sx = p->dx.slices > 1 ? (size_t)p->dx.slices * g.T * g.D * 4 : 0, sw = p->dw.slices > 1 ? (size_t)p->dw.slices * g.N * g.D * 4 : 0;
+        at = p->o_sum; // (the pre-activation's slices have been joined by then, and one of the two products may be asked for alone)
+        take(std::max(sums, sx));
+        p->o_sum2 = take(sw);
+        at = std::max(at, p->o_sum + (sw + 255) / 256 * 256);
+    }
     p->bytes = at;
     return true;
 }
@@ -708,16 +809,24 @@ template <typename T> struct Layer {
         t.across = (int)((N + 7) / 8);
         return t;
     }
-    void join(const Tail &t, long M, int slices)
+    Join joined(const Tail &t, long M, int slices, size_t o_sum) const
     {
         Join j;
         j.t = t;
-        j.sums = (const float *)(ws + p.o_sum);
+        j.sums = (const float *)(ws + o_sum);
         j.slice_stride = M * t.N;
         j.slices = slices;
         j.M = M;
         j.rows_per_block = (int)join_rows(M);
-        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)cdiv(M, j.rows_per_block), (unsigned)cdiv(t.cols_out, 256)), dim3(256), 0, st, j);
+        return j;
+    }
+    void join(const Join &a, const Join *b = nullptr)
+    {
+        auto across = [](const Join &j) { return (unsigned)cdiv(j.M, j.rows_per_block); };
+        auto down = [](const Join &j) { return (unsigned)cdiv(j.t.cols_out, 256); };
+        const Joins both = {{a, b ? *b : a}};
+        const dim3 grid(b ? std::max(across(a), across(*b)) : across(a), b ? std::max(down(a), down(*b)) : down(a), b ? 2 : 1);
+        hipLaunchKernelGGL((join_kernel<T>), grid, dim3(256), 0, st, both);
         err = hipGetLastError();
     }
     void few(const void *X, const void *W, const Tail &t, void *db)
@@ -748,30 +857,58 @@ template <typename T> struct Layer {
         else rows(std::integral_constant<int, 2>());
         err = hipGetLastError();
     }
-    // C = A B^T with a tail
+    // C = A B^T with a tail, the sums of whose slices go to o_sum
+    template <class Epi> void describe(mm::Params *m, typename Epi::Params *e, const void *a, long lda, const void *b, long ldb, long M, long N, long K, TileChoice c,
+                                       const Tail &t, size_t o_sum) const
+    {
+        *m = mm::Params{};
+        m->a = a;
+        m->b = b;
+        m->lda = lda * sizeof(T);
+        m->ldb = ldb * sizeof(T);
+        m->M = (int)M;
+        m->N = (int)N;
+        m->K = (int)K;
+        m->batch = 1;
+        e->t = t;
+        e->sums = c.slices > 1 ? (float *)(ws + o_sum) : nullptr;
+        e->slice_stride = M * N;
+        if (e->sums) {
+            e->t.kind = kSums;
+            e->t.cols_out = (int)N;
+        }
+    }
     template <Lay LA, Lay LB> void product(const void *a, long lda, const void *b, long ldb, long M, long N, long K, TileChoice c, const Tail &t)
     {
         if (err != hipSuccess) return;
-        mm::Params m = {};
-        m.a = a;
-        m.b = b;
-        m.lda = lda * sizeof(T);
-        m.ldb = ldb * sizeof(T);
-        m.M = (int)M;
-        m.N = (int)N;
-        m.K = (int)K;
-        m.batch = 1;
         typedef Ended<T, LB == Lay::kDown> Epi;
+        mm::Params m;
         typename Epi::Params e;
-        e.t = t;
-        e.sums = c.slices > 1 ? (float *)(ws + p.o_sum) : nullptr;
-        e.slice_stride = M * N;
-        if (e.sums) {
-            e.t.kind = kSums;
-            e.t.cols_out = (int)N;
-        }
+        describe<Epi>(&m, &e, a, lda, b, ldb, M, N, K, c, t, p.o_sum);
         err = launch_tiles<P, LA, LB, Epi>(m, e, c, st);
-        if (err == hipSuccess && c.slices > 1) join(t, M, c.slices);
+        if (err == hipSuccess && c.slices > 1) join(joined(t, M, c.slices, p.o_sum));
+    }
+    Bias bias(void *db) const { return Bias{(const float *)(ws + p.o_db), (int)p.parts, (int)g.N, g.alpha * d.scale, p.parts ? db : nullptr}; }
+    void pair(const void *u, void *dX, void *dW, void *db)
+    {
+        if (err != hipSuccess) return;
+        const Tail tx = tail(kScaled, g.D, dX, g.D), tw = tail(kScaled, g.D, dW, g.D);
+        Pair<T> a = {};
+        describe<Ended<T, true>>(&a.x, &a.ex, u, p.ld_u, w, p.ld_w, g.T, g.D, g.N, p.dx, tx, p.o_sum);
+        describe<Ended<T, true>>(&a.w, &a.ew, u, p.ld_u, x, p.ld_x, g.N, g.D, g.T, p.dw, tw, p.o_sum2);
+        a.b = bias(db);
+        if constexpr (kFloat) {
+            err = launch_pair<P, Small, T>(a, p.dx, p.dw, st);
+        } else {
+            if (p.dx.shape == kBig) err = launch_pair<P, Large, T>(a, p.dx, p.dw, st);
+            else if (p.dx.shape == kMiddle) err = launch_pair<P, Middle, T>(a, p.dx, p.dw, st);
+            else err = launch_pair<P, Small, T>(a, p.dx, p.dw, st);
+        }
+        if (err != hipSuccess) return;
+        const Join jx = joined(tx, g.T, p.dx.slices, p.o_sum), jw = joined(tw, g.N, p.dw.slices, p.o_sum2);
+        if (p.dx.slices > 1 && p.dw.slices > 1) join(jx, &jw);
+        else if (p.dx.slices > 1) join(jx);
+        else if (p.dw.slices > 1) join(jw);
     }
     hipError_t forward(const void *X, const void *W, const void *b, const void *R, void *Y)
     {
@@ -798,12 +935,15 @@ template <typename T> struct Layer {
         t.d = d;
         if (p.again && p.few) few(X, W, t, db);
         else if (p.again) product<Lay::kAlong, Lay::kAlong>(x, p.ld_x, w, p.ld_w, g.T, g.N, g.D, p.y, t);
-        else if (err == hipSuccess && (p.grad || db)) join(t, g.T, 0);
+        else if (err == hipSuccess && (p.grad || db)) join(joined(t, g.T, 0, p.o_sum));
+        if (dX && dW && p.together) {
+            pair(u, dX, dW, db);
+            return err;
+        }
         if (dX) product<Lay::kAlong, Lay::kDown>(u, p.ld_u, w, p.ld_w, g.T, g.D, g.N, p.dx, tail(kScaled, g.D, dX, g.D));
         if (dW) product<Lay::kDown, Lay::kDown>(u, p.ld_u, x, p.ld_x, g.N, g.D, g.T, p.dw, tail(kScaled, g.D, dW, g.D));
         if (db && p.parts && err == hipSuccess) {
-            hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)cdiv(g.N, 64)), dim3(1024), 0, st, (const float *)(ws + p.o_db), (int)p.parts, (int)g.N,
-                               g.alpha * d.scale, (T *)db);
+            hipLaunchKernelGGL((bias_join_kernel<T>), dim3((unsigned)cdiv(g.N, 64)), dim3(1024), 0, st, bias(db));
             err = hipGetLastError();
         }
         return err;
