@@ -57,6 +57,7 @@ template <int LANES_, int WPR_, int CH_, bool WHOLE_> struct Rows {
     static constexpr int kColumns = 8 * LANES * WPR * CH;
     static_assert(LANES == 64 || WPR == 1, "part of a wave, or waves");
     int n[CH], count[CH]; // the lane's first columns, and how many of its eights there are
+    int from[CH];         // where its eights are read from: a row's end may lie inside
     int slot;             // which of the workgroup's rows
     __device__ __forceinline__ Rows(int D, int first = 0)
     {
@@ -66,7 +67,22 @@ template <int LANES_, int WPR_, int CH_, bool WHOLE_> struct Rows {
         for (int c = 0; c < CH; ++c) {
             n[c] = first + ((c * WPR + wave % WPR) * LANES + threadIdx.x % LANES) * 8;
             count[c] = min(max(D - n[c], 0), 8);
+            from[c] = WHOLE ? n[c] : max(min(n[c], D - 8), 0);
         }
+    }
+    // Whole loads, a row's last eight where the lane's eights end past it; taken to their place when they have arrived, so that
+    // nothing waits for them here.
+    template <typename T> __device__ __forceinline__ Eight<T> ask(const T *row, int c, int D) const
+    {
+        if (!WHOLE && D < 8) return read_eight(row, n[c], D);
+        Eight<T> r;
+        r.read(row + from[c]);
+        return r;
+    }
+    template <typename T> __device__ __forceinline__ void get(Eight<T> x, int c, float (&v)[8]) const
+    {
+        if (!WHOLE && n[c] != from[c]) x.shift(n[c] - from[c]);
+        x.get(v);
     }
 };
 
@@ -229,8 +245,8 @@ template <typename T, class L> __global__ void __launch_bounds__(64 * kFwdWaves<
 #pragma unroll
         for (int c = 0; c < CH; ++c)
             if (l.count[c]) {
-                f[c] = read_eight<L::WHOLE>((const T *)a.F + row * a.ld_f, l.n[c], D);
-                if (a.R) r[c] = read_eight<L::WHOLE>((const T *)a.R + row * a.ld_r, l.n[c], D);
+                f[c] = l.ask((const T *)a.F + row * a.ld_f, c, D);
+                if (a.R) r[c] = l.ask((const T *)a.R + row * a.ld_r, c, D);
             }
     };
 #pragma unroll
@@ -253,8 +269,8 @@ template <typename T, class L> __global__ void __launch_bounds__(64 * kFwdWaves<
         float v[CH][8], s[CH][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            f[c].get(v[c]);
-            r[c].get(s[c]);
+            l.get(f[c], c, v[c]);
+            l.get(r[c], c, s[c]);
         }
         if (row + kSlots < r1) ask(row + kSlots);
         if (row > last) {
@@ -343,10 +359,10 @@ template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 *
 #pragma unroll
         for (int c = 0; c < CH; ++c)
             if (l.count[c]) {
-                if (a.F) x[0][c] = read_eight<L::WHOLE>((const T *)a.F + row * a.ld_f, l.n[c], D);
-                if (pre) x[1][c] = read_eight<L::WHOLE>((const T *)a.S_in + row * D, l.n[c], D);
-                if (pre) x[2][c] = read_eight<L::WHOLE>((const T *)a.dH + row * D, l.n[c], D);
-                if (a.dS) x[3][c] = read_eight<L::WHOLE>((const T *)a.dS + row * D, l.n[c], D);
+                if (a.F) x[0][c] = l.ask((const T *)a.F + row * a.ld_f, c, D);
+                if (pre) x[1][c] = l.ask((const T *)a.S_in + row * D, c, D);
+                if (pre) x[2][c] = l.ask((const T *)a.dH + row * D, c, D);
+                if (a.dS) x[3][c] = l.ask((const T *)a.dS + row * D, c, D);
             }
     };
 #pragma unroll
@@ -386,10 +402,10 @@ template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 *
         float f[CH][8], s[CH][8], g[CH][8], h[CH][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            x[0][c].get(f[c]);
-            x[1][c].get(s[c]);
-            x[2][c].get(h[c]);
-            x[3][c].get(g[c]);
+            l.get(x[0][c], c, f[c]);
+            l.get(x[1][c], c, s[c]);
+            l.get(x[2][c], c, h[c]);
+            l.get(x[3][c], c, g[c]);
         }
         if (kAhead) ask(now);
         Stats of_s = {0.f, 1.f}, of_f = {0.f, 1.f};

@@ -320,15 +320,24 @@ template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_r
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < 4; ++k) b[h][k] = t.b && n + h * 4 + k < t.N ? Elem<T>::load((const T *)t.b + n + h * 4 + k) : 0.f;
-    if (n < t.cols_out)
-        for (long m = (long)blockIdx.x * p.rows_per_block + turn; m < m1; m += 8) {
-            Quad<T> o[2];
-            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n < t.cols_out) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        Quad<T> ahead[2][2]; // of this row and the next
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                o[h].set(zero);
-                if (KIND != kScaled && t.other && n + h * 4 < t.N) o[h] = read_quad((const T *)t.other + m * t.ld_other + n + h * 4, n + h * 4, t.N);
-            }
+        for (int k = 0; k < 4; ++k) ahead[k >> 1][k & 1].set(zero);
+        const long m0 = (long)blockIdx.x * p.rows_per_block + turn;
+        auto ask = [&](long m, Quad<T> (&o)[2]) {
+            if (KIND == kScaled || !t.other || m >= m1) return;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (n + h * 4 < t.N) o[h] = read_quad((const T *)t.other + m * t.ld_other + n + h * 4, n + h * 4, t.N);
+        };
+        ask(m0, ahead[0]);
+        ask(m0 + 8, ahead[1]);
+        for (long m = m0; m < m1; m += 8) {
+            Quad<T> o[2] = {ahead[0][0], ahead[0][1]};
+            ahead[0][0] = ahead[1][0], ahead[0][1] = ahead[1][1];
+            ask(m + 16, ahead[1]);
             float s[2][4] = {};
             for (int k0 = 0; k0 < p.slices; k0 += 4) { // four slices on their way at a time
                 Quad<float> y[4][2];
@@ -363,6 +372,7 @@ template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_r
                 for (int k = 0; k < 4; ++k) columns[h][k] += s[h][k];
             }
         }
+    }
     if (KIND != kSlope || !t.columns) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[turn][col * 8 + e] = columns[e >> 2][e & 3];
