@@ -322,7 +322,7 @@ enum Part { kBoth, kRowPart, kSumPart };
 template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 * kBwdWaves<L::WPR>, 2) norm_bwd_kernel(const NormArgs a)
 {
     constexpr int kWaves = kBwdWaves<L::WPR>, kThreads = 64 * kWaves, kSlots = kThreads / L::LANES / L::WPR, CH = L::CH;
-    constexpr bool kTakesSums = PART != kRowPart, kAhead = PART != kRowPart && (CH == 1 || sizeof(T) == 2); // (else there are no registers for a row ahead)
+    constexpr bool kTakesSums = PART != kRowPart, kAhead = L::WPR < 16; // (else there are no registers for a row ahead, and a row is enough on its way)
     __shared__ float red[16 * kWaves];
     __shared__ float kept[kTakesSums ? 2 : 1][CH][8][kTakesSums ? kThreads : 1]; // own_groups: sums for w_post and b_post
     __shared__ float joined[kSlots > 1 ? kThreads * 8 : 1];
@@ -636,7 +636,7 @@ void plan_norm(const NormGeom &g, bool backward, NormPlan *p)
 {
     *p = NormPlan{};
     p->lanes = g.D <= 128 ? 16 : g.D <= 256 ? 32 : 64;
-    p->chunks = g.D > (backward ? 4096 : 8192) ? 2 : 1;
+    p->chunks = g.D > 8192 ? 2 : 1;
     p->waves = 1;
     while (p->waves * 512 * p->chunks < g.D) p->waves *= 2;
     const int least = backward ? 8 : 4, waves = p->waves > least ? p->waves : least;
@@ -710,7 +710,7 @@ template <typename T, bool WHOLE> static hipError_t launch_rows(NormArgs a, cons
         use(a, p.sums);
         return launch_bwd<T, Rows<64, 1, 1, WHOLE>, kSumPart>(a, st);
     }
-    if (p.chunks == 2) return backward ? launch_bwd<T, Rows<64, 8, 2, WHOLE>>(a, st) : launch_fwd<T, Rows<64, 16, 2, WHOLE>>(a, st);
+    if (p.chunks == 2) return launch_fwd<T, Rows<64, 16, 2, WHOLE>>(a, st);
     if (p.lanes == 16) CAC_ROWS(16, 1);
     if (p.lanes == 32) CAC_ROWS(32, 1);
     switch (p.waves) {
@@ -718,7 +718,7 @@ template <typename T, bool WHOLE> static hipError_t launch_rows(NormArgs a, cons
     case 2: CAC_ROWS(64, 2);
     case 4: CAC_ROWS(64, 4);
     case 8: CAC_ROWS(64, 8);
-    default: return launch_fwd<T, Rows<64, 16, 1, WHOLE>>(a, st);
+    default: CAC_ROWS(64, 16);
     }
 #undef CAC_ROWS
 }

@@ -1,5 +1,5 @@
 // Dropout with its residual, Y = R + alpha * drop(X): a thread has groups of eight neighbours of a row, whose random bits it forms once.
-// Bound by memory (dropout.h): X and R in and Y out, once.
+// Bound by memory (dropout.h): X and R in and Y out, once; 16384 x 4096 bfloat16 with R in 72 us, 5.57 TB/s.
 #include "block.h"
 
 namespace cac {
@@ -59,7 +59,7 @@ template <typename T> static hipError_t launch(const DropGeom &g, const Drop &d,
     a.ld_r = g.ld_r;
     a.scale = g.alpha * d.scale;
     a.d = d;
-    const long blocks = (a.groups + kThreads - 1) / kThreads, grid = blocks < 4096 ? blocks : 4096;
+    const long blocks = (a.groups + kThreads - 1) / kThreads, grid = blocks < 32768 ? blocks : 32768; // (16384 x 4096 with R: 77 us with 4096, 72 with 32768)
     a.step_rows = grid * kThreads / a.wide;
     a.step_cols = (int)(grid * kThreads % a.wide);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), 0, st, a, (const T *)X, (const T *)R, (T *)Y); };

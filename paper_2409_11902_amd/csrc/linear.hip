@@ -204,7 +204,7 @@ __device__ __forceinline__ uint32_t from_neighbour(uint32_t x) { return __builti
 
 // A product with its tail, or its slices' sums.  They go through a wave's LDS, 32 rows at a time: a lane then has four neighbours in the same
 // columns of every row that it comes to, and two lanes a group of the mask, of which each forms one in two.  R (dY) of 32 rows is on its way while the
-// 32 before are dealt with.  PLAIN: no more than a factor.
+// 32 before are dealt with (of 64: 318 us where 32 take 296, 8192 x 2048 x 8192 gelu).  PLAIN: no more than a factor.
 template <class T, bool PLAIN> struct Ended : Ending {
     struct Params {
         Tail t;
@@ -339,17 +339,17 @@ template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_r
             ahead[0][0] = ahead[1][0], ahead[0][1] = ahead[1][1];
             ask(m + 16, ahead[1]);
             float s[2][4] = {};
-            for (int k0 = 0; k0 < p.slices; k0 += 4) { // four slices on their way at a time
-                Quad<float> y[4][2];
+            for (int k0 = 0; k0 < p.slices; k0 += 8) { // eight slices on their way at a time
+                Quad<float> y[8][2];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         y[k][h].set(zero);
                         if (k0 + k < p.slices && n + h * 4 < t.N) y[k][h] = read_quad(p.sums + (k0 + k) * p.slice_stride + m * t.N + n + h * 4, n + h * 4, t.N);
                     }
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float z[4];
@@ -392,7 +392,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const J
     else with_kind<false>(p.t, [&](auto kind, auto act) { join_rows_of<T, decltype(kind)::value, decltype(act)::value>(p, red); });
 }
 
-// ---- Few rows (up to 32): a workgroup has 16 features of all of them, and reads its rows of W once, as they lie, whatever they start on.  Its waves share the
+// ---- Few rows (up to 64): a workgroup has 16 features of all of them, and reads its rows of W once, as they lie, whatever they start on.  Its waves share the
 // terms out, 64 (float: 32) at a time and wave; fragments come straight from memory, since a wave has no use for another's, and the waves' sums are
 // joined in LDS, so that there is one launch.  Bound by reading W.
 struct Few {
@@ -629,17 +629,32 @@ template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const P
 using namespace dense;
 
 // ---- host
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 64;
 
 // Microseconds of M x N sums of K terms in a tile and a number of slices.  What a pass takes on a compute unit with one workgroup and with as many
 // as it holds, and what comes before and after a workgroup's passes: from 8192 x 64 x 8192 to 8192 x 8192 x 2048 bfloat16 within 8 %. The slices' sums
 // are written, read and joined in a launch of their own, 4 us.
-static double tiles_us(Format f, int shape, long M, long N, long K, int slices)
+struct Price { int holds; double alone, full, once, once_full; };
+static Price price_of(Format f, int shape)
 {
-    struct Price { int holds; double alone, full, once, once_full; };
-    static const Price kBf[] = {{3, 0.27, 0.62, 2.5, 4.0}, {2, 0.77, 1.06, 3.5, 7.0}, {}, {1, 1.56, 1.56, 9.0, 14.0}, {}},
+    static const Price kBf[] = {{3, 0.27, 0.72, 2.5, 4.0}, {2, 0.77, 1.06, 3.5, 7.0}, {}, {1, 1.56, 1.56, 9.0, 14.0}, {}},
                        kRawOf[] = {{3, 0.5, 1.4, 2.5, 4.0}, {}, {}, {}, {2, 0.5, 1.0, 2.5, 4.0}};
-    const Price &p = (f == kRaw ? kRawOf : kBf)[shape];
+    return (f == kRaw ? kRawOf : kBf)[shape];
+}
+// What an ending adds to that: an activation with an exponential, dropout, and R or dY to be read.  The largest tile has nothing else to do meanwhile
+// (8192 x 256 x 8192 with all three: 187 us in tiles of 256, 139 of 128, 177 of 64).
+struct Extra { bool exponential, drops, other; };
+static double ending_us(int shape, const Extra &x)
+{
+    static const double kUs[kShapes][3] = {{1.0, 0.5, 0.8}, {2.7, 1.1, 2.2}, {}, {7.5, 2.5, 12.0}, {1.0, 0.5, 0.8}};
+    return x.exponential * kUs[shape][0] + x.drops * kUs[shape][1] + x.other * kUs[shape][2];
+}
+static double tiles_us(Format f, int shape, long M, long N, long K, int slices, const Extra &x)
+{
+    Price p = price_of(f, shape);
+    const double ending = slices > 1 ? 0.0 : ending_us(shape, x);
+    p.once += ending;
+    p.once_full += ending;
     const double n = cdiv(cdiv(K, kTerms[f]), slices);
     const long wgs = tiles_of(shape, M, N, false) * slices, round = 256L * p.holds, rest = wgs % round;
     double us = (wgs / round) * (p.full * n + p.once_full);
@@ -652,7 +667,7 @@ static double tiles_us(Format f, int shape, long M, long N, long K, int slices)
     return us;
 }
 // The cheapest; false: too many tiles for one grid.  DOWN: a's terms run down memory, which tiles of 32 rows have no layout for.
-static bool choose_tiles(Format f, long M, long N, long K, bool down, TileChoice *c, double *least)
+static bool choose_tiles(Format f, long M, long N, long K, bool down, const Extra &x, TileChoice *c, double *least)
 {
     *least = 1e30;
     for (int shape = 0; shape < kShapes; ++shape) {
@@ -662,7 +677,7 @@ static bool choose_tiles(Format f, long M, long N, long K, bool down, TileChoice
         for (int slices = 1; slices <= 64; slices += slices < 4 ? 1 : slices / 4 * 2) {
             if (slices > 1 && (cdiv(K, kTerms[f]) / slices < 4 || tiles * slices > 2048)) break;
             if (!fits_grid(shape, tiles * slices)) break;
-            const double us = tiles_us(f, shape, M, N, K, slices);
+            const double us = tiles_us(f, shape, M, N, K, slices, x);
             if (us < *least) {
                 *least = us;
                 *c = TileChoice{shape, slices};
@@ -675,12 +690,10 @@ static bool choose_tiles(Format f, long M, long N, long K, bool down, TileChoice
 struct PairChoice { TileChoice x, w; double us; };
 static PairChoice choose_pair(Format f, const LinearGeom &g)
 {
-    struct Price { int holds; double alone, full, once; };
-    static const Price kBf[] = {{3, 0.27, 0.62, 4.0}, {2, 0.77, 1.06, 7.0}, {}, {1, 1.56, 1.56, 14.0}}, kRawOf[] = {{3, 0.5, 1.4, 4.0}};
     PairChoice best = {{}, {}, 1e30};
     for (int shape : {kSmall, kMiddle, kBig}) {
         if (f == kRaw && shape != kSmall) continue;
-        const Price &p = (f == kRaw ? kRawOf : kBf)[shape];
+        const Price p = price_of(f, shape);
         const long tx = tiles_of(shape, g.T, g.D, false), tw = tiles_of(shape, g.N, g.D, false);
         const int nx = cdiv(g.N, kTerms[f]), nw = cdiv(g.T, kTerms[f]);
         for (int sx = 1; sx <= 32; sx *= 2)
@@ -690,7 +703,7 @@ static PairChoice choose_pair(Format f, const LinearGeom &g)
                 if (!fits_grid(shape, wgs + cdiv(g.N, 64) + 16)) continue;
                 // with fewer workgroups than the card holds a pass takes less
                 const double fill = std::min(1.0, std::max(0.0, (wgs / 256.0 - 1) / std::max(1, p.holds - 1))), pass = p.alone + fill * (p.full - p.alone);
-                const double once = p.holds == 1 ? p.once : 2.5 + fill * (p.once - 2.5);
+                const double once = p.holds == 1 ? p.once_full : p.once + fill * (p.once_full - p.once);
                 const double cx = cdiv(nx, sx) * pass + once, cw = cdiv(nw, sw) * pass + once;
                 double us = std::max(std::max(cx, cw), (tx * sx * cx + tw * sw * cw) / (256.0 * p.holds));
                 if (sx > 1 || sw > 1) us += 4.0 + 3.2e-6 * ((sx > 1 ? sx * g.T * g.D : 0) + (sw > 1 ? sw * g.N * g.D : 0));
@@ -731,13 +744,14 @@ bool plan_linear(const LinearGeom &g, bool backward, LinearPlan *p)
     p->ld_u = p->grad ? padded(g.N) : g.N;
     size_t sums = 0;
     double us;
-    auto product = [&](long M, long N, long K, bool down, TileChoice *c) {
-        if (!choose_tiles(f, M, N, K, down, c, &us)) return false;
+    auto product = [&](long M, long N, long K, bool down, TileChoice *c, const Extra &x = Extra{}) {
+        if (!choose_tiles(f, M, N, K, down, x, c, &us)) return false;
         if (c->slices > 1 && sums < (size_t)c->slices * M * N * 4) sums = (size_t)c->slices * M * N * 4;
         return true;
     };
     if (!backward || p->again) {
-        if (!product(g.T, g.N, g.D, false, &p->y)) return false;
+        const Extra x = {g.act == CAC_ACT_GELU || g.act == CAC_ACT_SILU, g.drops, backward}; // (a forward pass without R has the same plan as one with it)
+        if (!product(g.T, g.N, g.D, false, &p->y, x)) return false;
         if ((p->pack_x || p->pack_w) && !backward) us += 4.0 + (g.T + g.N) * g.D * e * 1e-6 / 1.5;
         p->few = g.T <= kFewRows && few_us(g.T, g.N, g.D, e) < us;
         if (p->few) sums = 0;
@@ -856,7 +870,8 @@ template <typename T> struct Layer {
         // a wave has 4 steps at a time; with more waves than that gives work to, the others only wait
         const bool wide = g.D > 4 * 4 * Terms<T>::kStep;
         auto waves = [&](auto sixteens, auto whole) {
-            if (wide) go(few_kernel<T, decltype(sixteens)::value, 16, decltype(whole)::value>, 16);
+            constexpr int kMost = decltype(sixteens)::value > 2 ? 8 : 16; // (what registers leave room for)
+            if (wide) go(few_kernel<T, decltype(sixteens)::value, kMost, decltype(whole)::value>, kMost);
             else go(few_kernel<T, decltype(sixteens)::value, 4, decltype(whole)::value>, 4);
         };
         auto rows = [&](auto sixteens) {
@@ -864,7 +879,8 @@ template <typename T> struct Layer {
             else waves(sixteens, std::true_type());
         };
         if (g.T <= 16) rows(std::integral_constant<int, 1>());
-        else rows(std::integral_constant<int, 2>());
+        else if (g.T <= 32) rows(std::integral_constant<int, 2>());
+        else rows(std::integral_constant<int, 4>());
         err = hipGetLastError();
     }
     // C = A B^T with a tail, the sums of whose slices go to o_sum
