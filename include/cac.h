@@ -442,7 +442,7 @@ int cac_block_norm_fwd(const cac_block_norm_desc *d, const void *F, const void *
  *   dR = dS + the gradient of S through H,  a = alpha * drop(dR),  dgate = sums of a * post(F),  dF = the gradient of F from gate * a,
  *   dw_*, db_*: sums over rows of a norm's gradient times its row before weights, and of the gradient.
  * F is read where there is a post or a gate, S (as the forward pass wrote it) where there is a pre.  Any gradient may be NULL and is not computed then.
- * dR may take the place of dS, dF of a dense F.  Each row's norm is a function of itself: with infinities or NaN it comes out as NaN, and in the sums. */
+ * Where D is at most 8192 dR may take the place of dS, dF of a dense F.  Each row's norm is a function of itself: with infinities or NaN it comes out as NaN, and in the sums. */
 int cac_block_norm_bwd(const cac_block_norm_desc *d, const void *F, const void *S, const float *gate, const float *w_post, const float *b_post,
                        const float *w_pre, const void *dH, const void *dS, const uint64_t *rng, void *dR, void *dF, float *dgate, float *dw_post,
                        float *db_post, float *dw_pre, float *db_pre, void *ws, size_t ws_bytes, void *stream);

@@ -309,7 +309,7 @@ int cac_block_norm_bwd(const cac_block_norm_desc *d, const void *F, const void *
     if ((rc = check_ws(p.bytes, ws, ws_bytes))) return rc;
     drop.rng = rng;
     const size_t e = bytes_of(g.dtype), whole = g.T * g.D * e, vec = g.D * 4;
-    const bool over_s = dR && dR == dS, over_f = dF && dF == F && g.ld_f == g.D;
+    const bool once = !p.two, over_s = once && dR && dR == dS, over_f = once && dF && dF == F && g.ld_f == g.D; // (else they are read again)
     const Buffer buffers[] = {{dR, whole, "dR"}, {dF, whole, "dF"}, {dgate, p.groups * vec, "dgate"}, {dw_post, vec, "dw_post"},
                               {db_post, vec, "db_post"}, {dw_pre, vec, "dw_pre"}, {db_pre, vec, "db_pre"},
                               {need_f && !over_f ? F : nullptr, rows_bytes(g.T, g.D, g.ld_f, e), "F"}, {pre ? S : nullptr, whole, "S"}, {dH, whole, "dH"},

@@ -125,9 +125,9 @@ def test_pointers_that_are_missing_or_not_aligned(dtype):
             refused(Linear.call(d, op, **{n: None}), -1, n)
         for n in names:
             refused(Linear.call(d, op, **{n: 64 * MB + 8}), -4, n)
-        refused(Linear.call(linear(dtype=dtype, D=63), op, ws=None), -3)
-        refused(Linear.call(linear(dtype=dtype, D=63), op, ws_bytes=16), -3)
-        refused(Linear.call(linear(dtype=dtype, D=63), op, ws=(1 << 33) + 4), -4)
+        refused(Linear.call(linear(dtype=dtype, T=400, D=63), op, ws=None), -3)
+        refused(Linear.call(linear(dtype=dtype, T=400, D=63), op, ws_bytes=16), -3)
+        refused(Linear.call(linear(dtype=dtype, T=400, D=63), op, ws=(1 << 33) + 4), -4)
     refused(Linear.call(linear(dtype=dtype), B.LINEAR_BWD, dX=None, dW=None, db=None), -1, "nothing")
     d = block(dtype=dtype)
     for op, names, need in ((B.BLOCK_NORM_FWD, Norm.fwd, ("F", "gate", "rng", "H")), (B.BLOCK_NORM_BWD, Norm.bwd, ("F", "S", "gate", "dH", "rng"))):
@@ -199,6 +199,15 @@ def test_outputs_share_no_memory(dtype):
         return B.lib().cac_dropout(d, *(p[k] for k in order), None)
 
     over(dropout, B.make_dropout_desc(T, D, dtype=dtype, p=0.1), 0, order, sizes, ("Y",), ws, 0, {("Y", "X"), ("Y", "R")})
+
+
+@pytest.mark.parametrize("dtype", ALL)
+def test_long_rows_are_read_twice_and_not_written_over(dtype):
+    """Above 8192 columns the sums over rows read F and dS again."""
+    a = addresses(Norm.bwd)
+    d = block(D=8200, dtype=dtype)
+    refused(Norm.call(d, B.BLOCK_NORM_BWD, dR=a["dS"]), -1, "dR shares memory with dS")
+    refused(Norm.call(d, B.BLOCK_NORM_BWD, dF=a["F"]), -1, "dF shares memory with F")
 
 
 def test_plans_follow_sizes():

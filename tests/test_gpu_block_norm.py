@@ -205,19 +205,23 @@ def test_some_gradients(dtype):
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("D", [512, 1001])
-def test_in_place(D, dtype):
-    t = make(90, D, dtype, 1, 1, gate_rows=30, p=0.2)
+@pytest.mark.parametrize("D", [3, 40, 513, 512, 1001, 4097, 8192])
+@pytest.mark.parametrize("post,pre", [(0, 0), (1, 1), (2, 2)])
+def test_in_place(D, post, pre, dtype):
+    """S over R, dR over dS and dF over F, with every other gradient."""
+    t = make(90, D, dtype, post, pre, gate_rows=30, p=0.2)
     want = {k: v.clone() for k, v in forward(t).items()}
     t["S"] = want["S"].clone()
     grads = {k: v.clone() for k, v in backward(t).items()}
-    H = torch.empty_like(want["H"])
+    H = torch.empty_like(want["H"]) if pre else None
     B.cac_block_norm_fwd(t["desc"], t["F"], t["R"], *(t[k] for k in NAMES), t["rng"], t["R"], H)
-    assert torch.equal(t["R"], want["S"]) and torch.equal(H, want["H"])
-    ws = torch.empty(B.cac_block_norm_workspace_size(t["desc"], B.BLOCK_NORM_BWD), dtype=torch.uint8, device=DEV)
-    B.cac_block_norm_bwd(t["desc"], t["F"], t["S"], t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["dH"], t["dS"], t["rng"], t["dS"], t["F"],
-                         None, None, None, None, None, ws)
+    assert torch.equal(t["R"], want["S"]) and (not pre or torch.equal(H, want["H"]))
+    ws = torch.empty(max(16, B.cac_block_norm_workspace_size(t["desc"], B.BLOCK_NORM_BWD)), dtype=torch.uint8, device=DEV)
+    out = {k: torch.empty_like(grads[k]) if k in grads else None for k in NAMES}
+    B.cac_block_norm_bwd(t["desc"], t["F"], t["S"] if pre else None, t["gate"], t["w_post"], t["b_post"], t["w_pre"], t["dH"], t["dS"], t["rng"], t["dS"],
+                         t["F"], *(out[k] for k in NAMES), ws)
     assert torch.equal(t["dS"], grads["dR"]) and torch.equal(t["F"], grads["dF"])
+    assert all(torch.equal(out[k], grads[k]) for k in NAMES if k in grads)
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
