@@ -52,8 +52,8 @@ __device__ __forceinline__ Bits128 drop_bits(const DropKey &key, uint32_t site, 
     return Bits128{{c0, c1, c2, c3}};
 }
 
-// element e of a word's two, e = 0 or 1: its 16 bits, on top of a word, against limit 2^16 - 1 (limit is at least 1)
-__device__ __forceinline__ bool drop_keeps(uint32_t word, int e, uint32_t limit) { return (e ? word | 0xffffu : word << 16 | 0xffffu) > (limit << 16) - 1; }
+// element e of a word's two, e = 0 or 1: its 16 bits, on top of a word, reach limit 2^16 (limit is at least 1; what lies below them makes no difference)
+__device__ __forceinline__ bool drop_keeps(uint32_t word, int e, uint32_t limit) { return (e ? word : word << 16) > (limit << 16) - 1; }
 
 // eight neighbours of one group: zeros for what is dropped (whatever stands there)
 __device__ __forceinline__ void drop_eight(const DropKey &key, const Drop &d, uint64_t group, float (&v)[8])
