@@ -321,56 +321,50 @@ template <typename T, Kind KIND, int ACT> __device__ __forceinline__ void join_r
 #pragma unroll
         for (int k = 0; k < 4; ++k) b[h][k] = t.b && n + h * 4 + k < t.N ? Elem<T>::load((const T *)t.b + n + h * 4 + k) : 0.f;
     if (n < t.cols_out) {
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        Quad<T> ahead[2][2]; // of this row and the next
-#pragma unroll
-        for (int k = 0; k < 4; ++k) ahead[k >> 1][k & 1].set(zero);
+        Eight<T> ahead[2]; // R's or dY's of this row and the next
+        ahead[0].clear();
+        ahead[1].clear();
         const long m0 = (long)blockIdx.x * p.rows_per_block + turn;
-        auto ask = [&](long m, Quad<T> (&o)[2]) {
-            if (KIND == kScaled || !t.other || m >= m1) return;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (n + h * 4 < t.N) o[h] = read_quad((const T *)t.other + m * t.ld_other + n + h * 4, n + h * 4, t.N);
+        auto ask = [&](long m, Eight<T> &o) {
+            if (KIND != kScaled && t.other && m < m1 && n < t.N) o = read_eight((const T *)t.other + m * t.ld_other, n, t.N);
         };
         ask(m0, ahead[0]);
         ask(m0 + 8, ahead[1]);
         for (long m = m0; m < m1; m += 8) {
-            Quad<T> o[2] = {ahead[0][0], ahead[0][1]};
-            ahead[0][0] = ahead[1][0], ahead[0][1] = ahead[1][1];
+            float from[8], v[8] = {};
+            ahead[0].get(from);
+            ahead[0] = ahead[1];
             ask(m + 16, ahead[1]);
-            float s[2][4] = {};
             for (int k0 = 0; k0 < p.slices; k0 += 8) { // eight slices on their way at a time
-                Quad<float> y[8][2];
+                Eight<float> y[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < 8; ++k) {
+                    y[k].clear();
+                    if (k0 + k < p.slices && n < t.N) y[k] = read_eight(p.sums + (k0 + k) * p.slice_stride + m * t.N, n, t.N);
+                }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        y[k][h].set(zero);
-                        if (k0 + k < p.slices && n + h * 4 < t.N) y[k][h] = read_quad(p.sums + (k0 + k) * p.slice_stride + m * t.N + n + h * 4, n + h * 4, t.N);
-                    }
+                for (int k = 0; k < 8; ++k) {
+                    float z[8];
+                    y[k].get(z);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float z[4];
-                        y[k][h].get(z);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) s[h][q] += z[q];
-                    }
+                    for (int e = 0; e < 8; ++e) v[e] += z[e];
+                }
             }
             Bits128 w = {{0, 0, 0, 0}};
             if (KIND != kScaled && t.d.limit) w = drop_bits(key, t.d.site, (uint64_t)m * t.across + (n >> 3));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (n + h * 4 >= t.cols_out) continue;
                 const uint32_t words[2] = {w.w[2 * h], w.w[2 * h + 1]};
-                float from[4];
-                o[h].get(from);
-                finish_four<KIND, ACT>(t, n + h * 4, b[h], from, words, s[h]);
-                if (t.out) write_quad((T *)t.out + m * t.ld_out + n + h * 4, n + h * 4, t.cols_out, s[h]);
+                float four[4] = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                const float other[4] = {from[4 * h], from[4 * h + 1], from[4 * h + 2], from[4 * h + 3]};
+                finish_four<KIND, ACT>(t, n + h * 4, b[h], other, words, four);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) columns[h][k] += s[h][k];
+                for (int k = 0; k < 4; ++k) {
+                    v[4 * h + k] = four[k];
+                    columns[h][k] += four[k];
+                }
             }
+            if (t.out) write_eight((T *)t.out + m * t.ld_out, n, t.cols_out, v);
         }
     }
     if (KIND != kSlope || !t.columns) return;
