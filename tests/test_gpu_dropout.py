@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from block_util import DEV, HALF, TYPES, close, keep_factor, make_rng, philox, rows
+from block_util import DEV, HALF, TYPES, close, keep_factor, limit_of, make_rng, philox, rows
 from paper_2409_11902_amd import binding as B
 
 
@@ -51,6 +51,16 @@ def test_dropout(shape, dtype, p):
 @pytest.mark.parametrize("D", [96, 97, 1])
 def test_strides(D, ld_x, ld_r, dtype):
     run(37, D, dtype, 0.25, ld_x=ld_x and max(ld_x, D), ld_r=ld_r and max(ld_r, D))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("p", [1e-5, 0.99999])
+def test_one_in_65536(p, dtype):
+    """The least and the most that 16 bits can tell from none and all."""
+    assert limit_of(p) in (1, 65535)
+    _, _, k = run(1000, 1003, dtype, p, seed=8)
+    assert 0 < int((k == 0).sum()) < k.numel()
 
 
 @pytest.mark.gpu
