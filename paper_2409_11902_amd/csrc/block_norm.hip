@@ -373,6 +373,8 @@ template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 *
 #pragma unroll
         for (int c = 0; c < CH; ++c) x[k][c].clear();
 
+    int now = kAhead ? next_row() : 0, in_group = 0;
+    if (kAhead) ask(now); // (before the weights, whose products are waited for)
     float w_pre[CH][8], factor[CH][8], sum_a[CH][8], sum_ax[CH][8], sum_h[CH][8], sum_hx[CH][8];
     auto gate_factor = [&](int g) { // gate times w_post times the branch's factor, zeros past a row's end
 #pragma unroll
@@ -395,8 +397,6 @@ template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 *
         }
     }
     gate_factor(group);
-    int now = kAhead ? next_row() : 0, in_group = 0;
-    if (kAhead) ask(now);
     for (int t = 0; t < turns; ++t) {
         if (!kAhead) ask(now = next_row());
         const long row = now;

@@ -14,6 +14,12 @@ HALF = 2.0 ** -8
 LOW = np.uint64(0xFFFFFFFF)
 
 
+@pytest.fixture(autouse=True)
+def give_memory_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def keep_of_rows(rows, cols, p, site, rng):
     t = int(p * 65536 + 0.5)
     across = -(-cols // 8)
