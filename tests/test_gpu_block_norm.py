@@ -185,6 +185,18 @@ def test_without_weights_or_residual(post, pre, dtype):
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("D,gate_rows", [(200, 0), (203, 7), (600, 2), (9001, 25)])
+def test_biases_of_both_kinds_with_and_without_weights(D, gate_rows, dtype):
+    t = make(50, D, dtype, B.NORM_RMS, B.NORM_RMS, gate_rows=gate_rows, p=0.1)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    t["b_post"], t["b_pre"] = (torch.randn(D, generator=g, device=DEV) * 0.3 for _ in range(2))
+    check(t)
+    t["w_post"] = t["w_pre"] = None
+    check(t)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
 def test_a_norm_alone(dtype):
     """H alone, of F as it is; S is F then."""
     t = make(60, 300, dtype, 0, 2, res=False)
