@@ -89,18 +89,21 @@ template <int LANES_, int WPR_, int CH_, bool WHOLE_> struct Rows {
     }
 };
 
-// Where the WPR waves of a row meet: lane i goes away with the numbers of wave i % WPR.  `red` holds two turns, so that one meeting is enough: a
-// wave that writes a turn's numbers has met since the others read those of the turn before.
+// Where the WPR waves of a row meet: lane i goes away with the numbers of wave i % kTurns, kTurns the power of two from WPR on, and with zeros where there is
+// no such wave.  `red` holds two turns, so that one meeting is enough: a wave that writes a turn's numbers has met since the others read those of the turn
+// before.
 template <class L> struct Meeting {
     float *red; // [2][waves of the workgroup][8]
     int waves, turn;
-    float columns; // of a row in wave lane % WPR
+    float columns; // of a row in the wave whose numbers the lane goes away with
+    static constexpr int kTurns = L::WPR <= 1 ? 1 : L::WPR <= 2 ? 2 : L::WPR <= 4 ? 4 : L::WPR <= 8 ? 8 : 16;
     __device__ __forceinline__ Meeting(float *lds, int all, int D) : red(lds), waves(all), turn(0)
     {
-        const int w = (threadIdx.x & 63) % L::WPR;
+        const int w = (threadIdx.x & 63) % kTurns;
         int n = 0;
 #pragma unroll
-        for (int c = 0; c < L::CH; ++c) n += min(max(D - (c * L::WPR + w) * L::LANES * 8, 0), L::LANES * 8);
+        for (int c = 0; c < L::CH; ++c)
+            if (w < L::WPR) n += min(max(D - (c * L::WPR + w) * L::LANES * 8, 0), L::LANES * 8);
         columns = (float)n;
     }
     // of which a wave's lanes all have the same
@@ -115,13 +118,14 @@ template <class L> struct Meeting {
             for (int i = 0; i < N; ++i) r[wave * 8 + i] = x[i];
         }
         __syncthreads();
-        r += (wave / L::WPR * L::WPR + lane % L::WPR) * 8;
+        const int w = lane % kTurns;
+        r += (wave / L::WPR * L::WPR + min(w, L::WPR - 1)) * 8;
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = r[i];
+        for (int i = 0; i < N; ++i) x[i] = w < L::WPR ? r[i] : 0.f;
         turn ^= 1;
     }
-    // over a row's waves, of a number that lane i has of wave i % WPR
-    __device__ __forceinline__ float total(float x) const { return lanes_total<L::WPR>(x); }
+    // over a row's waves, of a number that lane i has of wave i % kTurns
+    __device__ __forceinline__ float total(float x) const { return lanes_total<kTurns>(x); }
 };
 
 // 1 / sqrt(x): the instruction's 22 bits, and a step of Newton's
@@ -322,7 +326,7 @@ enum { kGate, kWPost, kBPost, kWPre, kBPre, kSums };
 // Both parts in one pass where a workgroup's registers hold a row and its sums; of longer rows the row part leaves what it knows of a row, eight numbers,
 // and the sum part has 512 columns to a workgroup and reads the rows again.
 enum Part { kBoth, kRowPart, kSumPart };
-template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 * kBwdWaves<L::WPR>, 2) norm_bwd_kernel(const NormArgs a)
+template <typename T, class L, Part PART> __global__ void __launch_bounds__(64 * kBwdWaves<L::WPR>, kBwdWaves<L::WPR> / 4) norm_bwd_kernel(const NormArgs a)
 {
     constexpr int kWaves = kBwdWaves<L::WPR>, kThreads = 64 * kWaves, kSlots = kThreads / L::LANES / L::WPR, CH = L::CH;
     constexpr bool kTakesSums = PART != kRowPart, kAhead = L::WPR < 16; // (else there are no registers for a row ahead, and a row is enough on its way)
@@ -642,6 +646,9 @@ void plan_norm(const NormGeom &g, bool backward, NormPlan *p)
     p->chunks = g.D > 8192 ? 2 : 1;
     p->waves = 1;
     while (p->waves * 512 * p->chunks < g.D) p->waves *= 2;
+    // Gradients of rows that twelve waves hold are faster with them than with sixteen, of which each then has registers for a row ahead (7523 x 4428 floats
+    // 177 us against 332, 4000 x 6144 bf16 73 against 132 and floats 144 against 162); outputs are slower (4000 x 6144 bf16 64 against 51).
+    if (backward && p->waves == 16 && g.D <= 12 * 512) p->waves = 12;
     const int least = backward ? 8 : 4, waves = p->waves > least ? p->waves : least;
     p->slots = waves * 64 / p->lanes / p->waves;
     p->groups = g.gate_rows ? cdiv(g.T, g.gate_rows) : 1;
@@ -721,6 +728,7 @@ template <typename T, bool WHOLE> static hipError_t launch_rows(NormArgs a, cons
     case 2: CAC_ROWS(64, 2);
     case 4: CAC_ROWS(64, 4);
     case 8: CAC_ROWS(64, 8);
+    case 12: return launch_bwd<T, Rows<64, 12, 1, WHOLE>>(a, st); // only gradients have them
     default: CAC_ROWS(64, 16);
     }
 #undef CAC_ROWS

@@ -25,7 +25,7 @@ __device__ __forceinline__ float normal_cdf(float u, float *bell)
     *bell = __builtin_amdgcn_exp2f(u * u * (-0.5f * kLog2e));
     float p = -0.020695475861430168f;
     p = fmaf(p, t, 0.09534360468387604f);
-    p = fmaf(p, t, -0.1502906233072281f);
+    p = fmaf(p, t, -0.15029062f);
     p = fmaf(p, t, 0.07119989395141602f);
     p = fmaf(p, t, -0.011178647167980671f);
     p = fmaf(p, t, 0.05997511371970177f);

@@ -148,7 +148,7 @@ def check(t):
         assert rel(v, r[k]) <= tight, (k, rel(v, r[k]))
 
 
-SHAPES = [(1, 1), (1, 8), (1, 512), (1, 2048), (2, 9), (3, 77), (5, 16384), (7, 513), (33, 1001), (64, 512), (130, 1024), (257, 2047), (300, 96), (1500, 520), (40, 4104), (33, 8192),
+SHAPES = [(1, 1), (1, 8), (1, 512), (1, 2048), (2, 9), (3, 77), (5, 16384), (7, 513), (33, 1001), (64, 512), (130, 1024), (257, 2047), (300, 96), (1500, 520), (40, 4104), (300, 5001), (70, 6144), (33, 8192),
           (20, 9000), (5000, 24)]
 
 
