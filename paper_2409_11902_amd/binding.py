@@ -349,8 +349,8 @@ def cac_muon_step(d, G, M, W, momentum, keep, lr, ws=None, stream=None):
 # (pointers in place: a call of _ptr costs as much as data_ptr does, and these have up to 17)
 
 def cac_dropout(d, X, R, rng, Y, stream=None):
-    _check((_lib or lib()).cac_dropout(d, X.data_ptr(), None if R is None else R.data_ptr(), None if rng is None else rng.data_ptr(), Y.data_ptr(),
-                                       _stream(stream)))
+    _check((_lib or lib()).cac_dropout(d, None if X is None else X.data_ptr(), None if R is None else R.data_ptr(), None if rng is None else rng.data_ptr(),
+                                       None if Y is None else Y.data_ptr(), _stream(stream)))
 
 
 def cac_linear_workspace_size(d: cac_linear_desc, op: int) -> int:
@@ -363,14 +363,14 @@ def cac_linear_describe_plan(d: cac_linear_desc, op: int) -> str:
 
 def cac_linear_fwd(d, X, W, b, R, rng, Y, ws=None, stream=None):
     _check((_lib or lib()).cac_linear_fwd(
-        d, X.data_ptr(), W.data_ptr(), None if b is None else b.data_ptr(), None if R is None else R.data_ptr(),
-        None if rng is None else rng.data_ptr(), Y.data_ptr(), *_ws(ws), _stream(stream)))
+        d, None if X is None else X.data_ptr(), None if W is None else W.data_ptr(), None if b is None else b.data_ptr(),
+        None if R is None else R.data_ptr(), None if rng is None else rng.data_ptr(), None if Y is None else Y.data_ptr(), *_ws(ws), _stream(stream)))
 
 
 def cac_linear_bwd(d, X, W, b, dY, rng, dX, dW, db, ws=None, stream=None):
     _check((_lib or lib()).cac_linear_bwd(
-        d, None if X is None else X.data_ptr(), None if W is None else W.data_ptr(), None if b is None else b.data_ptr(), dY.data_ptr(),
-        None if rng is None else rng.data_ptr(), None if dX is None else dX.data_ptr(), None if dW is None else dW.data_ptr(),
+        d, None if X is None else X.data_ptr(), None if W is None else W.data_ptr(), None if b is None else b.data_ptr(),
+        None if dY is None else dY.data_ptr(), None if rng is None else rng.data_ptr(), None if dX is None else dX.data_ptr(), None if dW is None else dW.data_ptr(),
         None if db is None else db.data_ptr(), *_ws(ws), _stream(stream)))
 
 
@@ -384,7 +384,7 @@ def cac_block_norm_describe_plan(d: cac_block_norm_desc, op: int) -> str:
 
 def cac_block_norm_fwd(d, F, R, gate, w_post, b_post, w_pre, b_pre, rng, S, H, stream=None):
     _check((_lib or lib()).cac_block_norm_fwd(
-        d, F.data_ptr(), None if R is None else R.data_ptr(), None if gate is None else gate.data_ptr(),
+        d, None if F is None else F.data_ptr(), None if R is None else R.data_ptr(), None if gate is None else gate.data_ptr(),
         None if w_post is None else w_post.data_ptr(), None if b_post is None else b_post.data_ptr(),
         None if w_pre is None else w_pre.data_ptr(), None if b_pre is None else b_pre.data_ptr(), None if rng is None else rng.data_ptr(),
         None if S is None else S.data_ptr(), None if H is None else H.data_ptr(), _stream(stream)))
