@@ -362,7 +362,7 @@ int cac_muon_step(const cac_muon_desc *d, const void *G, float *M, void *W, floa
  * element's row and column.  Philox 4x32 of ten rounds (Salmon, Moraes, Dror, Shaw, 2011) with key rng[0] makes 128 bits from the counter
  * (g low, g high | site << 8, step low, step high), words of 32 bits, g = row * ceil(columns / 8) + column / 8.  They are the 16 bits of
  * each of eight neighbours, column % 8 = 0 in the low half of the first word; an element whose bits are below round(65536 drop_p) is dropped, and
- * the others are multiplied by 65536 / (65536 - round(65536 drop_p)).  drop(x) is zero where x is dropped, whatever it is.  A forward
+ * the others are multiplied by 65536 / (65536 - round(65536 drop_p)), which times alpha is a finite float.  drop(x) is zero where x is dropped, whatever it is.  A forward
  * and a backward call have the same mask where rng's numbers, site, drop_p and the columns are the same.  rng is not read, and may be NULL, where
  * round(65536 drop_p) is 0. */
 

@@ -35,6 +35,7 @@ static int make_drop(float p, uint32_t site, float alpha, const uint64_t *rng, D
     d->limit = (uint32_t)floor((double)p * 65536.0 + 0.5);
     d->site = site;
     d->scale = d->limit == 65536 ? 0.f : (float)(65536.0 / (65536 - (int)d->limit));
+    if (!isfinite(alpha * d->scale)) return fail(CAC_ERR_INVALID_ARG, "alpha over the probability of being kept is not finite"); // (a kept zero would come out as NaN)
     d->rng = rng;
     return CAC_OK;
 }
