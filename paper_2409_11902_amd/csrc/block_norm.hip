@@ -618,24 +618,30 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const NormArgs a)
 // ---- host
 static long cdiv(long a, long b) { return (a + b - 1) / b; }
 
-// Which rows a workgroup of the backward pass has, of `slots` at once and `most` workgroups.
+// Which rows a workgroup of the backward pass has, of `slots` at once and `most` workgroups at a time.  Where gates are many a slot has whole groups to
+// itself, or a workgroup has (part of) one group: whichever takes fewer turns of a slot, 2 to 3 us each, where every round of workgroups costs as much as 4 turns
+// more and one for sixteen slots whose sums it joins.  Gradients of bfloat16 with both norms, us, slots with groups of their own / workgroups with one:
+//   2048 columns, gates of 49 rows: 255 gates 122 / 74, 256 gates 122 / 76, 257 122 / 130, 512 134 / 142, 513 229 / 195, 1024 254 / 276
+//   4608 x 196: 127 gates 572 / 333, 128 572 / 337, 129 572 / 568.  1024 x 16: 511 46 / 38, 512 46 / 38, 513 46 / 48, 1024 49 / 70
+//   128 x 49: 1024 gates 97 / 65, 2048 97 / 123, 4096 115 / 249.  2048 x 3: 128 17 / 22, 256 18 / 18, 512 21 / 29
 static NormSplit split_rows(const NormGeom &g, long groups, int slots, long most)
 {
     NormSplit s;
     const long G = g.gate_rows ? g.gate_rows : g.T;
-    s.own_groups = groups > 1 && (groups * 2 >= most * slots || G <= 4);
-    s.per_group = 1;
-    s.rows_per_block = 0;
-    if (s.own_groups) {
-        s.blocks = cdiv(groups, slots);
-        if (s.blocks > most) s.blocks = most;
-        return s;
-    }
     const long per = most / groups > 0 ? most / groups : 1;
     s.rows_per_block = cdiv(G, per);
     if (s.rows_per_block < slots) s.rows_per_block = slots;
     s.per_group = cdiv(G, s.rows_per_block);
     s.blocks = groups * s.per_group;
+    const double round = 4.0 + slots / 16.0;
+    const double turns = cdiv(s.blocks, most) * (cdiv(s.rows_per_block, slots) + round), turns_own = (double)cdiv(groups, most * slots) * G + round;
+    s.own_groups = groups > 1 && turns_own <= turns;
+    if (s.own_groups) {
+        s.per_group = 1;
+        s.rows_per_block = 0;
+        s.blocks = cdiv(groups, slots);
+        if (s.blocks > most) s.blocks = most;
+    }
     return s;
 }
 
