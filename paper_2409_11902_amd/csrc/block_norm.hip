@@ -128,11 +128,13 @@ template <class L> struct Meeting {
     __device__ __forceinline__ float total(float x) const { return lanes_total<kTurns>(x); }
 };
 
-// 1 / sqrt(x): the instruction's 22 bits, and a step of Newton's
+// 1 / sqrt(x): the instruction's 22 bits, and a step of Newton's.  The instruction takes numbers below the least normal one for zeros, so small ones go
+// through it times 2^64.
 __device__ __forceinline__ float inverse_root(float x)
 {
-    const float y = __builtin_amdgcn_rsqf(x), r = fmaf(-x * y, y, 1.f);
-    return x > 0.f && x < INFINITY ? fmaf(0.5f * y, r, y) : y;
+    const bool small = x < 0x1p-100f;
+    const float z = small ? x * 0x1p64f : x, y = __builtin_amdgcn_rsqf(z), r = fmaf(-z * y, y, 1.f);
+    return (x > 0.f && x < INFINITY ? fmaf(0.5f * y, r, y) : y) * (small ? 0x1p32f : 1.f);
 }
 
 // eight of a vector of weights, `otherwise` where there is none, zeros past its end
