@@ -98,8 +98,6 @@ static int make_norm(const cac_block_norm_desc *d, bool backward, NormGeom *g, N
     return CAC_OK;
 }
 
-// a matrix of rows, from its first number to behind its last
-static size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
 // null or well aligned
 static int check_optional(const void *p, const char *name) { return p ? check_ptr(p, name) : CAC_OK; }
 static int check_absent(const void *p, const char *name, const char *why)

@@ -30,5 +30,7 @@ inline int check_apart(const Buffer *b, int outputs, int all)
 }
 
 inline size_t bytes_of(int dtype) { return dtype == CAC_F32 ? 4 : 2; }
+// of a matrix of rows, from its first number to behind its last
+inline size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
 
 } // namespace cac

@@ -12,8 +12,6 @@ static const char *tile_name(const TileChoice &c)
     return names[c.shape];
 }
 
-// from the first number of a matrix to behind its last
-static size_t rows_bytes(long rows, long columns, long ld, size_t e) { return ((size_t)(rows - 1) * ld + columns) * e; }
 
 static int make_loss_geom(const cac_loss_desc *d, LossGeom *g)
 {
