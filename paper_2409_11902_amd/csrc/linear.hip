@@ -18,7 +18,9 @@ using namespace mm;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Phi(u) = erfc(-u / sqrt 2) / 2 and exp(-u^2 / 2). For u < 0, Phi = exp(-u^2 / 2) t P(t) with t = 1 / (1 + 0.45 |u| / sqrt 2): P is a least-squares
-// polynomial of erfcx(z) / (2 t), reweighted until its relative error, 3.2e-8, was level; in float 1.4e-7 in the mean, of small Phi too.
+// polynomial of erfcx(z) / (2 t), reweighted until its relative error was level; with the coefficients as they stand it is below 6e-8.  In float Phi is off by 1e-7 of
+// itself in the mean down to u = -2.  Below, the exponential's argument, rounded to 24 bits of u^2 / 2, makes that grow with u^2: 2.5e-7 at -4, 5.9e-7 at -6, 1.7e-6 at -10,
+// 2.3e-6 (at most 7.5e-6) at -12, where Phi is 2e-33.
 __device__ __forceinline__ float normal_cdf(float u, float *bell)
 {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.31819805153394637f, fabsf(u), 1.f)); // 0.45 / sqrt 2
@@ -387,9 +389,10 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const J
 }
 
 // ---- Few rows (up to 64): a workgroup has 16 features of all of them, and reads its rows of W once, as they lie, whatever they start on.  Its waves share the
-// terms out, 64 (float: 32) at a time and wave; fragments come straight from memory, since a wave has no use for another's, and the waves' sums are
-// joined in LDS, so that there is one launch.  Bound by what a compute unit takes in, 35 KB a us: 1 x 4096 x 4096
-// bfloat16 9.1 us (3.7 TB/s; 11.6 as tiles and a join), 1 x 512 x 2048 3.3 (5.3), 1 x 1001 x 2047 5.4 (11.3 with a copy of its odd rows).
+// terms out, four steps of 32 (float: 16) at a time and wave; fragments come straight from memory, since a wave has no use for another's, and the waves' sums are
+// joined in LDS, so that there is one launch.  bfloat16 with bias and gelu, weights that no cache holds, us in a graph (in brackets: as tiles, with a join or copy): bound by memory where weights
+// are many, 1 x 8192 x 8192 30.0 (38.3) and 1 x 4096 x 4096 9.9 (15.3), 4.5 to 4.9 TB/s behind the launch's 2.6 us; by what a compute unit takes in, 31 to 36 KB a us, where features are few, 1 x 8192 x 512 11.6
+// (11.6) and 16 x 8192 x 512 17.1 (12.5); by the launch where there is little, 1 x 512 x 2048 3.5 (5.8).  1 x 1001 x 2047 5.7 (15.1 with a copy of its odd rows).
 struct Few {
     Tail t;
     const void *X, *W;
@@ -602,7 +605,7 @@ template <class P, class S, typename T> hipError_t launch_pair(Pair<T> p, TileCh
 struct Pack {
     const void *from[2];
     void *to[2];
-    long rows[2], ld[2];
+    long ld[2];
     long groups[2]; // of eight elements, of all rows; 0: not this one
     int columns;    // (both have the same)
 };
@@ -708,8 +711,10 @@ static PairChoice choose_pair(Format f, const LinearGeom &g)
     }
     return best;
 }
-// Few rows by few_kernel: a compute unit takes in 35 KB a us, its features' rows of W and for each sixteen of them X (16 x 4096 x 4096
-// bfloat16 10.9 us, 16 x 8192 x 2048 17.9, 1 x 8192 x 512 float 22)
+// Few rows by few_kernel, as if all that bound it were what a compute unit takes in, 35 KB a us: its features' rows of W, and X.  Of one to four rows with many weights that is
+// too little (1 x 4096 x 4096 bfloat16 6.6 where it takes 9.9 us, 1 x 8192 x 8192 18.5 where 30.0), but so is what tiles are priced at there.  Of 154 layers of 1 to 64
+// rows, 512 to 8192 columns and features, in either type, none goes to few_kernel that tiles are faster with; 13 go to tiles that few_kernel does up to 14 %
+// (4 x 8192 x 8192 float 22 %) faster: 1 x 8192 x 2048 float 30.6 / 26.2 us, 2 x 8192 x 2048 bfloat16 15.4 / 13.8, 16 x 4096 x 1024 bfloat16 11.0 / 10.0.
 static double few_us(long T, long N, long K, long e) { return 2.6 + cdiv(cdiv(N, 16), 256) * (16.0 + T) * K * e / 35e3; }
 
 static int rows_of_a_part(int shape) // of a tile, that one wave sums over
@@ -806,7 +811,6 @@ template <typename T> struct Layer {
         Pack a;
         a.from[0] = X, a.from[1] = W;
         a.to[0] = ws + p.o_x, a.to[1] = ws + p.o_w;
-        a.rows[0] = g.T, a.rows[1] = g.N;
         a.ld[0] = g.ld_x, a.ld[1] = g.ld_w;
         const long across = (g.D + 7) / 8;
         a.groups[0] = px ? g.T * across : 0;
