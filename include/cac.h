@@ -414,7 +414,9 @@ int cac_linear_bwd(const cac_linear_desc *d, const void *X, const void *W, const
 /* What stands between two blocks: a norm behind the one, the gate and the factor of its branch, the residual, and the norm before the other:
  *   S = R + alpha * drop(gate * post(F)),   H = pre(S),   F, R, S, H [T, D] (S and H dense).
  * post and pre are no norm (x itself; for pre, no H), rms: x / sqrt(mean(x^2) + eps) * w + b, or layer: (x - mean) / sqrt(mean((x - mean)^2) + eps)
- * * w + b.  H is formed from S before S is rounded.  Weights, biases, the gate and their gradients are float; sums are float, in a fixed order. */
+ * * w + b.  H is formed from S before S is rounded.  Weights, biases, the gate and their gradients are float; sums are float, in a fixed order.
+ * A row's squares are summed in float: of a row whose sum of squares is above float's range (but not its sum) xhat is 0.  gate * w * alpha and gate * b * alpha are
+ * formed first, as floats: an infinite gate or weight leaves NaN or infinities in its column. */
 typedef enum cac_norm { CAC_NORM_NONE = 0, CAC_NORM_RMS = 1, CAC_NORM_LAYER = 2 } cac_norm;
 typedef enum cac_block_norm_op { CAC_BLOCK_NORM_FWD = 0, CAC_BLOCK_NORM_BWD = 1 } cac_block_norm_op;
 

@@ -1,4 +1,6 @@
-"""Rows of numbers so small that their mean square is below the least normal float, without an epsilon to hide it, and rows of zeros with an epsilon that
+"""The ends of float's range, as the header has them.
+
+Rows of numbers so small that their mean square is below the least normal float, without an epsilon to hide it, and rows of zeros with an epsilon that
 is itself below it.
 
 Tolerances.  Numbers are 2^-66 times small whole ones, ten of them 3 or -3 in each row of 40: a mean square is 2^-131 at least.  Squares, their sum and
@@ -50,3 +52,18 @@ def test_zeros_with_a_tiny_epsilon(kind, dtype):
     H = torch.empty_like(F)
     B.cac_block_norm_fwd(d, F, None, None, None, None, None, b, None, None, H)
     assert torch.equal(H.float(), b.expand(T, D))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("kind", [B.NORM_RMS, B.NORM_LAYER])
+@pytest.mark.parametrize("D", [40, 1001, 9000])
+def test_rows_whose_squares_leave_the_range(D, kind, dtype):
+    """Their xhat is 0: H is b, and no gradient comes through the norm."""
+    F, b = torch.randn(T, D, device=DEV).mul_(1e25).to(TYPES[dtype]), torch.arange(D, device=DEV).float()
+    d = B.make_block_norm_desc(T, D, dtype=dtype, post=B.NORM_NONE, pre=kind)
+    H, dR, dH, dS = (torch.randn(T, D, device=DEV).to(TYPES[dtype]) for _ in range(4))
+    B.cac_block_norm_fwd(d, F, None, None, None, None, None, b, None, None, H)
+    assert torch.equal(H, b.expand(T, D).to(TYPES[dtype]))
+    B.cac_block_norm_bwd(d, None, F, None, None, None, None, dH, dS, None, dR, None, None, None, None, None, None,
+                         torch.empty(max(16, B.cac_block_norm_workspace_size(d, B.BLOCK_NORM_BWD)), dtype=torch.uint8, device=DEV))
+    assert torch.equal(dR, dS)
